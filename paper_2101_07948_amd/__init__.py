@@ -451,3 +451,6 @@ def dense_gemm(W, B, C, bias=None, epi: str = "none", stream=None):
 
 def status_str(code: int) -> str:
     return lib().sdnn_status_str(code).decode()
+
+
+from .decode import BlockCache, Q4Plan, Rope, rope_frequencies  # noqa: E402  (uses the names above)

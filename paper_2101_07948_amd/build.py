@@ -9,7 +9,10 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libsdnn.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("sdnn_host.cpp", "sdnn_quad_pack.cpp",
-                                                   "sdnn_kernels.hip", "sdnn_quad.hip")]
+                                                   "sdnn_kernels.hip", "sdnn_quad.hip",
+                                                   "sdnn_decode_host.cpp", "sdnn_rope.hip",
+                                                   "sdnn_select.hip", "sdnn_attend.hip",
+                                                   "sdnn_qmat.hip")]
 PROBES_LIB = os.path.join(HERE, "libsdnn_probes.so")
 PROBES_SOURCES = [os.path.join(HERE, "csrc", "sdnn_probes.hip")]
 
