@@ -45,23 +45,30 @@ struct Step16 {
 
   static __device__ __forceinline__ int token(int half, int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }
 
+  // The keys and values of a step: 2 CHUNKS pieces each.
   template <int CHUNKS>
-  static __device__ __forceinline__ void scores(const T* k, int D, const V8 (&q)[CHUNKS], int r, int g,
-                                                float (&s)[8]) {
-    V8 kk[2][CHUNKS];
+  static __device__ __forceinline__ void load(const T* k, const T* v, int D, int P, int r, int g,
+                                              V8 (&kk)[2 * CHUNKS], V8 (&vv)[2 * CHUNKS]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) {
         const int d = (c * 4 + g) * 8;
-        kk[h][c] = V8{};
-        if (d < D) kk[h][c] = *reinterpret_cast<const V8*>(k + token(h, r) * D + d);
+        kk[h * CHUNKS + c] = V8{};
+        if (d < D) kk[h * CHUNKS + c] = *reinterpret_cast<const V8*>(k + token(h, r) * D + d);
       }
+#pragma unroll
+    for (int c = 0; c < 2 * CHUNKS; ++c)
+      vv[c] = *reinterpret_cast<const V8*>(v + min(c * 16 + r, D - 1) * P + 8 * g);
+  }
+
+  template <int CHUNKS>
+  static __device__ __forceinline__ void scores(const V8 (&kk)[2 * CHUNKS], const V8 (&q)[CHUNKS], float (&s)[8]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) acc = mfma(kk[h][c], q[c], acc);
+      for (int c = 0; c < CHUNKS; ++c) acc = mfma(kk[h * CHUNKS + c], q[c], acc);
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[4 * h + i] = acc[i];
     }
@@ -70,8 +77,8 @@ struct Step16 {
   // o += p v.  p is split into two 16-bit parts, so that it counts with all the bits that the sum
   // of probabilities counts it with (one part would add an error as large as the rounding of o).
   template <int CHUNKS>
-  static __device__ __forceinline__ void accumulate(const T* v, int D, int P, const float (&p)[8], int r,
-                                                    int g, int seen, f32x4 (&o)[2 * CHUNKS]) {
+  static __device__ __forceinline__ void accumulate(V8 (&vv)[2 * CHUNKS], const float (&p)[8], int g, int seen,
+                                                    f32x4 (&o)[2 * CHUNKS]) {
     V8 hi, lo;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -80,15 +87,13 @@ struct Step16 {
     }
 #pragma unroll
     for (int c = 0; c < 2 * CHUNKS; ++c) {
-      const int d = min(c * 16 + r, D - 1);
-      V8 x = *reinterpret_cast<const V8*>(v + d * P + 8 * g);
       if (seen < kTokens) {  // past the sequence's end a page holds anything
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (8 * g + j >= seen) x[j] = (T)0.0f;
+          if (8 * g + j >= seen) vv[c][j] = (T)0.0f;
       }
-      o[c] = mfma(x, hi, o[c]);
-      o[c] = mfma(x, lo, o[c]);
+      o[c] = mfma(vv[c], hi, o[c]);
+      o[c] = mfma(vv[c], lo, o[c]);
     }
   }
 };
@@ -113,15 +118,21 @@ struct Step<float> {
   typedef f32x4 Piece;
 
   template <int CHUNKS>
-  static __device__ __forceinline__ void scores(const float* k, int D, const f32x4 (&q)[CHUNKS], int r, int g,
-                                                float (&s)[4]) {
-    f32x4 kk[CHUNKS];
+  static __device__ __forceinline__ void load(const float* k, const float* v, int D, int P, int r, int g,
+                                              f32x4 (&kk)[CHUNKS], f32x4 (&vv)[CHUNKS]) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
       const int d = (c * 4 + g) * 4;
       kk[c] = f32x4{0, 0, 0, 0};
       if (d < D) kk[c] = *reinterpret_cast<const f32x4*>(k + r * D + d);
     }
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+      vv[c] = *reinterpret_cast<const f32x4*>(v + min(c * 16 + r, D - 1) * P + 4 * g);
+  }
+
+  template <int CHUNKS>
+  static __device__ __forceinline__ void scores(const f32x4 (&kk)[CHUNKS], const f32x4 (&q)[CHUNKS], float (&s)[4]) {
     f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
@@ -132,19 +143,17 @@ struct Step<float> {
   }
 
   template <int CHUNKS>
-  static __device__ __forceinline__ void accumulate(const float* v, int D, int P, const float (&p)[4], int r,
-                                                    int g, int seen, f32x4 (&o)[CHUNKS]) {
+  static __device__ __forceinline__ void accumulate(f32x4 (&vv)[CHUNKS], const float (&p)[4], int g, int seen,
+                                                    f32x4 (&o)[CHUNKS]) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-      const int d = min(c * 16 + r, D - 1);
-      f32x4 x = *reinterpret_cast<const f32x4*>(v + d * P + 4 * g);
       if (seen < kTokens) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (4 * g + j >= seen) x[j] = 0.0f;
+          if (4 * g + j >= seen) vv[c][j] = 0.0f;
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], p[e], o[c], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[c][e], p[e], o[c], 0, 0, 0);
     }
   }
 };
@@ -166,39 +175,37 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// Tokens [0, seen) of a page's `steps` steps are within the query's sight.
-template <typename T, int CHUNKS, int TILES>
-__device__ __forceinline__ void attend_page(const AttendArgs& a, const T* k, const T* v, int seen,
-                                            const typename Step<T>::Piece (&q)[CHUNKS], int r, int g,
-                                            State<TILES>& st) {
+// Tokens [0, seen) of the step's are within the query's sight (seen > 0).
+template <typename T, int CHUNKS, int TILES, int PIECES>
+__device__ __forceinline__ void attend_step(float scale2, const typename Step<T>::Piece (&kk)[PIECES],
+                                            typename Step<T>::Piece (&vv)[PIECES], int seen,
+                                            const typename Step<T>::Piece (&q)[CHUNKS], int g, State<TILES>& st) {
   constexpr int N = Step<T>::kTokens, E = N / 4;
-  for (int t0 = 0; t0 < seen; t0 += N) {
-    float s[E];
-    Step<T>::template scores<CHUNKS>(k + (int64_t)t0 * a.head_dim, a.head_dim, q, r, g, s);
-    float top = -INFINITY;
+  float s[E];
+  Step<T>::template scores<CHUNKS>(kk, q, s);
+  float top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      s[j] = E * g + j < seen - t0 ? s[j] * a.scale2 : -INFINITY;
-      top = fmaxf(top, s[j]);
-    }
-    top = over_groups_max(top);
-    if (__any(top > st.m)) {
-      const float m = fmaxf(st.m, top);
-      const float f = __builtin_amdgcn_exp2f(st.m - m);  // 0 for the first step (m is finite)
-      st.l *= f;
-      st.m = m;
-#pragma unroll
-      for (int c = 0; c < TILES; ++c) st.o[c] *= f;
-    }
-    float sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-      s[j] = __builtin_amdgcn_exp2f(s[j] - st.m);
-      sum += s[j];
-    }
-    st.l += sum;
-    Step<T>::template accumulate<CHUNKS>(v + t0, a.head_dim, a.block, s, r, g, seen - t0, st.o);
+  for (int j = 0; j < E; ++j) {
+    s[j] = E * g + j < seen ? s[j] * scale2 : -INFINITY;
+    top = fmaxf(top, s[j]);
   }
+  top = over_groups_max(top);
+  if (__any(top > st.m)) {
+    const float m = fmaxf(st.m, top);
+    const float f = __builtin_amdgcn_exp2f(st.m - m);  // 0 for the first step (m is finite)
+    st.l *= f;
+    st.m = m;
+#pragma unroll
+    for (int c = 0; c < TILES; ++c) st.o[c] *= f;
+  }
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    s[j] = __builtin_amdgcn_exp2f(s[j] - st.m);
+    sum += s[j];
+  }
+  st.l += sum;
+  Step<T>::template accumulate<CHUNKS>(vv, s, g, seen, st.o);
 }
 
 // A workgroup handles one token, cached head, tile of up to 16 of its queries and share of its
@@ -240,14 +247,21 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
   const int n = filler ? 0 : a.chosen ? a.blocks : min(own + 1, a.max_blocks);
   const int32_t* chosen = a.chosen ? a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks : nullptr;
   const int32_t* table = a.table + (int64_t)seq * a.max_blocks;
-  for (int j = split * kWaves + wave; j < n; j += a.splits * kWaves) {
+  // steps of all blocks, dealt to the waves of all shares in turn
+  constexpr int N = Step<T>::kTokens;
+  const int per_block = a.block / N;
+  for (int u = split * kWaves + wave; u < n * per_block; u += a.splits * kWaves) {
+    const int j = u / per_block, t0 = (u - j * per_block) * N;
     const int id = chosen ? chosen[j] : j;
     if (id < 0 || id > own || id >= a.max_blocks) continue;
     const int64_t page = table[id];
-    if (page < 0 || page >= a.pages) continue;
+    const int seen = p - id * a.block + 1 - t0;
+    if (page < 0 || page >= a.pages || seen <= 0) continue;
     const int64_t at = (page * a.kv_heads + h) * (int64_t)a.block * D;
-    attend_page<T, CHUNKS, TILES>(a, static_cast<const T*>(a.k_pages) + at, static_cast<const T*>(a.v_pages) + at,
-                                  min(a.block, p - id * a.block + 1), q, r, g, st);
+    typename Step<T>::Piece kk[TILES], vv[TILES];
+    Step<T>::template load<CHUNKS>(static_cast<const T*>(a.k_pages) + at + (int64_t)t0 * D,
+                                   static_cast<const T*>(a.v_pages) + at + t0, D, a.block, r, g, kk, vv);
+    attend_step<T, CHUNKS, TILES>(a.scale2, kk, vv, seen, q, g, st);
   }
 
   // join the waves: 2 and 3 into 0 and 1, then 1 into 0
@@ -303,31 +317,58 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
     a.lse[(int64_t)t * a.heads + head] = l > 0.0f ? (m + __log2f(l)) * 0.693147181f : -INFINITY;
 }
 
-// Joins the parts of a token's head: a wave for each.
+// Joins the parts of a token's head: a workgroup for each, a quarter of the parts to a wave.  Lane s has
+// the maximum and the total of part s, so that all factors are known before the first sum is needed;
+// the sums are loaded without conditions (a part that is not there repeats the last with factor 0), so
+// that a wave's loads are all under way at once (one after the other they took 0.75 us each).
 template <typename T>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64, rows = (int64_t)a.tokens * a.heads;
-  if (row >= rows) return;
-  const int lane = threadIdx.x % 64, D = a.head_dim;
+  constexpr int DIMS = kMaxHeadDim / 64, AHEAD = 8;
+  __shared__ float sums[3][kMaxHeadDim];
+  const int64_t row = blockIdx.x, rows = (int64_t)a.tokens * a.heads;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, D = a.head_dim;
   const float* ml = a.part + a.splits * rows * D;
-  float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[(s * rows + row) * 2]);
-  float l = 0.0f, o[kMaxHeadDim / 64] = {};
-  if (m > -INFINITY)
-    for (int s = 0; s < a.splits; ++s) {
-      const float* p = ml + (s * rows + row) * 2;
-      const float f = __builtin_amdgcn_exp2f(p[0] - m);
-      l += p[1] * f;
+  float m = -INFINITY, l = 0.0f;
+  if (lane < a.splits) m = ml[(lane * rows + row) * 2], l = ml[(lane * rows + row) * 2 + 1];
+  float o[DIMS] = {};
+  float top = m;
 #pragma unroll
-      for (int i = 0; i < kMaxHeadDim / 64; ++i)
-        if (i * 64 + lane < D) o[i] += a.part[(s * rows + row) * D + i * 64 + lane] * f;
+  for (int s = 32; s; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+  const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
+  l *= f;
+#pragma unroll
+  for (int s = 32; s; s >>= 1) l += __shfl_xor(l, s);
+  for (int s0 = wave; s0 < a.splits; s0 += 4 * AHEAD) {
+    float x[AHEAD][DIMS], fs[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int s = min(s0 + 4 * k, a.splits - 1);
+      fs[k] = s0 + 4 * k < a.splits ? __shfl(f, s) : 0.0f;
+      const float* part = a.part + (s * rows + row) * D;
+#pragma unroll
+      for (int i = 0; i < DIMS; ++i)
+        if (i * 64 < D) x[k][i] = part[min(i * 64 + lane, D - 1)];
     }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+      for (int i = 0; i < DIMS; ++i)
+        if (i * 64 < D) o[i] = fmaf(x[k][i], fs[k], o[i]);
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int i = 0; i < DIMS; ++i) sums[wave - 1][i * 64 + lane] = o[i];
+  }
+  __syncthreads();
+  if (wave > 0) return;
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   T* y = static_cast<T*>(a.o) + row / a.heads * a.o_token + row % a.heads * a.o_head;
 #pragma unroll
-  for (int i = 0; i < kMaxHeadDim / 64; ++i)
-    if (i * 64 + lane < D) y[i * 64 + lane] = (T)(o[i] * inv);
-  if (lane == 0 && a.lse) a.lse[row] = l > 0.0f ? (m + __log2f(l)) * 0.693147181f : -INFINITY;
+  for (int i = 0; i < DIMS; ++i) {
+    const int d = i * 64 + lane;
+    if (d < D) y[d] = (T)((((o[i] + sums[0][d]) + sums[1][d]) + sums[2][d]) * inv);
+  }
+  if (lane == 0 && a.lse) a.lse[row] = l > 0.0f ? (top + __log2f(l)) * 0.693147181f : -INFINITY;
 }
 
 template <typename T, int CHUNKS>
@@ -336,7 +377,7 @@ hipError_t start(const AttendArgs& a, hipStream_t stream) {
   attend_kernel<T, CHUNKS><<<grid, kWaves * 64, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  attend_join<T><<<(unsigned)(((int64_t)a.tokens * a.heads + 3) / 4), 256, 0, stream>>>(a);
+  attend_join<T><<<(unsigned)((int64_t)a.tokens * a.heads), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -351,11 +392,16 @@ hipError_t start_dim(const AttendArgs& a, hipStream_t stream) {
 
 }  // namespace
 
+// Shares of a token's blocks: so many that about 1024 workgroups (4 for each compute unit) are at
+// work, each wave with a step of its own at least; at most 64 (the lanes of attend_join).
 int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
   const int64_t units = (int64_t)tokens * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
   if (units == 0) return 1;
-  const int64_t wanted = (512 + units - 1) / units, most = (blocks + kWaves - 1) / kWaves;
-  return (int)(wanted < most ? wanted : most > 1 ? most : 1);
+  const int step = c.dtype == SDNN_F32 ? 16 : 32;
+  const int64_t steps = (int64_t)blocks * (c.block / step);
+  const int64_t wanted = (1024 + units - 1) / units, most = (steps + kWaves - 1) / kWaves;
+  const int64_t s = wanted < most ? wanted : most;
+  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
 
 int64_t attend_floats(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
