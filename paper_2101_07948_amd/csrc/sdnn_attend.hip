@@ -5,6 +5,7 @@ namespace sdnn {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int kTileWaves = 8;
 constexpr int kRows = 16;  // queries of a tile: the columns of one matrix instruction
 
 struct AttendArgs {
@@ -23,6 +24,7 @@ struct AttendArgs {
   int32_t tokens, sequences, max_blocks;
   int32_t heads, kv_heads, group, head_tiles, head_dim, block;
   int32_t blocks, splits;
+  int32_t tile_tokens;    // 0: attend_kernel; else attend_tiles, tokens of a wave's tile
   float scale2;           // scale * log2 e
   int32_t q_aligned, o_aligned;
 };
@@ -53,22 +55,22 @@ struct Step16 {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) {
-        const int d = (c * 4 + g) * 8;
-        kk[h * CHUNKS + c] = V8{};
-        if (d < D) kk[h * CHUNKS + c] = *reinterpret_cast<const V8*>(k + token(h, r) * D + d);
+        const int d = min((c * 4 + g) * 8, D - 8);  // past the head's end: any of its values, q is 0 there
+        kk[h * CHUNKS + c] = *reinterpret_cast<const V8*>(k + token(h, r) * D + d);
       }
 #pragma unroll
     for (int c = 0; c < 2 * CHUNKS; ++c)
       vv[c] = *reinterpret_cast<const V8*>(v + min(c * 16 + r, D - 1) * P + 8 * g);
   }
 
-  template <int CHUNKS>
-  static __device__ __forceinline__ void scores(const V8 (&kk)[2 * CHUNKS], const V8 (&q)[CHUNKS], float (&s)[8]) {
+  // kk(i), vv(i): piece i of the step's keys and values (what `load` puts there).
+  template <int CHUNKS, typename K>
+  static __device__ __forceinline__ void scores(const K& kk, const V8 (&q)[CHUNKS], float (&s)[8]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) acc = mfma(kk[h * CHUNKS + c], q[c], acc);
+      for (int c = 0; c < CHUNKS; ++c) acc = mfma(kk(h * CHUNKS + c), q[c], acc);
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[4 * h + i] = acc[i];
     }
@@ -76,8 +78,9 @@ struct Step16 {
 
   // o += p v.  p is split into two 16-bit parts, so that it counts with all the bits that the sum
   // of probabilities counts it with (one part would add an error as large as the rounding of o).
-  template <int CHUNKS>
-  static __device__ __forceinline__ void accumulate(V8 (&vv)[2 * CHUNKS], const float (&p)[8], int g, int seen,
+  // PART: tokens from `stored` on may hold anything (their p is 0).
+  template <bool PART, int CHUNKS, typename V>
+  static __device__ __forceinline__ void accumulate(const V& vv, const float (&p)[8], int g, int stored,
                                                     f32x4 (&o)[2 * CHUNKS]) {
     V8 hi, lo;
 #pragma unroll
@@ -87,13 +90,14 @@ struct Step16 {
     }
 #pragma unroll
     for (int c = 0; c < 2 * CHUNKS; ++c) {
-      if (seen < kTokens) {  // past the sequence's end a page holds anything
+      V8 x = vv(c);
+      if (PART) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (8 * g + j >= seen) vv[c][j] = (T)0.0f;
+          if (8 * g + j >= stored) x[j] = (T)0.0f;
       }
-      o[c] = mfma(vv[c], hi, o[c]);
-      o[c] = mfma(vv[c], lo, o[c]);
+      o[c] = mfma(x, hi, o[c]);
+      o[c] = mfma(x, lo, o[c]);
     }
   }
 };
@@ -122,38 +126,40 @@ struct Step<float> {
                                               f32x4 (&kk)[CHUNKS], f32x4 (&vv)[CHUNKS]) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-      const int d = (c * 4 + g) * 4;
-      kk[c] = f32x4{0, 0, 0, 0};
-      if (d < D) kk[c] = *reinterpret_cast<const f32x4*>(k + r * D + d);
+      const int d = min((c * 4 + g) * 4, D - 4);
+      kk[c] = *reinterpret_cast<const f32x4*>(k + r * D + d);
     }
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
       vv[c] = *reinterpret_cast<const f32x4*>(v + min(c * 16 + r, D - 1) * P + 4 * g);
   }
 
-  template <int CHUNKS>
-  static __device__ __forceinline__ void scores(const f32x4 (&kk)[CHUNKS], const f32x4 (&q)[CHUNKS], float (&s)[4]) {
+  template <int CHUNKS, typename K>
+  static __device__ __forceinline__ void scores(const K& kk, const f32x4 (&q)[CHUNKS], float (&s)[4]) {
     f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
+    for (int c = 0; c < CHUNKS; ++c) {
+      const f32x4 x = kk(c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[c][e], q[c][e], acc, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], q[c][e], acc, 0, 0, 0);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = acc[i];
   }
 
-  template <int CHUNKS>
-  static __device__ __forceinline__ void accumulate(f32x4 (&vv)[CHUNKS], const float (&p)[4], int g, int seen,
+  template <bool PART, int CHUNKS, typename V>
+  static __device__ __forceinline__ void accumulate(const V& vv, const float (&p)[4], int g, int stored,
                                                     f32x4 (&o)[CHUNKS]) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-      if (seen < kTokens) {
+      f32x4 x = vv(c);
+      if (PART) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (4 * g + j >= seen) vv[c][j] = 0.0f;
+          if (4 * g + j >= stored) x[j] = 0.0f;
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[c][e], p[e], o[c], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], p[e], o[c], 0, 0, 0);
     }
   }
 };
@@ -175,10 +181,10 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// Tokens [0, seen) of the step's are within the query's sight (seen > 0).
-template <typename T, int CHUNKS, int TILES, int PIECES>
-__device__ __forceinline__ void attend_step(float scale2, const typename Step<T>::Piece (&kk)[PIECES],
-                                            typename Step<T>::Piece (&vv)[PIECES], int seen,
+// One step: tokens [0, seen) of its are within the sight of this lane's query, tokens from `stored` on may
+// hold anything.  EMPTY: queries may have seen nothing yet (their maximum is -infinity) and see nothing here.
+template <bool EMPTY, typename T, int CHUNKS, int TILES, typename K, typename V>
+__device__ __forceinline__ void attend_step(float scale2, const K& kk, const V& vv, int seen, int stored,
                                             const typename Step<T>::Piece (&q)[CHUNKS], int g, State<TILES>& st) {
   constexpr int N = Step<T>::kTokens, E = N / 4;
   float s[E];
@@ -192,20 +198,25 @@ __device__ __forceinline__ void attend_step(float scale2, const typename Step<T>
   top = over_groups_max(top);
   if (__any(top > st.m)) {
     const float m = fmaxf(st.m, top);
-    const float f = __builtin_amdgcn_exp2f(st.m - m);  // 0 for the first step (m is finite)
+    // 0 where this is the first step that the query sees
+    const float f = EMPTY && m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - m);
     st.l *= f;
     st.m = m;
 #pragma unroll
     for (int c = 0; c < TILES; ++c) st.o[c] *= f;
   }
+  const float m = EMPTY && st.m == -INFINITY ? 0.0f : st.m;
   float sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < E; ++j) {
-    s[j] = __builtin_amdgcn_exp2f(s[j] - st.m);
+    s[j] = __builtin_amdgcn_exp2f(s[j] - m);
     sum += s[j];
   }
   st.l += sum;
-  Step<T>::template accumulate<CHUNKS>(vv, s, g, seen, st.o);
+  if (stored < N)
+    Step<T>::template accumulate<true, CHUNKS>(vv, s, g, stored, st.o);
+  else
+    Step<T>::template accumulate<false, CHUNKS>(vv, s, g, stored, st.o);
 }
 
 // A workgroup handles one token, cached head, tile of up to 16 of its queries and share of its
@@ -261,7 +272,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
     typename Step<T>::Piece kk[TILES], vv[TILES];
     Step<T>::template load<CHUNKS>(static_cast<const T*>(a.k_pages) + at + (int64_t)t0 * D,
                                    static_cast<const T*>(a.v_pages) + at + t0, D, a.block, r, g, kk, vv);
-    attend_step<T, CHUNKS, TILES>(a.scale2, kk, vv, seen, q, g, st);
+    attend_step<false, T, CHUNKS, TILES>(a.scale2, [&](int i) { return kk[i]; }, [&](int i) { return vv[i]; }, seen,
+                                         seen, q, g, st);
   }
 
   // join the waves: 2 and 3 into 0 and 1, then 1 into 0
@@ -371,8 +383,257 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
   if (lane == 0 && a.lse) a.lse[row] = l > 0.0f ? (top + __log2f(l)) * 0.693147181f : -INFINITY;
 }
 
+// ---------------------------------------------------------------- many tokens of a sequence
+
+// 16 bytes from global memory to LDS, one piece a lane: lane l's goes to `to` + 16 l (`to` is uniform over
+// the wave).
+__device__ __forceinline__ void copy_to_lds(const void* from, unsigned char* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// A stage of keys and values in LDS: STAGE tokens of a page, keys as rows of a head (of CHUNKS * 64 bytes,
+// also where the head is shorter), values as rows of STAGE tokens.  A row's 16-byte pieces are permuted by the
+// row (piece x at x ^ swap) so that the 16 rows that a wave reads one piece of lie in different banks.
+template <typename T, int CHUNKS, int STAGE>
+struct Tile {
+  static constexpr int kPiece = 16 / sizeof(T);
+  static constexpr int kKeyPieces = CHUNKS * 4, kValuePieces = STAGE / kPiece;
+  static constexpr int kDims = CHUNKS * 4 * kPiece;
+  static constexpr int kBytes = STAGE * kKeyPieces * 16;  // of either
+  static_assert(kDims * kValuePieces * 16 == kBytes, "both hold the same values");
+  static __device__ __forceinline__ int key_swap(int row) {
+    const int x = sizeof(T) == 4 ? row & 15 : (row & 3) | (row >> 3 & 3) << 2;  // see Step16::token
+    return x & (kKeyPieces - 1);
+  }
+  static __device__ __forceinline__ int value_swap(int d) {
+    return kValuePieces >= 8 ? d & (kValuePieces - 1) & 15 : d >> 1 & (kValuePieces - 1);
+  }
+  // Starts the copies of `tokens` tokens (at most STAGE) by all THREADS threads.
+  template <int THREADS>
+  static __device__ __forceinline__ void fetch(const T* k, const T* v, int tokens, int D, int P, unsigned char* lds) {
+    // Pieces past a row's end, and rows past the last, stay out.  The rows that a thread copies pieces of lie
+    // KR (VR) apart: mostly so far that the permutation is the same in all of them.
+    const int wave = threadIdx.x / 64;
+    constexpr int KR = THREADS / kKeyPieces, VR = THREADS / kValuePieces;
+    constexpr bool SAME = KR % (sizeof(T) == 4 ? 16 : 32) == 0;
+    static_assert(VR % 16 == 0, "value_swap has a period of at most 16");
+    {
+      const int row = threadIdx.x / kKeyPieces, piece = threadIdx.x % kKeyPieces;
+      const T* from = k + row * D;
+#pragma unroll
+      for (int i = 0; i < STAGE / KR; ++i) {
+        const int x = piece ^ key_swap(SAME ? row : row + i * KR);
+        if (x * kPiece < D && row + i * KR < tokens)
+          copy_to_lds(from + i * KR * D + x * kPiece, lds + (i * THREADS + wave * 64) * 16);
+      }
+    }
+    {
+      const int d = threadIdx.x / kValuePieces, x = (threadIdx.x % kValuePieces) ^ value_swap(d);
+      const T* from = v + d * P + x * kPiece;
+      if (x * kPiece < tokens) {
+#pragma unroll
+        for (int i = 0; i < kDims / VR; ++i)
+          if (d + i * VR < D) copy_to_lds(from + i * VR * P, lds + kBytes + (i * THREADS + wave * 64) * 16);
+      }
+    }
+  }
+  static __device__ __forceinline__ const unsigned char* key(const unsigned char* lds, int row, int piece) {
+    return lds + (row * kKeyPieces + (piece ^ key_swap(row))) * 16;
+  }
+  static __device__ __forceinline__ const unsigned char* value(const unsigned char* lds, int d, int piece) {
+    return lds + kBytes + (d * kValuePieces + (piece ^ value_swap(d))) * 16;
+  }
+};
+
+// Piece i of the keys and of the values of the step of tokens t0 ... of a stage (see Step::load).
+template <typename T, int CHUNKS, int STAGE>
+__device__ __forceinline__ typename Step<T>::Piece key_piece(const unsigned char* lds, int i, int t0, int D, int r, int g) {
+  typedef Tile<T, CHUNKS, STAGE> L;
+  const int x = min(i % CHUNKS * 4 + g, D / L::kPiece - 1);
+  const int row = t0 + (sizeof(T) == 4 ? r : 8 * (r >> 2) + 4 * (i / CHUNKS) + (r & 3));
+  return *reinterpret_cast<const typename Step<T>::Piece*>(L::key(lds, row, x));
+}
+template <typename T, int CHUNKS, int STAGE>
+__device__ __forceinline__ typename Step<T>::Piece value_piece(const unsigned char* lds, int i, int t0, int r, int g) {
+  typedef Tile<T, CHUNKS, STAGE> L;
+  return *reinterpret_cast<const typename Step<T>::Piece*>(L::value(lds, i * 16 + r, t0 / L::kPiece + g));
+}
+
+// Where a query is in the list of its blocks: the one it attends to next with its page, and what follows
+// it, loaded ahead so that no step waits for a list.
+struct Cursor {
+  int32_t t, seq, n, j, own;
+  int32_t id, page, next_id, next_page, after;
+  __device__ __forceinline__ int32_t block(const AttendArgs& a, int h, int i) const {
+    return i >= n ? -1 : a.chosen ? a.chosen[((int64_t)t * a.kv_heads + h) * a.blocks + i] : i;
+  }
+  __device__ __forceinline__ bool valid(const AttendArgs& a, int32_t b) const {
+    return b >= 0 && b <= own && b < a.max_blocks;
+  }
+  __device__ __forceinline__ int32_t page_of(const AttendArgs& a, int32_t b) const {
+    return valid(a, b) ? a.table[(int64_t)seq * a.max_blocks + b] : -1;
+  }
+  __device__ __forceinline__ void start(const AttendArgs& a, int h) {
+    id = block(a, h, 0), next_id = block(a, h, 1), after = block(a, h, 2), j = 2;
+    page = page_of(a, id), next_page = page_of(a, next_id);
+  }
+  __device__ __forceinline__ void advance(const AttendArgs& a, int h) {
+    id = next_id, page = next_page;
+    next_id = after, next_page = page_of(a, after);
+    after = block(a, h, ++j);
+  }
+};
+
+// Attention of many tokens of a sequence.  A wave has a tile of 16 queries, 16 / group neighbouring tokens of one
+// cached head; the WAVES waves of a workgroup, neighbouring tokens again, walk the union of their lists, block
+// by block in ascending order, through LDS: a block is read from L2 once for all of them, the next one while
+// they compute.  Waves whose tokens did not choose a block skip it; rows of a tile that did not are masked.
+// The union is found on the way, a block ahead: each wave offers its lowest block not yet passed.
+template <typename T, int CHUNKS, int STAGE, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void attend_tiles(AttendArgs a) {
+  typedef Tile<T, CHUNKS, STAGE> L;
+  constexpr int TILES = CHUNKS * L::kPiece / 4, N = Step<T>::kTokens;
+  constexpr int32_t END = 0x7fffffff;
+  __shared__ __align__(16) unsigned char lds[2][2 * L::kBytes];
+  __shared__ uint64_t turns[2];
+  __shared__ int2 offers[2][WAVES];  // key and page of each wave's lowest block
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane & 15, g = lane >> 4;
+  int b = blockIdx.x;
+  const int h = b % a.kv_heads;
+  b /= a.kv_heads;
+  const int first = b % a.head_tiles * kRows;
+  const int t0 = b / a.head_tiles * (a.tile_tokens * WAVES);
+  const int rows = min(kRows, a.group - first);     // queries of a token
+  const int per_token = kRows / a.tile_tokens;      // rows of the tile for a token (a power of two)
+  const int t = t0 + wave * a.tile_tokens + r / per_token, qr = r % per_token;
+  const bool row = t < a.tokens && qr < rows;
+  const int head = h * a.group + first + qr;
+  const int D = a.head_dim;
+  typename Step<T>::Piece q[CHUNKS];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int d = (c * 4 + g) * L::kPiece;
+    T x[L::kPiece] = {};
+    if (row && d < D)
+      load_n<L::kPiece>(static_cast<const T*>(a.q) + t * a.q_token + head * a.q_head + d, a.q_aligned, x);
+    __builtin_memcpy(&q[c], x, sizeof(x));
+  }
+  State<TILES> st;
+#pragma unroll
+  for (int c = 0; c < TILES; ++c) st.o[c] = f32x4{0, 0, 0, 0};
+  st.m = -INFINITY, st.l = 0.0f;
+
+  // A block's key: the run of tokens of one sequence within the workgroup's, then the block.
+  // Bit i of `turns`: token i is of another sequence than token i - 1 (a workgroup has at most 16 WAVES).
+  static_assert(16 * WAVES <= 128, "two words of bits");
+  if (wave < 2) {
+    const int i = wave * 64 + lane, ti = t0 + i;
+    const bool turn = i > 0 && i < a.tile_tokens * WAVES && ti < a.tokens && a.seq[ti] != a.seq[ti - 1];
+    const uint64_t bits = __ballot(turn);
+    if (lane == 0) turns[wave] = bits;
+  }
+  int32_t p = -1, seq = -1;
+  if (t < a.tokens) p = a.pos[t], seq = a.seq[t];
+  __syncthreads();
+  const int place = t - t0;
+  const int32_t run = __popcll(turns[0] & (place >= 63 ? ~0ull : (2ull << place) - 1)) +
+                      (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
+  const bool filler = p < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
+  Cursor at;
+  at.t = t, at.seq = seq, at.own = p / a.block;
+  at.n = filler ? 0 : a.chosen ? a.blocks : min(at.own + 1, a.max_blocks);
+  at.start(a, h);
+  const auto key = [&] { return at.valid(a, at.id) ? run << 20 | at.id : END; };
+  const auto offer = [&](int parity) {
+    int32_t k = key();
+    for (int s = per_token; s < 16; s <<= 1) k = min(k, __shfl_xor(k, s));
+    const int from = __builtin_ctzll(__ballot(key() == k));
+    const int32_t page = __shfl(at.page, from);
+    if (lane == 0) offers[parity][wave] = make_int2(k, page);
+  };
+  // The lowest of all offers; what this lane's query sees of it is left in `seen`, and it is passed.
+  int32_t block_key = END, block_page = -1, seen = 0;
+  const auto take = [&](int parity) {
+    int2 low = offers[parity][0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      const int2 x = offers[parity][w];
+      if (x.x < low.x) low = x;
+    }
+    block_key = __builtin_amdgcn_readfirstlane(low.x), block_page = __builtin_amdgcn_readfirstlane(low.y);
+    if (block_page < 0 || block_page >= a.pages) block_page = -1;
+    const bool mine = block_key != END && key() == block_key;
+    seen = mine && block_page >= 0 ? min(a.block, p - at.id * a.block + 1) : 0;
+    if (mine) at.advance(a, h);
+  };
+  const int stage = min(STAGE, a.block), stages = a.block / stage;
+  const auto fetch = [&](int s, int buffer) {
+    if (block_page < 0) return;
+    const int64_t from = ((int64_t)block_page * a.kv_heads + h) * a.block * D;
+    L::template fetch<WAVES * 64>(static_cast<const T*>(a.k_pages) + from + (int64_t)s * stage * D,
+                                  static_cast<const T*>(a.v_pages) + from + s * stage, stage, D, a.block, lds[buffer]);
+  };
+
+  int parity = 0, buffer = 0, s = 0;
+  offer(parity);
+  __syncthreads();
+  take(parity);
+  offer(parity ^= 1);
+  if (block_key != END) fetch(0, 0);
+  while (block_key != END) {
+    const int32_t now_seen = seen - s * stage;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // the stage is in LDS, the other buffer is free, the offers are made
+    if (++s == stages) {
+      s = 0;
+      take(parity);
+      if (block_key != END) offer(parity ^= 1);
+    }
+    if (block_key != END) fetch(s, buffer ^ 1);
+    for (int u = 0; u < stage; u += N) {
+      const int left = now_seen - u;
+      if (!__any(left > 0)) break;
+      // of the tokens past every query's sight the values are taken for zeros
+      int stored = N;
+      if (!__any(left >= N)) {
+        stored = max(left, 0);
+#pragma unroll
+        for (int x = 1; x < 16; x <<= 1) stored = max(stored, __shfl_xor(stored, x));
+      }
+      attend_step<true, T, CHUNKS, TILES>(
+          a.scale2, [&](int i) { return key_piece<T, CHUNKS, STAGE>(lds[buffer], i, u, D, r, g); },
+          [&](int i) { return value_piece<T, CHUNKS, STAGE>(lds[buffer], i, u, r, g); }, left, stored, q, g, st);
+    }
+    buffer ^= 1;
+  }
+
+  const float l = over_groups_sum(st.l);
+  if (!row) return;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  T* o = static_cast<T*>(a.o) + t * a.o_token + head * a.o_head;
+#pragma unroll
+  for (int c = 0; c < TILES; ++c) {
+    const int d = c * 16 + 4 * g;
+    if (d >= D) continue;
+    T x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (T)(st.o[c][i] * inv);
+    store_n<4>(o + d, a.o_aligned, x);
+  }
+  if (g == 0 && a.lse)
+    a.lse[(int64_t)t * a.heads + head] = l > 0.0f ? (st.m + __log2f(l)) * 0.693147181f : -INFINITY;
+}
+
 template <typename T, int CHUNKS>
 hipError_t start(const AttendArgs& a, hipStream_t stream) {
+  if (a.tile_tokens > 0) {
+    constexpr int STAGE = sizeof(T) == 2 ? (CHUNKS <= 4 ? 64 : 32) : CHUNKS <= 4 ? 64 : CHUNKS <= 8 ? 32 : 16;
+    const int64_t groups = (a.tokens + a.tile_tokens * kTileWaves - 1) / (a.tile_tokens * kTileWaves);
+    attend_tiles<T, CHUNKS, STAGE, kTileWaves>
+        <<<(unsigned)(groups * a.head_tiles * a.kv_heads), kTileWaves * 64, 0, stream>>>(a);
+    return hipGetLastError();
+  }
   const unsigned grid = (unsigned)((int64_t)a.tokens * a.head_tiles * a.splits * a.kv_heads);
   attend_kernel<T, CHUNKS><<<grid, kWaves * 64, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
@@ -390,6 +651,19 @@ hipError_t start_dim(const AttendArgs& a, hipStream_t stream) {
   return start<T, 4 * U>(a, stream);
 }
 
+}  // namespace
+
+namespace {
+// Tokens of a wave's tile in attend_tiles (a token's queries take a power of two of its 16 rows), or 0
+// where attend_kernel serves the call.
+int tile_tokens(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads) {
+  const int group = heads / c.kv_heads;
+  int rows = 1;
+  while (rows < group && rows < kRows) rows *= 2;
+  const int tile = kRows / rows;
+  const int64_t groups = (int64_t)(tokens / (tile * kTileWaves)) * c.kv_heads * ((group + kRows - 1) / kRows);
+  return max_blocks <= 1 << 20 && tokens >= (int64_t)16 * sequences && groups >= 128 ? tile : 0;
+}
 }  // namespace
 
 // Shares of a token's blocks: so many that about 1024 workgroups (4 for each compute unit) are at
@@ -422,7 +696,8 @@ hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.heads = q.heads, a.kv_heads = c.kv_heads, a.group = q.heads / c.kv_heads;
   a.head_tiles = (a.group + kRows - 1) / kRows;
   a.head_dim = c.head_dim, a.block = c.block;
-  a.blocks = blocks, a.splits = attend_splits(c, t.tokens, q.heads, blocks);
+  a.tile_tokens = tile_tokens(c, t.tokens, t.sequences, t.max_blocks, q.heads);
+  a.blocks = blocks, a.splits = a.tile_tokens ? 1 : attend_splits(c, t.tokens, q.heads, blocks);
   a.scale2 = scale * 1.44269504f;
   const int e = dtype_bytes(c.dtype), piece = 16 / e;
   a.q_aligned = (uintptr_t)q.data % 16 == 0 && q.token_stride % piece == 0 && q.head_stride % piece == 0;

@@ -137,3 +137,48 @@ def q4(packed, scales, zeros, K, group, x):
 def gelu(y):
     from math import erf, sqrt
     return np.vectorize(lambda v: 0.5 * v * (1.0 + erf(v / sqrt(2.0))))(y)
+
+
+def attend_many(q, pos, seq, table, k_pages, v_pages, chosen=None, scale=None):
+    """attend() for many tokens: all of a sequence's tokens and one head at a time, the tokens
+    that a query does not see masked out."""
+    T, H, D = q.shape
+    pages, Hk, P = k_pages.shape[:3]
+    S, width = table.shape
+    scale = D ** -0.5 if scale is None else scale
+    o, lse = np.zeros((T, H, D)), np.full((T, H), -np.inf)
+    o_tol, lse_tol = np.zeros((T, H, D)), np.zeros((T, H))
+    pos, seq = np.asarray(pos), np.asarray(seq)
+    for s in range(S):
+        ts = np.nonzero((seq == s) & (pos >= 0))[0]
+        if not len(ts):
+            continue
+        blocks = min(int(pos[ts].max()) // P + 1, width)
+        ok = (table[s, :blocks] >= 0) & (table[s, :blocks] < pages)
+        at = np.where(ok, table[s, :blocks], 0)
+        sight = (np.arange(blocks * P)[None] <= pos[ts][:, None]) & np.repeat(ok, P)[None]
+        for h in range(Hk):
+            k = np.nan_to_num(k_pages[at, h]).reshape(-1, D)
+            v = np.nan_to_num(v_pages[at, h]).transpose(0, 2, 1).reshape(-1, D)
+            seen = sight
+            if chosen is not None:
+                took = np.zeros((len(ts), blocks), bool)
+                for i, t in enumerate(ts):
+                    ids = chosen[t, h]
+                    took[i, ids[(ids >= 0) & (ids < blocks)]] = True
+                seen = sight & np.repeat(took, P, axis=1)
+            n = seen.sum(1)
+            some = n > 0
+            for g in range(h * H // Hk, (h + 1) * H // Hk):
+                x = q[ts, g] @ k.T * scale
+                x[~seen] = -np.inf
+                m = np.where(some, x.max(1), 0.0)
+                p = np.exp(x - m[:, None])
+                total = np.where(some, p.sum(1), 1.0)
+                mag = np.where(seen, np.abs(q[ts, g]) @ np.abs(k).T * abs(scale), 0.0).max(1)
+                e = (D + 8) * 2.0 ** -24 * mag + 2.0 ** -22
+                o[ts, g] = (p @ v) / total[:, None]
+                lse[ts, g] = np.where(some, m + np.log(total), -np.inf)
+                o_tol[ts, g] = ((4 * e + 2.0 ** -16 + 2 * n * 2.0 ** -24) / total)[:, None] * (p @ np.abs(v))
+                lse_tol[ts, g] = 2 * e + n * 2.0 ** -24 + 2.0 ** -21 * (1 + np.abs(np.where(some, lse[ts, g], 0.0)))
+    return o, lse, o_tol, lse_tol

@@ -331,13 +331,13 @@ def filled(seed, S, lens, Hk, P, D, dtype, spare=2):
     return cache, table
 
 
-def check_attend(cache, table, q, pos, seq, chosen=None, scale=None, how="plain", **kw):
+def check_attend(cache, table, q, pos, seq, chosen=None, scale=None, how="plain", oracle=od.attend, **kw):
     dtype, (T, H, D) = q.dtype, q.shape
     out = strided(torch.full((T, H, D), 7.0, dtype=dtype, device=DEV), how)
     lse = torch.full((T, H), 7.0, device=DEV)
     cache.attend(strided(q, how), out, i32(pos), i32(seq), i32(table), None if chosen is None else i32(chosen),
                  scale=scale, lse=lse, **kw)
-    o, l, ot, lt = od.attend(od.f64(q), pos, seq, table, np.nan_to_num(od.f64(cache.k_pages)),
+    o, l, ot, lt = oracle(od.f64(q), pos, seq, table, np.nan_to_num(od.f64(cache.k_pages)),
                              np.nan_to_num(od.f64(cache.v_pages)), chosen, scale)
     close(out, o, ot + od.U[dtype] * np.abs(o) * 1.01 + od.TINY[dtype], "out")
     got = lse.cpu().numpy().astype(np.float64)
@@ -402,6 +402,47 @@ def test_attend_prompt(dtype):
         ids = np.sort(rng.permutation(n)[: rng.integers(0, 4)])
         chosen[t, 0, : len(ids)] = ids
     check_attend(cache, table, randn(8, (195, Hq, D), dtype), pos, seq, chosen)
+
+
+def random_choice(seed, pos, Hk, blocks, P):
+    """Ascending random blocks that each token sees, half of them its neighbours' too; some lists empty."""
+    rng = np.random.default_rng(seed)
+    chosen = np.full((len(pos), Hk, blocks), -1, np.int32)
+    base = rng.random((Hk, max(pos) // P + 1))
+    for t, p in enumerate(pos):
+        for h in range(Hk):
+            n = p // P + 1
+            k = min(n, int(rng.integers(0, blocks + 1)))
+            order = np.argsort(base[h, :n] + 0.5 * rng.random(n))[:k] if n > 0 else []
+            chosen[t, h, :k] = np.sort(order)
+    return chosen
+
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("Hq,Hk,D,P,tokens,blocks,how", [
+    (32, 32, 64, 32, [700], 7, "plain"),            # a head of its own to each query: 16 tokens to a tile
+    (32, 8, 128, 64, [517, 100], 6, "padded"),
+    (64, 4, 96, 128, [300, 5, 40], 3, "odd"),       # 16 queries to a head: one token to a tile
+    (40, 8, 40, 64, [333], 4, "heads_first"),       # 5 queries to a head: a tile with empty rows
+    (34, 2, 256, 32, [260], 9, "plain"),            # 17: two tiles of a token, one nearly empty
+    (24, 24, 192, 128, [900], 4, "plain"),
+])
+def test_attend_many_tokens(dtype, Hq, Hk, D, P, tokens, blocks, how):
+    """Prompts: neighbouring tokens share the blocks that they read (attend_tiles), each seeing its
+    own past and its own list; every block, chosen ones, a chunk that starts late, fillers between
+    sequences, a missing page."""
+    late = 150
+    cache, table = filled(9, len(tokens), [n + late for n in tokens], Hk, P, D, dtype)
+    seq, pos = [], []
+    for s, n in enumerate(tokens):
+        seq += [s] * n + [s, 99]
+        pos += list(range(late, late + n)) + [-1, 3]
+    q = randn(10, (len(pos), Hq, D), dtype)
+    check_attend(cache, table, q, pos, seq, how=how, oracle=od.attend_many)
+    chosen = random_choice(4, pos, Hk, blocks, P)
+    chosen[:9] = -1                              # tokens that see nothing
+    table[0, 1] = cache.pages + 5
+    check_attend(cache, table, q, pos, seq, chosen, how=how, oracle=od.attend_many)
 
 
 @pytest.mark.parametrize("dtype", od.DTYPES)
