@@ -25,7 +25,8 @@ struct AttendArgs {
   int32_t heads, kv_heads, group, head_tiles, head_dim, block;
   int32_t blocks, splits;
   int32_t tile_tokens;    // 0: attend_kernel; else attend_tiles, tokens of a wave's tile
-  float scale2;           // scale * log2 e
+  float scale2;           // |scale| * log2 e
+  int32_t negate;         // scale < 0: the queries are negated
   int32_t q_aligned, o_aligned;
 };
 
@@ -164,8 +165,8 @@ struct Step<float> {
   }
 };
 
-// A wave's state: of query lane & 15 the running maximum (in units of log 2) and the lane's share of
-// the total (tokens of its lane group), and the sums o[c][i] of value 16 c + 4 (lane / 16) + i.
+// A wave's state: of query lane & 15 the reference that exponents are taken from (in units of log 2, see
+// attend_step) and the lane's share of the total (tokens of its lane group), and the sums o[c][i] of value 16 c + 4 (lane / 16) + i.
 template <int TILES>
 struct State {
   f32x4 o[TILES];
@@ -182,22 +183,27 @@ __device__ __forceinline__ float over_groups_sum(float x) {
 }
 
 // One step: tokens [0, seen) of its are within the sight of this lane's query, tokens from `stored` on may
-// hold anything.  EMPTY: queries may have seen nothing yet (their maximum is -infinity) and see nothing here.
+// hold anything.  EMPTY: queries may see nothing here (seen <= 0), or have seen nothing yet (m = -infinity).
+//   m is a reference near the running maximum rather than the maximum: it moves only where a score is over
+// 2^8 times above it, so that most steps neither reduce over lanes nor rescale the sums (p <= 2^8 costs no bits:
+// p is a float, and its 16-bit parts are floating too).  Scores are masked one by one only where a query's
+// sight ends within the step; a query that sees nothing of it gets m = infinity for the step, p = 0.
 template <bool EMPTY, typename T, int CHUNKS, int TILES, typename K, typename V>
 __device__ __forceinline__ void attend_step(float scale2, const K& kk, const V& vv, int seen, int stored,
                                             const typename Step<T>::Piece (&q)[CHUNKS], int g, State<TILES>& st) {
   constexpr int N = Step<T>::kTokens, E = N / 4;
+  constexpr float SLACK = 8.0f;
   float s[E];
   Step<T>::template scores<CHUNKS>(kk, q, s);
-  float top = -INFINITY;
+  if (!EMPTY || __any(seen > 0 && seen < N)) {
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    s[j] = E * g + j < seen ? s[j] * scale2 : -INFINITY;
-    top = fmaxf(top, s[j]);
+    for (int j = 0; j < E; ++j) s[j] = E * g + j < seen ? s[j] : -INFINITY;
   }
-  top = over_groups_max(top);
-  if (__any(top > st.m)) {
-    const float m = fmaxf(st.m, top);
+  float top = s[0];
+#pragma unroll
+  for (int j = 1; j < E; ++j) top = fmaxf(top, s[j]);
+  if (__any((!EMPTY || seen > 0) && top * scale2 > st.m + SLACK)) {
+    const float m = fmaxf(st.m, over_groups_max(!EMPTY || seen > 0 ? top * scale2 : -INFINITY));
     // 0 where this is the first step that the query sees
     const float f = EMPTY && m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - m);
     st.l *= f;
@@ -205,13 +211,12 @@ __device__ __forceinline__ void attend_step(float scale2, const K& kk, const V& 
 #pragma unroll
     for (int c = 0; c < TILES; ++c) st.o[c] *= f;
   }
-  const float m = EMPTY && st.m == -INFINITY ? 0.0f : st.m;
-  float sum = 0.0f;
+  const float m = !EMPTY || seen > 0 ? st.m : INFINITY;
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    s[j] = __builtin_amdgcn_exp2f(s[j] - m);
-    sum += s[j];
-  }
+  for (int j = 0; j < E; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], scale2, -m));
+  float sum = s[0];
+#pragma unroll
+  for (int j = 1; j < E; ++j) sum += s[j];
   st.l += sum;
   if (stored < N)
     Step<T>::template accumulate<true, CHUNKS>(vv, s, g, stored, st.o);
@@ -228,7 +233,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
   constexpr int TILES = CHUNKS * PIECE / 4;  // of 16 values of a head
   __shared__ float sums[2][kRows][TILES * 16 + 4];
   __shared__ float tops[kWaves][kRows], totals[kWaves][kRows];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane & 15, g = lane >> 4;
   int b = blockIdx.x;
   const int h = b % a.kv_heads;
   b /= a.kv_heads;
@@ -239,6 +245,26 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
   const int rows = min(kRows, a.group - first);
   const int64_t head = (int64_t)h * a.group + first + r;  // of this lane
   const int D = a.head_dim;
+  const int32_t p = a.pos[t], seq = a.seq[t];
+  const bool filler = p < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
+  const int own = p / a.block;
+  const int n = filler ? 0 : a.chosen ? a.blocks : min(own + 1, a.max_blocks);
+  const int32_t* chosen = a.chosen ? a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks : nullptr;
+  const int32_t* table = a.table + (int64_t)seq * a.max_blocks;
+  // Steps of all blocks, dealt to the waves of all shares in turn.  The block of the next step but one and the
+  // page of the next are looked up (by scalar loads) while this one's keys and values arrive; those are all
+  // asked for before the first product (left to itself the compiler takes them one by one, to save registers).
+  constexpr int N = Step<T>::kTokens;
+  const int per_block = a.block / N, deal = a.splits * kWaves, last = n * per_block;
+  const auto block_of = [&](int u) {
+    if (u >= last) return -1;
+    const int id = chosen ? chosen[u / per_block] : u / per_block;
+    return id > own || id >= a.max_blocks ? -1 : id;
+  };
+  const auto page_of = [&](int id) { return id < 0 ? -1 : table[id]; };
+  int u = split * kWaves + wave;
+  int id = block_of(u), next_id = block_of(u + deal);
+  int page = page_of(id);
   typename Step<T>::Piece q[CHUNKS];
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
@@ -247,33 +273,26 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
     if (r < rows && d < D)
       load_n<PIECE>(static_cast<const T*>(a.q) + t * a.q_token + head * a.q_head + d, a.q_aligned, x);
     __builtin_memcpy(&q[c], x, sizeof(x));
+    if (a.negate) q[c] = -q[c];
   }
   State<TILES> st;
 #pragma unroll
   for (int c = 0; c < TILES; ++c) st.o[c] = f32x4{0, 0, 0, 0};
   st.m = -INFINITY, st.l = 0.0f;
-  const int32_t p = a.pos[t], seq = a.seq[t];
-  const bool filler = p < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
-  const int own = p / a.block;
-  const int n = filler ? 0 : a.chosen ? a.blocks : min(own + 1, a.max_blocks);
-  const int32_t* chosen = a.chosen ? a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks : nullptr;
-  const int32_t* table = a.table + (int64_t)seq * a.max_blocks;
-  // steps of all blocks, dealt to the waves of all shares in turn
-  constexpr int N = Step<T>::kTokens;
-  const int per_block = a.block / N;
-  for (int u = split * kWaves + wave; u < n * per_block; u += a.splits * kWaves) {
-    const int j = u / per_block, t0 = (u - j * per_block) * N;
-    const int id = chosen ? chosen[j] : j;
-    if (id < 0 || id > own || id >= a.max_blocks) continue;
-    const int64_t page = table[id];
+  for (; u < last; u += deal) {
+    const int after = block_of(u + 2 * deal), next_page = page_of(next_id);
+    const int t0 = u % per_block * N;
     const int seen = p - id * a.block + 1 - t0;
-    if (page < 0 || page >= a.pages || seen <= 0) continue;
-    const int64_t at = (page * a.kv_heads + h) * (int64_t)a.block * D;
-    typename Step<T>::Piece kk[TILES], vv[TILES];
-    Step<T>::template load<CHUNKS>(static_cast<const T*>(a.k_pages) + at + (int64_t)t0 * D,
-                                   static_cast<const T*>(a.v_pages) + at + t0, D, a.block, r, g, kk, vv);
-    attend_step<false, T, CHUNKS, TILES>(a.scale2, [&](int i) { return kk[i]; }, [&](int i) { return vv[i]; }, seen,
-                                         seen, q, g, st);
+    if (page >= 0 && page < a.pages && seen > 0) {
+      const int64_t at = ((int64_t)page * a.kv_heads + h) * a.block * D;
+      typename Step<T>::Piece kk[TILES], vv[TILES];
+      Step<T>::template load<CHUNKS>(static_cast<const T*>(a.k_pages) + at + t0 * D,
+                                     static_cast<const T*>(a.v_pages) + at + t0, D, a.block, r, g, kk, vv);
+      __builtin_amdgcn_sched_barrier(0);
+      attend_step<false, T, CHUNKS, TILES>(a.scale2, [&](int i) { return kk[i]; }, [&](int i) { return vv[i]; },
+                                           seen, seen, q, g, st);
+    }
+    id = next_id, next_id = after, page = next_page;
   }
 
   // join the waves: 2 and 3 into 0 and 1, then 1 into 0
@@ -416,6 +435,7 @@ struct Tile {
     // KR (VR) apart: mostly so far that the permutation is the same in all of them.
     const int wave = threadIdx.x / 64;
     constexpr int KR = THREADS / kKeyPieces, VR = THREADS / kValuePieces;
+    const bool whole = D == kDims && tokens == STAGE;
     constexpr bool SAME = KR % (sizeof(T) == 4 ? 16 : 32) == 0;
     static_assert(VR % 16 == 0, "value_swap has a period of at most 16");
     {
@@ -424,17 +444,17 @@ struct Tile {
 #pragma unroll
       for (int i = 0; i < STAGE / KR; ++i) {
         const int x = piece ^ key_swap(SAME ? row : row + i * KR);
-        if (x * kPiece < D && row + i * KR < tokens)
+        if (whole || (x * kPiece < D && row + i * KR < tokens))
           copy_to_lds(from + i * KR * D + x * kPiece, lds + (i * THREADS + wave * 64) * 16);
       }
     }
     {
       const int d = threadIdx.x / kValuePieces, x = (threadIdx.x % kValuePieces) ^ value_swap(d);
       const T* from = v + d * P + x * kPiece;
-      if (x * kPiece < tokens) {
+      if (whole || x * kPiece < tokens) {
 #pragma unroll
         for (int i = 0; i < kDims / VR; ++i)
-          if (d + i * VR < D) copy_to_lds(from + i * VR * P, lds + kBytes + (i * THREADS + wave * 64) * 16);
+          if (whole || d + i * VR < D) copy_to_lds(from + i * VR * P, lds + kBytes + (i * THREADS + wave * 64) * 16);
       }
     }
   }
@@ -518,6 +538,7 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
     if (row && d < D)
       load_n<L::kPiece>(static_cast<const T*>(a.q) + t * a.q_token + head * a.q_head + d, a.q_aligned, x);
     __builtin_memcpy(&q[c], x, sizeof(x));
+    if (a.negate) q[c] = -q[c];
   }
   State<TILES> st;
 #pragma unroll
@@ -698,7 +719,9 @@ hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.head_dim = c.head_dim, a.block = c.block;
   a.tile_tokens = tile_tokens(c, t.tokens, t.sequences, t.max_blocks, q.heads);
   a.blocks = blocks, a.splits = a.tile_tokens ? 1 : attend_splits(c, t.tokens, q.heads, blocks);
-  a.scale2 = scale * 1.44269504f;
+  // (a scale of 0 makes all scores equal: so does one that is too small to part them)
+  a.scale2 = fmaxf(fabsf(scale), 1e-30f) * 1.44269504f;
+  a.negate = scale < 0.0f;
   const int e = dtype_bytes(c.dtype), piece = 16 / e;
   a.q_aligned = (uintptr_t)q.data % 16 == 0 && q.token_stride % piece == 0 && q.head_stride % piece == 0;
   a.o_aligned = (uintptr_t)o.data % (4 * e) == 0 && o.token_stride % 4 == 0 && o.head_stride % 4 == 0;
