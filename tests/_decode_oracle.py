@@ -65,18 +65,18 @@ def choose(q, pos, seq, table, means, scales, block, blocks, sink, local):
             if n <= blocks:
                 out[t, h, :n] = np.arange(n)
                 continue
-            score = np.full(n, -np.inf)
-            for b in range(sink, n - local):
-                page = table[seq[t], b]
-                if not 0 <= page < pages:
-                    continue
-                best = -np.inf
-                for g in range(h * H // Hk, (h + 1) * H // Hk):
-                    a = np.max(np.abs(q[t, g]))
-                    f = np.float32(127.0) * (np.float32(1.0) / a) if a > 0 else np.float32(0)
-                    m = np.rint(q[t, g] * f).astype(np.int64)
-                    best = max(best, np.float32(m @ means[page, h].astype(np.int64)) * a)
-                score[b] = np.float32(best) * scales[page, h]
+            x = q[t, h * H // Hk:(h + 1) * H // Hk]
+            top = np.abs(x).max(1, keepdims=True)
+            f = np.where(top > 0, np.float32(127.0) * (np.float32(1.0) / np.where(top > 0, top, np.float32(1))),
+                         np.float32(0))
+            m = np.rint(x * f).astype(np.int64)
+            page = table[seq[t], :n].astype(np.int64)
+            there = (page >= 0) & (page < pages)
+            at = np.where(there, page, 0)
+            dot = (m @ means[at, h].astype(np.int64).T).astype(np.float32)
+            score = (dot * top).max(0) * scales[at, h]
+            assert score.dtype == np.float32
+            score = np.where(there, score.astype(np.float64), -np.inf)
             forced = set(range(sink)) | set(range(n - local, n))
             rest = sorted((b for b in range(n) if b not in forced), key=lambda b: (-score[b], b))
             out[t, h] = sorted(forced | set(rest[: blocks - len(forced)]))

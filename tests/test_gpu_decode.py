@@ -271,6 +271,33 @@ def test_select(dtype, Hq, Hk, D, P, blocks, sink, local, ctx):
     assert np.array_equal(chosen.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("Hq,Hk,D,P,blocks,sink,local,tokens", [
+    (32, 8, 128, 64, 9, 1, 2, [(300, 6000), (40, 0)]),   # four tokens to a tile, two sequences and fillers
+    (16, 16, 64, 32, 4, 0, 1, [(700, 3000)]),            # sixteen
+    (20, 4, 40, 32, 6, 2, 3, [(517, 32 * 500)]),         # five queries: eight rows, two tokens
+    (24, 12, 256, 128, 33, 1, 1, [(515, 128 * 900)]),    # two queries: eight tokens
+])
+def test_select_many_tokens(dtype, Hq, Hk, D, P, blocks, sink, local, tokens):
+    """Prompts: several tokens share what they read of the summaries (tiles), each choosing for
+    itself; a missing page, fillers, a sequence out of range."""
+    seq, pos = [], []
+    for s, (n, start) in enumerate(tokens):
+        seq += [s] * n + [s, 50]
+        pos += list(range(start, start + n)) + [-1, 9]
+    S, width = len(tokens), max(pos) // P + 1
+    means, scales = random_means(11, S * width, Hk, D)
+    table = np.random.default_rng(6).permutation(S * width).reshape(S, width).astype(np.int32)
+    table[0, sink + 2] = -1
+    q = randn(12, (len(pos), Hq, D), dtype)
+    cache = sd.BlockCache(None, None, means, scales, block=P)
+    chosen = torch.full((len(pos), Hk, blocks), 77, dtype=torch.int32, device=DEV)
+    cache.select(strided(q, "padded"), i32(pos), i32(seq), i32(table), chosen, sink=sink, local=local)
+    want = od.choose(q.float().cpu().numpy(), pos, seq, table, means.cpu().numpy(), scales.cpu().numpy(), P, blocks,
+                     sink, local)
+    assert np.array_equal(chosen.cpu().numpy(), want)
+
+
 def test_select_ties_fillers_and_missing_pages():
     """Equal scores go to the lower block, zero queries score zero everywhere, -0 is 0, a missing
     page is taken last, fillers choose nothing."""
