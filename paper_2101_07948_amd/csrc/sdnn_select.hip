@@ -17,13 +17,15 @@ struct SelectArgs {
   int32_t tokens, sequences, max_blocks;
   int32_t kv_heads, group, head_dim, block_shift;
   int32_t blocks, sink, local;
-  int32_t tile, per_token;  // tokens of a workgroup, rows of a token (tile > 1: 1, 2, 4 or 8)
+  int32_t tile, per_token;  // tokens of a workgroup, rows of a token (up to 16: a power of two)
+  int32_t q_aligned;
 };
 
-// A number whose order as an unsigned integer is the order of the floats (-0 counts as 0).
+// A number whose order as an unsigned integer is the order of the floats (-0 counts as 0); below 2^32 - 1, so
+// that the next number exists.
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);
-  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+  return min(u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u), 0xfffffffeu);
 }
 
 // 16 bytes of a summary from byte k on, zeros past its end (D is a multiple of 8).
@@ -44,98 +46,224 @@ __device__ __forceinline__ i32x4 load_mean(const int8_t* row, int k, int D, bool
   return v;
 }
 
-// Sums of two counts over the workgroup's threads before this one.  `parts`: a word for each wave.
-__device__ __forceinline__ uint2 before(uint2 n, uint2* parts) {
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+// Sums of two counts over the workgroup's threads before this one, and over all of them.  `parts`: a word for
+// each wave.
+__device__ __forceinline__ uint2 before(uint2 n, uint2* parts, uint2* all) {
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
   uint2 s = n;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const uint32_t x = __shfl_up(s.x, d), y = __shfl_up(s.y, d);
     if (lane >= d) s.x += x, s.y += y;
   }
-  __syncthreads();
   if (lane == 63) parts[wave] = s;
   __syncthreads();
   uint2 r = make_uint2(s.x - n.x, s.y - n.y);
-  for (int w = 0; w < wave; ++w) r.x += parts[w].x, r.y += parts[w].y;
+  *all = make_uint2(0, 0);
+  for (int w = 0; w < waves; ++w) {
+    if (w < wave) r.x += parts[w].x, r.y += parts[w].y;
+    all->x += parts[w].x, all->y += parts[w].y;
+  }
   return r;
 }
 
-constexpr int kMaxWaves = 16;
-constexpr int kWaveKeys = 16;  // keys of a lane where a wave selects alone: up to 1024 blocks
-
-// What is taken: all keys above `above`, and of those equal to it the first `equal`.
-struct Threshold {
-  uint32_t above, equal;
-};
-
-// The `want` largest of a wave's keys (want >= 1, fewer than count), bit by bit from the top: `t` is the
-// largest prefix with at least `want` keys at or over it.  Most searches end early, at a prefix that exactly
-// `want` reach.
-__device__ __forceinline__ Threshold wave_threshold(const uint32_t (&key)[kWaveKeys], int count, uint32_t want) {
+// The largest number that at least `want` of a wave's 64 keys reach (0 if fewer are above 0), bit by bit
+// from the top, or a smaller one that exactly `want` reach.
+__device__ __forceinline__ uint32_t wave_kth(uint32_t key, uint32_t want) {
   uint32_t t = 0;
   for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
-    const uint32_t c = t | bit;
-    uint32_t n = 0;
-#pragma unroll
-    for (int i = 0; i < kWaveKeys; ++i)
-      if (i * 64 < count) n += __popcll(__ballot(key[i] >= c));  // (past the end a key is 0, and c is not)
-    if (n == want) return {c - 1, 0};
-    if (n > want) t = c;
+    const uint32_t n = __popcll(__ballot(key >= (t | bit)));
+    if (n >= want) t |= bit;
+    if (n == want) break;
   }
-  uint32_t more = 0;
-#pragma unroll
-  for (int i = 0; i < kWaveKeys; ++i)
-    if (i * 64 < count) more += __popcll(__ballot(key[i] > t));
-  return {t, want - more};
+  return t;
 }
 
-// The same over the keys of a workgroup in LDS, two bits at a time.  counts: [17][4], zero.
-__device__ __forceinline__ Threshold group_threshold(const uint32_t* key, int count, uint32_t want, uint32_t (*counts)[4]) {
-  const int threads = blockDim.x, lane = threadIdx.x % 64;
-  const int first = threadIdx.x - lane;
-  uint32_t t = 0;
-  for (int round = 0; round < 16; ++round) {
-    const int shift = 30 - 2 * round;
-    uint32_t n[3] = {0, 0, 0};
-    for (int i = first; i < count; i += threads) {
-      const uint32_t k = i + lane < count ? key[i + lane] : 0;
+// Writes the blocks of the `want` largest of a wave's keys in lane order, ties to the lower lane.  Lanes without
+// a key have 0 and are the last.
+__device__ __forceinline__ void write_largest(uint32_t key, int32_t block, uint32_t want, int32_t* chosen) {
+  const uint32_t t = wave_kth(key, want);
+  const uint64_t lower = (1ull << (threadIdx.x % 64)) - 1;
+  const uint64_t above = __ballot(key > t), same = __ballot(key == t);
+  const uint32_t left = want - __popcll(above);  // of the keys equal to t
+  const bool taken = key > t || (key == t && __popcll(same & lower) < left);
+  const uint64_t all = __ballot(taken);
+  if (taken) chosen[__popcll(all & lower)] = block;
+}
+
+// A key and its block that may be among the largest.
+struct Candidate {
+  uint32_t key;
+  int32_t block;
+};
+
+// Of one token's `count` keys in LDS a wave writes the blocks of the `want` largest in order (want < count).
+// The want-th largest of the lanes' own maxima is reached by at least `want` keys, and by few more: those are
+// put together, one to a lane, and searched again.  Where more than 64 reach it (or more are wanted), all keys
+// are searched.  KEYS: of a lane, 64 KEYS >= count.
+template <int KEYS>
+__device__ __forceinline__ void wave_choose(const uint32_t* keys, int count, uint32_t want, int32_t first, int32_t* chosen,
+                                            Candidate* few) {
+  const int lane = threadIdx.x % 64;
+  const uint64_t lower = (1ull << lane) - 1;
+  uint32_t key[KEYS], top = 0;
 #pragma unroll
-      for (int j = 0; j < 3; ++j) n[j] += __popcll(__ballot(k >= (t | (uint32_t)(j + 1) << shift)));
+  for (int i = 0; i < KEYS; ++i) {
+    key[i] = i * 64 + lane < count ? keys[i * 64 + lane] : 0;
+    top = max(top, key[i]);
+  }
+  uint32_t t = want <= 64 ? wave_kth(top, want) : 0, n = 0;
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) n += __popcll(__ballot(key[i] >= t));
+  if (t > 0 && n <= 64) {
+    uint32_t at = 0;
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
+      const uint64_t in = __ballot(key[i] >= t);
+      if (key[i] >= t) few[at + __popcll(in & lower)] = {key[i], first + i * 64 + lane};
+      at += __popcll(in);
     }
-    if (lane < 3 && n[0]) atomicAdd(&counts[round][lane], lane == 0 ? n[0] : lane == 1 ? n[1] : n[2]);
+    __threadfence_block();  // the wave's own writes
+    const Candidate c = lane < (int)n ? few[lane] : Candidate{0, 0};
+    write_largest(c.key, c.block, want, chosen);
+    return;
+  }
+  t = 0;
+  for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
+    n = 0;
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) n += __popcll(__ballot(key[i] >= (t | bit)));
+    if (n >= want) t |= bit;
+    if (n == want) break;
+  }
+  uint32_t left = want, at = 0, equal = 0;
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) left -= __popcll(__ballot(key[i] > t));
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    const bool same = i * 64 + lane < count && key[i] == t;
+    const uint64_t sames = __ballot(same);
+    const bool taken = key[i] > t || (same && equal + __popcll(sames & lower) < left);
+    const uint64_t all = __ballot(taken);
+    if (taken) chosen[at + __popcll(all & lower)] = first + i * 64 + lane;
+    at += __popcll(all), equal += __popcll(sames);
+  }
+}
+
+constexpr int kMaxWaves = 16;
+constexpr int kMaxTile = 64;
+constexpr int kWaveKeys = 16;  // keys of a lane where a wave chooses alone: up to 1024 blocks
+
+struct GroupLds {
+  uint32_t top[64];       // of the keys whose number is l modulo 64
+  uint32_t counts[16][4];
+  uint32_t few_of[kMaxWaves];
+  uint2 parts[kMaxWaves];
+};
+
+// The same by all waves of a workgroup, each with a run of the keys.  `g` is zero but for few_of.
+__device__ __forceinline__ void group_choose(const uint32_t* keys, int count, uint32_t want, int32_t first,
+                                             int32_t* chosen, Candidate* few, GroupLds& g) {
+  const int threads = blockDim.x, waves = threads / 64, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const uint64_t lower = (1ull << lane) - 1;
+  const int run = ((count + threads - 1) / threads) * 64;  // keys of a wave
+  const int i0 = min(wave * run, count), i1 = min(i0 + run, count);
+  uint32_t top = 0;
+  for (int i = i0 + lane; i < i1; i += 64) top = max(top, keys[i]);
+  atomicMax(&g.top[lane], top);
+  __syncthreads();
+  const uint32_t t = want <= 64 ? wave_kth(g.top[lane], want) : 0;
+  uint32_t n = 0;
+  for (int i = i0; i < i1; i += 64) n += __popcll(__ballot(i + lane < i1 && keys[i + lane] >= t));
+  if (lane == 0) g.few_of[wave] = n;
+  __syncthreads();
+  uint32_t at = 0, total = 0;
+  for (int w = 0; w < waves; ++w) {
+    at += w < wave ? g.few_of[w] : 0;
+    total += g.few_of[w];
+  }
+  if (t > 0 && total <= 64) {
+    for (int i = i0; i < i1; i += 64) {
+      const uint32_t k = i + lane < i1 ? keys[i + lane] : 0;
+      const uint64_t in = __ballot(k >= t);
+      if (k >= t) few[at + __popcll(in & lower)] = {k, first + i + lane};
+      at += __popcll(in);
+    }
     __syncthreads();
-    uint32_t next = t;
+    if (wave > 0) return;
+    const Candidate c = lane < (int)total ? few[lane] : Candidate{0, 0};
+    write_largest(c.key, c.block, want, chosen);
+    return;
+  }
+  // all keys, two bits a round
+  uint32_t s = 0;
+  bool exact = false;
+  for (int round = 0; round < 16 && !exact; ++round) {
+    const int shift = 30 - 2 * round;
+    uint32_t m[3] = {0, 0, 0};
+    for (int i = i0; i < i1; i += 64) {
+      const uint32_t k = i + lane < i1 ? keys[i + lane] : 0;
+#pragma unroll
+      for (int j = 0; j < 3; ++j) m[j] += __popcll(__ballot(k >= (s | (uint32_t)(j + 1) << shift)));
+    }
+    if (lane < 3) atomicAdd(&g.counts[round][lane], lane == 0 ? m[0] : lane == 1 ? m[1] : m[2]);
+    __syncthreads();
+    const uint32_t s0 = s;
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
-      const uint32_t c = t | (uint32_t)(j + 1) << shift, m = counts[round][j];
-      if (m == want) return {c - 1, 0};
-      if (m > want) next = c;
+      const uint32_t all = g.counts[round][j];
+      if (all >= want) s = s0 | (uint32_t)(j + 1) << shift, exact = all == want;
     }
-    t = next;
   }
-  uint32_t more = 0;
-  for (int i = first; i < count; i += threads)
-    more += __popcll(__ballot((i + lane < count ? key[i + lane] : 0) > t));
-  if (lane == 0 && more) atomicAdd(&counts[16][0], more);
-  __syncthreads();
-  return {t, want - counts[16][0]};
+  uint2 mine = make_uint2(0, 0);  // keys above s, and equal to it
+  const int each = (count + threads - 1) / threads;
+  const int b0 = min((int)threadIdx.x * each, count), b1 = min(b0 + each, count);
+  for (int i = b0; i < b1; ++i) mine.x += keys[i] > s, mine.y += keys[i] == s;
+  uint2 all;
+  const uint2 prior = before(mine, g.parts, &all);
+  const uint32_t left = want - all.x;
+  uint32_t equal = prior.y, to = prior.x + min(prior.y, left);
+  for (int i = b0; i < b1; ++i)
+    if (keys[i] > s || (keys[i] == s && equal++ < left)) chosen[to++] = first + i;
 }
 
+// The summaries of 64 blocks on their way to a wave's registers: block 16 k + lane % 16 of them, bytes
+// 16 (lane / 16) ... of each 64.
+template <int STEPS>
+struct Summaries {
+  i32x4 m[4][STEPS];
+  float scale[4];
+  int32_t page[4];
+  __device__ __forceinline__ void load(const SelectArgs& a, int h, int32_t entry, int r, int g, bool wide) {
+    const int32_t mine = entry < a.pages ? entry : -1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      page[k] = __shfl(mine, k * 16 + r);
+      const int64_t row = (int64_t)max(page[k], 0) * a.kv_heads + h;  // (in a missing page's place: page 0)
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) m[k][s] = load_mean(a.means + row * a.head_dim, s * 64 + g * 16, a.head_dim, wide);
+      scale[k] = a.scales[row];
+    }
+    __builtin_amdgcn_sched_barrier(0);  // all loads under way before the first is used
+  }
+};
+
 // A workgroup chooses the blocks of one cached head for `tile` tokens.  Scores: the dot products of 16 queries
-// (the rows: a power of two of them to a token) and 16 summaries are one matrix instruction for 64 values of
-// a head, bytes in, whole numbers out; a lane's four results are rows 4 g ... 4 g + 3 of its own block, so that
-// a group of up to four queries takes its maximum within a lane.  A wave has 64 blocks under way at a time.
-// The scores go to LDS as ordered integers.  Then, of one token, all waves search the threshold together; of
-// several, each wave takes whole tokens, whose keys stay in its registers.
+// (the rows: a power of two of them to a token, or several tiles of rows) and 16 summaries are one matrix
+// instruction for 64 values of a head, bytes in, whole numbers out; a lane's four results are rows 4 g ...
+// 4 g + 3 of its own block, so that a group of up to four queries takes its maximum within a lane.  A wave has
+// 64 blocks under way at a time, the first of them before the queries are there.  The scores go to LDS as
+// ordered integers.  Then, of one token, all waves search the threshold together; of several, each wave takes
+// whole tokens, whose keys stay in its registers.
 template <typename T, int STEPS>
 __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
   extern __shared__ __align__(16) unsigned char lds[];
-  __shared__ uint32_t counts[17][4];
-  __shared__ uint2 parts[kMaxWaves];
-  __shared__ int32_t seqs[16], seen[16];      // of the tile's tokens; blocks that they see
+  __shared__ GroupLds group;
+  __shared__ Candidate few[kMaxWaves / 4][64];
+  __shared__ int32_t seqs[kMaxTile], seen[kMaxTile];  // of the tile's tokens; blocks that they see
   constexpr int ROW = STEPS * 64;
   const int rows = a.tile * a.per_token;      // a multiple of 16
+  const int shift = a.per_token >= 16 ? 4 : __builtin_ctz(a.per_token);  // of a tile of rows to its tokens
   int8_t* m8 = reinterpret_cast<int8_t*>(lds);                // [rows][ROW]
   float* top = reinterpret_cast<float*>(m8 + rows * ROW);     // [rows]; -1: no query
   uint32_t* keys = reinterpret_cast<uint32_t*>(top + rows);   // [tile][max_blocks]
@@ -145,55 +273,78 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
   const int D = a.head_dim, r = lane & 15, g = lane >> 4;
   const int forced = a.sink + a.local;
   const uint32_t take = a.blocks - forced;    // of the blocks that are scored
+  const bool wide = D % 16 == 0;
+  const auto sees = [&](int32_t p, int32_t seq) {
+    return p < 0 || (uint32_t)seq >= (uint32_t)a.sequences ? 0 : min((p >> a.block_shift) + 1, a.max_blocks);
+  };
 
-  if (threadIdx.x < 17 * 4) counts[threadIdx.x / 4][threadIdx.x % 4] = 0;
+  // of the first token's sequence: what every wave needs to begin with its first blocks
+  const int32_t first_seq = a.seq[t0];
+  const int first_last = min(t0 + a.tile, a.tokens) - 1;  // (positions ascend within a sequence)
+  int ahead = max(sees(a.pos[t0], first_seq), a.seq[first_last] == first_seq ? sees(a.pos[first_last], first_seq) : 0);
+  ahead = take > 0 && ahead > a.blocks ? ahead - forced : 0;
+  Summaries<STEPS> sum;
+  if (wave * 64 < ahead) {
+    const int b = wave * 64 + lane;
+    sum.load(a, h, b < ahead ? a.table[(int64_t)first_seq * a.max_blocks + a.sink + b] : -1, r, g, wide);
+  }
+
+  if (threadIdx.x < 64) group.top[threadIdx.x] = 0, group.counts[threadIdx.x / 4][threadIdx.x % 4] = 0;
   if ((int)threadIdx.x < a.tile) {
     const int t = t0 + threadIdx.x;
     int32_t p = -1, seq = -1;
     if (t < a.tokens) p = a.pos[t], seq = a.seq[t];
     seqs[threadIdx.x] = seq;
-    seen[threadIdx.x] =
-        p < 0 || (uint32_t)seq >= (uint32_t)a.sequences ? 0 : min((p >> a.block_shift) + 1, a.max_blocks);
+    seen[threadIdx.x] = sees(p, seq);
+  }
+  // queries in 8 bits, four rows of 16 lanes to a wave
+  for (int row0 = wave * 4; row0 < rows; row0 += waves * 4) {
+    const int row = row0 + g, i = row / a.per_token, gq = row % a.per_token;
+    const bool live = gq < a.group && t0 + i < a.tokens;
+    const T* q = static_cast<const T*>(a.q) + (t0 + i) * a.q_token + (int64_t)(h * a.group + gq) * a.q_head;
+    float x[STEPS][4], m = 0.0f;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int d = s * 64 + r * 4;
+      T v[4] = {};
+      if (live && d < D) load_n<4>(q + d, a.q_aligned, v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[s][k] = (float)v[k], m = fmaxf(m, fabsf(x[s][k]));
+    }
+#pragma unroll
+    for (int s = 8; s; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
+    const float f = m > 0.0f ? 127.0f * (1.0f / m) : 0.0f;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        w |= ((uint32_t)(int)fminf(fmaxf(rintf(x[s][k] * f), -127.0f), 127.0f) & 255u) << (8 * k);
+      *reinterpret_cast<uint32_t*>(m8 + row * ROW + s * 64 + r * 4) = w;
+    }
+    if (r == 0) top[row] = live ? m : -1.0f;
   }
   __syncthreads();
   // without a choice: everything the token sees; else the blocks that are always taken
   bool some = false;
-  for (int i = 0; i < a.tile; ++i) {
+  for (int i = 0; i < a.tile; ++i) some |= seen[i] > a.blocks && take > 0;
+  for (int i = wave; i < a.tile; i += waves) {
     const int n = seen[i];
-    some |= n > a.blocks && take > 0;
-    if (t0 + i >= a.tokens) continue;
+    if (t0 + i >= a.tokens) break;
     int32_t* chosen = a.chosen + ((int64_t)(t0 + i) * a.kv_heads + h) * a.blocks;
     if (n <= a.blocks) {
-      for (int j = threadIdx.x; j < a.blocks; j += threads) chosen[j] = j < n ? j : -1;
+      for (int j = lane; j < a.blocks; j += 64) chosen[j] = j < n ? j : -1;
     } else {
-      for (int j = threadIdx.x; j < a.sink; j += threads) chosen[j] = j;
-      for (int j = threadIdx.x; j < a.local; j += threads) chosen[a.blocks - a.local + j] = n - a.local + j;
+      for (int j = lane; j < forced; j += 64) chosen[j < a.sink ? j : a.blocks - forced + j] = j < a.sink ? j : n - forced + j;
     }
   }
   if (!some) return;
 
-  for (int row = wave; row < rows; row += waves) {
-    const int i = row / a.per_token, gq = row % a.per_token;
-    const bool live = gq < a.group && t0 + i < a.tokens;
-    const T* q = static_cast<const T*>(a.q) + (t0 + i) * a.q_token + (int64_t)(h * a.group + gq) * a.q_head;
-    float x[STEPS], m = 0.0f;
+  // of a lane's four results of a tile of rows: the tokens whose scores they become, after the maximum over the
+  // token's rows, counted from the tile's first; -1: none
+  int token_of[4];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      const int d = s * 64 + lane;
-      x[s] = live && d < D ? (float)q[d] : 0.0f;
-      m = fmaxf(m, fabsf(x[s]));
-    }
-#pragma unroll
-    for (int s = 32; s; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
-    const float f = m > 0.0f ? 127.0f * (1.0f / m) : 0.0f;
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s)
-      m8[row * ROW + s * 64 + lane] = (int8_t)fminf(fmaxf(rintf(x[s] * f), -127.0f), 127.0f);
-    if (lane == 0) top[row] = live ? m : -1.0f;
-  }
-  __syncthreads();
-
-  const bool wide = D % 16 == 0;
+  for (int i = 0; i < 4; ++i) token_of[i] = (4 * g + i) & ((1 << shift) - 1) ? -1 : (4 * g + i) >> shift;
   for (int i0 = 0; i0 < a.tile;) {  // tokens i0 ... i1 - 1 are of one sequence
     const int32_t seq = seqs[i0];
     int i1 = i0, most = 0;
@@ -201,20 +352,8 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
     const int count = most > a.blocks ? most - forced : 0;
     const int32_t* table = a.table + (int64_t)seq * a.max_blocks + a.sink;
     for (int b0 = wave * 64; b0 < count; b0 += waves * 64) {
-      const int32_t entry = b0 + lane < count ? table[b0 + lane] : -1;
-      const int32_t mine = entry < a.pages ? entry : -1;
-      i32x4 m[4][STEPS];
-      float scale[4];
-      int32_t page[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        page[k] = __shfl(mine, k * 16 + r);
-        const int64_t row = (int64_t)max(page[k], 0) * a.kv_heads + h;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) m[k][s] = load_mean(a.means + row * D, s * 64 + g * 16, D, wide);
-        scale[k] = a.scales[row];
-      }
-      __builtin_amdgcn_sched_barrier(0);
+      if (!(i0 == 0 && b0 < waves * 64 && ahead >= count))
+        sum.load(a, h, b0 + lane < count ? table[b0 + lane] : -1, r, g, wide);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         if (b0 + k * 16 >= count) break;
@@ -225,26 +364,29 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
 #pragma unroll
           for (int s = 0; s < STEPS; ++s) {
             const i32x4 qv = *reinterpret_cast<const i32x4*>(m8 + (row0 + r) * ROW + s * 64 + g * 16);
-            dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(qv, m[k][s], dot, 0, 0, 0);
+            dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(qv, sum.m[k][s], dot, 0, 0, 0);
           }
           const f32x4 tq = *reinterpret_cast<const f32x4*>(top + row0 + 4 * g);
+          const bool more = a.per_token > 16 && row0 > 0;  // rows of the same token
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float x = tq[i] < 0.0f ? -INFINITY : (float)dot[i] * tq[i];
-            best[i] = row0 == 0 ? x : fmaxf(best[i], x);
+            best[i] = more ? fmaxf(best[i], x) : x;
           }
-        }
-        // over the queries of a token
-        int each = 1;  // of the four: a token's rows are `each` of them, or all four in several lane groups
-        if (a.per_token >= 2) best[0] = fmaxf(best[0], best[1]), best[2] = fmaxf(best[2], best[3]), each = 2;
-        if (a.per_token >= 4) best[0] = fmaxf(best[0], best[2]), each = 4;
-        if (a.per_token >= 8) best[0] = fmaxf(best[0], __shfl_xor(best[0], 16));
-        if (a.per_token >= 16) best[0] = fmaxf(best[0], __shfl_xor(best[0], 32));
+          if (a.per_token > 16 && row0 + 16 < rows) continue;
+          // over the queries of a token
+          if (shift >= 1) best[0] = fmaxf(best[0], best[1]), best[2] = fmaxf(best[2], best[3]);
+          if (shift >= 2) best[0] = fmaxf(best[0], best[2]);
+          if (shift >= 3) best[0] = fmaxf(best[0], __shfl_xor(best[0], 16));
+          if (shift >= 4) best[0] = fmaxf(best[0], __shfl_xor(best[0], 32));
+          const int first = a.per_token > 16 ? 0 : row0 >> shift;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token = (4 * g + i) / a.per_token;
-          if (i % each == 0 && (4 * g + i) % a.per_token == 0 && token >= i0 && token < i1 && b < count)
-            keys[token * a.max_blocks + b] = page[k] < 0 ? 0u : ordered(best[i] * scale[k]);
+          for (int i = 0; i < 4; ++i) {
+            if (i > 0 && shift >= 2) break;
+            const int token = first + token_of[i];
+            if (token_of[i] >= 0 && token >= i0 && token < i1 && b < count)
+              keys[token * a.max_blocks + b] = sum.page[k] < 0 ? 0u : ordered(best[i] * sum.scale[k]);
+          }
         }
       }
     }
@@ -253,43 +395,21 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
   __syncthreads();
 
   if (a.tile == 1) {
-    const int count = seen[0] - forced;
-    const Threshold th = group_threshold(keys, count, take, counts);
-    const int run = (count + threads - 1) / threads;  // blocks of a thread, in order
-    const int b0 = min((int)threadIdx.x * run, count), b1 = min(b0 + run, count);
-    uint2 n = make_uint2(0, 0);
-    for (int b = b0; b < b1; ++b) n.x += keys[b] > th.above, n.y += keys[b] == th.above;
-    const uint2 prior = before(n, parts);
-    uint32_t equal = prior.y, at = a.sink + prior.x + min(prior.y, th.equal);
-    int32_t* chosen = a.chosen + ((int64_t)t0 * a.kv_heads + h) * a.blocks;
-    for (int b = b0; b < b1; ++b) {
-      const uint32_t k = keys[b];
-      if (k > th.above || (k == th.above && equal++ < th.equal)) chosen[at++] = a.sink + b;
-    }
+    group_choose(keys, seen[0] - forced, take, a.sink,
+                 a.chosen + ((int64_t)t0 * a.kv_heads + h) * a.blocks + a.sink, few[0], group);
     return;
   }
   for (int i = wave; i < a.tile; i += waves) {
-    const int count = seen[i] - forced;
     if (seen[i] <= a.blocks) continue;
-    uint32_t key[kWaveKeys];
-#pragma unroll
-    for (int k = 0; k < kWaveKeys; ++k)
-      key[k] = k * 64 + lane < count ? keys[i * a.max_blocks + k * 64 + lane] : 0;
-    const Threshold th = wave_threshold(key, count, take);
+    const int count = seen[i] - forced;
     int32_t* chosen = a.chosen + ((int64_t)(t0 + i) * a.kv_heads + h) * a.blocks + a.sink;
-    const uint64_t lower = (1ull << lane) - 1;
-    uint32_t at = 0, equal = 0;
-#pragma unroll
-    for (int k = 0; k < kWaveKeys; ++k) {
-      if (k * 64 >= count) break;
-      const bool in = k * 64 + lane < count;
-      const bool same = in && key[k] == th.above;
-      const uint64_t sames = __ballot(same);
-      const bool taken = (in && key[k] > th.above) || (same && equal + __popcll(sames & lower) < th.equal);
-      const uint64_t takens = __ballot(taken);
-      if (taken) chosen[at + __popcll(takens & lower)] = a.sink + k * 64 + lane;
-      at += __popcll(takens), equal += __popcll(sames);
-    }
+    const uint32_t* key = keys + i * a.max_blocks;
+    if (count <= 256)
+      wave_choose<4>(key, count, take, a.sink, chosen, few[wave]);
+    else if (count <= 512)
+      wave_choose<8>(key, count, take, a.sink, chosen, few[wave]);
+    else
+      wave_choose<kWaveKeys>(key, count, take, a.sink, chosen, few[wave]);
   }
 }
 
@@ -325,14 +445,22 @@ hipError_t launch_select(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.kv_heads = c.kv_heads, a.group = q.heads / c.kv_heads, a.head_dim = c.head_dim;
   a.block_shift = __builtin_ctz(c.block);
   a.blocks = blocks, a.sink = sink, a.local = local;
-  // Tiles of 16 rows hold several tokens where most of a tile's are of one sequence and a wave can select
-  // alone; otherwise a workgroup has one token, and so many waves that each has some blocks.
+  // A workgroup has several tokens where most of them are of one sequence and a wave can select alone: so
+  // many that their rows fill four matrix operands and their keys 64 KiB of LDS, and that the device is full.
+  // Otherwise it has one token, and so many waves that each has some blocks.
   int rows = 1;
   while (rows < a.group && rows < 16) rows *= 2;
-  const bool tiles = rows < 16 && t.tokens >= (int64_t)16 * t.sequences && t.max_blocks <= 64 * kWaveKeys &&
-                     (int64_t)(t.tokens / (16 / rows)) * c.kv_heads >= 512;
-  a.tile = tiles ? 16 / rows : 1;
+  const bool tiles = t.tokens >= (int64_t)16 * t.sequences && t.max_blocks <= 64 * kWaveKeys &&
+                     (int64_t)(t.tokens / (16 / rows)) * c.kv_heads >= 512 && a.group <= 16;
+  a.tile = 1;
+  if (tiles) {
+    a.tile = 16 / rows;
+    while (a.tile * rows < 64 && a.tile * 2 * t.max_blocks <= 16384 &&
+           (int64_t)(t.tokens / (a.tile * 2)) * c.kv_heads >= 1024)
+      a.tile *= 2;
+  }
   a.per_token = tiles ? rows : (a.group + 15) & ~15;
+  a.q_aligned = (uintptr_t)q.data % (4 * dtype_bytes(c.dtype)) == 0 && q.token_stride % 4 == 0 && q.head_stride % 4 == 0;
   int threads = 64;
   while (threads < 1024 && threads < t.max_blocks) threads *= 2;
   if (tiles) threads = 256;
