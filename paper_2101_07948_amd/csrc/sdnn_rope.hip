@@ -152,7 +152,7 @@ RopeRows rope_args(const sdnn_heads& x, const sdnn_heads& y, int dtype, int32_t 
 
 struct AppendArgs {
   RopeRows q;      // heads 0: no queries
-  int32_t q_blocks;
+  int32_t kv_blocks;
   const void* k;
   const void* v;
   int64_t k_token, k_head, v_token, v_head;
@@ -169,80 +169,113 @@ struct AppendArgs {
   int32_t tokens, sequences, max_blocks;
   int32_t kv_heads, head_dim, block, pairs;
   int32_t window;  // tokens of a workgroup
+  int32_t k_aligned, v_aligned;
+  int32_t k_whole;  // keys can be read and rotated 16 bytes at a time
 };
 
-constexpr int kWindow = 64;      // the most
-constexpr int kTileBytes = 32768;
-constexpr int kSumDims = 32;     // values of a head that are summed at a time
+constexpr int kWindow = 64;       // the most
+constexpr int kTileBytes = 32768; // the most of a window's keys
+constexpr int kSumRows = 8;       // keys of a block that a thread adds
 
+// The window's rotated keys [token][head_dim], its values with rows a piece longer (so that the rows of one
+// column lie in different banks), whose place the sums of a mean take afterwards.
 struct AppendLds {
-  alignas(16) unsigned char tile[kTileBytes];  // the window's rotated keys, then its values
-  float stage[128][kSumDims];                  // a full block's keys
-  float part[8][kSumDims];
-  float sum[kMaxHeadDim];
-  int64_t page[kWindow];                       // -1: nothing to store
+  int64_t page[kWindow];  // -1: nothing to store
   int32_t pos[kWindow], seq[kWindow];
+  float sum[kMaxHeadDim];
   float top;
 };
+__host__ __device__ constexpr int key_bytes(int window, int head_dim, int size) { return (window * head_dim * size + 15) & ~15; }
+__host__ __device__ constexpr int value_bytes(int window, int head_dim, int size) {
+  return window * (head_dim * size + 16);
+}
 
-// Sum of slots first, first + stride, ... below block, halves added pairwise (slot i with i +
-// block / 2 first).
-template <int STRIDE, int BLOCK, typename GET>
-__device__ __forceinline__ float halves(int first, const GET& get) {
-  if constexpr (STRIDE == BLOCK)
+// Sum of get(0) ... get(N - 1), halves added pairwise (i with i + N / 2 first).
+template <int N, int STRIDE = 1, typename GET>
+__device__ __forceinline__ float halves(const GET& get, int first = 0) {
+  if constexpr (STRIDE == N)
     return get(first);
   else
-    return halves<STRIDE * 2, BLOCK>(first, get) + halves<STRIDE * 2, BLOCK>(first + STRIDE, get);
+    return halves<N, STRIDE * 2>(get, first) + halves<N, STRIDE * 2>(get, first + STRIDE);
 }
 
-// Value d of the key of token t as it is stored.
+// V values of the key of token t from value d on, as they are stored: with k_whole 16 bytes at a time.
 template <typename T, bool INTERLEAVED>
-__device__ __forceinline__ T stored_key(const AppendArgs& a, int t, int h, int d) {
+__device__ __forceinline__ void stored_key(const AppendArgs& a, int t, int h, int d, T (&out)[16 / sizeof(T)]) {
+  constexpr int V = 16 / sizeof(T);
   const T* x = static_cast<const T*>(a.k) + t * a.k_token + h * a.k_head;
-  if (d >= 2 * a.pairs) return x[d];
-  const int i = INTERLEAVED ? d / 2 : d % a.pairs;
-  const bool second = INTERLEAVED ? d & 1 : d >= a.pairs;
-  const float2 f = rotation_of(a.freq, a.amplitude, a.pos[t], i);
-  float y0, y1;
-  rotate((float)x[INTERLEAVED ? 2 * i : i], (float)x[INTERLEAVED ? 2 * i + 1 : i + a.pairs], f, &y0, &y1);
-  return (T)(second ? y1 : y0);
+  if (a.k_whole) {
+    load_n<V>(x + d, true, out);
+    if (d >= 2 * a.pairs) return;
+    const int32_t p = a.pos[t];
+    T other[V] = {};
+    if (!INTERLEAVED) load_n<V>(x + (d < a.pairs ? d + a.pairs : d - a.pairs), true, other);
+    const int pair = INTERLEAVED ? d / 2 : d < a.pairs ? d : d - a.pairs;
+#pragma unroll
+    for (int e = 0; e < (INTERLEAVED ? V / 2 : V); ++e) {
+      const float2 f = rotation_of(a.freq, a.amplitude, p, pair + e);
+      float y0, y1;
+      if (INTERLEAVED) {
+        rotate((float)out[2 * e], (float)out[2 * e + 1], f, &y0, &y1);
+        out[2 * e] = (T)y0, out[2 * e + 1] = (T)y1;
+      } else {
+        const bool second = d >= a.pairs;
+        rotate((float)(second ? other[e] : out[e]), (float)(second ? out[e] : other[e]), f, &y0, &y1);
+        out[e] = (T)(second ? y1 : y0);
+      }
+    }
+    return;
+  }
+#pragma unroll 1
+  for (int e = 0; e < V; ++e, ++d) {
+    T v = x[d];
+    if (d < 2 * a.pairs) {
+      const int i = INTERLEAVED ? d / 2 : d % a.pairs;
+      float y0, y1;
+      rotate((float)x[INTERLEAVED ? 2 * i : i], (float)x[INTERLEAVED ? 2 * i + 1 : i + a.pairs],
+             rotation_of(a.freq, a.amplitude, a.pos[t], i), &y0, &y1);
+      v = (T)((INTERLEAVED ? d & 1 : d >= a.pairs) ? y1 : y0);
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k == e) out[k] = v;
+  }
 }
 
-// The mean of the block that token i of the window fills.  Its keys come from the window's tile,
-// from the call's earlier tokens (rotated again: another workgroup stores them at this moment) or
-// from the page, where an earlier call stored them.
+// The mean of the block that token i of the window fills.  Its keys come from the window's tile, from the
+// call's tokens before the window (rotated again: another workgroup stores them at this moment; `earlier`:
+// the token before the window may be one) or from the page, where an earlier call stored them.  A thread adds
+// keys q, q + P/8, ... of 16 bytes of a row, all loads under way together, and the P/8 sums are added from LDS.
 template <typename T, bool INTERLEAVED>
-__device__ void block_mean(const AppendArgs& a, AppendLds& l, int t0, int i, int h) {
-  const int P = a.block, D = a.head_dim, t = t0 + i;
+__device__ void block_mean(const AppendArgs& a, AppendLds& l, const T* tile, float* sums, int t0, int i, int h,
+                           bool earlier) {
+  constexpr int V = 16 / sizeof(T);
+  const int P = a.block, D = a.head_dim, t = t0 + i, parts = P / kSumRows, chunks = D / V;
   const int32_t pos = l.pos[i], seq = l.seq[i];
-  const T* tile = reinterpret_cast<const T*>(l.tile);
-  const T* page = static_cast<const T*>(a.k_pages) + (l.page[i] * a.kv_heads + h) * (int64_t)P * D;
-  for (int d0 = 0; d0 < D; d0 += kSumDims) {
-    __syncthreads();
-    const int dn = min(kSumDims, D - d0);
-    for (int j = threadIdx.x; j < P * kSumDims; j += kThreads) {
-      const int s = j / kSumDims, d = j % kSumDims;
-      if (d >= dn) continue;
-      const int back = P - 1 - s;  // tokens before the one that fills the block
-      const int from = t - back;
-      T v;
-      if (i >= back && l.seq[i - back] == seq && l.pos[i - back] == pos - back)
-        v = tile[(i - back) * D + d0 + d];
-      else if (from >= 0 && a.seq[from] == seq && a.pos[from] == pos - back)
-        v = stored_key<T, INTERLEAVED>(a, from, h, d0 + d);
-      else
-        v = page[(int64_t)s * D + d0 + d];
-      l.stage[s][d] = (float)v;
+  const int64_t row = l.page[i] * a.kv_heads + h;
+  const T* page = static_cast<const T*>(a.k_pages) + row * P * D;
+  for (int j = threadIdx.x; j < parts * chunks; j += kThreads) {
+    const int q = j / chunks, d = (j - q * chunks) * V;
+    T x[kSumRows][V];
+#pragma unroll
+    for (int k = 0; k < kSumRows; ++k)  // what the page holds, where it is from this call too: replaced below
+      load_n<V>(page + (int64_t)(q + k * parts) * D + d, true, x[k]);
+#pragma unroll
+    for (int k = 0; k < kSumRows; ++k) {
+      const int back = P - 1 - (q + k * parts), from = t - back;  // tokens before the one that fills the block
+      if (back <= i) {
+        if (l.seq[i - back] == seq && l.pos[i - back] == pos - back) load_n<V>(tile + (i - back) * D + d, true, x[k]);
+      } else if (earlier && from >= 0 && a.seq[from] == seq && a.pos[from] == pos - back) {
+        stored_key<T, INTERLEAVED>(a, from, h, d, x[k]);
+      }
     }
-    __syncthreads();
-    const int d = threadIdx.x % kSumDims, u = threadIdx.x / kSumDims;  // 8 parts of each value
-    const auto get = [&](int s) { return l.stage[s][d]; };
-    const float part = P == 32 ? halves<8, 32>(u, get) : P == 64 ? halves<8, 64>(u, get) : halves<8, 128>(u, get);
-    l.part[u][d] = part;
-    __syncthreads();
-    if (u == 0 && d < dn)
-      l.sum[d0 + d] = ((l.part[0][d] + l.part[4][d]) + (l.part[2][d] + l.part[6][d])) +
-                      ((l.part[1][d] + l.part[5][d]) + (l.part[3][d] + l.part[7][d]));
+#pragma unroll
+    for (int e = 0; e < V; ++e) sums[q * D + d + e] = halves<kSumRows>([&](int k) { return (float)x[k][e]; });
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < D; d += kThreads) {
+    const auto get = [&](int q) { return sums[q * D + d]; };
+    l.sum[d] = parts == 4 ? halves<4>(get) : parts == 8 ? halves<8>(get) : halves<16>(get);
   }
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -255,28 +288,37 @@ __device__ void block_mean(const AppendArgs& a, AppendLds& l, int t0, int i, int
   __syncthreads();
   const float top = l.top;
   const float f = top > 0.0f ? 127.0f * (1.0f / top) : 0.0f;
-  const int64_t row = l.page[i] * a.kv_heads + h;
   for (int d = threadIdx.x; d < D; d += kThreads)
     a.means[row * D + d] = (int8_t)fminf(fmaxf(rintf(l.sum[d] * f), -127.0f), 127.0f);
   if (threadIdx.x == 0) a.mean_scales[row] = top / (127.0f * P);
   __syncthreads();
 }
 
-// Workgroups below q_blocks rotate queries; the others each store one head of a window of tokens:
-// keys rotated into an LDS tile and written as rows, values turned through LDS so that the tokens
-// of a page lie side by side, and the mean of each block that the window fills.  One launch,
-// no workgroup waits for another.
-template <typename T, bool INTERLEAVED>
+// Workgroups below kv_blocks, which take longest and start first, each store one head of a window of tokens:
+// keys rotated into an LDS tile and written as rows, values turned through LDS so that the tokens of a page
+// lie side by side, and the mean of each block that the window fills; the others rotate queries.  One launch, no
+// workgroup waits for another.
+//   VP: pairs (and values past the rotated part) of a thread's unit, as in rope_rows.  For single tokens 1: a
+// thread's cosines and sines are then all that it waits for.
+template <typename T, bool INTERLEAVED, int VP>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
+  extern __shared__ __align__(16) unsigned char lds[];
   __shared__ AppendLds l;
-  if ((int)blockIdx.x < a.q_blocks) {
-    rope_rows_vec<T, INTERLEAVED>(a.q, blockIdx.x, reinterpret_cast<float2*>(l.tile));
+  if ((int)blockIdx.x >= a.kv_blocks) {
+    rope_rows_vec<T, INTERLEAVED>(a.q, blockIdx.x - a.kv_blocks, reinterpret_cast<float2*>(lds));
     return;
   }
-  const int b = blockIdx.x - a.q_blocks;
-  const int h = b % a.kv_heads, t0 = b / a.kv_heads * a.window;
-  const int n = min(a.window, a.tokens - t0);
-  const int P = a.block, D = a.head_dim;
+  constexpr int V = 16 / sizeof(T);
+  const int b = blockIdx.x;
+  // windows begin where the first token's block does, as if it had been stored from its first position on, so that
+  // in a prompt they hold whole blocks
+  const int h = b % a.kv_heads;
+  const int begin = b / a.kv_heads * a.window - (a.pos[0] & (a.window - 1)), t0 = max(begin, 0);
+  const int n = min(begin + a.window, a.tokens) - t0;
+  if (n <= 0) return;
+  const int P = a.block, D = a.head_dim, chunks = D / V, stride = D + V;
+  T* tile = reinterpret_cast<T*>(lds);
+  T* turn = reinterpret_cast<T*>(lds + key_bytes(a.window, D, sizeof(T)));
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const int32_t p = a.pos[t0 + i], s = a.seq[t0 + i];
     int64_t page = -1;
@@ -285,51 +327,96 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     if (page < 0 || page >= a.pages) page = -1;
     l.pos[i] = p, l.seq[i] = s, l.page[i] = page;
   }
-  T* tile = reinterpret_cast<T*>(l.tile);
+  const T* v = static_cast<const T*>(a.v) + t0 * a.v_token + h * a.v_head;
+#pragma unroll 4
+  for (int j = threadIdx.x; j < n * chunks; j += kThreads) {
+    const int i = j / chunks, d = (j - i * chunks) * V;
+    T x[V];
+    load_n<V>(v + i * a.v_token + d, a.v_aligned, x);
+    store_n<V>(turn + i * stride + d, true, x);
+  }
   const T* k = static_cast<const T*>(a.k) + t0 * a.k_token + h * a.k_head;
-  const int units = D - a.pairs;  // pairs, then single values
+  const int turning = a.pairs / VP, units = turning + (D - 2 * a.pairs) / VP;
+#pragma unroll 2
   for (int j = threadIdx.x; j < n * units; j += kThreads) {
     const int i = j / units, u = j - i * units;
     const T* x = k + i * a.k_token;
-    if (u < a.pairs) {
-      const int d0 = INTERLEAVED ? 2 * u : u, d1 = INTERLEAVED ? 2 * u + 1 : u + a.pairs;
-      float y0, y1;
-      rotate((float)x[d0], (float)x[d1], rotation_of(a.freq, a.amplitude, a.pos[t0 + i], u), &y0, &y1);
-      tile[i * D + d0] = (T)y0;
-      tile[i * D + d1] = (T)y1;
+    T* y = tile + i * D;
+    if (u >= turning) {
+      const int d = 2 * a.pairs + (u - turning) * VP;
+      T w[VP];
+      load_n<VP>(x + d, a.k_aligned, w);
+      store_n<VP>(y + d, VP > 1, w);
+      continue;
+    }
+    T lo[VP], hi[VP];
+    if (INTERLEAVED) {
+      T w[2 * VP];
+      load_n<2 * VP>(x + 2 * u * VP, a.k_aligned, w);
+#pragma unroll
+      for (int e = 0; e < VP; ++e) lo[e] = w[2 * e], hi[e] = w[2 * e + 1];
     } else {
-      tile[i * D + u + a.pairs] = x[u + a.pairs];
+      load_n<VP>(x + u * VP, a.k_aligned, lo);
+      load_n<VP>(x + a.pairs + u * VP, a.k_aligned, hi);
+    }
+    const int32_t p = a.pos[t0 + i];
+#pragma unroll
+    for (int e = 0; e < VP; ++e) {
+      float y0, y1;
+      rotate((float)lo[e], (float)hi[e], rotation_of(a.freq, a.amplitude, p, u * VP + e), &y0, &y1);
+      lo[e] = (T)y0, hi[e] = (T)y1;
+    }
+    if (INTERLEAVED) {
+      T w[2 * VP];
+#pragma unroll
+      for (int e = 0; e < VP; ++e) w[2 * e] = lo[e], w[2 * e + 1] = hi[e];
+      store_n<2 * VP>(y + 2 * u * VP, VP > 1, w);
+    } else {
+      store_n<VP>(y + u * VP, VP > 1, lo);
+      store_n<VP>(y + a.pairs + u * VP, VP > 1, hi);
     }
   }
   __syncthreads();
-  constexpr int V = 16 / sizeof(T);
   T* kp = static_cast<T*>(a.k_pages);
-  const int chunks = D / V;
   for (int j = threadIdx.x; j < n * chunks; j += kThreads) {
     const int i = j / chunks, d = (j - i * chunks) * V;
     if (l.page[i] < 0) continue;
-    T v[V];
-    load_n<V>(tile + i * D + d, true, v);
-    store_n<V>(kp + ((l.page[i] * a.kv_heads + h) * P + l.pos[i] % P) * (int64_t)D + d, true, v);
+    T x[V];
+    load_n<V>(tile + i * D + d, true, x);
+    store_n<V>(kp + ((l.page[i] * a.kv_heads + h) * P + l.pos[i] % P) * (int64_t)D + d, true, x);
   }
-  if (a.means) {
-    const int i = threadIdx.x % 64;  // a window has at most 64 tokens: one to a lane, in every wave
-    for (uint64_t full = __ballot(i < n && l.page[i] >= 0 && l.pos[i] % P == P - 1); full; full &= full - 1)
-      block_mean<T, INTERLEAVED>(a, l, t0, __builtin_ctzll(full), h);
-  }
-  __syncthreads();
-  const T* v = static_cast<const T*>(a.v) + t0 * a.v_token + h * a.v_head;
-  for (int j = threadIdx.x; j < n * D; j += kThreads) {
-    const int i = j / D, d = j - i * D;
-    tile[j] = v[i * a.v_token + d];
-  }
-  __syncthreads();
+  // Values: runs of V tokens whose places are 16 bytes of a row of the page are written at once.  Groups of tokens
+  // begin where the first token's place says that such runs do; the tokens before make a group too.
   T* vp = static_cast<T*>(a.v_pages);
-  for (int j = threadIdx.x; j < n * D; j += kThreads) {
-    const int d = j / n, i = j - d * n;
-    if (l.page[i] < 0) continue;
-    vp[((l.page[i] * a.kv_heads + h) * D + d) * (int64_t)P + l.pos[i] % P] = tile[i * D + d];
+  const int lead = a.window == 1 ? 0 : (V - (l.pos[0] & (V - 1))) & (V - 1);
+  const int groups = (n - lead + V - 1) / V + (lead > 0);
+  for (int j = threadIdx.x; j < groups * D; j += kThreads) {
+    const int q = j / D, d = j - q * D;
+    const int i0 = lead > 0 ? (q == 0 ? 0 : lead + (q - 1) * V) : q * V;
+    const int i1 = min(lead > 0 && q == 0 ? lead : i0 + V, n);
+    T x[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = turn[min(i0 + e, n - 1) * stride + d];
+    const int64_t page = i0 < n ? l.page[i0] : -1;
+    const int32_t p = i0 < n ? l.pos[i0] : 0;
+    // (the tokens of a sequence ascend by one, so that a run's ends tell of all of it)
+    if (i1 - i0 == V && page >= 0 && p % V == 0 && l.pos[i0 + V - 1] == p + V - 1 && l.seq[i0 + V - 1] == l.seq[i0]) {
+      store_n<V>(vp + ((page * a.kv_heads + h) * D + d) * (int64_t)P + p % P, true, x);
+      continue;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (i0 + e < i1 && l.page[i0 + e] >= 0)
+        vp[((l.page[i0 + e] * a.kv_heads + h) * D + d) * (int64_t)P + l.pos[i0 + e] % P] = x[e];
   }
+  if (!a.means) return;
+  const int i = threadIdx.x % 64;  // a window has at most 64 tokens: one to a lane, in every wave
+  uint64_t full = __ballot(i < n && l.page[i] >= 0 && l.pos[i] % P == P - 1);
+  if (!full) return;
+  const bool earlier = t0 > 0 && a.seq[t0 - 1] == l.seq[0] && a.pos[t0 - 1] == l.pos[0] - 1;
+  __syncthreads();  // the values are written: their place is free
+  for (; full; full &= full - 1)
+    block_mean<T, INTERLEAVED>(a, l, tile, reinterpret_cast<float*>(turn), t0, __builtin_ctzll(full), h, earlier);
 }
 
 template <typename F>
@@ -358,10 +445,11 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
                          const sdnn_heads& v, const sdnn_rotation* r, const sdnn_heads* q,
                          const sdnn_heads* q_out, hipStream_t stream) {
   AppendArgs a = {};
+  int64_t q_blocks = 0;
   if (q && q->heads > 0) {
     a.q = rope_args(*q, *q_out, c.dtype, t.tokens, c.head_dim, t.pos, r);
     a.q.seq = t.seq, a.q.sequences = t.sequences;
-    a.q_blocks = (t.tokens + a.q.tile - 1) / a.q.tile;
+    q_blocks = (t.tokens + a.q.tile - 1) / a.q.tile;
   }
   a.k = k.data, a.k_token = k.token_stride, a.k_head = k.head_stride;
   a.v = v.data, a.v_token = v.token_stride, a.v_head = v.head_stride;
@@ -371,14 +459,36 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.freq = r ? r->freq : nullptr, a.amplitude = r ? r->amplitude : 1.0, a.pairs = r ? r->pairs : 0;
   a.tokens = t.tokens, a.sequences = t.sequences, a.max_blocks = t.max_blocks;
   a.kv_heads = c.kv_heads, a.head_dim = c.head_dim, a.block = c.block;
-  // one token to a workgroup until they fill the device several times, then windows whose values
-  // are written in runs
+  // one token to a workgroup; in prompts, and where single tokens fill the device several times, windows
+  // whose values are written in runs
+  const int size = dtype_bytes(c.dtype), layout = r ? r->layout : SDNN_ROPE_HALF;
   a.window = 1;
-  if ((int64_t)t.tokens * c.kv_heads > 4096)
-    a.window = kWindow * c.head_dim * dtype_bytes(c.dtype) <= kTileBytes ? kWindow : kWindow / 2;
-  const int64_t blocks = a.q_blocks + (int64_t)((t.tokens + a.window - 1) / a.window) * c.kv_heads;
-  return by_type(c.dtype, r ? r->layout : SDNN_ROPE_HALF, [&](auto ty, auto il) {
-    append_kernel<decltype(ty), decltype(il)::value><<<(unsigned)blocks, kThreads, 0, stream>>>(a);
+  if (t.tokens >= kWindow && ((int64_t)t.tokens * c.kv_heads > 4096 || t.tokens >= (int64_t)16 * t.sequences))
+    a.window = kWindow * c.head_dim * size <= kTileBytes ? kWindow : kWindow / 2;
+  // The keys' units are 16-byte ones where windows have many and the head divides by them.
+  const int wide = 16 / size / (layout == SDNN_ROPE_INTERLEAVED ? 2 : 1);
+  const bool whole = rope_vec(c.dtype, layout, a.pairs, c.head_dim) == wide, vec = a.window > 1 && whole;
+  a.k_whole = whole && rows_aligned(k.data, k.token_stride, k.head_stride, 16 / size, c.dtype);
+  a.k_aligned = !vec || rows_aligned(k.data, k.token_stride, k.head_stride, 16 / size, c.dtype);
+  if (!vec && layout == SDNN_ROPE_INTERLEAVED) a.k_aligned = rows_aligned(k.data, k.token_stride, k.head_stride, 2, c.dtype);
+  a.v_aligned = rows_aligned(v.data, v.token_stride, v.head_stride, 16 / size, c.dtype);
+  // LDS: the keys, then the values or the sums of a mean; the queries' cosines and sines
+  size_t lds = value_bytes(a.window, c.head_dim, size), sums = (size_t)c.block / kSumRows * c.head_dim * sizeof(float);
+  lds = key_bytes(a.window, c.head_dim, size) + (lds > sums ? lds : sums);
+  if (lds < (size_t)a.q.tile * a.q.pairs * sizeof(float2)) lds = (size_t)a.q.tile * a.q.pairs * sizeof(float2);
+  const int64_t windows = (t.tokens + a.window - 1) / a.window + (a.window > 1);  // one more where they are shifted
+  a.kv_blocks = (int32_t)(windows * c.kv_heads);
+  const int64_t blocks = a.kv_blocks + q_blocks;
+  return by_type(c.dtype, layout, [&](auto ty, auto il) {
+    typedef decltype(ty) T;
+    constexpr bool IL = decltype(il)::value;
+    const auto kernel = vec ? append_kernel<T, IL, 16 / (int)sizeof(T) / (IL ? 2 : 1)> : append_kernel<T, IL, 1>;
+    if (lds > 65536) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+    }
+    kernel<<<(unsigned)blocks, kThreads, lds, stream>>>(a);
     return hipGetLastError();
   });
 }
