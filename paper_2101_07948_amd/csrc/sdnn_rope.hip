@@ -24,10 +24,14 @@ struct RopeRows {
   int32_t x_aligned, y_aligned;
 };
 
+// Values of a unit past the rotated part, where one of VP pairs turns: as many bytes as that takes in one access.
+template <bool INTERLEAVED>
+__host__ __device__ constexpr int rest_values(int vp) { return INTERLEAVED && vp > 1 ? 2 * vp : vp; }
+
 // A workgroup rotates all heads of `tile` tokens.  The work is moving bytes: each value is read
 // and written once.  The cosines and sines, 64-bit arithmetic, are computed once per token and pair
-// and shared by the heads through LDS.  A thread keeps one unit of a row, VP pairs or VP values
-// past the rotated part, and walks tokens and heads.
+// and shared by the heads through LDS.  A thread keeps one unit of a row, VP pairs or the values
+// of one access past the rotated part, and walks tokens and heads.
 template <typename T, int VP, bool INTERLEAVED>
 __device__ __forceinline__ void rope_rows(const RopeRows& a, int block, float2* cs) {
   const int t0 = block * a.tile;
@@ -39,8 +43,9 @@ __device__ __forceinline__ void rope_rows(const RopeRows& a, int block, float2* 
     cs[i] = f;
   }
   __syncthreads();
+  constexpr int REST = rest_values<INTERLEAVED>(VP);
   const int turning = a.pairs / VP;
-  const int units = turning + (a.head_dim - 2 * a.pairs) / VP;
+  const int units = turning + (a.head_dim - 2 * a.pairs) / REST;
   const int rows = kThreads / units;  // units <= head_dim <= kThreads
   const int u = threadIdx.x % units, h0 = threadIdx.x / units;
   if (h0 >= rows) return;
@@ -50,15 +55,15 @@ __device__ __forceinline__ void rope_rows(const RopeRows& a, int block, float2* 
     const bool empty =
         a.seq && (a.pos[t0 + t] < 0 || (uint32_t)a.seq[t0 + t] >= (uint32_t)a.sequences);
     if (u >= turning) {
-      const int d = 2 * a.pairs + (u - turning) * VP;
+      const int d = 2 * a.pairs + (u - turning) * REST;
       for (int h = h0; h < a.heads; h += rows) {
-        T v[VP];
-        load_n<VP>(xt + h * a.x_head + d, a.x_aligned, v);
+        T v[REST];
+        load_n<REST>(xt + h * a.x_head + d, a.x_aligned, v);
         if (empty) {
 #pragma unroll
-          for (int i = 0; i < VP; ++i) v[i] = (T)0.0f;
+          for (int i = 0; i < REST; ++i) v[i] = (T)0.0f;
         }
-        store_n<VP>(yt + h * a.y_head + d, a.y_aligned, v);
+        store_n<REST>(yt + h * a.y_head + d, a.y_aligned, v);
       }
       continue;
     }
@@ -120,7 +125,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeRows a) {
 // fewer where a row's two parts do not divide by it.
 int rope_vec(int dtype, int layout, int pairs, int head_dim) {
   int v = 16 / dtype_bytes(dtype) / (layout == SDNN_ROPE_INTERLEAVED ? 2 : 1);
-  while (v > 1 && (pairs % v || (head_dim - 2 * pairs) % v)) v /= 2;
+  const bool il = layout == SDNN_ROPE_INTERLEAVED;
+  while (v > 1 && (pairs % v || (head_dim - 2 * pairs) % (il ? rest_values<true>(v) : rest_values<false>(v)))) v /= 2;
   return v;
 }
 
@@ -336,17 +342,18 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     store_n<V>(turn + i * stride + d, true, x);
   }
   const T* k = static_cast<const T*>(a.k) + t0 * a.k_token + h * a.k_head;
-  const int turning = a.pairs / VP, units = turning + (D - 2 * a.pairs) / VP;
+  constexpr int REST = rest_values<INTERLEAVED>(VP);
+  const int turning = a.pairs / VP, units = turning + (D - 2 * a.pairs) / REST;
 #pragma unroll 2
   for (int j = threadIdx.x; j < n * units; j += kThreads) {
     const int i = j / units, u = j - i * units;
     const T* x = k + i * a.k_token;
     T* y = tile + i * D;
     if (u >= turning) {
-      const int d = 2 * a.pairs + (u - turning) * VP;
-      T w[VP];
-      load_n<VP>(x + d, a.k_aligned, w);
-      store_n<VP>(y + d, VP > 1, w);
+      const int d = 2 * a.pairs + (u - turning) * REST;
+      T w[REST];
+      load_n<REST>(x + d, a.k_aligned, w);
+      store_n<REST>(y + d, VP > 1, w);
       continue;
     }
     T lo[VP], hi[VP];
