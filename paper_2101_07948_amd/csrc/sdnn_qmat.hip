@@ -10,7 +10,7 @@ namespace {
 // chunk, i = 0 ... 7, number i at bit 8 i (i < 4) or 8 (i - 4) + 4: what the lane gives to matrix
 // instruction j as its operand, one mask and four byte conversions for each half.  A wave reads
 // 1 KiB in one access.  The scales and zero points follow: [tile][group][16 rows].
-constexpr int kWaves = 8;
+constexpr int kMaxWaves = 16;
 
 __global__ __launch_bounds__(256) void qmat_pack(const uint8_t* packed, int32_t M, int32_t K, int32_t chunks,
                                                  int64_t dwords, uint32_t* out) {
@@ -53,12 +53,29 @@ struct QmatArgs {
   const float* bias;
   int32_t M, K, N, chunks, groups, group_chunks;  // chunks of a group of 128 columns or more
   int32_t scale_dtype, epi;
-  int32_t x_aligned;  // a column's values are contiguous and 16-byte aligned
 };
 
-// What a lane gives to the matrix instruction of columns [k, k + 8) for the column of x that it has.
+// What a lane gives to the matrix instruction of columns [k, k + 8) for the column of x that it has: the values
+// as loaded, and as the operand.
 template <typename T>
 struct Operand;
+
+// 8 values from x + k * x_feature on.  Contiguous ones come in 16-byte loads whatever their alignment (the
+// hardware takes any; one by one, the 13 columns of an odd-sized layer took 7 times as long).
+template <typename T>
+__device__ __forceinline__ void load8(const T* x, const QmatArgs& a, int k, T (&v)[8]) {
+  if (k + 8 <= a.K) {
+    if (a.x_feature == 1) {
+      __builtin_memcpy(v, x + k, sizeof(v));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = x[(k + i) * a.x_feature];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = k + i < a.K ? x[(k + i) * a.x_feature] : (T)0.0f;
+  }
+}
 
 template <typename T, typename V8>
 struct Operand16 {
@@ -67,16 +84,7 @@ struct Operand16 {
   // Row p of the operand is column p / 4 + 4 (p % 4) of x: with up to four columns, the results are in
   // the first of a lane's four registers.
   static __device__ __forceinline__ int token(int p) { return (p >> 2) + 4 * (p & 3); }
-  static __device__ __forceinline__ V8 load(const T* x, const QmatArgs& a, int k, bool live, int) {
-    V8 v = {};
-    if (live && a.x_aligned && k + 8 <= a.K) return *reinterpret_cast<const V8*>(x + k);
-    if (live) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < a.K) v[i] = x[(k + i) * a.x_feature];
-    }
-    return v;
-  }
+  static __device__ __forceinline__ V8 operand(const T (&v)[8], int) { return *reinterpret_cast<const V8*>(v); }
   static __device__ __forceinline__ V8 weights(uint32_t w) {
     const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
     V8 v;
@@ -108,17 +116,7 @@ struct Operand<float> {
   typedef bf16x8 type;
   static constexpr int kTokens = 4;
   static __device__ __forceinline__ int token(int p) { return p >> 2; }
-  static __device__ __forceinline__ bf16x8 load(const float* x, const QmatArgs& a, int k, bool live, int part) {
-    float f[8] = {};
-    if (live && a.x_aligned && k + 8 <= a.K) {
-      const f32x4 u = *reinterpret_cast<const f32x4*>(x + k), v = *reinterpret_cast<const f32x4*>(x + k + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = u[i], f[4 + i] = v[i];
-    } else if (live) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i < a.K) f[i] = x[(k + i) * a.x_feature];
-    }
+  static __device__ __forceinline__ bf16x8 operand(const float (&f)[8], int part) {
     const float second = part >= 1 ? 1.0f : 0.0f, third = part >= 2 ? 1.0f : 0.0f;
     bf16x8 v;
 #pragma unroll
@@ -140,17 +138,50 @@ __device__ __forceinline__ float scale_at(const QmatArgs& a, int64_t i) {
   return (float)reinterpret_cast<const __bf16*>(a.scales)[i];
 }
 
-// A workgroup has 16 rows of W and up to 16 columns of x (4 in 32 bits); its waves share the chunks.
-// With n the 4-bit numbers, a group of columns adds  s (sum n x - z sum x):  both sums come from the
-// matrix unit, the second with ones for the numbers, and are scaled once a group.
+// A chunk of a tile on its way to the registers: 16 bytes of weights, the lane's column of x, scales and zeros.
+template <typename T, int STEPS>
+struct Chunk {
+  i32x4 w;
+  T x[4][8];
+  float scale[4 / STEPS], zero[4 / STEPS];
+  __device__ __forceinline__ void load(const QmatArgs& a, const i32x4* w0, const T* x0, bool live, int64_t meta0,
+                                       int c, int g) {
+    w = w0[(int64_t)c * 64];
+#pragma unroll
+    for (int i = 0; i < 4 / STEPS; ++i) {
+      // (a group past the last, where K ends within the chunk, meets zeros of x)
+      const int group = STEPS == 4 ? c / a.group_chunks : min(c * (4 / STEPS) + i, a.groups - 1);
+      const int64_t at = meta0 + (int64_t)group * kQTileRows;
+      scale[i] = scale_at(a, at);
+      zero[i] = a.zeros ? (float)a.zeros[at] : 8.0f;
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (live) {
+        load8(x0, a, c * kQChunk + s * 32 + g * 8, x[s]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[s][i] = (T)0.0f;
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);  // under way before the chunk before is multiplied
+  }
+};
+
+// A workgroup has 16 rows of W and up to 16 columns of x (4 in 32 bits); its waves share the chunks, each with
+// the next one under way while it multiplies.  With n the 4-bit numbers, a group of columns adds
+// s (sum n x - z sum x): both sums come from the matrix unit, the second with ones for the numbers, and are
+// scaled once a group.  What bounds it: reading the weights (half a byte each; the conversion takes two vector
+// instructions of 64 lanes for 64 of them).
 //   STEPS: matrix instructions (of 32 columns) of a group within a chunk.
 //   REGS: of a lane's four result registers, those that hold columns of x.
 template <typename T, int STEPS, int REGS>
-__global__ __launch_bounds__(kWaves * 64) void qmat_kernel(QmatArgs a) {
+__global__ __launch_bounds__(kMaxWaves * 64) void qmat_kernel(QmatArgs a) {
   typedef Operand<T> Op;
   constexpr bool kParts = sizeof(T) == 4;
-  __shared__ float sums[kWaves][REGS][64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane & 15, g = lane >> 4;
+  __shared__ float sums[kMaxWaves][REGS][64];
+  const int lane = threadIdx.x % 64, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
   const int64_t tile = blockIdx.x;
   const int n0 = blockIdx.y * Op::kTokens, part = r & 3;
   const int token = n0 + Op::token(r);
@@ -162,36 +193,41 @@ __global__ __launch_bounds__(kWaves * 64) void qmat_kernel(QmatArgs a) {
   typename Op::type ones;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = 1.0f;
-  for (int c = wave; c < a.chunks; c += kWaves) {
-    const i32x4 wc = w[(int64_t)c * 64];
+  const auto add = [&](const Chunk<T, STEPS>& b) {
 #pragma unroll
-    for (int s0 = 0; s0 < 4; s0 += STEPS) {
+    for (int i = 0; i < 4 / STEPS; ++i) {
       f32x4 d = {0, 0, 0, 0}, sx = {0, 0, 0, 0};
 #pragma unroll
-      for (int s = s0; s < s0 + STEPS; ++s) {
-        const auto xv = Op::load(x, a, c * kQChunk + s * 32 + g * 8, live, part);
-        d = Op::mfma(xv, Op::weights((uint32_t)wc[s]), d);
+      for (int s = i * STEPS; s < (i + 1) * STEPS; ++s) {
+        const auto xv = Op::operand(b.x[s], part);
+        d = Op::mfma(xv, Op::weights((uint32_t)b.w[s]), d);
         sx = Op::mfma(xv, ones, sx);
       }
-      const int group = STEPS == 4 ? c / a.group_chunks : c * (4 / STEPS) + s0 / STEPS;
-      if (STEPS < 4 && group >= a.groups) break;  // columns past K
-      const int64_t at = meta0 + (int64_t)group * kQTileRows;
-      const float s = scale_at(a, at), z = a.zeros ? (float)a.zeros[at] : 8.0f;
+      const float s = b.scale[i], z = b.zero[i];
       if (kParts) {
         acc[0] = fmaf(s, fmaf(-z, (sx[0] + sx[1]) + sx[2], (d[0] + d[1]) + d[2]), acc[0]);
       } else {
 #pragma unroll
-        for (int i = 0; i < REGS; ++i) acc[i] = fmaf(s, fmaf(-z, sx[i], d[i]), acc[i]);
+        for (int k = 0; k < REGS; ++k) acc[k] = fmaf(s, fmaf(-z, sx[k], d[k]), acc[k]);
       }
     }
+  };
+  Chunk<T, STEPS> even, odd;
+  int c = wave;
+  if (c < a.chunks) even.load(a, w, x, live, meta0, c, g);
+  for (; c < a.chunks; c += 2 * waves) {
+    if (c + waves < a.chunks) odd.load(a, w, x, live, meta0, c + waves, g);
+    add(even);
+    if (c + waves >= a.chunks) break;
+    if (c + 2 * waves < a.chunks) even.load(a, w, x, live, meta0, c + 2 * waves, g);
+    add(odd);
   }
 #pragma unroll
   for (int i = 0; i < REGS; ++i) sums[wave][i][lane] = acc[i];
   __syncthreads();
   if (wave >= REGS) return;
   float v = 0.0f;
-#pragma unroll
-  for (int k = 0; k < kWaves; ++k) v += sums[k][wave][lane];
+  for (int k = 0; k < waves; ++k) v += sums[k][wave][lane];
   const int64_t m = tile * kQTileRows + r;
   const int n = n0 + g + 4 * wave;  // row 4 g + wave of the result
   if (m >= a.M || n >= a.N) return;
@@ -203,12 +239,16 @@ template <typename T, int STEPS>
 hipError_t start_regs(const QmatArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.M + kQTileRows - 1) / kQTileRows),
                   (unsigned)((a.N + Operand<T>::kTokens - 1) / Operand<T>::kTokens));
+  // 8 waves to a tile of rows, 16 where there are fewer tiles than compute units; not more than chunks
+  const int most = grid.x * grid.y < 256 ? kMaxWaves : 8;
+  int waves = 4;
+  while (waves < most && waves < a.chunks) waves *= 2;
   if (sizeof(T) == 4 || a.N <= 4)
-    qmat_kernel<T, STEPS, 1><<<grid, kWaves * 64, 0, stream>>>(a);
+    qmat_kernel<T, STEPS, 1><<<grid, waves * 64, 0, stream>>>(a);
   else if (a.N <= 8)
-    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 2><<<grid, kWaves * 64, 0, stream>>>(a);
+    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 2><<<grid, waves * 64, 0, stream>>>(a);
   else
-    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 4><<<grid, kWaves * 64, 0, stream>>>(a);
+    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 4><<<grid, waves * 64, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -254,8 +294,6 @@ hipError_t launch_qmat(const sdnn_qmat_s& w, const void* x, int64_t x_feature, i
   a.bias = bias, a.M = w.M, a.K = w.K, a.N = N, a.chunks = w.chunks;
   a.group_chunks = w.group >= kQChunk ? w.group / kQChunk : 1;
   a.scale_dtype = w.scale_dtype, a.epi = epi;
-  const int e = dtype_bytes(dtype);
-  a.x_aligned = x_feature == 1 && (uintptr_t)x % 16 == 0 && (N == 1 || x_column * e % 16 == 0);
   if (dtype == SDNN_F32) return start<float>(a, w.group, stream);
   if (dtype == SDNN_F16) return start<_Float16>(a, w.group, stream);
   return start<__bf16>(a, w.group, stream);
