@@ -7,9 +7,12 @@ namespace {
 
 // Layout of the weights: tiles of 16 rows, of these chunks of 128 columns, of these 16 bytes for
 // each of 64 lanes.  Lane l has row l & 15; its dword j holds columns 32 j + 8 (l / 16) + i of the
-// chunk, i = 0 ... 7, number i at bit 8 i (i < 4) or 8 (i - 4) + 4: what the lane gives to matrix
-// instruction j as its operand, one mask and four byte conversions for each half.  A wave reads
-// 1 KiB in one access.  The scales and zero points follow: [tile][group][16 rows].
+// chunk, i = 0 ... 7: what the lane gives to matrix instruction j as its operand.  Columns 2 p and 2 p + 1 have
+// their 4 bits at bit 3 + 4 p of the dword's lower and upper half (turned by 12 for p = 3, where the upper ones
+// wrap around): after a shift and one mask they are the upper mantissa bits of two bf16 numbers 16 + n.  A wave reads
+// 1 KiB in one access.  The scales and zero points follow: [tile][group][16 rows] where groups are whole chunks,
+// else [tile][chunk][16 rows][group of the chunk], so that a lane has those of a chunk in one access.
+__host__ __device__ constexpr int bit_of(int i) { return (3 + 4 * (i / 2) + 16 * (i % 2)) % 32; }
 constexpr int kMaxWaves = 16;
 
 __global__ __launch_bounds__(256) void qmat_pack(const uint8_t* packed, int32_t M, int32_t K, int32_t chunks,
@@ -26,21 +29,26 @@ __global__ __launch_bounds__(256) void qmat_pack(const uint8_t* packed, int32_t 
       const int k = k0 + i;
       if (k >= K) break;
       const uint32_t b = packed[row * ((K + 1) / 2) + k / 2];
-      w |= (k & 1 ? b >> 4 : b & 15) << (i < 4 ? 8 * i : 8 * (i - 4) + 4);
+      const uint32_t n = k & 1 ? b >> 4 : b & 15, at = bit_of(i);
+      w |= n << at | (at > 28 ? n >> (32 - at) : 0);
     }
   out[at] = w;
 }
 
-// scales (of `bytes` each) and zero points to [tile][group][16 rows]; rows past M get zeros.
+// Scales (of `bytes` each) and zero points in that order, zeros past M and past the last group.  `outer`: groups of
+// whole chunks, or chunks; `inner`: groups of a chunk, or 1.
 __global__ __launch_bounds__(256) void qmat_pack_meta(const uint8_t* scales, int32_t bytes, const uint8_t* zeros,
-                                                      int32_t M, int32_t groups, int64_t count, uint8_t* out) {
+                                                      int32_t M, int32_t groups, int32_t outer, int32_t inner,
+                                                      int64_t count, uint8_t* out) {
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= count) return;
-  const int64_t tg = at / kQTileRows;
-  const int64_t row = tg / groups * kQTileRows + at % kQTileRows;
-  const int64_t from = row * groups + tg % groups;
-  for (int i = 0; i < bytes; ++i) out[at * bytes + i] = row < M ? scales[from * bytes + i] : 0;
-  if (zeros) out[count * bytes + at] = row < M ? zeros[from] : 0;
+  const int64_t to = at / (kQTileRows * inner);
+  const int64_t row = to / outer * kQTileRows + at / inner % kQTileRows;
+  const int64_t group = to % outer * inner + at % inner;
+  const bool there = row < M && group < groups;
+  const int64_t from = row * groups + group;
+  for (int i = 0; i < bytes; ++i) out[at * bytes + i] = there ? scales[from * bytes + i] : 0;
+  if (zeros) out[count * bytes + at] = there ? zeros[from] : 0;
 }
 
 struct QmatArgs {
@@ -51,7 +59,9 @@ struct QmatArgs {
   void* y;
   int64_t x_feature, x_column, y_feature, y_column;
   const float* bias;
-  int32_t M, K, N, chunks, groups, group_chunks;  // chunks of a group of 128 columns or more
+  int32_t M, K, N, chunks;
+  int32_t metas;      // groups of whole chunks of a tile, or its chunks
+  uint32_t group_of;  // of chunk c, where groups are whole chunks: the upper 32 bits of c * group_of (0: c)
   int32_t scale_dtype, epi;
 };
 
@@ -60,21 +70,29 @@ struct QmatArgs {
 template <typename T>
 struct Operand;
 
-// 8 values from x + k * x_feature on.  Contiguous ones come in 16-byte loads whatever their alignment (the
-// hardware takes any; one by one, the 13 columns of an odd-sized layer took 7 times as long).
-template <typename T>
+// 8 values of a column of x from value k on.  PART: zeros from K on.  Contiguous ones come in 16-byte loads whatever
+// their alignment (the hardware takes any; one by one, the 13 columns of an odd-sized layer took twice as long).
+template <bool CONTIGUOUS, bool PART, typename T>
 __device__ __forceinline__ void load8(const T* x, const QmatArgs& a, int k, T (&v)[8]) {
-  if (k + 8 <= a.K) {
-    if (a.x_feature == 1) {
-      __builtin_memcpy(v, x + k, sizeof(v));
-    } else {
+  if (PART) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = x[(k + i) * a.x_feature];
+    for (int i = 0; i < 8; ++i) {
+      const T e = x[(int64_t)min(k + i, a.K - 1) * a.x_feature];
+      v[i] = k + i < a.K ? e : (T)0.0f;
     }
+  } else if (CONTIGUOUS) {
+    __builtin_memcpy(v, x + k, sizeof(v));
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k + i < a.K ? x[(k + i) * a.x_feature] : (T)0.0f;
+    for (int i = 0; i < 8; ++i) v[i] = x[(k + i) * a.x_feature];
   }
+}
+
+// Pair p of a dword's numbers, at bits AT and 16 + AT.
+template <int AT>
+__device__ __forceinline__ uint32_t pair_at(uint32_t w, int p) {
+  const int right = (3 + 4 * p - AT) & 31;
+  return right == 0 ? w : __builtin_amdgcn_alignbit(w, w, right);
 }
 
 template <typename T, typename V8>
@@ -85,15 +103,15 @@ struct Operand16 {
   // the first of a lane's four registers.
   static __device__ __forceinline__ int token(int p) { return (p >> 2) + 4 * (p & 3); }
   static __device__ __forceinline__ V8 operand(const T (&v)[8], int) { return *reinterpret_cast<const V8*>(v); }
+  // The 8 numbers of a dword as 16 + n, two a mask: with 16 the 4 bits are the upper ones of the mantissa.
   static __device__ __forceinline__ V8 weights(uint32_t w) {
-    const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
-    V8 v;
+    constexpr bool HALF = __is_same(T, _Float16);
+    constexpr int AT = HALF ? 6 : 3;
+    constexpr uint32_t SIXTEEN = HALF ? 0x4c004c00u : 0x41804180u, MASK = 0x000f000fu << AT;
+    i32x4 v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = (T)(float)((lo >> (8 * i)) & 255u);
-      v[4 + i] = (T)(float)((hi >> (8 * i)) & 255u);
-    }
-    return v;
+    for (int p = 0; p < 4; ++p) v[p] = (int32_t)((pair_at<AT>(w, p) & MASK) | SIXTEEN);
+    return __builtin_bit_cast(V8, v);
   }
 };
 template <>
@@ -109,8 +127,8 @@ struct Operand<__bf16> : Operand16<__bf16, bf16x8> {
   }
 };
 // 32-bit activations as the exact sum of three bf16 numbers of 8 bits each, in three rows of the
-// operand: row p is part p % 4 of column p / 4 (part 3: nothing).  The 4-bit numbers are exact in
-// bf16, so every product is exact.
+// operand: row p is part p % 4 of column p / 4 (part 3 is not used).  The numbers are exact in bf16, so
+// every product is exact.
 template <>
 struct Operand<float> {
   typedef bf16x8 type;
@@ -132,10 +150,28 @@ struct Operand<float> {
   static __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return Operand<__bf16>::mfma(a, b, c); }
 };
 
-__device__ __forceinline__ float scale_at(const QmatArgs& a, int64_t i) {
-  if (a.scale_dtype == SDNN_F32) return reinterpret_cast<const float*>(a.scales)[i];
-  if (a.scale_dtype == SDNN_F16) return (float)reinterpret_cast<const _Float16*>(a.scales)[i];
-  return (float)reinterpret_cast<const __bf16*>(a.scales)[i];
+// N scales from scale i on (N bytes or more apart: one access), and zero points.
+template <int N>
+__device__ __forceinline__ void load_scales(const QmatArgs& a, int64_t i, float (&scale)[N], float (&zero)[N]) {
+  if (a.scale_dtype == SDNN_F32) {
+    load_n<N>(reinterpret_cast<const float*>(a.scales) + i, true, scale);
+  } else if (a.scale_dtype == SDNN_F16) {
+    _Float16 s[N];
+    load_n<N>(reinterpret_cast<const _Float16*>(a.scales) + i, true, s);
+#pragma unroll
+    for (int k = 0; k < N; ++k) scale[k] = (float)s[k];
+  } else {
+    __bf16 s[N];
+    load_n<N>(reinterpret_cast<const __bf16*>(a.scales) + i, true, s);
+#pragma unroll
+    for (int k = 0; k < N; ++k) scale[k] = (float)s[k];
+  }
+  uint8_t z[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) z[k] = 8;
+  if (a.zeros) load_n<N>(a.zeros + i, true, z);
+#pragma unroll
+  for (int k = 0; k < N; ++k) zero[k] = (float)z[k];
 }
 
 // A chunk of a tile on its way to the registers: 16 bytes of weights, the lane's column of x, scales and zeros.
@@ -144,38 +180,27 @@ struct Chunk {
   i32x4 w;
   T x[4][8];
   float scale[4 / STEPS], zero[4 / STEPS];
-  __device__ __forceinline__ void load(const QmatArgs& a, const i32x4* w0, const T* x0, bool live, int64_t meta0,
-                                       int c, int g) {
+  // w0: of the lane in the first chunk; x0: the lane's column; meta0: the lane's row of the first scales.
+  template <bool CONTIGUOUS, bool PART>
+  __device__ __forceinline__ void load(const QmatArgs& a, const i32x4* w0, const T* x0, int64_t meta0, int c, int g) {
     w = w0[(int64_t)c * 64];
+    const int meta = STEPS == 4 && a.group_of ? (int)__umulhi((uint32_t)c, a.group_of) : c;
+    load_scales<4 / STEPS>(a, meta0 + (int64_t)meta * (kQTileRows * (4 / STEPS)), scale, zero);
 #pragma unroll
-    for (int i = 0; i < 4 / STEPS; ++i) {
-      // (a group past the last, where K ends within the chunk, meets zeros of x)
-      const int group = STEPS == 4 ? c / a.group_chunks : min(c * (4 / STEPS) + i, a.groups - 1);
-      const int64_t at = meta0 + (int64_t)group * kQTileRows;
-      scale[i] = scale_at(a, at);
-      zero[i] = a.zeros ? (float)a.zeros[at] : 8.0f;
-    }
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (live) {
-        load8(x0, a, c * kQChunk + s * 32 + g * 8, x[s]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[s][i] = (T)0.0f;
-      }
-    }
+    for (int s = 0; s < 4; ++s) load8<CONTIGUOUS, PART>(x0, a, c * kQChunk + s * 32 + g * 8, x[s]);
     __builtin_amdgcn_sched_barrier(0);  // under way before the chunk before is multiplied
   }
 };
 
 // A workgroup has 16 rows of W and up to 16 columns of x (4 in 32 bits); its waves share the chunks, each with
 // the next one under way while it multiplies.  With n the 4-bit numbers, a group of columns adds
-// s (sum n x - z sum x): both sums come from the matrix unit, the second with ones for the numbers, and are
-// scaled once a group.  What bounds it: reading the weights (half a byte each; the conversion takes two vector
-// instructions of 64 lanes for 64 of them).
+// s (sum (16 + n) x - (16 + z) sum x): both sums come from the matrix unit, the second with ones for the
+// numbers, and are scaled once a group.  The 16 costs a bit of the 32-bit sums, and saves half of the
+// instructions that make numbers of the bits.
 //   STEPS: matrix instructions (of 32 columns) of a group within a chunk.
 //   REGS: of a lane's four result registers, those that hold columns of x.
-template <typename T, int STEPS, int REGS>
+//   CONTIGUOUS: a column's values are.
+template <typename T, int STEPS, int REGS, bool CONTIGUOUS>
 __global__ __launch_bounds__(kMaxWaves * 64) void qmat_kernel(QmatArgs a) {
   typedef Operand<T> Op;
   constexpr bool kParts = sizeof(T) == 4;
@@ -185,10 +210,9 @@ __global__ __launch_bounds__(kMaxWaves * 64) void qmat_kernel(QmatArgs a) {
   const int64_t tile = blockIdx.x;
   const int n0 = blockIdx.y * Op::kTokens, part = r & 3;
   const int token = n0 + Op::token(r);
-  const bool live = token < a.N && !(kParts && part == 3);
-  const T* x = static_cast<const T*>(a.x) + (live ? token : 0) * a.x_column;
+  const T* x = static_cast<const T*>(a.x) + (token < a.N ? token : 0) * a.x_column;  // (others' rows are not used)
   const i32x4* w = a.weights + tile * a.chunks * 64 + lane;
-  const int64_t meta0 = tile * a.groups * kQTileRows + r;
+  const int64_t meta0 = (tile * a.metas * kQTileRows + r) * (4 / STEPS);
   float acc[REGS] = {};
   typename Op::type ones;
 #pragma unroll
@@ -203,7 +227,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void qmat_kernel(QmatArgs a) {
         d = Op::mfma(xv, Op::weights((uint32_t)b.w[s]), d);
         sx = Op::mfma(xv, ones, sx);
       }
-      const float s = b.scale[i], z = b.zero[i];
+      const float s = b.scale[i], z = b.zero[i] + 16.0f;
       if (kParts) {
         acc[0] = fmaf(s, fmaf(-z, (sx[0] + sx[1]) + sx[2], (d[0] + d[1]) + d[2]), acc[0]);
       } else {
@@ -212,15 +236,23 @@ __global__ __launch_bounds__(kMaxWaves * 64) void qmat_kernel(QmatArgs a) {
       }
     }
   };
-  Chunk<T, STEPS> even, odd;
-  int c = wave;
-  if (c < a.chunks) even.load(a, w, x, live, meta0, c, g);
-  for (; c < a.chunks; c += 2 * waves) {
-    if (c + waves < a.chunks) odd.load(a, w, x, live, meta0, c + waves, g);
-    add(even);
-    if (c + waves >= a.chunks) break;
-    if (c + 2 * waves < a.chunks) even.load(a, w, x, live, meta0, c + 2 * waves, g);
-    add(odd);
+  const int whole = a.K / kQChunk;  // chunks; of one more, K ends within
+  {
+    Chunk<T, STEPS> even, odd;
+    int c = wave;
+    if (c < whole) even.template load<CONTIGUOUS, false>(a, w, x, meta0, c, g);
+    for (; c < whole; c += 2 * waves) {
+      if (c + waves < whole) odd.template load<CONTIGUOUS, false>(a, w, x, meta0, c + waves, g);
+      add(even);
+      if (c + waves >= whole) break;
+      if (c + 2 * waves < whole) even.template load<CONTIGUOUS, false>(a, w, x, meta0, c + 2 * waves, g);
+      add(odd);
+    }
+  }
+  if (whole < a.chunks && wave == whole % waves) {
+    Chunk<T, STEPS> last;
+    last.template load<CONTIGUOUS, true>(a, w, x, meta0, whole, g);
+    add(last);
   }
 #pragma unroll
   for (int i = 0; i < REGS; ++i) sums[wave][i][lane] = acc[i];
@@ -235,48 +267,58 @@ __global__ __launch_bounds__(kMaxWaves * 64) void qmat_kernel(QmatArgs a) {
   static_cast<T*>(a.y)[m * a.y_feature + n * a.y_column] = (T)activation(v, a.epi);
 }
 
-template <typename T, int STEPS>
+template <typename T, int STEPS, bool CONTIGUOUS>
 hipError_t start_regs(const QmatArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.M + kQTileRows - 1) / kQTileRows),
                   (unsigned)((a.N + Operand<T>::kTokens - 1) / Operand<T>::kTokens));
-  // 8 waves to a tile of rows, 16 where there are fewer tiles than compute units; not more than chunks
+  // 8 waves to a tile of rows, 16 where there are fewer tiles than compute units, with as many chunks each as
+  // the one with most of them; 4 at least, which write the results
   const int most = grid.x * grid.y < 256 ? kMaxWaves : 8;
-  int waves = 4;
-  while (waves < most && waves < a.chunks) waves *= 2;
+  const int each = (a.chunks + most - 1) / most, needed = (a.chunks + each - 1) / each;
+  const int waves = needed < 4 ? 4 : needed;
   if (sizeof(T) == 4 || a.N <= 4)
-    qmat_kernel<T, STEPS, 1><<<grid, waves * 64, 0, stream>>>(a);
+    qmat_kernel<T, STEPS, 1, CONTIGUOUS><<<grid, waves * 64, 0, stream>>>(a);
   else if (a.N <= 8)
-    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 2><<<grid, waves * 64, 0, stream>>>(a);
+    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 2, CONTIGUOUS><<<grid, waves * 64, 0, stream>>>(a);
   else
-    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 4><<<grid, waves * 64, 0, stream>>>(a);
+    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 4, CONTIGUOUS><<<grid, waves * 64, 0, stream>>>(a);
   return hipGetLastError();
+}
+
+template <typename T, int STEPS>
+hipError_t start_steps(const QmatArgs& a, hipStream_t stream) {
+  return a.x_feature == 1 ? start_regs<T, STEPS, true>(a, stream) : start_regs<T, STEPS, false>(a, stream);
 }
 
 template <typename T>
 hipError_t start(const QmatArgs& a, int group, hipStream_t stream) {
-  if (group == 32) return start_regs<T, 1>(a, stream);
-  if (group == 64) return start_regs<T, 2>(a, stream);
-  return start_regs<T, 4>(a, stream);
+  if (group == 32) return start_steps<T, 1>(a, stream);
+  if (group == 64) return start_steps<T, 2>(a, stream);
+  return start_steps<T, 4>(a, stream);
 }
 
-int64_t groups_of(const sdnn_qmat_s& w) { return (w.K + w.group - 1) / w.group; }
+int32_t groups_of(const sdnn_qmat_s& w) { return (w.K + w.group - 1) / w.group; }
+// Of a tile's scales: entries along K, and scales of each entry and row.
+int32_t metas_of(const sdnn_qmat_s& w) { return w.group >= kQChunk ? groups_of(w) : w.chunks; }
+int32_t inner_of(const sdnn_qmat_s& w) { return w.group >= kQChunk ? 1 : kQChunk / w.group; }
+int64_t scales_of(const sdnn_qmat_s& w) { return (int64_t)w.tiles * metas_of(w) * inner_of(w) * kQTileRows; }
 
 }  // namespace
 
 int64_t qmat_weight_bytes(const sdnn_qmat_s& w) { return (int64_t)w.tiles * w.chunks * 1024; }
 int64_t qmat_meta_bytes(const sdnn_qmat_s& w) {
-  return w.tiles * groups_of(w) * kQTileRows * (dtype_bytes(w.scale_dtype) + (w.zeros ? 1 : 0));
+  return scales_of(w) * (dtype_bytes(w.scale_dtype) + (w.zeros ? 1 : 0));
 }
 
 hipError_t launch_qmat_pack(const sdnn_qmat_s& w, const uint8_t* packed, const void* scales,
                             const uint8_t* zeros, hipStream_t stream) {
-  const int64_t dwords = qmat_weight_bytes(w) / 4, entries = w.tiles * groups_of(w) * kQTileRows;
+  const int64_t dwords = qmat_weight_bytes(w) / 4, entries = scales_of(w);
   qmat_pack<<<(unsigned)((dwords + 255) / 256), 256, 0, stream>>>(
       packed, w.M, w.K, w.chunks, dwords, reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(w.weights)));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   qmat_pack_meta<<<(unsigned)((entries + 255) / 256), 256, 0, stream>>>(
-      static_cast<const uint8_t*>(scales), dtype_bytes(w.scale_dtype), zeros, w.M, (int32_t)groups_of(w), entries,
+      static_cast<const uint8_t*>(scales), dtype_bytes(w.scale_dtype), zeros, w.M, groups_of(w), metas_of(w), inner_of(w), entries,
       const_cast<uint8_t*>(w.meta));
   return hipGetLastError();
 }
@@ -287,12 +329,14 @@ hipError_t launch_qmat(const sdnn_qmat_s& w, const void* x, int64_t x_feature, i
   QmatArgs a = {};
   a.weights = reinterpret_cast<const i32x4*>(w.weights);
   a.scales = w.meta;
-  a.groups = (int32_t)groups_of(w);
-  a.zeros = w.zeros ? w.meta + (int64_t)w.tiles * a.groups * kQTileRows * dtype_bytes(w.scale_dtype) : nullptr;
+  a.metas = metas_of(w);
+  a.zeros = w.zeros ? w.meta + scales_of(w) * dtype_bytes(w.scale_dtype) : nullptr;
   a.x = x, a.x_feature = x_feature, a.x_column = x_column;
   a.y = y, a.y_feature = y_feature, a.y_column = y_column;
+  if (w.K == 1) a.x_feature = 1;  // one value is contiguous
   a.bias = bias, a.M = w.M, a.K = w.K, a.N = N, a.chunks = w.chunks;
-  a.group_chunks = w.group >= kQChunk ? w.group / kQChunk : 1;
+  const uint32_t group_chunks = w.group / kQChunk;  // (c * group_chunks < 2^32: the quotients are exact)
+  a.group_of = group_chunks > 1 ? (uint32_t)(((1ull << 32) + group_chunks - 1) / group_chunks) : 0;
   a.scale_dtype = w.scale_dtype, a.epi = epi;
   if (dtype == SDNN_F32) return start<float>(a, w.group, stream);
   if (dtype == SDNN_F16) return start<_Float16>(a, w.group, stream);
