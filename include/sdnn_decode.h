@@ -181,7 +181,8 @@ sdnn_status sdnn_qmat_create(const uint8_t* packed, const void* scales, sdnn_dty
  * x[k * x_feature + n * x_column] and value m of column n y[m * y_feature + n * y_column]:
  * a K x N matrix as sdnn_spmm takes it has strides (N, 1), rows of tokens (1, K).
  *   bias: device, M floats, or NULL.  The products are exact and are summed in 32 bits; x
- *   must be finite.  Made for few columns: the weights are read once for up to 64 of them.
+ *   must be finite.  Made for few columns: the weights are read once for every 16 of them (8 in
+ *   32 bits).
  * Errors: SDNN_ERR_NULL, SDNN_ERR_DIM, SDNN_ERR_DEVICE, SDNN_ERR_HIP. */
 sdnn_status sdnn_qmat_apply(sdnn_qmat w, const void* x, int64_t x_feature, int64_t x_column, void* y,
                             int64_t y_feature, int64_t y_column, int32_t N, sdnn_dtype dtype,

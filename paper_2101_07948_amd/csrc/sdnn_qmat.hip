@@ -1,4 +1,6 @@
 // Products of 4-bit weights with the activations of few tokens.
+#include <type_traits>
+
 #include "sdnn_decode_device.h"
 #include "sdnn_device.h"
 
@@ -65,29 +67,6 @@ struct QmatArgs {
   int32_t scale_dtype, epi;
 };
 
-// What a lane gives to the matrix instruction of columns [k, k + 8) for the column of x that it has: the values
-// as loaded, and as the operand.
-template <typename T>
-struct Operand;
-
-// 8 values of a column of x from value k on.  PART: zeros from K on.  Contiguous ones come in 16-byte loads whatever
-// their alignment (the hardware takes any; one by one, the 13 columns of an odd-sized layer took twice as long).
-template <bool CONTIGUOUS, bool PART, typename T>
-__device__ __forceinline__ void load8(const T* x, const QmatArgs& a, int k, T (&v)[8]) {
-  if (PART) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const T e = x[(int64_t)min(k + i, a.K - 1) * a.x_feature];
-      v[i] = k + i < a.K ? e : (T)0.0f;
-    }
-  } else if (CONTIGUOUS) {
-    __builtin_memcpy(v, x + k, sizeof(v));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = x[(k + i) * a.x_feature];
-  }
-}
-
 // Pair p of a dword's numbers, at bits AT and 16 + AT.
 template <int AT>
 __device__ __forceinline__ uint32_t pair_at(uint32_t w, int p) {
@@ -95,15 +74,11 @@ __device__ __forceinline__ uint32_t pair_at(uint32_t w, int p) {
   return right == 0 ? w : __builtin_amdgcn_alignbit(w, w, right);
 }
 
+// The matrix instruction of a type.  `weights`: the 8 numbers of a dword as 16 + n, two a mask: with 16 the 4 bits
+// are the upper ones of the mantissa.
 template <typename T, typename V8>
-struct Operand16 {
+struct Op16 {
   typedef V8 type;
-  static constexpr int kTokens = 16;
-  // Row p of the operand is column p / 4 + 4 (p % 4) of x: with up to four columns, the results are in
-  // the first of a lane's four registers.
-  static __device__ __forceinline__ int token(int p) { return (p >> 2) + 4 * (p & 3); }
-  static __device__ __forceinline__ V8 operand(const T (&v)[8], int) { return *reinterpret_cast<const V8*>(v); }
-  // The 8 numbers of a dword as 16 + n, two a mask: with 16 the 4 bits are the upper ones of the mantissa.
   static __device__ __forceinline__ V8 weights(uint32_t w) {
     constexpr bool HALF = __is_same(T, _Float16);
     constexpr int AT = HALF ? 6 : 3;
@@ -114,41 +89,98 @@ struct Operand16 {
     return __builtin_bit_cast(V8, v);
   }
 };
+template <typename T>
+struct Op;
 template <>
-struct Operand<_Float16> : Operand16<_Float16, f16x8> {
+struct Op<_Float16> : Op16<_Float16, f16x8> {
   static __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
 };
 template <>
-struct Operand<__bf16> : Operand16<__bf16, bf16x8> {
+struct Op<__bf16> : Op16<__bf16, bf16x8> {
   static __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
 };
-// 32-bit activations as the exact sum of three bf16 numbers of 8 bits each, in three rows of the
-// operand: row p is part p % 4 of column p / 4 (part 3 is not used).  The numbers are exact in bf16, so
-// every product is exact.
 template <>
-struct Operand<float> {
-  typedef bf16x8 type;
-  static constexpr int kTokens = 4;
-  static __device__ __forceinline__ int token(int p) { return p >> 2; }
-  static __device__ __forceinline__ bf16x8 operand(const float (&f)[8], int part) {
-    const float second = part >= 1 ? 1.0f : 0.0f, third = part >= 2 ? 1.0f : 0.0f;
-    bf16x8 v;
+struct Op<float> : Op<__bf16> {};
+
+// Columns of x on their way to LDS: a chunk's 128 values of up to TOKENS columns, TOKENS pairs of values to a lane.
+// Where a column's values are contiguous, pair t is values 2 lane, 2 lane + 1 of column t, one load whatever its
+// alignment (the hardware takes any); else (FEATURES) a lane has column lane % TOKENS, and a wave's loads are
+// neighbouring columns of a few values.  Columns past the last repeat it (without conditions the loads are under way
+// together).  Columns of 16 bits are a row of LDS each; 32-bit values are the exact sum of three bf16 numbers
+// of 8 bits each, and have three.
+constexpr int kRowBytes = kQChunk * 2 + 16;  // (16 more: the rows of one piece lie in different banks)
+template <typename T, int TOKENS, bool FEATURES>
+struct Columns {
+  typedef T Pair __attribute__((ext_vector_type(2)));
+  static constexpr int kSide = FEATURES ? 64 / TOKENS : 64;  // pairs of a column that a wave's load takes
+  // As loaded: taken apart or put together only when they are stored (anything else would wait for them).
+  typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type Bits;
+  Pair pair[FEATURES ? 1 : TOKENS];
+  uint32_t lo[FEATURES ? TOKENS : 1], hi[FEATURES ? TOKENS : 1];
+  // x: the first of the N columns, k0: the chunk's first value.  PART: K may end within.
+  template <bool PART>
+  __device__ __forceinline__ void load(const QmatArgs& a, const T* x, int N, int k0, int lane) {
+    if constexpr (FEATURES) {
+      const T* c = x + min(lane % TOKENS, N - 1) * a.x_column;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {  // the upper 16 bits of a float are its first 8 bits as a bf16
-      float r = f[i];
-      r -= second * __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-      r -= third * __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-      v[i] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(r) >> 16));
+      for (int j = 0; j < TOKENS; ++j) {
+        const int k = k0 + 2 * (lane / TOKENS + kSide * j);
+        const int64_t u = PART ? min(k, a.K - 1) : k, v = PART ? min(k + 1, a.K - 1) : k + 1;
+        lo[j] = __builtin_bit_cast(Bits, c[u * a.x_feature]), hi[j] = __builtin_bit_cast(Bits, c[v * a.x_feature]);
+        if (PART) lo[j] = k < a.K ? lo[j] : 0, hi[j] = k + 1 < a.K ? hi[j] : 0;
+      }
+    } else {
+      const int k = k0 + 2 * lane;
+#pragma unroll
+      for (int t = 0; t < TOKENS; ++t) {
+        const T* c = x + min(t, N - 1) * a.x_column;
+        if (PART) {
+          const T u = c[min(k, a.K - 1)], v = c[min(k + 1, a.K - 1)];
+          pair[t] = Pair{k < a.K ? u : (T)0.0f, k + 1 < a.K ? v : (T)0.0f};
+        } else {
+          __builtin_memcpy(&pair[t], c + k, sizeof(Pair));
+        }
+      }
     }
-    return v;
   }
-  static __device__ __forceinline__ bf16x8 weights(uint32_t w) { return Operand<__bf16>::weights(w); }
-  static __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return Operand<__bf16>::mfma(a, b, c); }
+  // Row t of LDS is column t; of 32-bit values rows 4 t + part with up to four columns, else TOKENS part + t.
+  __device__ __forceinline__ void store(unsigned char* rows, int lane) const {
+#pragma unroll
+    for (int j = 0; j < TOKENS; ++j) {
+      const int t = FEATURES ? lane % TOKENS : j;
+      unsigned char* at = rows + (FEATURES ? lane / TOKENS + kSide * j : lane) * 4;
+      if constexpr (sizeof(T) == 2) {
+        if constexpr (FEATURES)
+          *reinterpret_cast<uint32_t*>(at + t * kRowBytes) = lo[j] | hi[j] << 16;
+        else
+          *reinterpret_cast<Pair*>(at + t * kRowBytes) = pair[j];
+      } else {
+        float u, v;
+        if constexpr (FEATURES)
+          u = __uint_as_float(lo[j]), v = __uint_as_float(hi[j]);
+        else
+          u = pair[j][0], v = pair[j][1];
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {  // the upper 16 bits of a float are its first 8 bits as a bf16
+          const uint32_t ub = __float_as_uint(u), vb = __float_as_uint(v);
+          *reinterpret_cast<uint32_t*>(at + (TOKENS <= 4 ? 4 * t + part : TOKENS * part + t) * kRowBytes) =
+              __builtin_amdgcn_perm(vb, ub, 0x07060302u);
+          u -= __uint_as_float(ub & 0xffff0000u), v -= __uint_as_float(vb & 0xffff0000u);
+        }
+      }
+    }
+  }
 };
+template <typename T, int TOKENS>
+constexpr int kRowsOf = sizeof(T) == 2 ? TOKENS : TOKENS <= 4 ? 4 * TOKENS : 3 * TOKENS;
+
+// The most waves of a workgroup: 16, where their rows take 64 KiB of LDS at most.
+template <typename T, int TOKENS>
+constexpr int kWavesOf = kRowsOf<T, TOKENS> * kRowBytes * kMaxWaves <= 65536 ? kMaxWaves : kMaxWaves / 2;
 
 // N scales from scale i on (N bytes or more apart: one access), and zero points.
 template <int N>
@@ -174,92 +206,110 @@ __device__ __forceinline__ void load_scales(const QmatArgs& a, int64_t i, float 
   for (int k = 0; k < N; ++k) zero[k] = (float)z[k];
 }
 
-// A chunk of a tile on its way to the registers: 16 bytes of weights, the lane's column of x, scales and zeros.
-template <typename T, int STEPS>
+// A chunk of a tile on its way to the registers: 16 bytes of weights, scales and zeros, and the columns of x.
+template <typename T, int STEPS, int TOKENS, bool FEATURES>
 struct Chunk {
   i32x4 w;
-  T x[4][8];
   float scale[4 / STEPS], zero[4 / STEPS];
-  // w0: of the lane in the first chunk; x0: the lane's column; meta0: the lane's row of the first scales.
-  template <bool CONTIGUOUS, bool PART>
-  __device__ __forceinline__ void load(const QmatArgs& a, const i32x4* w0, const T* x0, int64_t meta0, int c, int g) {
+  Columns<T, TOKENS, FEATURES> x;
+  // w0: of the lane in the first chunk; meta0: the lane's row of the first scales.
+  template <bool PART>
+  __device__ __forceinline__ void load(const QmatArgs& a, const i32x4* w0, const T* x0, int N, int64_t meta0, int c,
+                                       int lane) {
     w = w0[(int64_t)c * 64];
     const int meta = STEPS == 4 && a.group_of ? (int)__umulhi((uint32_t)c, a.group_of) : c;
     load_scales<4 / STEPS>(a, meta0 + (int64_t)meta * (kQTileRows * (4 / STEPS)), scale, zero);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) load8<CONTIGUOUS, PART>(x0, a, c * kQChunk + s * 32 + g * 8, x[s]);
+    x.template load<PART>(a, x0, N, c * kQChunk, lane);
     __builtin_amdgcn_sched_barrier(0);  // under way before the chunk before is multiplied
   }
 };
 
-// A workgroup has 16 rows of W and up to 16 columns of x (4 in 32 bits); its waves share the chunks, each with
-// the next one under way while it multiplies.  With n the 4-bit numbers, a group of columns adds
-// s (sum (16 + n) x - (16 + z) sum x): both sums come from the matrix unit, the second with ones for the
-// numbers, and are scaled once a group.  The 16 costs a bit of the 32-bit sums, and saves half of the
+// A workgroup has 16 rows of W and up to TOKENS columns of x; its waves share the chunks, each with the next one
+// under way while it multiplies.  The columns go through LDS (a wave's own part), where they are turned into
+// operands: rows of the first operand are columns of x, columns of the second rows of W.  With n the 4-bit numbers,
+// a group adds s (sum (16 + n) x - (16 + z) sum x): both sums come from the matrix unit, the second with ones for
+// the numbers, and are scaled once a group.  The 16 costs a bit of the 32-bit sums, and saves half of the
 // instructions that make numbers of the bits.
-//   STEPS: matrix instructions (of 32 columns) of a group within a chunk.
-//   REGS: of a lane's four result registers, those that hold columns of x.
-//   CONTIGUOUS: a column's values are.
-template <typename T, int STEPS, int REGS, bool CONTIGUOUS>
-__global__ __launch_bounds__(kMaxWaves * 64) void qmat_kernel(QmatArgs a) {
-  typedef Operand<T> Op;
-  constexpr bool kParts = sizeof(T) == 4;
-  __shared__ float sums[kMaxWaves][REGS][64];
+//   Row p of the operand is column p / 4 + 4 (p % 4) of x, so that up to four columns are in the first of a lane's
+// four results, up to eight in two; of four columns in 32 bits rows 4 t + part, and a lane adds its results.
+//   STEPS: matrix instructions (of 32 columns of W) of a group within a chunk.
+template <typename T, int STEPS, int TOKENS, bool FEATURES>
+__global__ __launch_bounds__((kWavesOf<T, TOKENS> * 64)) void qmat_kernel(QmatArgs a) {
+  constexpr bool PARTS = sizeof(T) == 4, PACKED = PARTS && TOKENS <= 4;
+  constexpr int REGS = TOKENS < 4 ? 1 : TOKENS / 4, SETS = PARTS && !PACKED ? 3 : 1, ROWS = kRowsOf<T, TOKENS>;
+  extern __shared__ __align__(16) unsigned char lds[];  // a wave's rows, then its sums
   const int lane = threadIdx.x % 64, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
   const int64_t tile = blockIdx.x;
-  const int n0 = blockIdx.y * Op::kTokens, part = r & 3;
-  const int token = n0 + Op::token(r);
-  const T* x = static_cast<const T*>(a.x) + (token < a.N ? token : 0) * a.x_column;  // (others' rows are not used)
+  const int n0 = blockIdx.y * TOKENS, N = min(TOKENS, a.N - n0);
+  const T* x = static_cast<const T*>(a.x) + n0 * a.x_column;
   const i32x4* w = a.weights + tile * a.chunks * 64 + lane;
   const int64_t meta0 = (tile * a.metas * kQTileRows + r) * (4 / STEPS);
+  unsigned char* rows = lds + wave * ROWS * kRowBytes;
+  const unsigned char* row =
+      rows + (PACKED ? 4 * min(r >> 2, TOKENS - 1) + min(r & 3, 2) : min((r >> 2) + 4 * (r & 3), TOKENS - 1)) * kRowBytes +
+      g * 16;  // (rows of the operand that are no column repeat one)
   float acc[REGS] = {};
-  typename Op::type ones;
+  typename Op<T>::type ones;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = 1.0f;
-  const auto add = [&](const Chunk<T, STEPS>& b) {
+  const auto add = [&](const Chunk<T, STEPS, TOKENS, FEATURES>& b) {
+    b.x.store(rows, lane);
+    // what the lanes of the wave wrote, before they read each other's
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
     for (int i = 0; i < 4 / STEPS; ++i) {
       f32x4 d = {0, 0, 0, 0}, sx = {0, 0, 0, 0};
 #pragma unroll
       for (int s = i * STEPS; s < (i + 1) * STEPS; ++s) {
-        const auto xv = Op::operand(b.x[s], part);
-        d = Op::mfma(xv, Op::weights((uint32_t)b.w[s]), d);
-        sx = Op::mfma(xv, ones, sx);
+        const auto wv = Op<T>::weights((uint32_t)b.w[s]);
+#pragma unroll
+        for (int k = 0; k < SETS; ++k) {
+          const auto xv =
+              *reinterpret_cast<const typename Op<T>::type*>(row + s * 64 + k * TOKENS * kRowBytes);
+          d = Op<T>::mfma(xv, wv, d);
+          sx = Op<T>::mfma(xv, ones, sx);
+        }
       }
       const float s = b.scale[i], z = b.zero[i] + 16.0f;
-      if (kParts) {
+      if (PACKED) {
         acc[0] = fmaf(s, fmaf(-z, (sx[0] + sx[1]) + sx[2], (d[0] + d[1]) + d[2]), acc[0]);
       } else {
 #pragma unroll
         for (int k = 0; k < REGS; ++k) acc[k] = fmaf(s, fmaf(-z, sx[k], d[k]), acc[k]);
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   };
   const int whole = a.K / kQChunk;  // chunks; of one more, K ends within
   {
-    Chunk<T, STEPS> even, odd;
+    Chunk<T, STEPS, TOKENS, FEATURES> even, odd;
     int c = wave;
-    if (c < whole) even.template load<CONTIGUOUS, false>(a, w, x, meta0, c, g);
+    if (c < whole) even.template load<false>(a, w, x, N, meta0, c, lane);
     for (; c < whole; c += 2 * waves) {
-      if (c + waves < whole) odd.template load<CONTIGUOUS, false>(a, w, x, meta0, c + waves, g);
+      if (c + waves < whole) odd.template load<false>(a, w, x, N, meta0, c + waves, lane);
       add(even);
       if (c + waves >= whole) break;
-      if (c + 2 * waves < whole) even.template load<CONTIGUOUS, false>(a, w, x, meta0, c + 2 * waves, g);
+      if (c + 2 * waves < whole) even.template load<false>(a, w, x, N, meta0, c + 2 * waves, lane);
       add(odd);
     }
   }
   if (whole < a.chunks && wave == whole % waves) {
-    Chunk<T, STEPS> last;
-    last.template load<CONTIGUOUS, true>(a, w, x, meta0, whole, g);
+    Chunk<T, STEPS, TOKENS, FEATURES> last;
+    last.template load<true>(a, w, x, N, meta0, whole, lane);
     add(last);
   }
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(lds);  // [wave][REGS][64]
 #pragma unroll
-  for (int i = 0; i < REGS; ++i) sums[wave][i][lane] = acc[i];
+  for (int i = 0; i < REGS; ++i) sums[(wave * REGS + i) * 64 + lane] = acc[i];
   __syncthreads();
   if (wave >= REGS) return;
   float v = 0.0f;
-  for (int k = 0; k < waves; ++k) v += sums[k][wave][lane];
+  for (int k = 0; k < waves; ++k) v += sums[(k * REGS + wave) * 64 + lane];
   const int64_t m = tile * kQTileRows + r;
   const int n = n0 + g + 4 * wave;  // row 4 g + wave of the result
   if (m >= a.M || n >= a.N) return;
@@ -267,27 +317,34 @@ __global__ __launch_bounds__(kMaxWaves * 64) void qmat_kernel(QmatArgs a) {
   static_cast<T*>(a.y)[m * a.y_feature + n * a.y_column] = (T)activation(v, a.epi);
 }
 
-template <typename T, int STEPS, bool CONTIGUOUS>
-hipError_t start_regs(const QmatArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.M + kQTileRows - 1) / kQTileRows),
-                  (unsigned)((a.N + Operand<T>::kTokens - 1) / Operand<T>::kTokens));
-  // 8 waves to a tile of rows, 16 where there are fewer tiles than compute units, with as many chunks each as
-  // the one with most of them; 4 at least, which write the results
-  const int most = grid.x * grid.y < 256 ? kMaxWaves : 8;
+template <typename T, int STEPS, int TOKENS>
+hipError_t start_tokens(const QmatArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.M + kQTileRows - 1) / kQTileRows), (unsigned)((a.N + TOKENS - 1) / TOKENS));
+  // 8 waves to a tile of rows, 16 where there are fewer tiles than compute units (and LDS holds their columns), with
+  // as many chunks each as the one with most of them; 4 at least, which write the results
+  constexpr size_t per_wave = (size_t)kRowsOf<T, TOKENS> * kRowBytes;
+  const int most = grid.x * grid.y < 256 ? kWavesOf<T, TOKENS> : 8;
   const int each = (a.chunks + most - 1) / most, needed = (a.chunks + each - 1) / each;
   const int waves = needed < 4 ? 4 : needed;
-  if (sizeof(T) == 4 || a.N <= 4)
-    qmat_kernel<T, STEPS, 1, CONTIGUOUS><<<grid, waves * 64, 0, stream>>>(a);
-  else if (a.N <= 8)
-    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 2, CONTIGUOUS><<<grid, waves * 64, 0, stream>>>(a);
-  else
-    qmat_kernel<T, STEPS, sizeof(T) == 4 ? 1 : 4, CONTIGUOUS><<<grid, waves * 64, 0, stream>>>(a);
+  constexpr size_t sums = (TOKENS < 4 ? 4 : TOKENS) * 64;  // of a wave
+  const size_t lds = waves * (per_wave > sums ? per_wave : sums);
+  const auto kernel = a.x_feature == 1 ? qmat_kernel<T, STEPS, TOKENS, false> : qmat_kernel<T, STEPS, TOKENS, true>;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<grid, waves * 64, lds, stream>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, int STEPS>
 hipError_t start_steps(const QmatArgs& a, hipStream_t stream) {
-  return a.x_feature == 1 ? start_regs<T, STEPS, true>(a, stream) : start_regs<T, STEPS, false>(a, stream);
+  if (a.N == 1) return start_tokens<T, STEPS, 1>(a, stream);
+  if (a.N <= 4) return start_tokens<T, STEPS, 4>(a, stream);
+  if constexpr (sizeof(T) == 2)
+    if (a.N > 8) return start_tokens<T, STEPS, 16>(a, stream);
+  return start_tokens<T, STEPS, 8>(a, stream);  // (the three parts of 16 in 32 bits do not fit the registers)
 }
 
 template <typename T>
