@@ -433,30 +433,25 @@ struct Tile {
   static __device__ __forceinline__ void fetch(const T* k, const T* v, int tokens, int D, int P, unsigned char* lds) {
     // Pieces past a row's end, and rows past the last, stay out.  The rows that a thread copies pieces of lie
     // KR (VR) apart: mostly so far that the permutation is the same in all of them.
-    const int wave = threadIdx.x / 64;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     constexpr int KR = THREADS / kKeyPieces, VR = THREADS / kValuePieces;
-    const bool whole = D == kDims && tokens == STAGE;
     constexpr bool SAME = KR % (sizeof(T) == 4 ? 16 : 32) == 0;
     static_assert(VR % 16 == 0, "value_swap has a period of at most 16");
-    {
-      const int row = threadIdx.x / kKeyPieces, piece = threadIdx.x % kKeyPieces;
-      const T* from = k + row * D;
+    const int row = threadIdx.x / kKeyPieces, piece = threadIdx.x % kKeyPieces;
+    const int d = threadIdx.x / kValuePieces, x = (threadIdx.x % kValuePieces) ^ value_swap(d);
+    const T* from_k = k + row * D;
+    const T* from_v = v + d * P + x * kPiece;
+    unsigned char* to = lds + wave * 1024;
+    const bool whole = D == kDims && tokens == STAGE;  // nothing is left out
 #pragma unroll
-      for (int i = 0; i < STAGE / KR; ++i) {
-        const int x = piece ^ key_swap(SAME ? row : row + i * KR);
-        if (whole || (x * kPiece < D && row + i * KR < tokens))
-          copy_to_lds(from + i * KR * D + x * kPiece, lds + (i * THREADS + wave * 64) * 16);
-      }
+    for (int i = 0; i < STAGE / KR; ++i) {
+      const int kx = piece ^ key_swap(SAME ? row : row + i * KR);
+      if (whole || (kx * kPiece < D && row + i * KR < tokens))
+        copy_to_lds(from_k + i * KR * D + kx * kPiece, to + i * THREADS * 16);
     }
-    {
-      const int d = threadIdx.x / kValuePieces, x = (threadIdx.x % kValuePieces) ^ value_swap(d);
-      const T* from = v + d * P + x * kPiece;
-      if (whole || x * kPiece < tokens) {
 #pragma unroll
-        for (int i = 0; i < kDims / VR; ++i)
-          if (whole || d + i * VR < D) copy_to_lds(from + i * VR * P, lds + kBytes + (i * THREADS + wave * 64) * 16);
-      }
-    }
+    for (int i = 0; i < kDims / VR; ++i)
+      if (whole || (x * kPiece < tokens && d + i * VR < D)) copy_to_lds(from_v + i * VR * P, to + kBytes + i * THREADS * 16);
   }
   static __device__ __forceinline__ const unsigned char* key(const unsigned char* lds, int row, int piece) {
     return lds + (row * kKeyPieces + (piece ^ key_swap(row))) * 16;
@@ -509,7 +504,7 @@ struct Cursor {
 // cached head; the WAVES waves of a workgroup, neighbouring tokens again, walk the union of their lists, block
 // by block in ascending order, through LDS: a block is read from L2 once for all of them, the next one while
 // they compute.  Waves whose tokens did not choose a block skip it; rows of a tile that did not are masked.
-// The union is found on the way, a block ahead: each wave offers its lowest block not yet passed.
+// The union is found on the way, a block ahead: each token offers its lowest block not yet passed.
 template <typename T, int CHUNKS, int STAGE, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void attend_tiles(AttendArgs a) {
   typedef Tile<T, CHUNKS, STAGE> L;
@@ -517,8 +512,9 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   constexpr int32_t END = 0x7fffffff;
   __shared__ __align__(16) unsigned char lds[2][2 * L::kBytes];
   __shared__ uint64_t turns[2];
-  __shared__ int2 offers[2][WAVES];  // key and page of each wave's lowest block
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane & 15, g = lane >> 4;
+  __shared__ uint64_t lowest[3];  // key and page of the lowest block that is offered, in turn
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int r = lane & 15, g = lane >> 4;
   int b = blockIdx.x;
   const int h = b % a.kv_heads;
   b /= a.kv_heads;
@@ -554,6 +550,7 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
     const uint64_t bits = __ballot(turn);
     if (lane == 0) turns[wave] = bits;
   }
+  if (threadIdx.x < 3) lowest[threadIdx.x] = ~0ull;
   int32_t p = -1, seq = -1;
   if (t < a.tokens) p = a.pos[t], seq = a.seq[t];
   __syncthreads();
@@ -566,24 +563,21 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   at.n = filler ? 0 : a.chosen ? a.blocks : min(at.own + 1, a.max_blocks);
   at.start(a, h);
   const auto key = [&] { return at.valid(a, at.id) ? run << 20 | at.id : END; };
-  const auto offer = [&](int parity) {
-    int32_t k = key();
-    for (int s = per_token; s < 16; s <<= 1) k = min(k, __shfl_xor(k, s));
-    const int from = __builtin_ctzll(__ballot(key() == k));
-    const int32_t page = __shfl(at.page, from);
-    if (lane == 0) offers[parity][wave] = make_int2(k, page);
+  // One row of each token offers its next block.
+  const auto offer = [&](int turn) {
+    if (g == 0 && qr == 0)
+      atomicMin(reinterpret_cast<unsigned long long*>(&lowest[turn]),
+                (unsigned long long)(uint32_t)key() << 32 | (uint32_t)at.page);
   };
-  // The lowest of all offers; what this lane's query sees of it is left in `seen`, and it is passed.
+  // The lowest block of those offered; what this lane's query sees of it is left in `seen`, and it is passed.  The
+  // offers before it, which all waves have read, make room for the next but one.
   int32_t block_key = END, block_page = -1, seen = 0;
-  const auto take = [&](int parity) {
-    int2 low = offers[parity][0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) {
-      const int2 x = offers[parity][w];
-      if (x.x < low.x) low = x;
-    }
-    block_key = __builtin_amdgcn_readfirstlane(low.x), block_page = __builtin_amdgcn_readfirstlane(low.y);
-    if (block_page < 0 || block_page >= a.pages) block_page = -1;
+  const auto take = [&](int turn) {
+    const uint64_t low = lowest[turn];
+    if (threadIdx.x == 0) lowest[turn == 0 ? 2 : turn - 1] = ~0ull;
+    block_key = __builtin_amdgcn_readfirstlane((int32_t)(low >> 32));
+    block_page = __builtin_amdgcn_readfirstlane((int32_t)low);
+    if (block_page >= a.pages) block_page = -1;
     const bool mine = block_key != END && key() == block_key;
     seen = mine && block_page >= 0 ? min(a.block, p - at.id * a.block + 1) : 0;
     if (mine) at.advance(a, h);
@@ -596,11 +590,12 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
                                   static_cast<const T*>(a.v_pages) + from + s * stage, stage, D, a.block, lds[buffer]);
   };
 
-  int parity = 0, buffer = 0, s = 0;
-  offer(parity);
+  int turn = 0, buffer = 0, s = 0;
+  const auto next = [&] { return turn == 2 ? 0 : turn + 1; };
+  offer(turn);
   __syncthreads();
-  take(parity);
-  offer(parity ^= 1);
+  take(turn);
+  offer(turn = next());
   if (block_key != END) fetch(0, 0);
   while (block_key != END) {
     const int32_t now_seen = seen - s * stage;
@@ -608,8 +603,8 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
     __syncthreads();  // the stage is in LDS, the other buffer is free, the offers are made
     if (++s == stages) {
       s = 0;
-      take(parity);
-      if (block_key != END) offer(parity ^= 1);
+      take(turn);
+      if (block_key != END) offer(turn = next());
     }
     if (block_key != END) fetch(s, buffer ^ 1);
     for (int u = 0; u < stage; u += N) {
