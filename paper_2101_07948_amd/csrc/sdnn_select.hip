@@ -28,24 +28,6 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return min(u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u), 0xfffffffeu);
 }
 
-// 16 bytes of a summary from byte k on, zeros past its end (D is a multiple of 8).
-__device__ __forceinline__ i32x4 load_mean(const int8_t* row, int k, int D, bool wide) {
-  i32x4 v = {0, 0, 0, 0};
-  if (wide) {
-    if (k < D) v = *reinterpret_cast<const i32x4*>(row + k);
-  } else {
-    if (k < D) {
-      const int2 lo = *reinterpret_cast<const int2*>(row + k);
-      v[0] = lo.x, v[1] = lo.y;
-    }
-    if (k + 8 < D) {
-      const int2 hi = *reinterpret_cast<const int2*>(row + k + 8);
-      v[2] = hi.x, v[3] = hi.y;
-    }
-  }
-  return v;
-}
-
 // Sums of two counts over the workgroup's threads before this one, and over all of them.  `parts`: a word for
 // each wave.
 __device__ __forceinline__ uint2 before(uint2 n, uint2* parts, uint2* all) {
@@ -234,15 +216,32 @@ struct Summaries {
   i32x4 m[4][STEPS];
   float scale[4];
   int32_t page[4];
+  // (Bytes past a head's end meet zeros of the queries: any will do.  `wide`: whole 16-byte pieces.)
   __device__ __forceinline__ void load(const SelectArgs& a, int h, int32_t entry, int r, int g, bool wide) {
     const int32_t mine = entry < a.pages ? entry : -1;
+    const int8_t* row[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       page[k] = __shfl(mine, k * 16 + r);
-      const int64_t row = (int64_t)max(page[k], 0) * a.kv_heads + h;  // (in a missing page's place: page 0)
+      const int64_t at = (int64_t)max(page[k], 0) * a.kv_heads + h;  // (in a missing page's place: page 0)
+      row[k] = a.means + at * a.head_dim;
+      scale[k] = a.scales[at];
+    }
+    if (wide) {
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) m[k][s] = load_mean(a.means + row * a.head_dim, s * 64 + g * 16, a.head_dim, wide);
-      scale[k] = a.scales[row];
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+          m[k][s] = *reinterpret_cast<const i32x4*>(row[k] + min(s * 64 + g * 16, a.head_dim - 16));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          const int2 lo = *reinterpret_cast<const int2*>(row[k] + min(s * 64 + g * 16, a.head_dim - 8));
+          const int2 hi = *reinterpret_cast<const int2*>(row[k] + min(s * 64 + g * 16 + 8, a.head_dim - 8));
+          m[k][s] = i32x4{lo.x, lo.y, hi.x, hi.y};
+        }
     }
     __builtin_amdgcn_sched_barrier(0);  // all loads under way before the first is used
   }
