@@ -173,13 +173,12 @@ struct State {
   float m, l;
 };
 
-__device__ __forceinline__ float over_groups_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
+__device__ __forceinline__ float over_groups_max(float x) { return max_over_32(max_over_16(x)); }
 __device__ __forceinline__ float over_groups_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  float u, v;
+  with_16(x, &u, &v);
+  with_32(u + v, &u, &v);
+  return u + v;
 }
 
 // One step: tokens [0, seen) of its are within the sight of this lane's query, tokens from `stored` on may

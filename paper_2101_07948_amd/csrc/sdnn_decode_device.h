@@ -49,6 +49,27 @@ __device__ __forceinline__ void store_n(T* p, bool aligned, const T (&in)[N]) {
   }
 }
 
+// x and the value of the lane 16 (32) away, exchanged within the registers (gfx950's row swaps: with the same
+// value as both operands, one result holds the even rows twice and the other the odd ones).
+__device__ __forceinline__ void with_16(float x, float* u, float* v) {
+  const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  *u = __uint_as_float(p[0]), *v = __uint_as_float(p[1]);
+}
+__device__ __forceinline__ void with_32(float x, float* u, float* v) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  *u = __uint_as_float(p[0]), *v = __uint_as_float(p[1]);
+}
+__device__ __forceinline__ float max_over_16(float x) {
+  float u, v;
+  with_16(x, &u, &v);
+  return fmaxf(u, v);
+}
+__device__ __forceinline__ float max_over_32(float x) {
+  float u, v;
+  with_32(x, &u, &v);
+  return fmaxf(u, v);
+}
+
 // cos and sin of a (radians) in 64 bits.  a = n pi/2 + r, |r| <= pi/4, with pi/2 as the sum of
 // three doubles (53 bits each, so that n pi/2 is exact far past n = 2^31), then the Taylor
 // series of both to r^17 / r^16 (the next terms are below 2^-55 at pi/4).  About 35 instructions

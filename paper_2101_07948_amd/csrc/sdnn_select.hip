@@ -247,6 +247,9 @@ struct Summaries {
   }
 };
 
+// A query's 8-bit row in LDS: 16 bytes longer, so that the rows of one piece lie in different banks.
+constexpr int row_bytes(int steps) { return steps * 64 + 16; }
+
 // A workgroup chooses the blocks of one cached head for `tile` tokens.  Scores: the dot products of 16 queries
 // (the rows: a power of two of them to a token, or several tiles of rows) and 16 summaries are one matrix
 // instruction for 64 values of a head, bytes in, whole numbers out; a lane's four results are rows 4 g ...
@@ -260,12 +263,13 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
   __shared__ GroupLds group;
   __shared__ Candidate few[kMaxWaves / 4][64];
   __shared__ int32_t seqs[kMaxTile], seen[kMaxTile];  // of the tile's tokens; blocks that they see
-  constexpr int ROW = STEPS * 64;
+  constexpr int ROW = row_bytes(STEPS);
   const int rows = a.tile * a.per_token;      // a multiple of 16
   const int shift = a.per_token >= 16 ? 4 : __builtin_ctz(a.per_token);  // of a tile of rows to its tokens
   int8_t* m8 = reinterpret_cast<int8_t*>(lds);                // [rows][ROW]
-  float* top = reinterpret_cast<float*>(m8 + rows * ROW);     // [rows]; -1: no query
-  uint32_t* keys = reinterpret_cast<uint32_t*>(top + rows);   // [tile][max_blocks]
+  float* top = reinterpret_cast<float*>(m8 + rows * ROW);     // [rows]: largest value of each query
+  float* dead = top + rows;                                   // [rows]: 0, or -infinity where there is no query
+  uint32_t* keys = reinterpret_cast<uint32_t*>(dead + rows);  // [tile][max_blocks]
   const int threads = blockDim.x, lane = threadIdx.x % 64;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = threads / 64;
   const int h = blockIdx.x % a.kv_heads, t0 = blockIdx.x / a.kv_heads * a.tile;
@@ -321,7 +325,7 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
         w |= ((uint32_t)(int)fminf(fmaxf(rintf(x[s][k] * f), -127.0f), 127.0f) & 255u) << (8 * k);
       *reinterpret_cast<uint32_t*>(m8 + row * ROW + s * 64 + r * 4) = w;
     }
-    if (r == 0) top[row] = live ? m : -1.0f;
+    if (r == 0) top[row] = m, dead[row] = live ? 0.0f : -INFINITY;
   }
   __syncthreads();
   // without a choice: everything the token sees; else the blocks that are always taken
@@ -339,11 +343,11 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
   }
   if (!some) return;
 
-  // of a lane's four results of a tile of rows: the tokens whose scores they become, after the maximum over the
-  // token's rows, counted from the tile's first; -1: none
-  int token_of[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) token_of[i] = (4 * g + i) & ((1 << shift) - 1) ? -1 : (4 * g + i) >> shift;
+  // The first of a lane's four results of a tile of rows becomes, after the maximum over its token's rows, the score
+  // of this token, counted from the tile's first (a token's rows are 1 << shift neighbours, and lanes whose result
+  // is not a token's first leave it to the one that is); with fewer than four rows to a token others do too.
+  const bool leads = !(4 * g & ((1 << shift) - 1));
+  const int lead = 4 * g >> shift;
   for (int i0 = 0; i0 < a.tile;) {  // tokens i0 ... i1 - 1 are of one sequence
     const int32_t seq = seqs[i0];
     int i1 = i0, most = 0;
@@ -366,25 +370,30 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
             dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(qv, sum.m[k][s], dot, 0, 0, 0);
           }
           const f32x4 tq = *reinterpret_cast<const f32x4*>(top + row0 + 4 * g);
+          const f32x4 none = *reinterpret_cast<const f32x4*>(dead + row0 + 4 * g);
           const bool more = a.per_token > 16 && row0 > 0;  // rows of the same token
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float x = tq[i] < 0.0f ? -INFINITY : (float)dot[i] * tq[i];
+            const float x = fmaf((float)dot[i], tq[i], none[i]);  // (a product rounded once, or -infinity)
             best[i] = more ? fmaxf(best[i], x) : x;
           }
           if (a.per_token > 16 && row0 + 16 < rows) continue;
-          // over the queries of a token
-          if (shift >= 1) best[0] = fmaxf(best[0], best[1]), best[2] = fmaxf(best[2], best[3]);
-          if (shift >= 2) best[0] = fmaxf(best[0], best[2]);
-          if (shift >= 3) best[0] = fmaxf(best[0], __shfl_xor(best[0], 16));
-          if (shift >= 4) best[0] = fmaxf(best[0], __shfl_xor(best[0], 32));
           const int first = a.per_token > 16 ? 0 : row0 >> shift;
+          const auto put = [&](int token, float x, bool is) {
+            if (is && token >= i0 && token < i1 && b < count)
+              keys[token * a.max_blocks + b] = sum.page[k] < 0 ? 0u : ordered(x * sum.scale[k]);
+          };
+          if (shift >= 2) {
+            float x = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
+            if (shift >= 3) x = max_over_16(x);
+            if (shift >= 4) x = max_over_32(x);
+            put(first + lead, x, leads);
+          } else if (shift == 1) {
+            put(first + lead, fmaxf(best[0], best[1]), true);
+            put(first + lead + 1, fmaxf(best[2], best[3]), true);
+          } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (i > 0 && shift >= 2) break;
-            const int token = first + token_of[i];
-            if (token_of[i] >= 0 && token >= i0 && token < i1 && b < count)
-              keys[token * a.max_blocks + b] = sum.page[k] < 0 ? 0u : ordered(best[i] * sum.scale[k]);
+            for (int i = 0; i < 4; ++i) put(first + lead + i, best[i], true);
           }
         }
       }
@@ -414,7 +423,7 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
 
 template <typename T, int STEPS>
 hipError_t start(const SelectArgs& a, int threads, hipStream_t stream) {
-  const size_t lds = (size_t)a.tile * (a.per_token * (STEPS * 64 + 4) + (size_t)a.max_blocks * 4);
+  const size_t lds = (size_t)a.tile * (a.per_token * (row_bytes(STEPS) + 8) + (size_t)a.max_blocks * 4);
   if (lds > 60000) {  // with the kernel's own arrays past what a launch gives by default
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(select_kernel<T, STEPS>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
