@@ -133,7 +133,7 @@ __device__ __forceinline__ void wave_choose(const uint32_t* keys, int count, uin
 }
 
 constexpr int kMaxWaves = 16;
-constexpr int kMaxTile = 64;
+constexpr int kMaxTile = 32;
 constexpr int kWaveKeys = 16;  // keys of a lane where a wave chooses alone: up to 1024 blocks
 
 struct GroupLds {
@@ -454,7 +454,9 @@ hipError_t launch_select(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.block_shift = __builtin_ctz(c.block);
   a.blocks = blocks, a.sink = sink, a.local = local;
   // A workgroup has several tokens where most of them are of one sequence and a wave can select alone: so
-  // many that their rows fill four matrix operands and their keys 64 KiB of LDS, and that the device is full.
+  // many that their rows fill two matrix operands (2048 tokens of 4 queries to a head over 512 blocks: one operand
+  // 52 us, two 41, four 54, whose LDS leaves fewer workgroups to a compute unit), their keys at most 64 KiB of
+  // LDS, and that the device is full.
   // Otherwise it has one token, and so many waves that each has some blocks.
   int rows = 1;
   while (rows < a.group && rows < 16) rows *= 2;
@@ -463,7 +465,7 @@ hipError_t launch_select(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.tile = 1;
   if (tiles) {
     a.tile = 16 / rows;
-    while (a.tile * rows < 64 && a.tile * 2 * t.max_blocks <= 16384 &&
+    while (a.tile * rows < 32 && a.tile * 2 * t.max_blocks <= 16384 &&
            (int64_t)(t.tokens / (a.tile * 2)) * c.kv_heads >= 1024)
       a.tile *= 2;
   }
