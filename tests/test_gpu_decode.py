@@ -580,6 +580,77 @@ def strided_2d(x):
     return v
 
 
+def test_q4_refusals():
+    packed, scales, z = random_q4(1, 40, 70, 32, torch.float32, True)
+    plan = sd.Q4Plan(packed, scales, z, K=70, group=32)
+    x, y = randn(2, (70, 3), torch.float32), torch.full((40, 3), 5.0, device=DEV)
+    for bad in (lambda: plan.matvec(x[:69], y), lambda: plan.matvec(x, y[:, :2]), lambda: plan.matvec(x, y.t()),
+                lambda: plan.matvec(x, y, torch.zeros(39, device=DEV)),
+                lambda: sd.Q4Plan(packed, scales, z, K=72, group=32),
+                lambda: sd.Q4Plan(packed, scales[:, :2], z, K=70, group=32)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: plan.matvec(x.half(), y), lambda: plan.matvec(x.cpu(), y), lambda: plan.matvec(x.double(), y.double()),
+                lambda: sd.Q4Plan(packed.float(), scales, z, K=70, group=32)):
+        with pytest.raises(TypeError):
+            bad()
+    both = torch.zeros((70 + 40) * 3, device=DEV)
+    for bad in (lambda: plan.matvec(both[:210].view(70, 3), both[200:320].view(40, 3)),  # overlapping
+                lambda: plan.matvec(x, y[:, :1].expand(40, 3)), lambda: sd.Q4Plan(packed, scales, z, K=70, group=33 - 9)):
+        with pytest.raises((sd.SdnnError, ValueError)):
+            bad()
+    assert (y == 5.0).all()
+    plan.matvec(x[:, :0], y[:, :0])  # no columns: nothing to do
+    plan.close()
+    with pytest.raises(RuntimeError):
+        plan.matvec(x, y)
+
+
+def test_binding_refusals_on_the_gpu():
+    cache = make_cache(0, 4, 2, 32, 16, torch.float16)
+    pos, seq, table = i32([0, 1]), i32([0, 0]), i32([[0, 1]])
+    k = randn(1, (2, 2, 16), torch.float16)
+    q, out = randn(2, (2, 4, 16), torch.float16), torch.empty((2, 4, 16), dtype=torch.float16, device=DEV)
+    for bad in (lambda: cache.append(k[:1], k, pos, seq, table), lambda: cache.append(k, k[:, :1], pos, seq, table),
+                lambda: cache.append(k.transpose(1, 2).contiguous().transpose(1, 2), k, pos, seq, table),
+                lambda: cache.append(k, k, pos, seq[:1], table), lambda: cache.attend(q[..., :8], out, pos, seq, table),
+                lambda: cache.select(q, pos, seq, table, i32([[1]]))):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: cache.append(k.float(), k, pos, seq, table), lambda: cache.append(k, k, pos.long(), seq, table),
+                lambda: cache.attend(q, out.float(), pos, seq, table), lambda: cache.append(k, k, pos.cpu(), seq, table)):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises(sd.SdnnError):
+        cache.attend(randn(1, (2, 3, 16), torch.float16), torch.empty((2, 3, 16), dtype=torch.float16, device=DEV), pos, seq, table)
+    with pytest.raises(sd.SdnnError):
+        cache.select(q, pos, seq, table, torch.empty((2, 2, 3), dtype=torch.int32, device=DEV), sink=2, local=2)
+    no_keys = sd.BlockCache(None, None, cache.means, cache.mean_scales, block=32)
+    with pytest.raises(ValueError):
+        no_keys.append(k, k, pos, seq, table)
+    torch.cuda.synchronize()
+
+
+def test_no_tokens_no_blocks_no_sequences():
+    cache = make_cache(0, 2, 1, 32, 16, torch.float32)
+    none = torch.empty((0, 1, 16), device=DEV)
+    empty, table = i32([]), i32([[0, 1]])
+    cache.append(none, none, empty, empty, table)
+    cache.select(none, empty, empty, table, torch.empty((0, 1, 4), dtype=torch.int32, device=DEV))
+    cache.attend(none, none.clone(), empty, empty, table)
+    sd.Rope(16).apply(none, none.clone(), empty)
+    q = randn(1, (2, 1, 16), torch.float32)
+    for tab, seq in ((torch.empty((1, 0), dtype=torch.int32, device=DEV), [0, 0]),
+                     (torch.empty((0, 3), dtype=torch.int32, device=DEV), [0, 1])):
+        out, lse = torch.full_like(q, 3.0), torch.zeros((2, 1), device=DEV)
+        cache.append(q, q, i32([0, 1]), i32(seq), tab)
+        cache.attend(q, out, i32([0, 1]), i32(seq), tab, lse=lse)
+        chosen = torch.full((2, 1, 4), 9, dtype=torch.int32, device=DEV)
+        cache.select(q, i32([0, 1]), i32(seq), tab, chosen)
+        assert (out == 0).all() and torch.isneginf(lse).all() and (chosen == -1).all()
+    assert torch.isnan(cache.k_pages).all()
+
+
 def test_q4_same_result_every_time():
     packed, scales, z = random_q4(9, 300, 2000, 64, torch.float16, True)
     plan = sd.Q4Plan(packed, scales, z, K=2000, group=64)
