@@ -177,7 +177,7 @@ sdnn_status sdnn_qmat_create(const uint8_t* packed, const void* scales, sdnn_dty
                              const uint8_t* zeros, int32_t M, int32_t K, int32_t group,
                              void* stream, sdnn_qmat* out);
 
-/* y = epi(W x + bias) for the N columns of x.  Value k of column n is
+/* y = epi(W x + bias) for the N <= 2^18 columns of x.  Value k of column n is
  * x[k * x_feature + n * x_column] and value m of column n y[m * y_feature + n * y_column]:
  * a K x N matrix as sdnn_spmm takes it has strides (N, 1), rows of tokens (1, K).
  *   bias: device, M floats, or NULL.  The products are exact and are summed in 32 bits; x

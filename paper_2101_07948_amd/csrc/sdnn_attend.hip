@@ -181,19 +181,17 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return u + v;
 }
 
-// One step: tokens [0, seen) of its are within the sight of this lane's query, tokens from `stored` on may
+// One step, its scores s given: tokens [0, seen) of its are within the sight of this lane's query, tokens from `stored` on may
 // hold anything.  EMPTY: queries may see nothing here (seen <= 0), or have seen nothing yet (m = -infinity).
 //   m is a reference near the running maximum rather than the maximum: it moves only where a score is over
 // 2^8 times above it, so that most steps neither reduce over lanes nor rescale the sums (p <= 2^8 costs no bits:
 // p is a float, and its 16-bit parts are floating too).  Scores are masked one by one only where a query's
 // sight ends within the step; a query that sees nothing of it gets m = infinity for the step, p = 0.
-template <bool EMPTY, typename T, int CHUNKS, int TILES, typename K, typename V>
-__device__ __forceinline__ void attend_step(float scale2, const K& kk, const V& vv, int seen, int stored,
-                                            const typename Step<T>::Piece (&q)[CHUNKS], int g, State<TILES>& st) {
+template <bool EMPTY, typename T, int CHUNKS, int TILES, typename V>
+__device__ __forceinline__ void attend_step(float scale2, float (&s)[Step<T>::kTokens / 4], const V& vv, int seen,
+                                            int stored, int g, State<TILES>& st) {
   constexpr int N = Step<T>::kTokens, E = N / 4;
   constexpr float SLACK = 8.0f;
-  float s[E];
-  Step<T>::template scores<CHUNKS>(kk, q, s);
   if (!EMPTY || __any(seen > 0 && seen < N)) {
 #pragma unroll
     for (int j = 0; j < E; ++j) s[j] = E * g + j < seen ? s[j] : -INFINITY;
@@ -288,8 +286,9 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
       Step<T>::template load<CHUNKS>(static_cast<const T*>(a.k_pages) + at + t0 * D,
                                      static_cast<const T*>(a.v_pages) + at + t0, D, a.block, r, g, kk, vv);
       __builtin_amdgcn_sched_barrier(0);
-      attend_step<false, T, CHUNKS, TILES>(a.scale2, [&](int i) { return kk[i]; }, [&](int i) { return vv[i]; },
-                                           seen, seen, q, g, st);
+      float s[N / 4];
+      Step<T>::template scores<CHUNKS>([&](int i) { return kk[i]; }, q, s);
+      attend_step<false, T, CHUNKS, TILES>(a.scale2, s, [&](int i) { return vv[i]; }, seen, seen, g, st);
     }
     id = next_id, next_id = after, page = next_page;
   }
@@ -606,19 +605,34 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
       if (block_key != END) offer(turn = next());
     }
     if (block_key != END) fetch(s, buffer ^ 1);
-    for (int u = 0; u < stage; u += N) {
-      const int left = now_seen - u;
-      if (!__any(left > 0)) break;
+    const auto scores = [&](int u, float (&x)[N / 4]) {
+      Step<T>::template scores<CHUNKS>([&](int i) { return key_piece<T, CHUNKS, STAGE>(lds[buffer], i, u, D, r, g); }, q, x);
+    };
+    const auto step = [&](int u, float (&x)[N / 4], int stored) {
+      attend_step<true, T, CHUNKS, TILES>(
+          a.scale2, x, [&](int i) { return value_piece<T, CHUNKS, STAGE>(lds[buffer], i, u, r, g); }, now_seen - u, stored,
+          g, st);
+    };
+    int u = 0;
+    // two steps that some query sees all of: the second one's scores are under way while the first is taken in
+    for (; u + 2 * N <= stage && __any(now_seen >= u + 2 * N); u += 2 * N) {
+      float x[N / 4], y[N / 4];
+      scores(u, x);
+      scores(u + N, y);
+      step(u, x, N);
+      step(u + N, y, N);
+    }
+    for (; u < stage && __any(now_seen > u); u += N) {
       // of the tokens past every query's sight the values are taken for zeros
       int stored = N;
-      if (!__any(left >= N)) {
-        stored = max(left, 0);
+      if (!__any(now_seen >= u + N)) {
+        stored = max(now_seen - u, 0);
 #pragma unroll
         for (int x = 1; x < 16; x <<= 1) stored = max(stored, __shfl_xor(stored, x));
       }
-      attend_step<true, T, CHUNKS, TILES>(
-          a.scale2, [&](int i) { return key_piece<T, CHUNKS, STAGE>(lds[buffer], i, u, D, r, g); },
-          [&](int i) { return value_piece<T, CHUNKS, STAGE>(lds[buffer], i, u, r, g); }, left, stored, q, g, st);
+      float x[N / 4];
+      scores(u, x);
+      step(u, x, stored);
     }
     buffer ^= 1;
   }

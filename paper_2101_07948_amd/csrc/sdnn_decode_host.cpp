@@ -208,7 +208,7 @@ sdnn_status sdnn_qmat_apply(sdnn_qmat w, const void* x, int64_t x_feature, int64
                             int64_t y_feature, int64_t y_column, int32_t N, sdnn_dtype dtype,
                             const float* bias, sdnn_epilogue epi, void* stream) {
   if (!w) return SDNN_ERR_NULL;
-  if (bad_dtype(dtype) || N < 0 || N > (1 << 20)) return SDNN_ERR_DIM;
+  if (bad_dtype(dtype) || N < 0 || N > (1 << 18)) return SDNN_ERR_DIM;
   if (epi != SDNN_EPI_NONE && epi != SDNN_EPI_RELU && epi != SDNN_EPI_GELU) return SDNN_ERR_DIM;
   if (bad_stride(x_feature) || bad_stride(x_column) || bad_stride(y_feature) || bad_stride(y_column))
     return SDNN_ERR_DIM;
