@@ -76,30 +76,38 @@ def _on_gpu(t, name: str):
 
 
 def _dense(t, name: str, dtype, shape) -> int:
-    """Device address of a contiguous tensor of the given type and shape."""
+    """Device address of a contiguous tensor of the given type and shape (checked on a fast path;
+    the slow path only builds the error message)."""
+    try:
+        if t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     _on_gpu(t, name)
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _rows(t, name: str, dtype, tokens: int, heads, head_dim: int) -> bytes:
     """sdnn_heads of a (tokens, heads, head_dim) tensor; any strides but the last's."""
+    try:
+        T, H, D = t.shape
+        by_token, by_head, by_value = t.stride()
+        if t.is_cuda and t.dtype is dtype and T == tokens and D == head_dim and (heads is None or heads == H) and \
+                (by_value == 1 or D == 1):
+            return _HEADS.pack(t.data_ptr(), by_token, by_head, H, 0)
+    except (AttributeError, ValueError):
+        pass
     _on_gpu(t, name)
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    shape = t.shape
-    if len(shape) != 3 or shape[0] != tokens or shape[2] != head_dim or heads not in (None, shape[1]):
-        want = (tokens, "heads" if heads is None else heads, head_dim)
-        raise ValueError(f"{name} has shape {tuple(shape)}, expected {want}")
-    stride = t.stride()
-    if stride[2] != 1 and head_dim > 1:
-        raise ValueError(f"{name}: the values of a head must be contiguous")
-    return _HEADS.pack(t.data_ptr(), stride[0], stride[1], shape[1], 0)
+    want = (tokens, "heads" if heads is None else heads, head_dim)
+    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != head_dim or heads not in (None, t.shape[1]):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {want}")
+    raise ValueError(f"{name}: the values of a head must be contiguous")
 
 
 def _check(code: int, where: str):
@@ -162,7 +170,6 @@ class Rope:
         """y = x (tokens, heads, head_dim) rotated to the positions pos (tokens, int32); by the
         negative angles with inverse (which is also the gradient).  y may be x."""
         torch = _torch_mod()
-        _on_gpu(x, "x")
         if x.dim() != 3:
             raise ValueError("x must be 3-d (tokens, heads, head_dim)")
         T, H, D = x.shape
@@ -340,16 +347,16 @@ class Q4Plan:
     def matvec(self, x, y, bias=None, epi: str = "none", stream=None):
         """y (M, N) = epi(W @ x + bias) for x (K, N) of the same type, N few; any strides (rows of
         tokens are x.t(), y.t()).  bias: float32 (M,)."""
-        _on_gpu(x, "x")
-        _on_gpu(y, "y")
         torch = _torch_mod()
-        if x.dim() != 2 or x.shape[0] != self.K:
+        K, N = x.shape if x.dim() == 2 else (None, None)
+        if K != self.K:
             raise ValueError(f"x has shape {tuple(x.shape)}, expected ({self.K}, N)")
-        N = x.shape[1]
-        if tuple(y.shape) != (self.M, N):
+        if y.shape != (self.M, N):
             raise ValueError(f"y has shape {tuple(y.shape)}, expected {(self.M, N)}")
         if y.dtype is not x.dtype:
             raise TypeError(f"y must be {x.dtype}, not {y.dtype}")
+        if not (x.is_cuda and y.is_cuda):
+            raise TypeError("x and y must be CUDA/HIP torch tensors")
         pb = None if bias is None else _dense(bias, "bias", torch.float32, (self.M,))
         (xf, xc), (yf, yc) = x.stride(), y.stride()
         _check(self._lib.sdnn_qmat_apply(self.handle, x.data_ptr(), xf, xc, y.data_ptr(), yf, yc, N,
