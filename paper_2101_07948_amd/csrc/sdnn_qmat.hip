@@ -26,14 +26,20 @@ __global__ __launch_bounds__(256) void qmat_pack(const uint8_t* packed, int32_t 
   const int64_t row = tc / chunks * kQTileRows + (lane & 15);
   const int k0 = (int)(tc % chunks) * kQChunk + j * 32 + (lane >> 4) * 8;
   uint32_t w = 0;
-  if (row < M)
+  if (row < M && k0 < K) {
+    const uint8_t* from = packed + row * ((K + 1) / 2) + k0 / 2;
+    uint32_t eight = 0;  // numbers, 4 bits each
+    if (k0 + 8 <= K)
+      __builtin_memcpy(&eight, from, 4);
+    else
+      for (int i = 0; 2 * i < K - k0; ++i) eight |= (uint32_t)from[i] << (8 * i);
+#pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int k = k0 + i;
-      if (k >= K) break;
-      const uint32_t b = packed[row * ((K + 1) / 2) + k / 2];
-      const uint32_t n = k & 1 ? b >> 4 : b & 15, at = bit_of(i);
-      w |= n << at | (at > 28 ? n >> (32 - at) : 0);
+      const uint32_t n = k0 + i < K ? eight >> (4 * i) & 15u : 0;
+      const int to = bit_of(i);
+      w |= n << to | (to > 28 ? n >> (32 - to) : 0);
     }
+  }
   out[at] = w;
 }
 
