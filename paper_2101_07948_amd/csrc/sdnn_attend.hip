@@ -48,10 +48,9 @@ struct Step16 {
 
   static __device__ __forceinline__ int token(int half, int r) { return 8 * (r >> 2) + 4 * half + (r & 3); }
 
-  // The keys and values of a step: 2 CHUNKS pieces each.
+  // The keys and the values of a step: 2 CHUNKS pieces each.
   template <int CHUNKS>
-  static __device__ __forceinline__ void load(const T* k, const T* v, int D, int P, int r, int g,
-                                              V8 (&kk)[2 * CHUNKS], V8 (&vv)[2 * CHUNKS]) {
+  static __device__ __forceinline__ void load_keys(const T* k, int D, int r, int g, V8 (&kk)[2 * CHUNKS]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -59,6 +58,9 @@ struct Step16 {
         const int d = min((c * 4 + g) * 8, D - 8);  // past the head's end: any of its values, q is 0 there
         kk[h * CHUNKS + c] = *reinterpret_cast<const V8*>(k + token(h, r) * D + d);
       }
+  }
+  template <int CHUNKS>
+  static __device__ __forceinline__ void load_values(const T* v, int D, int P, int r, int g, V8 (&vv)[2 * CHUNKS]) {
 #pragma unroll
     for (int c = 0; c < 2 * CHUNKS; ++c)
       vv[c] = *reinterpret_cast<const V8*>(v + min(c * 16 + r, D - 1) * P + 8 * g);
@@ -123,13 +125,15 @@ struct Step<float> {
   typedef f32x4 Piece;
 
   template <int CHUNKS>
-  static __device__ __forceinline__ void load(const float* k, const float* v, int D, int P, int r, int g,
-                                              f32x4 (&kk)[CHUNKS], f32x4 (&vv)[CHUNKS]) {
+  static __device__ __forceinline__ void load_keys(const float* k, int D, int r, int g, f32x4 (&kk)[CHUNKS]) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
       const int d = min((c * 4 + g) * 4, D - 4);
       kk[c] = *reinterpret_cast<const f32x4*>(k + r * D + d);
     }
+  }
+  template <int CHUNKS>
+  static __device__ __forceinline__ void load_values(const float* v, int D, int P, int r, int g, f32x4 (&vv)[CHUNKS]) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
       vv[c] = *reinterpret_cast<const f32x4*>(v + min(c * 16 + r, D - 1) * P + 4 * g);
@@ -282,12 +286,19 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
     const int seen = p - id * a.block + 1 - t0;
     if (page >= 0 && page < a.pages && seen > 0) {
       const int64_t at = ((int64_t)page * a.kv_heads + h) * a.block * D;
+      const T* v = static_cast<const T*>(a.v_pages) + at + t0;
       typename Step<T>::Piece kk[TILES], vv[TILES];
-      Step<T>::template load<CHUNKS>(static_cast<const T*>(a.k_pages) + at + t0 * D,
-                                     static_cast<const T*>(a.v_pages) + at + t0, D, a.block, r, g, kk, vv);
+      Step<T>::template load_keys<CHUNKS>(static_cast<const T*>(a.k_pages) + at + t0 * D, D, r, g, kk);
+      // (the keys and values of a long head are more than the registers of two waves hold beside each other)
+      if (TILES <= 8) Step<T>::template load_values<CHUNKS>(v, D, a.block, r, g, vv);
       __builtin_amdgcn_sched_barrier(0);
       float s[N / 4];
       Step<T>::template scores<CHUNKS>([&](int i) { return kk[i]; }, q, s);
+      if (TILES > 8) {
+        __builtin_amdgcn_sched_barrier(0);
+        Step<T>::template load_values<CHUNKS>(v, D, a.block, r, g, vv);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       attend_step<false, T, CHUNKS, TILES>(a.scale2, s, [&](int i) { return vv[i]; }, seen, seen, g, st);
     }
     id = next_id, next_id = after, page = next_page;
@@ -409,14 +420,15 @@ __device__ __forceinline__ void copy_to_lds(const void* from, unsigned char* to)
                                    (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// A stage of keys and values in LDS: STAGE tokens of a page, keys as rows of a head (of CHUNKS * 64 bytes,
-// also where the head is shorter), values as rows of STAGE tokens.  A row's 16-byte pieces are permuted by the
+// A stage of keys and values in LDS: STAGE tokens of a page, keys as rows of a head (of a power of two of
+// bytes, also where the head is shorter), values as rows of STAGE tokens.  A row's 16-byte pieces are permuted by the
 // row (piece x at x ^ swap) so that the 16 rows that a wave reads one piece of lie in different banks.
+constexpr int power_of_two(int n) { return n <= 1 ? 1 : 2 * power_of_two((n + 1) / 2); }
 template <typename T, int CHUNKS, int STAGE>
 struct Tile {
   static constexpr int kPiece = 16 / sizeof(T);
-  static constexpr int kKeyPieces = CHUNKS * 4, kValuePieces = STAGE / kPiece;
-  static constexpr int kDims = CHUNKS * 4 * kPiece;
+  static constexpr int kKeyPieces = power_of_two(CHUNKS) * 4, kValuePieces = STAGE / kPiece;
+  static constexpr int kDims = kKeyPieces * kPiece;
   static constexpr int kBytes = STAGE * kKeyPieces * 16;  // of either
   static_assert(kDims * kValuePieces * 16 == kBytes, "both hold the same values");
   static __device__ __forceinline__ int key_swap(int row) {
@@ -657,7 +669,8 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
 template <typename T, int CHUNKS>
 hipError_t start(const AttendArgs& a, hipStream_t stream) {
   if (a.tile_tokens > 0) {
-    constexpr int STAGE = sizeof(T) == 2 ? (CHUNKS <= 4 ? 64 : 32) : CHUNKS <= 4 ? 64 : CHUNKS <= 8 ? 32 : 16;
+    constexpr int LONG = power_of_two(CHUNKS) * 64;  // bytes of a head's row in LDS; 16 KiB of keys to a stage at most
+    constexpr int STAGE = LONG <= 256 ? 64 : 16384 / LONG;
     const int64_t groups = (a.tokens + a.tile_tokens * kTileWaves - 1) / (a.tile_tokens * kTileWaves);
     attend_tiles<T, CHUNKS, STAGE, kTileWaves>
         <<<(unsigned)(groups * a.head_tiles * a.kv_heads), kTileWaves * 64, 0, stream>>>(a);
@@ -671,27 +684,40 @@ hipError_t start(const AttendArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Pieces of a lane: a head of up to 64, 128 or 256 values.
+// Pieces of a lane: a head of up to 64, 96, 128, 192 or 256 values.
 template <typename T>
 hipError_t start_dim(const AttendArgs& a, hipStream_t stream) {
-  constexpr int U = 16 / Step<T>::kPiece;
-  if (a.head_dim <= 64) return start<T, U>(a, stream);
-  if (a.head_dim <= 128) return start<T, 2 * U>(a, stream);
-  return start<T, 4 * U>(a, stream);
+  constexpr int U = 8 / Step<T>::kPiece;  // pieces of 32 values
+  if (a.head_dim <= 64) return start<T, 2 * U>(a, stream);
+  if (a.head_dim <= 96) return start<T, 3 * U>(a, stream);
+  if (a.head_dim <= 128) return start<T, 4 * U>(a, stream);
+  if (a.head_dim <= 192) return start<T, 6 * U>(a, stream);
+  return start<T, 8 * U>(a, stream);
 }
 
 }  // namespace
 
 namespace {
 // Tokens of a wave's tile in attend_tiles (a token's queries take a power of two of its 16 rows), or 0
-// where attend_kernel serves the call.
-int tile_tokens(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads) {
-  const int group = heads / c.kv_heads;
+// where attend_kernel serves the call: where few tokens of a sequence are neighbours, and where it is estimated to
+// be faster.  attend_kernel reads every token's blocks from L2, at about 8 TB/s (16384 heads of 16 blocks of 32 KiB:
+// 994 us; 8760 of 3 of 128 KiB: 683).  attend_tiles takes its workgroups' unions of blocks, 512 workgroups at a
+// time, at about 3 us for 32 KiB (38 of them: 145 us; four times that in 32 bits, whose matrix instructions take
+// as much longer); how large a union is depends on the lists, three of them are taken for it.
+int tile_tokens(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads,
+                int32_t chosen) {
+  const int group = heads / c.kv_heads, head_tiles = (group + kRows - 1) / kRows;
   int rows = 1;
   while (rows < group && rows < kRows) rows *= 2;
   const int tile = kRows / rows;
-  const int64_t groups = (int64_t)(tokens / (tile * kTileWaves)) * c.kv_heads * ((group + kRows - 1) / kRows);
-  return max_blocks <= 1 << 20 && tokens >= (int64_t)16 * sequences && groups >= 128 ? tile : 0;
+  if (max_blocks > 1 << 20 || tokens < (int64_t)16 * sequences) return 0;
+  const double page = 2.0 * c.block * c.head_dim * dtype_bytes(c.dtype);
+  const int each = chosen > 0 && chosen < max_blocks ? chosen : max_blocks;
+  const int all = chosen > 0 && chosen < max_blocks / 3 ? 3 * chosen : max_blocks;
+  const double groups = (double)((tokens + tile * kTileWaves - 1) / (tile * kTileWaves)) * c.kv_heads * head_tiles;
+  const double one_by_one = (double)tokens * c.kv_heads * head_tiles * each * page / 8e6;
+  const double tiled = (groups > 512 ? groups / 512 : 1.0) * all * (page / 32768) * (c.dtype == SDNN_F32 ? 12 : 3);
+  return tiled < one_by_one ? tile : 0;
 }
 }  // namespace
 
@@ -725,7 +751,7 @@ hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.heads = q.heads, a.kv_heads = c.kv_heads, a.group = q.heads / c.kv_heads;
   a.head_tiles = (a.group + kRows - 1) / kRows;
   a.head_dim = c.head_dim, a.block = c.block;
-  a.tile_tokens = tile_tokens(c, t.tokens, t.sequences, t.max_blocks, q.heads);
+  a.tile_tokens = tile_tokens(c, t.tokens, t.sequences, t.max_blocks, q.heads, chosen ? blocks : 0);
   a.blocks = blocks, a.splits = a.tile_tokens ? 1 : attend_splits(c, t.tokens, q.heads, blocks);
   // (a scale of 0 makes all scores equal: so does one that is too small to part them)
   a.scale2 = fmaxf(fabsf(scale), 1e-30f) * 1.44269504f;
