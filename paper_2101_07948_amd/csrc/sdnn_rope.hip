@@ -177,6 +177,9 @@ struct AppendArgs {
   int32_t window;  // tokens of a workgroup
   int32_t k_aligned, v_aligned;
   int32_t k_whole;  // keys can be read and rotated 16 bytes at a time
+  int32_t k_pairs;  // or, where pairs are neighbours, a pair at a time
+  int32_t before;   // bytes of LDS before the rows of a block's keys that lie before the window
+  int32_t passes;   // of a mean, each with a part of those rows
 };
 
 constexpr int kWindow = 64;       // the most
@@ -188,6 +191,7 @@ constexpr int kSumRows = 8;       // keys of a block that a thread adds
 struct AppendLds {
   int64_t page[kWindow];  // -1: nothing to store
   int32_t pos[kWindow], seq[kWindow];
+  uint8_t there[128];
   float sum[kMaxHeadDim];
   float top;
 };
@@ -205,78 +209,109 @@ __device__ __forceinline__ float halves(const GET& get, int first = 0) {
     return halves<N, STRIDE * 2>(get, first) + halves<N, STRIDE * 2>(get, first + STRIDE);
 }
 
-// V values of the key of token t from value d on, as they are stored: with k_whole 16 bytes at a time.
-template <typename T, bool INTERLEAVED>
-__device__ __forceinline__ void stored_key(const AppendArgs& a, int t, int h, int d, T (&out)[16 / sizeof(T)]) {
-  constexpr int V = 16 / sizeof(T);
-  const T* x = static_cast<const T*>(a.k) + t * a.k_token + h * a.k_head;
-  if (a.k_whole) {
-    load_n<V>(x + d, true, out);
-    if (d >= 2 * a.pairs) return;
-    const int32_t p = a.pos[t];
-    T other[V] = {};
-    if (!INTERLEAVED) load_n<V>(x + (d < a.pairs ? d + a.pairs : d - a.pairs), true, other);
-    const int pair = INTERLEAVED ? d / 2 : d < a.pairs ? d : d - a.pairs;
-#pragma unroll
-    for (int e = 0; e < (INTERLEAVED ? V / 2 : V); ++e) {
-      const float2 f = rotation_of(a.freq, a.amplitude, p, pair + e);
-      float y0, y1;
-      if (INTERLEAVED) {
-        rotate((float)out[2 * e], (float)out[2 * e + 1], f, &y0, &y1);
-        out[2 * e] = (T)y0, out[2 * e + 1] = (T)y1;
-      } else {
-        const bool second = d >= a.pairs;
-        rotate((float)(second ? other[e] : out[e]), (float)(second ? out[e] : other[e]), f, &y0, &y1);
-        out[e] = (T)(second ? y1 : y0);
-      }
+// Rotates n keys into rows of LDS: key i, at position pos_of(i), from x_of(i) to y_of(i); those without a row (NULL)
+// are left out.  VP: pairs (and values past the rotated part) of a thread's unit, as in rope_rows.
+template <typename T, bool INTERLEAVED, int VP, typename X, typename Y, typename POS>
+__device__ __forceinline__ void rotate_keys(const AppendArgs& a, int n, bool aligned, const X& x_of, const Y& y_of,
+                                            const POS& pos_of) {
+  constexpr int REST = rest_values<INTERLEAVED>(VP);
+  const int D = a.head_dim, turning = a.pairs / VP, units = turning + (D - 2 * a.pairs) / REST;
+#pragma unroll 2
+  for (int j = threadIdx.x; j < n * units; j += kThreads) {
+    const int i = j / units, u = j - i * units;
+    T* y = y_of(i);
+    if (!y) continue;
+    const T* x = x_of(i);
+    if (u >= turning) {
+      const int d = 2 * a.pairs + (u - turning) * REST;
+      T w[REST];
+      load_n<REST>(x + d, aligned, w);
+      store_n<REST>(y + d, VP > 1, w);
+      continue;
     }
-    return;
-  }
-#pragma unroll 1
-  for (int e = 0; e < V; ++e, ++d) {
-    T v = x[d];
-    if (d < 2 * a.pairs) {
-      const int i = INTERLEAVED ? d / 2 : d % a.pairs;
-      float y0, y1;
-      rotate((float)x[INTERLEAVED ? 2 * i : i], (float)x[INTERLEAVED ? 2 * i + 1 : i + a.pairs],
-             rotation_of(a.freq, a.amplitude, a.pos[t], i), &y0, &y1);
-      v = (T)((INTERLEAVED ? d & 1 : d >= a.pairs) ? y1 : y0);
-    }
+    T lo[VP], hi[VP];
+    if (INTERLEAVED) {
+      T w[2 * VP];
+      load_n<2 * VP>(x + 2 * u * VP, aligned, w);
 #pragma unroll
-    for (int k = 0; k < V; ++k)
-      if (k == e) out[k] = v;
+      for (int e = 0; e < VP; ++e) lo[e] = w[2 * e], hi[e] = w[2 * e + 1];
+    } else {
+      load_n<VP>(x + u * VP, aligned, lo);
+      load_n<VP>(x + a.pairs + u * VP, aligned, hi);
+    }
+    const int32_t p = pos_of(i);
+#pragma unroll
+    for (int e = 0; e < VP; ++e) {
+      float y0, y1;
+      rotate((float)lo[e], (float)hi[e], rotation_of(a.freq, a.amplitude, p, u * VP + e), &y0, &y1);
+      lo[e] = (T)y0, hi[e] = (T)y1;
+    }
+    if (INTERLEAVED) {
+      T w[2 * VP];
+#pragma unroll
+      for (int e = 0; e < VP; ++e) w[2 * e] = lo[e], w[2 * e + 1] = hi[e];
+      store_n<2 * VP>(y + 2 * u * VP, VP > 1, w);
+    } else {
+      store_n<VP>(y + u * VP, VP > 1, lo);
+      store_n<VP>(y + a.pairs + u * VP, VP > 1, hi);
+    }
   }
 }
 
 // The mean of the block that token i of the window fills.  Its keys come from the window's tile, from the
-// call's tokens before the window (rotated again: another workgroup stores them at this moment; `earlier`:
-// the token before the window may be one) or from the page, where an earlier call stored them.  A thread adds
-// keys q, q + P/8, ... of 16 bytes of a row, all loads under way together, and the P/8 sums are added from LDS.
+// call's tokens before the window (rotated again into `before`, since another workgroup stores them at this
+// moment; `earlier`: the token before the window may be one) or from the page, where an earlier call stored
+// them.  A thread adds keys q, q + P/8, ... of 16 bytes of a row, all loads under way together, and the P/8 sums
+// are added from LDS.
 template <typename T, bool INTERLEAVED>
-__device__ void block_mean(const AppendArgs& a, AppendLds& l, const T* tile, float* sums, int t0, int i, int h,
+__device__ void block_mean(const AppendArgs& a, AppendLds& l, const T* tile, T* before, float* sums, int t0, int i, int h,
                            bool earlier) {
-  constexpr int V = 16 / sizeof(T);
-  const int P = a.block, D = a.head_dim, t = t0 + i, parts = P / kSumRows, chunks = D / V;
+  constexpr int V = 16 / sizeof(T), WIDE = V / (INTERLEAVED ? 2 : 1);
+  const int P = a.block, D = a.head_dim, parts = P / kSumRows, chunks = D / V;
   const int32_t pos = l.pos[i], seq = l.seq[i];
   const int64_t row = l.page[i] * a.kv_heads + h;
   const T* page = static_cast<const T*>(a.k_pages) + row * P * D;
-  for (int j = threadIdx.x; j < parts * chunks; j += kThreads) {
-    const int q = j / chunks, d = (j - q * chunks) * V;
-    T x[kSumRows][V];
-#pragma unroll
-    for (int k = 0; k < kSumRows; ++k)  // what the page holds, where it is from this call too: replaced below
-      load_n<V>(page + (int64_t)(q + k * parts) * D + d, true, x[k]);
-#pragma unroll
-    for (int k = 0; k < kSumRows; ++k) {
-      const int back = P - 1 - (q + k * parts), from = t - back;  // tokens before the one that fills the block
-      if (back <= i) {
-        if (l.seq[i - back] == seq && l.pos[i - back] == pos - back) load_n<V>(tile + (i - back) * D + d, true, x[k]);
-      } else if (earlier && from >= 0 && a.seq[from] == seq && a.pos[from] == pos - back) {
-        stored_key<T, INTERLEAVED>(a, from, h, d, x[k]);
-      }
+  const int missing = earlier ? min(P - 1 - i, t0) : 0;  // tokens t0 - 1, t0 - 2, ... that may be the block's
+  for (int j = threadIdx.x; j < missing; j += kThreads)
+    l.there[j] = a.seq[t0 - 1 - j] == seq && a.pos[t0 - 1 - j] == pos - i - 1 - j;
+  // In a pass the sums q0 ... q0 + share - 1 are made, of all keys that go into them: key s of the block has row
+  // place(s) of `before`.
+  const int share = parts / a.passes;
+  const auto place = [&](int s) { return s / parts * share + s % share; };
+  for (int q0 = 0; q0 < parts; q0 += share) {
+    __syncthreads();
+    if (missing > 0) {
+      const T* k = static_cast<const T*>(a.k) + (t0 - 1) * a.k_token + h * a.k_head;
+      const auto x_of = [&](int j) { return k - j * a.k_token; };
+      const auto y_of = [&](int j) -> T* {
+        const int s = P - 2 - i - j, q = s % parts;
+        return l.there[j] && q >= q0 && q < q0 + share ? before + place(s) * D : nullptr;
+      };
+      const auto pos_of = [&](int j) { return pos - i - 1 - j; };
+      if (a.k_whole)
+        rotate_keys<T, INTERLEAVED, WIDE>(a, missing, true, x_of, y_of, pos_of);
+      else
+        rotate_keys<T, INTERLEAVED, 1>(a, missing, a.k_pairs, x_of, y_of, pos_of);
+      __syncthreads();
     }
+    for (int j = threadIdx.x; j < share * chunks; j += kThreads) {
+      const int q = q0 + j / chunks, d = j % chunks * V;
+      T x[kSumRows][V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) sums[q * D + d + e] = halves<kSumRows>([&](int k) { return (float)x[k][e]; });
+      for (int k = 0; k < kSumRows; ++k)  // what the page holds, where it is from this call too: replaced below
+        load_n<V>(page + (int64_t)(q + k * parts) * D + d, true, x[k]);
+#pragma unroll
+      for (int k = 0; k < kSumRows; ++k) {
+        const int s = q + k * parts, back = P - 1 - s;  // tokens before the one that fills the block
+        if (back <= i) {
+          if (l.seq[i - back] == seq && l.pos[i - back] == pos - back) load_n<V>(tile + (i - back) * D + d, true, x[k]);
+        } else if (back - i - 1 < missing && l.there[back - i - 1]) {
+          load_n<V>(before + place(s) * D + d, true, x[k]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) sums[q * D + d + e] = halves<kSumRows>([&](int k) { return (float)x[k][e]; });
+    }
   }
   __syncthreads();
   for (int d = threadIdx.x; d < D; d += kThreads) {
@@ -342,47 +377,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     store_n<V>(turn + i * stride + d, true, x);
   }
   const T* k = static_cast<const T*>(a.k) + t0 * a.k_token + h * a.k_head;
-  constexpr int REST = rest_values<INTERLEAVED>(VP);
-  const int turning = a.pairs / VP, units = turning + (D - 2 * a.pairs) / REST;
-#pragma unroll 2
-  for (int j = threadIdx.x; j < n * units; j += kThreads) {
-    const int i = j / units, u = j - i * units;
-    const T* x = k + i * a.k_token;
-    T* y = tile + i * D;
-    if (u >= turning) {
-      const int d = 2 * a.pairs + (u - turning) * REST;
-      T w[REST];
-      load_n<REST>(x + d, a.k_aligned, w);
-      store_n<REST>(y + d, VP > 1, w);
-      continue;
-    }
-    T lo[VP], hi[VP];
-    if (INTERLEAVED) {
-      T w[2 * VP];
-      load_n<2 * VP>(x + 2 * u * VP, a.k_aligned, w);
-#pragma unroll
-      for (int e = 0; e < VP; ++e) lo[e] = w[2 * e], hi[e] = w[2 * e + 1];
-    } else {
-      load_n<VP>(x + u * VP, a.k_aligned, lo);
-      load_n<VP>(x + a.pairs + u * VP, a.k_aligned, hi);
-    }
-    const int32_t p = a.pos[t0 + i];
-#pragma unroll
-    for (int e = 0; e < VP; ++e) {
-      float y0, y1;
-      rotate((float)lo[e], (float)hi[e], rotation_of(a.freq, a.amplitude, p, u * VP + e), &y0, &y1);
-      lo[e] = (T)y0, hi[e] = (T)y1;
-    }
-    if (INTERLEAVED) {
-      T w[2 * VP];
-#pragma unroll
-      for (int e = 0; e < VP; ++e) w[2 * e] = lo[e], w[2 * e + 1] = hi[e];
-      store_n<2 * VP>(y + 2 * u * VP, VP > 1, w);
-    } else {
-      store_n<VP>(y + u * VP, VP > 1, lo);
-      store_n<VP>(y + a.pairs + u * VP, VP > 1, hi);
-    }
-  }
+  rotate_keys<T, INTERLEAVED, VP>(
+      a, n, a.k_aligned, [&](int i) { return k + i * a.k_token; }, [&](int i) { return tile + i * D; },
+      [&](int i) { return a.pos[t0 + i]; });
   __syncthreads();
   T* kp = static_cast<T*>(a.k_pages);
   for (int j = threadIdx.x; j < n * chunks; j += kThreads) {
@@ -422,8 +419,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   if (!full) return;
   const bool earlier = t0 > 0 && a.seq[t0 - 1] == l.seq[0] && a.pos[t0 - 1] == l.pos[0] - 1;
   __syncthreads();  // the values are written: their place is free
+  T* rows = reinterpret_cast<T*>(lds + a.before);
   for (; full; full &= full - 1)
-    block_mean<T, INTERLEAVED>(a, l, tile, reinterpret_cast<float*>(turn), t0, __builtin_ctzll(full), h, earlier);
+    block_mean<T, INTERLEAVED>(a, l, tile, rows, reinterpret_cast<float*>(turn), t0, __builtin_ctzll(full), h, earlier);
 }
 
 template <typename F>
@@ -470,18 +468,28 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   // whose values are written in runs
   const int size = dtype_bytes(c.dtype), layout = r ? r->layout : SDNN_ROPE_HALF;
   a.window = 1;
-  if (t.tokens >= kWindow && ((int64_t)t.tokens * c.kv_heads > 4096 || t.tokens >= (int64_t)16 * t.sequences))
+  if ((int64_t)t.tokens * c.kv_heads > 4096 || t.tokens >= (int64_t)16 * t.sequences)
     a.window = kWindow * c.head_dim * size <= kTileBytes ? kWindow : kWindow / 2;
   // The keys' units are 16-byte ones where windows have many and the head divides by them.
   const int wide = 16 / size / (layout == SDNN_ROPE_INTERLEAVED ? 2 : 1);
   const bool whole = rope_vec(c.dtype, layout, a.pairs, c.head_dim) == wide, vec = a.window > 1 && whole;
   a.k_whole = whole && rows_aligned(k.data, k.token_stride, k.head_stride, 16 / size, c.dtype);
-  a.k_aligned = !vec || rows_aligned(k.data, k.token_stride, k.head_stride, 16 / size, c.dtype);
-  if (!vec && layout == SDNN_ROPE_INTERLEAVED) a.k_aligned = rows_aligned(k.data, k.token_stride, k.head_stride, 2, c.dtype);
+  a.k_pairs = layout == SDNN_ROPE_HALF || rows_aligned(k.data, k.token_stride, k.head_stride, 2, c.dtype);
+  a.k_aligned = vec ? a.k_whole : a.k_pairs;
   a.v_aligned = rows_aligned(v.data, v.token_stride, v.head_stride, 16 / size, c.dtype);
-  // LDS: the keys, then the values or the sums of a mean; the queries' cosines and sines
+  // LDS: the keys, then the values or the sums of a mean, then a block's keys from before the window; the queries'
+  // cosines and sines
   size_t lds = value_bytes(a.window, c.head_dim, size), sums = (size_t)c.block / kSumRows * c.head_dim * sizeof(float);
   lds = key_bytes(a.window, c.head_dim, size) + (lds > sums ? lds : sums);
+  a.before = (int32_t)((lds + 15) & ~(size_t)15);
+  a.passes = 1;
+  if (c.means && t.tokens > a.window) {
+    // (the rows may take the place that the values had, past the sums)
+    a.before = (int32_t)(key_bytes(a.window, c.head_dim, size) + ((sums + 15) & ~(size_t)15));
+    while (a.before + key_bytes(c.block / a.passes, c.head_dim, size) > 128 * 1024) a.passes *= 2;
+    const size_t with = a.before + key_bytes(c.block / a.passes, c.head_dim, size);
+    if (with > lds) lds = with;
+  }
   if (lds < (size_t)a.q.tile * a.q.pairs * sizeof(float2)) lds = (size_t)a.q.tile * a.q.pairs * sizeof(float2);
   const int64_t windows = (t.tokens + a.window - 1) / a.window + (a.window > 1);  // one more where they are shifted
   a.kv_blocks = (int32_t)(windows * c.kv_heads);

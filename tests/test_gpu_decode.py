@@ -175,6 +175,8 @@ def check_means(cache, written):
     (32, 256, 3, 256, "half", [33, 200, 2]),
     (64, 8, 1, 8, "interleaved", [300]),
     (64, 128, 8, 128, "half", [47, 700]),              # windows of several tokens to a workgroup
+    (128, 256, 2, 256, "half", [3, 260, 130]),         # blocks of more than a window, the longest keys
+    (128, 64, 1, 62, "interleaved", [30, 300]),        # pairs that no wide access holds
 ])
 def test_append(dtype, P, D, Hk, rot, layout, chunks):
     total = sum(chunks)
@@ -190,6 +192,31 @@ def test_append(dtype, P, D, Hk, rot, layout, chunks):
         at += n
     pos, seq = np.arange(total), np.zeros(total, int)
     written = check_pages(cache, table, seq, pos, k, v, freq, layout, dtype)
+    check_means(cache, written)
+
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("how", ["plain", "heads_first", "odd"])
+@pytest.mark.parametrize("P,starts,new", [(64, [11, 40, 0, 63], [150, 70, 64, 1]), (32, [5, 31, 16], [4, 6, 3]),
+                                          (128, [100, 3], [300, 260])])
+def test_append_prompts_of_several_sequences(dtype, how, P, starts, new):
+    """Prompts that begin anywhere in their blocks after an earlier call, side by side in one call:
+    means take keys from the window, from the call before it and from the page."""
+    Hk, D = 2, 128
+    S, width = len(new), max(-(-(a + n) // P) for a, n in zip(starts, new))
+    table = np.random.default_rng(4).permutation(S * width).reshape(S, width).astype(np.int32)
+    cache = make_cache(0, S * width, Hk, P, D, dtype)
+    rope, freq = sd.Rope(D), sd.rope_frequencies(D)
+    calls = [[(s, p) for s in range(S) for p in range(starts[s])],
+             [(s, starts[s] + p) for s in range(S) for p in range(new[s])]]
+    keys, values = [], []
+    for i, call in enumerate(calls):
+        k, v = randn(20 + i, (len(call), Hk, D), dtype), randn(30 + i, (len(call), Hk, D), dtype)
+        keys.append(k), values.append(v)
+        seq, pos = zip(*call)
+        cache.append(strided(k, how), strided(v, how), i32(pos), i32(seq), i32(table), rope=rope)
+    seq, pos = zip(*(calls[0] + calls[1]))
+    written = check_pages(cache, table, list(seq), list(pos), torch.cat(keys), torch.cat(values), freq, "half", dtype)
     check_means(cache, written)
 
 
