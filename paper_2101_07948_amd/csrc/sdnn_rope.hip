@@ -184,6 +184,7 @@ struct AppendArgs {
 
 constexpr int kWindow = 64;       // the most
 constexpr int kTileBytes = 32768; // the most of a window's keys
+constexpr int kCus = 256;
 constexpr int kSumRows = 8;       // keys of a block that a thread adds
 
 // The window's rotated keys [token][head_dim], its values with rows a piece longer (so that the rows of one
@@ -470,6 +471,11 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.window = 1;
   if ((int64_t)t.tokens * c.kv_heads > 4096 || t.tokens >= (int64_t)16 * t.sequences)
     a.window = kWindow * c.head_dim * size <= kTileBytes ? kWindow : kWindow / 2;
+  // Prompts that leave compute units without one take shorter windows: a window's steps follow one another, and so do
+  // its means, while what a shorter one rotates again of a block it shares is little.  (Kernel, us: windows of 64, 32
+  // and 16: 941 tokens of 3 heads of 128, blocks of 32: 26, 15, 15; 714 of 1 head, blocks of 64: 22, 20, 17; 186 of
+  // 12 heads of 192, blocks of 128: 18, 12, 9; 1000 of 8 heads of 128 in 32 bits, blocks of 128: 29, 31, 31.)
+  while (a.window > kWindow / 4 && (int64_t)t.tokens * c.kv_heads < (int64_t)kCus * a.window) a.window /= 2;
   // The keys' units are 16-byte ones where windows have many and the head divides by them.
   const int wide = 16 / size / (layout == SDNN_ROPE_INTERLEAVED ? 2 : 1);
   const bool whole = rope_vec(c.dtype, layout, a.pairs, c.head_dim) == wide, vec = a.window > 1 && whole;

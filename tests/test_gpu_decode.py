@@ -177,6 +177,7 @@ def check_means(cache, written):
     (64, 128, 8, 128, "half", [47, 700]),              # windows of several tokens to a workgroup
     (128, 256, 2, 256, "half", [3, 260, 130]),         # blocks of more than a window, the longest keys
     (128, 64, 1, 62, "interleaved", [30, 300]),        # pairs that no wide access holds
+    (64, 16, 64, 16, "half", [47, 200, 300]),          # windows of every length
 ])
 def test_append(dtype, P, D, Hk, rot, layout, chunks):
     total = sum(chunks)
