@@ -413,13 +413,6 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
 
 // ---------------------------------------------------------------- many tokens of a sequence
 
-// 16 bytes from global memory to LDS, one piece a lane: lane l's goes to `to` + 16 l (`to` is uniform over
-// the wave).
-__device__ __forceinline__ void copy_to_lds(const void* from, unsigned char* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-}
-
 // A stage of keys and values in LDS: STAGE tokens of a page, keys as rows of a head (of a power of two of
 // bytes, also where the head is shorter), values as rows of STAGE tokens.  A row's 16-byte pieces are permuted by the
 // row (piece x at x ^ swap) so that the 16 rows that a wave reads one piece of lie in different banks.

@@ -49,6 +49,13 @@ __device__ __forceinline__ void store_n(T* p, bool aligned, const T (&in)[N]) {
   }
 }
 
+// 16 bytes from global memory to LDS, one piece a lane: lane l's goes to `to` + 16 l (`to` is uniform over
+// the wave).
+__device__ __forceinline__ void copy_to_lds(const void* from, unsigned char* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
 // x and the value of the lane 16 (32) away, exchanged within the registers (gfx950's row swaps: with the same
 // value as both operands, one result holds the even rows twice and the other the odd ones).
 __device__ __forceinline__ void with_16(float x, float* u, float* v) {

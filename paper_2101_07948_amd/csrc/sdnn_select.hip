@@ -18,7 +18,8 @@ struct SelectArgs {
   int32_t kv_heads, group, head_dim, block_shift;
   int32_t blocks, sink, local;
   int32_t tile, per_token;  // tokens of a workgroup, rows of a token (up to 16: a power of two)
-  int32_t q_aligned;
+  int32_t keys, stride;     // where the keys begin in LDS; of a token
+  int32_t dtype, q_aligned;
 };
 
 // A number whose order as an unsigned integer is the order of the floats (-0 counts as 0); below 2^32 - 1, so
@@ -49,11 +50,41 @@ __device__ __forceinline__ uint2 before(uint2 n, uint2* parts, uint2* all) {
   return r;
 }
 
+// x of the lane N further on among 16.
+template <int N, typename X>
+__device__ __forceinline__ X rotated(X x) {
+  return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + N, 0xf, 0xf, false));
+}
+
+// The largest of a wave's 64 keys.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = max(x, rotated<8>(x));
+  x = max(x, rotated<4>(x));
+  x = max(x, rotated<2>(x));
+  x = max(x, rotated<1>(x));
+  const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max(p[0], p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return __builtin_amdgcn_readfirstlane(max(q[0], q[1]));
+}
+
 // The largest number that at least `want` of a wave's 64 keys reach (0 if fewer are above 0), bit by bit
-// from the top, or a smaller one that exactly `want` reach.
+// from the top, or a smaller one that exactly `want` reach.  Most often it has the exponent of the largest key or one
+// of the next below: these are tried first.
 __device__ __forceinline__ uint32_t wave_kth(uint32_t key, uint32_t want) {
-  uint32_t t = 0;
-  for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
+  constexpr uint32_t kExponent = 1u << 23;
+  uint32_t t = wave_max(key) & ~(kExponent - 1), bit = kExponent >> 1;
+  for (int i = 0;; ++i) {
+    const uint32_t n = __popcll(__ballot(key >= t));
+    if (n == want) return t;
+    if (n > want) break;
+    if (i == 4 || t == 0) {
+      t = 0, bit = 1u << 31;
+      break;
+    }
+    t -= kExponent;
+  }
+  for (; bit; bit >>= 1) {
     const uint32_t n = __popcll(__ballot(key >= (t | bit)));
     if (n >= want) t |= bit;
     if (n == want) break;
@@ -133,6 +164,7 @@ __device__ __forceinline__ void wave_choose(const uint32_t* keys, int count, uin
 }
 
 constexpr int kMaxWaves = 16;
+constexpr int kUnit = 32;
 constexpr int kMaxTile = 32;
 constexpr int kWaveKeys = 16;  // keys of a lane where a wave chooses alone: up to 1024 blocks
 
@@ -209,67 +241,83 @@ __device__ __forceinline__ void group_choose(const uint32_t* keys, int count, ui
     if (keys[i] > s || (keys[i] == s && equal++ < left)) chosen[to++] = first + i;
 }
 
-// The summaries of 64 blocks on their way to a wave's registers: block 16 k + lane % 16 of them, bytes
-// 16 (lane / 16) ... of each 64.
-template <int STEPS>
+// The summaries of UNIT blocks on their way to a wave's part of LDS: rows of PIECES times 16 bytes, whose pieces are
+// permuted by the row (piece x at x ^ swap) so that the 16 rows that a wave reads one piece of lie in different banks.
+// (Read from the summaries straight into operands, neighbouring lanes have different rows: four times the cache
+// lines an access, which took 5 of 16 us for 2048 blocks of 128 values to a token and 10 of 38 us for prompts.)
+template <int STEPS, int UNIT>
 struct Summaries {
-  i32x4 m[4][STEPS];
-  float scale[4];
-  int32_t page[4];
+  static constexpr int PIECES = STEPS * 4, ROWS = 64 / PIECES;  // of an access
+  static constexpr int kBytes = UNIT * PIECES * 16;
+  static __device__ __forceinline__ int swap(int row) { return row * PIECES / 16 & (PIECES - 1); }
+  int32_t page;  // of block `lane` of the unit; -1: missing
+  float scale;
   // (Bytes past a head's end meet zeros of the queries: any will do.  `wide`: whole 16-byte pieces.)
-  __device__ __forceinline__ void load(const SelectArgs& a, int h, int32_t entry, int r, int g, bool wide) {
-    const int32_t mine = entry < a.pages ? entry : -1;
-    const int8_t* row[4];
+  __device__ __forceinline__ void fetch(const SelectArgs& a, int h, int32_t entry, bool wide, unsigned char* to) {
+    const int lane = threadIdx.x % 64;
+    page = entry < a.pages ? entry : -1;
+    const int32_t p = max(page, 0);  // (in a missing page's place: page 0)
+    const int8_t* from[UNIT / ROWS];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      page[k] = __shfl(mine, k * 16 + r);
-      const int64_t at = (int64_t)max(page[k], 0) * a.kv_heads + h;  // (in a missing page's place: page 0)
-      row[k] = a.means + at * a.head_dim;
-      scale[k] = a.scales[at];
-    }
+    for (int i = 0; i < UNIT / ROWS; ++i)
+      from[i] = a.means + ((int64_t)__shfl(p, i * ROWS + lane / PIECES) * a.kv_heads + h) * a.head_dim;
     if (wide) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-          m[k][s] = *reinterpret_cast<const i32x4*>(row[k] + min(s * 64 + g * 16, a.head_dim - 16));
+      for (int i = 0; i < UNIT / ROWS; ++i) {
+        const int piece = (lane % PIECES) ^ swap(i * ROWS + lane / PIECES);
+        copy_to_lds(from[i] + min(piece * 16, a.head_dim - 16), to + i * 1024);
+      }
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-          const int2 lo = *reinterpret_cast<const int2*>(row[k] + min(s * 64 + g * 16, a.head_dim - 8));
-          const int2 hi = *reinterpret_cast<const int2*>(row[k] + min(s * 64 + g * 16 + 8, a.head_dim - 8));
-          m[k][s] = i32x4{lo.x, lo.y, hi.x, hi.y};
-        }
+      for (int i = 0; i < UNIT / ROWS; ++i) {
+        const int piece = (lane % PIECES) ^ swap(i * ROWS + lane / PIECES);
+        const int2 lo = *reinterpret_cast<const int2*>(from[i] + min(piece * 16, a.head_dim - 8));
+        const int2 hi = *reinterpret_cast<const int2*>(from[i] + min(piece * 16 + 8, a.head_dim - 8));
+        *reinterpret_cast<i32x4*>(to + i * 1024 + lane * 16) = i32x4{lo.x, lo.y, hi.x, hi.y};
+      }
     }
-    __builtin_amdgcn_sched_barrier(0);  // all loads under way before the first is used
+    scale = a.scales[(int64_t)p * a.kv_heads + h];
+  }
+  static __device__ __forceinline__ i32x4 piece(const unsigned char* unit, int row, int x) {
+    return *reinterpret_cast<const i32x4*>(unit + (row * PIECES + (x ^ swap(row))) * 16);
   }
 };
 
 // A query's 8-bit row in LDS: 16 bytes longer, so that the rows of one piece lie in different banks.
 constexpr int row_bytes(int steps) { return steps * 64 + 16; }
 
+// Four values of a query.
+__device__ __forceinline__ void load_values(const void* q, int64_t at, int dtype, bool aligned, float (&x)[4]) {
+  if (dtype == SDNN_F32) {
+    load_n<4>(static_cast<const float*>(q) + at, aligned, x);
+    return;
+  }
+  uint16_t v[4];
+  load_n<4>(static_cast<const uint16_t*>(q) + at, aligned, v);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    x[k] = dtype == SDNN_F16 ? (float)__builtin_bit_cast(_Float16, v[k]) : __uint_as_float((uint32_t)v[k] << 16);
+}
+
 // A workgroup chooses the blocks of one cached head for `tile` tokens.  Scores: the dot products of 16 queries
-// (the rows: a power of two of them to a token, or several tiles of rows) and 16 summaries are one matrix
+// (the rows: 2^SHIFT of them to a token, or several tiles of 16, SHIFT = 5) and 16 summaries are one matrix
 // instruction for 64 values of a head, bytes in, whole numbers out; a lane's four results are rows 4 g ...
 // 4 g + 3 of its own block, so that a group of up to four queries takes its maximum within a lane.  A wave has
-// 64 blocks under way at a time, the first of them before the queries are there.  The scores go to LDS as
+// UNIT blocks under way at a time, the first of them before the queries are there.  The scores go to LDS as
 // ordered integers.  Then, of one token, all waves search the threshold together; of several, each wave takes
 // whole tokens, whose keys stay in its registers.
-template <typename T, int STEPS>
-__global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
+template <int STEPS, int SHIFT, int UNIT>
+__global__ __launch_bounds__((SHIFT < 4 ? 256 : 1024), 4) void select_kernel(SelectArgs a) {
   extern __shared__ __align__(16) unsigned char lds[];
   __shared__ GroupLds group;
-  __shared__ Candidate few[kMaxWaves / 4][64];
   __shared__ int32_t seqs[kMaxTile], seen[kMaxTile];  // of the tile's tokens; blocks that they see
   constexpr int ROW = row_bytes(STEPS);
-  const int rows = a.tile * a.per_token;      // a multiple of 16
-  const int shift = a.per_token >= 16 ? 4 : __builtin_ctz(a.per_token);  // of a tile of rows to its tokens
+  const int rows = a.tile * a.per_token;                      // a multiple of 16
   int8_t* m8 = reinterpret_cast<int8_t*>(lds);                // [rows][ROW]
   float* top = reinterpret_cast<float*>(m8 + rows * ROW);     // [rows]: largest value of each query
   float* dead = top + rows;                                   // [rows]: 0, or -infinity where there is no query
-  uint32_t* keys = reinterpret_cast<uint32_t*>(dead + rows);  // [tile][max_blocks]
+  uint32_t* keys = reinterpret_cast<uint32_t*>(lds + a.keys); // [tile][stride]
+  Candidate* few = reinterpret_cast<Candidate*>(lds);         // [waves][64], in the queries' place afterwards
   const int threads = blockDim.x, lane = threadIdx.x % 64;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = threads / 64;
   const int h = blockIdx.x % a.kv_heads, t0 = blockIdx.x / a.kv_heads * a.tile;
@@ -286,10 +334,12 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
   const int first_last = min(t0 + a.tile, a.tokens) - 1;  // (positions ascend within a sequence)
   int ahead = max(sees(a.pos[t0], first_seq), a.seq[first_last] == first_seq ? sees(a.pos[first_last], first_seq) : 0);
   ahead = take > 0 && ahead > a.blocks ? ahead - forced : 0;
-  Summaries<STEPS> sum;
-  if (wave * 64 < ahead) {
-    const int b = wave * 64 + lane;
-    sum.load(a, h, b < ahead ? a.table[(int64_t)first_seq * a.max_blocks + a.sink + b] : -1, r, g, wide);
+  typedef Summaries<STEPS, UNIT> Unit;
+  Unit sum;
+  unsigned char* unit = lds + a.keys + a.tile * a.stride * 4 + wave * Unit::kBytes;
+  if (wave * UNIT < ahead) {
+    const int b = wave * UNIT + lane;
+    sum.fetch(a, h, lane < UNIT && b < ahead ? a.table[(int64_t)first_seq * a.max_blocks + a.sink + b] : -1, wide, unit);
   }
 
   if (threadIdx.x < 64) group.top[threadIdx.x] = 0, group.counts[threadIdx.x / 4][threadIdx.x % 4] = 0;
@@ -304,18 +354,21 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
   for (int row0 = wave * 4; row0 < rows; row0 += waves * 4) {
     const int row = row0 + g, i = row / a.per_token, gq = row % a.per_token;
     const bool live = gq < a.group && t0 + i < a.tokens;
-    const T* q = static_cast<const T*>(a.q) + (t0 + i) * a.q_token + (int64_t)(h * a.group + gq) * a.q_head;
+    const int64_t q = (t0 + i) * a.q_token + (int64_t)(h * a.group + gq) * a.q_head;
     float x[STEPS][4], m = 0.0f;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       const int d = s * 64 + r * 4;
-      T v[4] = {};
-      if (live && d < D) load_n<4>(q + d, a.q_aligned, v);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[s][k] = (float)v[k], m = fmaxf(m, fabsf(x[s][k]));
+      for (int k = 0; k < 4; ++k) x[s][k] = 0.0f;
+      if (live && d < D) load_values(a.q, q + d, a.dtype, a.q_aligned, x[s]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m = fmaxf(m, fabsf(x[s][k]));
     }
-#pragma unroll
-    for (int s = 8; s; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
+    m = fmaxf(m, rotated<8>(m));
+    m = fmaxf(m, rotated<4>(m));
+    m = fmaxf(m, rotated<2>(m));
+    m = fmaxf(m, rotated<1>(m));
     const float f = m > 0.0f ? 127.0f * (1.0f / m) : 0.0f;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
@@ -343,102 +396,122 @@ __global__ __launch_bounds__(1024) void select_kernel(SelectArgs a) {
   }
   if (!some) return;
 
-  // The first of a lane's four results of a tile of rows becomes, after the maximum over its token's rows, the score
-  // of this token, counted from the tile's first (a token's rows are 1 << shift neighbours, and lanes whose result
-  // is not a token's first leave it to the one that is); with fewer than four rows to a token others do too.
-  const bool leads = !(4 * g & ((1 << shift) - 1));
-  const int lead = 4 * g >> shift;
   for (int i0 = 0; i0 < a.tile;) {  // tokens i0 ... i1 - 1 are of one sequence
     const int32_t seq = seqs[i0];
     int i1 = i0, most = 0;
     for (; i1 < a.tile && seqs[i1] == seq; ++i1) most = max(most, seen[i1]);
     const int count = most > a.blocks ? most - forced : 0;
     const int32_t* table = a.table + (int64_t)seq * a.max_blocks + a.sink;
-    for (int b0 = wave * 64; b0 < count; b0 += waves * 64) {
-      if (!(i0 == 0 && b0 < waves * 64 && ahead >= count))
-        sum.load(a, h, b0 + lane < count ? table[b0 + lane] : -1, r, g, wide);
+    for (int b0 = wave * UNIT; b0 < count; b0 += waves * UNIT) {
+      if (!(i0 == 0 && b0 < waves * UNIT && ahead >= count))
+        sum.fetch(a, h, lane < UNIT && b0 + lane < count ? table[b0 + lane] : -1, wide, unit);
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the wave's own copies
+      const uint64_t gone = __ballot(sum.page < 0);
+      float most_yet[UNIT / 16];  // (SHIFT 5) of block 16 k + r, over the rows so far
+      for (int row0 = 0; row0 < rows; row0 += 16) {
+        i32x4 qv[STEPS];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (b0 + k * 16 >= count) break;
-        const int b = b0 + k * 16 + r;
-        float best[4];
-        for (int row0 = 0; row0 < rows; row0 += 16) {
+        for (int s = 0; s < STEPS; ++s) qv[s] = *reinterpret_cast<const i32x4*>(m8 + (row0 + r) * ROW + s * 64 + g * 16);
+        const f32x4 tq = *reinterpret_cast<const f32x4*>(top + row0 + 4 * g);
+        const f32x4 none = *reinterpret_cast<const f32x4*>(dead + row0 + 4 * g);
+        // A lane's results become, after the maximum over the rows of a token, scores of tokens first, first + 1, ...
+        // (of 8 or more rows to a token, lanes of 2 or 4 groups have the same ones, and share the
+        // blocks).  Those of blocks past the last one are written too: a token has place for whole 64.
+        const int first = SHIFT == 5 ? 0 : (row0 + 4 * g) >> SHIFT;
+        uint32_t* key = keys + first * a.stride + b0 + r;
+        uint32_t y[UNIT / 16];
+#pragma unroll
+        for (int k = 0; k < UNIT / 16; ++k) {
           i32x4 dot = {0, 0, 0, 0};
 #pragma unroll
-          for (int s = 0; s < STEPS; ++s) {
-            const i32x4 qv = *reinterpret_cast<const i32x4*>(m8 + (row0 + r) * ROW + s * 64 + g * 16);
-            dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(qv, sum.m[k][s], dot, 0, 0, 0);
-          }
-          const f32x4 tq = *reinterpret_cast<const f32x4*>(top + row0 + 4 * g);
-          const f32x4 none = *reinterpret_cast<const f32x4*>(dead + row0 + 4 * g);
-          const bool more = a.per_token > 16 && row0 > 0;  // rows of the same token
+          for (int s = 0; s < STEPS; ++s)
+            dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(qv[s], Unit::piece(unit, 16 * k + r, 4 * s + g), dot, 0, 0, 0);
+          const float scale = __shfl(sum.scale, 16 * k + r);
+          float x[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = fmaf((float)dot[i], tq[i], none[i]);  // (a product rounded once, or -infinity)
-            best[i] = more ? fmaxf(best[i], x) : x;
-          }
-          if (a.per_token > 16 && row0 + 16 < rows) continue;
-          const int first = a.per_token > 16 ? 0 : row0 >> shift;
-          const auto put = [&](int token, float x, bool is) {
-            if (is && token >= i0 && token < i1 && b < count)
-              keys[token * a.max_blocks + b] = sum.page[k] < 0 ? 0u : ordered(x * sum.scale[k]);
-          };
-          if (shift >= 2) {
-            float x = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
-            if (shift >= 3) x = max_over_16(x);
-            if (shift >= 4) x = max_over_32(x);
-            put(first + lead, x, leads);
-          } else if (shift == 1) {
-            put(first + lead, fmaxf(best[0], best[1]), true);
-            put(first + lead + 1, fmaxf(best[2], best[3]), true);
+          for (int i = 0; i < 4; ++i) x[i] = fmaf((float)dot[i], tq[i], none[i]);  // (a product rounded once, or -infinity)
+          const auto number = [&](float x) { return gone >> (16 * k + r) & 1 ? 0u : ordered(x * scale); };
+          if (SHIFT >= 2) {
+            float m = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+            if (SHIFT >= 3) m = max_over_16(m);
+            if (SHIFT >= 4) m = max_over_32(m);
+            if (SHIFT == 5) m = most_yet[k] = row0 ? fmaxf(most_yet[k], m) : m;
+            y[k] = number(m);
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) put(first + lead + i, best[i], true);
+            for (int i = 0; i < 4; i += 1 << SHIFT)
+              if (first + (i >> SHIFT) >= i0 && first + (i >> SHIFT) < i1)
+                key[(i >> SHIFT) * a.stride + 16 * k] = number(SHIFT ? fmaxf(x[i], x[i + (SHIFT ? 1 : 0)]) : x[i]);
           }
         }
+        if (SHIFT < 2 || first < i0 || first >= i1) continue;
+        if (SHIFT == 2) {
+#pragma unroll
+          for (int k = 0; k < UNIT / 16; ++k) key[16 * k] = y[k];
+          continue;
+        }
+        if (SHIFT == 5 && row0 + 16 < rows) continue;
+#pragma unroll
+        for (int k = 0; k + 1 < UNIT / 16; k += 2) {
+          const uint32_t even = y[k], odd = y[k + 1];
+          if (SHIFT == 3 || g >> 1 == k / 2) key[16 * (k + (g & 1))] = g & 1 ? odd : even;
+        }
       }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // everything read: the unit's place is free
     }
     i0 = i1;
   }
   __syncthreads();
 
-  if (a.tile == 1) {
+  if (SHIFT >= 4 && a.tile == 1) {
     group_choose(keys, seen[0] - forced, take, a.sink,
-                 a.chosen + ((int64_t)t0 * a.kv_heads + h) * a.blocks + a.sink, few[0], group);
+                 a.chosen + ((int64_t)t0 * a.kv_heads + h) * a.blocks + a.sink, few, group);
     return;
   }
   for (int i = wave; i < a.tile; i += waves) {
     if (seen[i] <= a.blocks) continue;
     const int count = seen[i] - forced;
     int32_t* chosen = a.chosen + ((int64_t)(t0 + i) * a.kv_heads + h) * a.blocks + a.sink;
-    const uint32_t* key = keys + i * a.max_blocks;
+    const uint32_t* key = keys + i * a.stride;
     if (count <= 256)
-      wave_choose<4>(key, count, take, a.sink, chosen, few[wave]);
+      wave_choose<4>(key, count, take, a.sink, chosen, few + 64 * wave);
     else if (count <= 512)
-      wave_choose<8>(key, count, take, a.sink, chosen, few[wave]);
+      wave_choose<8>(key, count, take, a.sink, chosen, few + 64 * wave);
     else
-      wave_choose<kWaveKeys>(key, count, take, a.sink, chosen, few[wave]);
+      wave_choose<kWaveKeys>(key, count, take, a.sink, chosen, few + 64 * wave);
   }
 }
 
-template <typename T, int STEPS>
-hipError_t start(const SelectArgs& a, int threads, hipStream_t stream) {
-  const size_t lds = (size_t)a.tile * (a.per_token * (row_bytes(STEPS) + 8) + (size_t)a.max_blocks * 4);
+template <int STEPS, int SHIFT>
+hipError_t start(SelectArgs a, int threads, hipStream_t stream) {
+  constexpr int UNIT = kUnit;
+  const auto kernel = select_kernel<STEPS, SHIFT, UNIT>;
+  a.keys = a.tile * a.per_token * (row_bytes(STEPS) + 8);
+  const int few = (a.tile == 1 ? 1 : threads / 64) * 64 * (int)sizeof(Candidate);
+  if (a.keys < few) a.keys = few;
+  size_t lds = a.keys + (size_t)a.tile * a.stride * sizeof(uint32_t);
+  while (threads > 64 && lds + threads / 64 * Summaries<STEPS, UNIT>::kBytes > 156 * 1024) threads /= 2;
+  lds += threads / 64 * Summaries<STEPS, UNIT>::kBytes;
   if (lds > 60000) {  // with the kernel's own arrays past what a launch gives by default
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(select_kernel<T, STEPS>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
   const unsigned grid = (unsigned)((a.tokens + a.tile - 1) / a.tile) * a.kv_heads;
-  select_kernel<T, STEPS><<<grid, threads, lds, stream>>>(a);
+  kernel<<<grid, threads, lds, stream>>>(a);
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t start_steps(const SelectArgs& a, int threads, hipStream_t stream) {
-  if (a.head_dim <= 64) return start<T, 1>(a, threads, stream);
-  if (a.head_dim <= 128) return start<T, 2>(a, threads, stream);
-  return start<T, 4>(a, threads, stream);
+template <int STEPS>
+hipError_t start_rows(const SelectArgs& a, int threads, hipStream_t stream) {
+  switch (a.per_token) {
+    case 1: return start<STEPS, 0>(a, threads, stream);
+    case 2: return start<STEPS, 1>(a, threads, stream);
+    case 4: return start<STEPS, 2>(a, threads, stream);
+    case 8: return start<STEPS, 3>(a, threads, stream);
+    case 16: return start<STEPS, 4>(a, threads, stream);
+    default: return start<STEPS, 5>(a, threads, stream);
+  }
 }
 
 }  // namespace
@@ -455,7 +528,7 @@ hipError_t launch_select(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.blocks = blocks, a.sink = sink, a.local = local;
   // A workgroup has several tokens where most of them are of one sequence and a wave can select alone: so
   // many that their rows fill two matrix operands (2048 tokens of 4 queries to a head over 512 blocks: one operand
-  // 52 us, two 41, four 54, whose LDS leaves fewer workgroups to a compute unit), their keys at most 64 KiB of
+  // 44 us, two 38, four 51, whose LDS leaves fewer workgroups to a compute unit), their keys at most 64 KiB of
   // LDS, and that the device is full.
   // Otherwise it has one token, and so many waves that each has some blocks.
   int rows = 1;
@@ -474,9 +547,11 @@ hipError_t launch_select(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   int threads = 64;
   while (threads < 1024 && threads < t.max_blocks) threads *= 2;
   if (tiles) threads = 256;
-  if (c.dtype == SDNN_F32) return start_steps<float>(a, threads, stream);
-  if (c.dtype == SDNN_F16) return start_steps<_Float16>(a, threads, stream);
-  return start_steps<__bf16>(a, threads, stream);
+  a.stride = (t.max_blocks + 63) & ~63;
+  a.dtype = c.dtype;
+  if (a.head_dim <= 64) return start_rows<1>(a, threads, stream);
+  if (a.head_dim <= 128) return start_rows<2>(a, threads, stream);
+  return start_rows<4>(a, threads, stream);
 }
 
 }  // namespace sdnn
