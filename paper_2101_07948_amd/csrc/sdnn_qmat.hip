@@ -238,6 +238,9 @@ struct Chunk {
 // instructions that make numbers of the bits.
 //   Row p of the operand is column p / 4 + 4 (p % 4) of x, so that up to four columns are in the first of a lane's
 // four results, up to eight in two; of four columns in 32 bits rows 4 t + part, and a lane adds its results.
+//   Reading the weights bounds it: 16384 x 8192 with one column in 16 bits 14.2 us, 69 MB at 4.9 TB/s, the rate of a
+// large copy.  5003 x 4099 with 13 columns: 11.4 us for 12.5 MB: each of 313 workgroups, one or two to a compute unit,
+// brings all of x through LDS.  Small ones are a launch: 768 x 3072 3.8 us.
 //   STEPS: matrix instructions (of 32 columns of W) of a group within a chunk.
 template <typename T, int STEPS, int TOKENS, bool FEATURES>
 __global__ __launch_bounds__((kWavesOf<T, TOKENS> * 64)) void qmat_kernel(QmatArgs a) {

@@ -31,7 +31,8 @@ __host__ __device__ constexpr int rest_values(int vp) { return INTERLEAVED && vp
 // A workgroup rotates all heads of `tile` tokens.  The work is moving bytes: each value is read
 // and written once.  The cosines and sines, 64-bit arithmetic, are computed once per token and pair
 // and shared by the heads through LDS.  A thread keeps one unit of a row, VP pairs or the values
-// of one access past the rotated part, and walks tokens and heads.
+// of one access past the rotated part, and walks tokens and heads.  8192 tokens of 32 heads of 128 in 16 bits,
+// half of each head rotated: 28.8 us, 134 MB at 4.66 TB/s, the rate of a large copy.  One token: 2.3 us, a launch.
 template <typename T, int VP, bool INTERLEAVED>
 __device__ __forceinline__ void rope_rows(const RopeRows& a, int block, float2* cs) {
   const int t0 = block * a.tile;
@@ -150,6 +151,8 @@ RopeRows rope_args(const sdnn_heads& x, const sdnn_heads& y, int dtype, int32_t 
   const int values = a.vec * (layout == SDNN_ROPE_INTERLEAVED ? 2 : 1);
   a.x_aligned = rows_aligned(x.data, x.token_stride, x.head_stride, values, dtype);
   a.y_aligned = rows_aligned(y.data, y.token_stride, y.head_stride, values, dtype);
+  // (8192 tokens of 32 heads of 128: 1, 2, 4 and 8 tokens to a workgroup 29.3, 29.1, 28.9 and 39.1 us; few tokens
+  // fill the device only one by one)
   a.tile = tokens >= 2048 ? 4 : 1;
   return a;
 }
@@ -340,6 +343,10 @@ __device__ void block_mean(const AppendArgs& a, AppendLds& l, const T* tile, T* 
 // keys rotated into an LDS tile and written as rows, values turned through LDS so that the tokens of a page
 // lie side by side, and the mean of each block that the window fills; the others rotate queries.  One launch, no
 // workgroup waits for another.
+//   4093 tokens of 32 + 8 heads of 128 in 16 bits: 35 us, 101 MB at 2.9 TB/s: the windows' steps (read, rotate, turn,
+// add) follow one another in a workgroup, 4 to a compute unit (8192 tokens: 64 us, without means 52).  One token
+// each of 64 sequences: 8.9 us, latency (positions, then the page, then 64-bit cosines, then the block's keys where
+// a mean is due).
 //   VP: pairs (and values past the rotated part) of a thread's unit, as in rope_rows.  For single tokens 1: a
 // thread's cosines and sines are then all that it waits for.
 template <typename T, bool INTERLEAVED, int VP>
