@@ -1,4 +1,7 @@
 // Attention over the chosen blocks of the cache.
+#include <algorithm>
+#include <cmath>
+
 #include "sdnn_decode_device.h"
 
 namespace sdnn {
@@ -225,13 +228,19 @@ __device__ __forceinline__ void attend_step(float scale2, float (&s)[Step<T>::kT
     Step<T>::template accumulate<false, CHUNKS>(vv, s, g, stored, st.o);
 }
 
+// Waves of a SIMD that the registers of attend_kernel leave room for, and so its workgroups at work at once on a compute
+// unit, for heads of up to 16 * tiles values.  (For the compiler a bound: without one it takes registers of both kinds
+// and leaves room for one wave less.  3 waves fit for heads of 128 in 16 bits too, but read worse: 64 tokens of 8 heads
+// over 32 blocks of 64 tokens, 537 MB, 107 us with 3 and 95 with 2.)
+constexpr int attend_waves(int tiles) { return tiles <= 4 ? 4 : tiles <= 6 ? 3 : tiles <= 12 ? 2 : 1; }
+
 // A workgroup handles one token, cached head, tile of up to 16 of its queries and share of its
 // blocks; its waves take blocks in turn and join their states through LDS.  Reading keys and values
 // bounds it: each page is read once for the tile of queries that shares it.  32 tokens of 12 heads of 64 in 32 bits
 // over up to 2048 tokens each: 55 us, 244 MB at 4.4 TB/s.  One token of 8 cached heads over 64 blocks of 64 tokens:
 // 8.3 us for 17 MB, latency: list, page, keys and values, then two joins.
 template <typename T, int CHUNKS>
-__global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kWaves * 64, attend_waves(CHUNKS * Step<T>::kPiece / 4)) void attend_kernel(AttendArgs a) {
   constexpr int PIECE = Step<T>::kPiece;
   constexpr int TILES = CHUNKS * PIECE / 4;  // of 16 values of a head
   __shared__ float sums[2][kRows][TILES * 16 + 4];
@@ -254,20 +263,10 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
   const int n = filler ? 0 : a.chosen ? a.blocks : min(own + 1, a.max_blocks);
   const int32_t* chosen = a.chosen ? a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks : nullptr;
   const int32_t* table = a.table + (int64_t)seq * a.max_blocks;
-  // Steps of all blocks, dealt to the waves of all shares in turn.  The block of the next step but one and the
-  // page of the next are looked up (by scalar loads) while this one's keys and values arrive; those are all
-  // asked for before the first product (left to itself the compiler takes them one by one, to save registers).
+  // Steps of all blocks, dealt to the waves of all shares in turn.  A lane looks up the block and the page of one of the
+  // wave's next 64 steps, and those that hold something are taken one after the other.
   constexpr int N = Step<T>::kTokens;
-  const int per_block = a.block / N, deal = a.splits * kWaves, last = n * per_block;
-  const auto block_of = [&](int u) {
-    if (u >= last) return -1;
-    const int id = chosen ? chosen[u / per_block] : u / per_block;
-    return id > own || id >= a.max_blocks ? -1 : id;
-  };
-  const auto page_of = [&](int id) { return id < 0 ? -1 : table[id]; };
-  int u = split * kWaves + wave;
-  int id = block_of(u), next_id = block_of(u + deal);
-  int page = page_of(id);
+  const int shift = __builtin_ctz(a.block / N), deal = a.splits * kWaves, last = n << shift;
   typename Step<T>::Piece q[CHUNKS];
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
@@ -282,13 +281,22 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
 #pragma unroll
   for (int c = 0; c < TILES; ++c) st.o[c] = f32x4{0, 0, 0, 0};
   st.m = -INFINITY, st.l = 0.0f;
-  for (; u < last; u += deal) {
-    const int after = block_of(u + 2 * deal), next_page = page_of(next_id);
-    const int t0 = u % per_block * N;
-    const int seen = p - id * a.block + 1 - t0;
-    if (page >= 0 && page < a.pages && seen > 0) {
+  for (int first_step = split * kWaves + wave; first_step < last; first_step += 64 * deal) {
+    const int mine = first_step + lane * deal;
+    int id = -1, page_mine = -1;
+    if (lane < (last - first_step + deal - 1) / deal) id = chosen ? chosen[mine >> shift] : mine >> shift;
+    const auto seen_of = [&](int id, int t0) { return p - id * a.block + 1 - t0; };
+    const auto token_of = [&](int u) { return (u & ((1 << shift) - 1)) * N; };
+    if (id >= 0 && id <= own && id < a.max_blocks && seen_of(id, token_of(mine)) > 0) page_mine = table[id];
+    uint64_t todo = __ballot(page_mine >= 0 && page_mine < a.pages);
+    for (; todo; todo &= todo - 1) {
+      const int j = __builtin_ctzll(todo);
+      const int page = __builtin_amdgcn_readlane(page_mine, j), t0 = token_of(first_step + j * deal);
+      const int seen = seen_of(__builtin_amdgcn_readlane(id, j), t0);
       const int64_t at = ((int64_t)page * a.kv_heads + h) * a.block * D;
       const T* v = static_cast<const T*>(a.v_pages) + at + t0;
+      // all keys and values are asked for before the first product (left to itself the compiler takes them one by one,
+      // to save registers)
       typename Step<T>::Piece kk[TILES], vv[TILES];
       Step<T>::template load_keys<CHUNKS>(static_cast<const T*>(a.k_pages) + at + t0 * D, D, r, g, kk);
       // (the keys and values of a long head are more than the registers of two waves hold beside each other)
@@ -303,7 +311,6 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a) {
       }
       attend_step<false, T, CHUNKS, TILES>(a.scale2, s, [&](int i) { return vv[i]; }, seen, seen, g, st);
     }
-    id = next_id, next_id = after, page = next_page;
   }
 
   // join the waves: 2 and 3 into 0 and 1, then 1 into 0
@@ -703,7 +710,9 @@ namespace {
 // be faster.  attend_kernel reads every token's blocks from L2, at about 8 TB/s (16384 heads of 16 blocks of 32 KiB:
 // 994 us; 8760 of 3 of 128 KiB: 683).  attend_tiles takes its workgroups' unions of blocks, 512 workgroups at a
 // time, at about 3 us for 32 KiB (38 of them: 145 us; four times that in 32 bits, whose matrix instructions take
-// as much longer); how large a union is depends on the lists, three of them are taken for it.
+// as much longer); how large a union is depends on the lists: between three of them, where neighbours choose alike,
+// and what lists that have nothing in common cover (107 tokens of 4 of 468 blocks of 4 KiB, 12 heads: 280 blocks,
+// 74 us; one by one 20), whose geometric mean is taken.
 int tile_tokens(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads,
                 int32_t chosen) {
   const int group = heads / c.kv_heads, head_tiles = (group + kRows - 1) / kRows;
@@ -713,7 +722,9 @@ int tile_tokens(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, in
   if (max_blocks > 1 << 20 || tokens < (int64_t)16 * sequences) return 0;
   const double page = 2.0 * c.block * c.head_dim * dtype_bytes(c.dtype);
   const int each = chosen > 0 && chosen < max_blocks ? chosen : max_blocks;
-  const int all = chosen > 0 && chosen < max_blocks / 3 ? 3 * chosen : max_blocks;
+  const double few = chosen > 0 && chosen < max_blocks / 3 ? 3.0 * chosen : max_blocks;
+  const double many = max_blocks * (1.0 - std::pow(1.0 - (double)each / max_blocks, std::min(tokens, tile * kTileWaves)));
+  const double all = few < many ? std::sqrt(few * many) : few;
   const double groups = (double)((tokens + tile * kTileWaves - 1) / (tile * kTileWaves)) * c.kv_heads * head_tiles;
   const double one_by_one = (double)tokens * c.kv_heads * head_tiles * each * page / 8e6;
   const double tiled = (groups > 512 ? groups / 512 : 1.0) * all * (page / 32768) * (c.dtype == SDNN_F32 ? 12 : 3);
@@ -721,14 +732,19 @@ int tile_tokens(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, in
 }
 }  // namespace
 
-// Shares of a token's blocks: so many that about 1024 workgroups (4 for each compute unit) are at
-// work, each wave with a step of its own at least; at most 64 (the lanes of attend_join).
+// Shares of a token's blocks: so many that about 1024 workgroups (4 for each compute unit) are at work, so that those of
+// long sequences have company to the end; but where a wave would have fewer than 4 steps, no more than are at work at
+// once, since another round of workgroups costs more than it shares out (732 tokens of a head of 192 over 4 blocks of
+// 128: 2 shares 53 us and the join, 1 share 31; 22 tokens of 2 heads over lists of 64 blocks that are nearly empty: 24
+// shares 24 us, 11 shares 8).  A wave has a step of its own at least, and there are at most 64 shares (the lanes of
+// attend_join).
 int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
   const int64_t units = (int64_t)tokens * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
   if (units == 0) return 1;
   const int step = c.dtype == SDNN_F32 ? 16 : 32;
-  const int64_t steps = (int64_t)blocks * (c.block / step);
-  const int64_t wanted = (1024 + units - 1) / units, most = (steps + kWaves - 1) / kWaves;
+  const int64_t steps = (int64_t)blocks * (c.block / step), most = (steps + kWaves - 1) / kWaves;
+  int64_t wanted = (1024 + units - 1) / units;
+  if (steps < 4 * kWaves * wanted) wanted = 256 * attend_waves((c.head_dim + 15) / 16) / units;
   const int64_t s = wanted < most ? wanted : most;
   return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
