@@ -188,6 +188,20 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return u + v;
 }
 
+// A share's part of a query: the sums, then for all parts their reference and total.
+template <int TILES>
+__device__ __forceinline__ void store_part(const AttendArgs& a, int split, int t, int64_t head, int g, const State<TILES>& st,
+                                           float l) {
+  const int64_t row = ((int64_t)split * a.tokens + t) * a.heads + head;
+#pragma unroll
+  for (int c = 0; c < TILES; ++c)
+    if (c * 16 + 4 * g < a.head_dim) *reinterpret_cast<f32x4*>(a.part + row * a.head_dim + c * 16 + 4 * g) = st.o[c];
+  if (g == 0) {
+    float* ml = a.part + (int64_t)a.splits * a.tokens * a.heads * a.head_dim + row * 2;
+    ml[0] = st.m, ml[1] = l;
+  }
+}
+
 // One step, its scores s given: tokens [0, seen) of its are within the sight of this lane's query, tokens from `stored` on may
 // hold anything.  EMPTY: queries may see nothing here (seen <= 0), or have seen nothing yet (m = -infinity).
 //   m is a reference near the running maximum rather than the maximum: it moves only where a score is over
@@ -341,14 +355,8 @@ __global__ __launch_bounds__(kWaves * 64, attend_waves(CHUNKS * Step<T>::kPiece 
   }
   if (wave != 0 || r >= rows) return;
   if (a.splits > 1) {
-    const int64_t row = ((int64_t)split * a.tokens + t) * a.heads + head;
-#pragma unroll
-    for (int c = 0; c < TILES; ++c)
-      if (c * 16 + 4 * g < D) *reinterpret_cast<f32x4*>(a.part + row * D + c * 16 + 4 * g) = st.o[c];
-    if (g == 0) {
-      float* ml = a.part + (int64_t)a.splits * a.tokens * a.heads * D + row * 2;
-      ml[0] = m, ml[1] = l;
-    }
+    st.m = m;
+    store_part(a, split, t, head, g, st, l);
     return;
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
@@ -418,6 +426,44 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
     if (d < D) y[d] = (T)((((o[i] + sums[0][d]) + sums[1][d]) + sums[2][d]) * inv);
   }
   if (lane == 0 && a.lse) a.lse[row] = l > 0.0f ? (top + __log2f(l)) * 0.693147181f : -INFINITY;
+}
+
+// The same for at most kFewParts parts: a thread has four values of a row and loads all that they are made of at once.
+constexpr int kFewParts = 8;
+template <typename T>
+__global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
+  const int D = a.head_dim, units = D / 4;
+  const int64_t rows = (int64_t)a.tokens * a.heads, at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / units;
+  if (row >= rows) return;
+  const int d = (int)(at - row * units) * 4;
+  const float* ml = a.part + a.splits * rows * D;
+  float m[kFewParts], l[kFewParts];
+  f32x4 x[kFewParts];
+#pragma unroll
+  for (int s = 0; s < kFewParts; ++s) {  // (past the last part: that again, with factor 0)
+    const int64_t part = min(s, a.splits - 1) * rows + row;
+    x[s] = *reinterpret_cast<const f32x4*>(a.part + part * D + d);
+    m[s] = ml[part * 2], l[s] = ml[part * 2 + 1];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  float top = m[0];
+#pragma unroll
+  for (int s = 1; s < kFewParts; ++s) top = fmaxf(top, m[s]);
+  f32x4 o = {0, 0, 0, 0};
+  float sum = 0.0f;
+#pragma unroll
+  for (int s = 0; s < kFewParts; ++s) {
+    const float f = s < a.splits && m[s] > -INFINITY ? __builtin_amdgcn_exp2f(m[s] - top) : 0.0f;
+    sum = fmaf(l[s], f, sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(x[s][i], f, o[i]);
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  T y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (T)(o[i] * inv);
+  store_n<4>(static_cast<T*>(a.o) + row / a.heads * a.o_token + row % a.heads * a.o_head + d, a.o_aligned, y);
+  if (d == 0 && a.lse) a.lse[row] = sum > 0.0f ? (top + __log2f(sum)) * 0.693147181f : -INFINITY;
 }
 
 // ---------------------------------------------------------------- many tokens of a sequence
@@ -491,9 +537,18 @@ __device__ __forceinline__ typename Step<T>::Piece value_piece(const unsigned ch
 // it, loaded ahead so that no step waits for a list.
 struct Cursor {
   int32_t t, seq, n, j, own;
+  int32_t share;  // blocks share, share + splits, ... are this workgroup's (splits: a power of two)
   int32_t id, page, next_id, next_page, after;
-  __device__ __forceinline__ int32_t block(const AttendArgs& a, int h, int i) const {
-    return i >= n ? -1 : a.chosen ? a.chosen[((int64_t)t * a.kv_heads + h) * a.blocks + i] : i;
+  // The next entry of the list that is this share's; -1 past its end.
+  __device__ __forceinline__ int32_t following(const AttendArgs& a, int h) {
+    if (!a.chosen) {
+      const int32_t b = j++ * a.splits + share;
+      return b < n ? b : -1;
+    }
+    const int32_t* list = a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks;
+    int32_t b = -1;
+    while (j < n && (b = list[j++]) >= 0 && (b & (a.splits - 1)) != share) b = -1;
+    return b;
   }
   __device__ __forceinline__ bool valid(const AttendArgs& a, int32_t b) const {
     return b >= 0 && b <= own && b < a.max_blocks;
@@ -502,13 +557,14 @@ struct Cursor {
     return valid(a, b) ? a.table[(int64_t)seq * a.max_blocks + b] : -1;
   }
   __device__ __forceinline__ void start(const AttendArgs& a, int h) {
-    id = block(a, h, 0), next_id = block(a, h, 1), after = block(a, h, 2), j = 2;
+    j = 0;
+    id = following(a, h), next_id = following(a, h), after = following(a, h);
     page = page_of(a, id), next_page = page_of(a, next_id);
   }
   __device__ __forceinline__ void advance(const AttendArgs& a, int h) {
     id = next_id, page = next_page;
     next_id = after, next_page = page_of(a, after);
-    after = block(a, h, ++j);
+    after = following(a, h);
   }
 };
 
@@ -535,6 +591,8 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   int b = blockIdx.x;
   const int h = b % a.kv_heads;
   b /= a.kv_heads;
+  const int split = b % a.splits;
+  b /= a.splits;
   const int first = b % a.head_tiles * kRows;
   const int t0 = b / a.head_tiles * (a.tile_tokens * WAVES);
   const int rows = min(kRows, a.group - first);     // queries of a token
@@ -576,7 +634,7 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
                       (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
   const bool filler = p < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
   Cursor at;
-  at.t = t, at.seq = seq, at.own = p / a.block;
+  at.t = t, at.seq = seq, at.own = p / a.block, at.share = split;
   at.n = filler ? 0 : a.chosen ? a.blocks : min(at.own + 1, a.max_blocks);
   at.start(a, h);
   const auto key = [&] { return at.valid(a, at.id) ? run << 20 | at.id : END; };
@@ -658,6 +716,10 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
 
   const float l = over_groups_sum(st.l);
   if (!row) return;
+  if (a.splits > 1) {
+    store_part(a, split, t, head, g, st, l);
+    return;
+  }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   T* o = static_cast<T*>(a.o) + t * a.o_token + head * a.o_head;
 #pragma unroll
@@ -673,6 +735,16 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
     a.lse[(int64_t)t * a.heads + head] = l > 0.0f ? (st.m + __log2f(l)) * 0.693147181f : -INFINITY;
 }
 
+template <typename T>
+hipError_t join(const AttendArgs& a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.tokens * a.heads;
+  if (a.splits > 1 && a.splits <= kFewParts)
+    attend_join_few<T><<<(unsigned)((rows * (a.head_dim / 4) + 255) / 256), 256, 0, stream>>>(a);
+  else if (a.splits > 1)
+    attend_join<T><<<(unsigned)rows, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
 template <typename T, int CHUNKS>
 hipError_t start(const AttendArgs& a, hipStream_t stream) {
   if (a.tile_tokens > 0) {
@@ -680,15 +752,13 @@ hipError_t start(const AttendArgs& a, hipStream_t stream) {
     constexpr int STAGE = LONG <= 256 ? 64 : 16384 / LONG;
     const int64_t groups = (a.tokens + a.tile_tokens * kTileWaves - 1) / (a.tile_tokens * kTileWaves);
     attend_tiles<T, CHUNKS, STAGE, kTileWaves>
-        <<<(unsigned)(groups * a.head_tiles * a.kv_heads), kTileWaves * 64, 0, stream>>>(a);
-    return hipGetLastError();
+        <<<(unsigned)(groups * a.head_tiles * a.splits * a.kv_heads), kTileWaves * 64, 0, stream>>>(a);
+  } else {
+    const unsigned grid = (unsigned)((int64_t)a.tokens * a.head_tiles * a.splits * a.kv_heads);
+    attend_kernel<T, CHUNKS><<<grid, kWaves * 64, 0, stream>>>(a);
   }
-  const unsigned grid = (unsigned)((int64_t)a.tokens * a.head_tiles * a.splits * a.kv_heads);
-  attend_kernel<T, CHUNKS><<<grid, kWaves * 64, 0, stream>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  attend_join<T><<<(unsigned)((int64_t)a.tokens * a.heads), 256, 0, stream>>>(a);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : join<T>(a, stream);
 }
 
 // Pieces of a lane: a head of up to 64, 96, 128, 192 or 256 values.
@@ -705,30 +775,61 @@ hipError_t start_dim(const AttendArgs& a, hipStream_t stream) {
 }  // namespace
 
 namespace {
-// Tokens of a wave's tile in attend_tiles (a token's queries take a power of two of its 16 rows), or 0
-// where attend_kernel serves the call: where few tokens of a sequence are neighbours, and where it is estimated to
-// be faster.  attend_kernel reads every token's blocks from L2, at about 8 TB/s (16384 heads of 16 blocks of 32 KiB:
-// 994 us; 8760 of 3 of 128 KiB: 683).  attend_tiles takes its workgroups' unions of blocks, 512 workgroups at a
-// time, at about 3 us for 32 KiB (38 of them: 145 us; four times that in 32 bits, whose matrix instructions take
-// as much longer); how large a union is depends on the lists: between three of them, where neighbours choose alike,
-// and what lists that have nothing in common cover (107 tokens of 4 of 468 blocks of 4 KiB, 12 heads: 280 blocks,
-// 74 us; one by one 20), whose geometric mean is taken.
-int tile_tokens(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads,
-                int32_t chosen) {
-  const int group = heads / c.kv_heads, head_tiles = (group + kRows - 1) / kRows;
+// How attend_tiles takes a call: tokens of a wave's tile (a token's queries take a power of two of its 16 rows), and
+// shares of the blocks; tokens 0: attend_kernel does.
+struct Tiles {
+  int tokens, splits;
+};
+int tile_of(const sdnn_block_cache& c, int32_t heads) {
   int rows = 1;
-  while (rows < group && rows < kRows) rows *= 2;
-  const int tile = kRows / rows;
-  if (max_blocks > 1 << 20 || tokens < (int64_t)16 * sequences) return 0;
+  while (rows < heads / c.kv_heads && rows < kRows) rows *= 2;
+  return kRows / rows;
+}
+int64_t tile_groups(const sdnn_block_cache& c, int32_t tokens, int32_t heads) {
+  const int each = tile_of(c, heads) * kTileWaves;
+  return (int64_t)((tokens + each - 1) / each) * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
+}
+constexpr int64_t kTileRoom = 512;  // workgroups at work at once
+// The most shares that a call of so many tokens is split into.
+int tile_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads) {
+  const int64_t groups = tile_groups(c, tokens, heads);
+  int s = 1;
+  while (s < kFewParts && tokens >= 16 && groups * 2 * s <= kTileRoom) s *= 2;
+  return s;
+}
+
+// attend_tiles serves a call where many tokens of a sequence are neighbours and it is estimated to be faster.
+// attend_kernel reads every token's blocks from L2, at about 8 TB/s (16384 heads of 16 blocks of 32 KiB:
+// 994 us; 8760 of 3 of 128 KiB: 683).  attend_tiles takes its workgroups' unions of blocks, 512 workgroups at a
+// time, two to a compute unit, at about 3.7 us for 32 KiB, or 2.2 where they have a unit each (38 and 133 of them: 142 and
+// 288 us; the matrix instructions of 32 bits take four times as long).  How large a union is depends on the lists:
+// between three of them, where neighbours choose alike, and what lists that have nothing in common cover (107 tokens of
+// 4 of 468 blocks of 4 KiB, 12 heads: 280 blocks, 74 us; one by one 20), whose geometric mean is taken.  Where few
+// workgroups leave compute units idle the blocks are shared out, and the parts joined at the rate of a copy (512 tokens
+// at the end of 8512, 8 heads of 128: 1 share 288 us, 4 shares 123 and 8 to join; 900 tokens of a sequence's first 900,
+// whose longest lists have 15 blocks: 41, and 2 shares 33 and 11 to join).
+Tiles tiles_of(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads,
+               int32_t chosen) {
+  if (max_blocks > 1 << 20 || tokens < (int64_t)16 * sequences) return {0, 1};
+  const int tile = tile_of(c, heads), head_tiles = (heads / c.kv_heads + kRows - 1) / kRows;
   const double page = 2.0 * c.block * c.head_dim * dtype_bytes(c.dtype);
   const int each = chosen > 0 && chosen < max_blocks ? chosen : max_blocks;
   const double few = chosen > 0 && chosen < max_blocks / 3 ? 3.0 * chosen : max_blocks;
   const double many = max_blocks * (1.0 - std::pow(1.0 - (double)each / max_blocks, std::min(tokens, tile * kTileWaves)));
   const double all = few < many ? std::sqrt(few * many) : few;
-  const double groups = (double)((tokens + tile * kTileWaves - 1) / (tile * kTileWaves)) * c.kv_heads * head_tiles;
+  const double groups = (double)tile_groups(c, tokens, heads);
   const double one_by_one = (double)tokens * c.kv_heads * head_tiles * each * page / 8e6;
-  const double tiled = (groups > 512 ? groups / 512 : 1.0) * all * (page / 32768) * (c.dtype == SDNN_F32 ? 12 : 3);
-  return tiled < one_by_one ? tile : 0;
+  const double parts = 8.0 * tokens * heads * (c.head_dim + 2) / 4e6;
+  const auto tiled_in = [&](int shares) {
+    const double at_once = std::min(std::max(groups * shares / 256, 1.0), 2.0), rounds = std::max(groups * shares / kTileRoom, 1.0);
+    const double block = page / 32768 * (0.7 + 1.5 * at_once * (c.dtype == SDNN_F32 ? 4 : 1));
+    return rounds * all / shares * block + (shares > 1 ? shares * parts + 5 : 0.0);
+  };
+  int best = 1;
+  for (int s = 2; s <= tile_splits(c, tokens, heads); s *= 2)
+    if (tiled_in(s) < tiled_in(best)) best = s;
+  const double tiled = tiled_in(best);
+  return tiled < one_by_one ? Tiles{tile, best} : Tiles{0, 1};
 }
 }  // namespace
 
@@ -750,7 +851,7 @@ int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int3
 }
 
 int64_t attend_floats(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
-  const int s = attend_splits(c, tokens, heads, blocks);
+  const int s = std::max(attend_splits(c, tokens, heads, blocks), tile_splits(c, tokens, heads));
   return s > 1 ? (int64_t)s * tokens * heads * (c.head_dim + 2) : 0;
 }
 
@@ -767,8 +868,9 @@ hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.heads = q.heads, a.kv_heads = c.kv_heads, a.group = q.heads / c.kv_heads;
   a.head_tiles = (a.group + kRows - 1) / kRows;
   a.head_dim = c.head_dim, a.block = c.block;
-  a.tile_tokens = tile_tokens(c, t.tokens, t.sequences, t.max_blocks, q.heads, chosen ? blocks : 0);
-  a.blocks = blocks, a.splits = a.tile_tokens ? 1 : attend_splits(c, t.tokens, q.heads, blocks);
+  const Tiles tiles = tiles_of(c, t.tokens, t.sequences, t.max_blocks, q.heads, chosen ? blocks : 0);
+  a.tile_tokens = tiles.tokens;
+  a.blocks = blocks, a.splits = a.tile_tokens ? tiles.splits : attend_splits(c, t.tokens, q.heads, blocks);
   // (a scale of 0 makes all scores equal: so does one that is too small to part them)
   a.scale2 = fmaxf(fabsf(scale), 1e-30f) * 1.44269504f;
   a.negate = scale < 0.0f;

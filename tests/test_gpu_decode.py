@@ -501,6 +501,31 @@ def test_attend_many_tokens(dtype, Hq, Hk, D, P, tokens, blocks, how):
 
 
 @pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("Hq,Hk,D,P,lens,new,blocks", [
+    (8, 8, 64, 64, [6000], 120, 20),
+    (8, 2, 64, 64, [3000], 90, 12),
+    (4, 4, 128, 32, [3000, 2500], 70, 24),
+    (2, 2, 256, 128, [6000], 120, 15),
+])
+def test_attend_end_of_a_long_context(dtype, Hq, Hk, D, P, lens, new, blocks):
+    """A chunk's few tokens over many blocks, which are shared out over workgroups and joined: every block,
+    chosen ones, lists that are empty or end early, a share that sees nothing, fillers, a missing page."""
+    cache, table = filled(11, len(lens), lens, Hk, P, D, dtype)
+    seq, pos = [], []
+    for s, n in enumerate(lens):
+        seq += [s] * new + [99]
+        pos += list(range(n - new, n)) + [n - 1]
+    q = randn(12, (len(pos), Hq, D), dtype)
+    assert cache.workspace_floats(len(pos), Hq, table.shape[1]) > 0
+    check_attend(cache, table, q, pos, seq, oracle=od.attend_many)
+    chosen = random_choice(5, pos, Hk, blocks, P)
+    chosen[:9] = -1
+    chosen[9:12, :, 1:] = -1
+    table[0, 2] = -1
+    check_attend(cache, table, q, pos, seq, chosen, how="padded", oracle=od.attend_many)
+
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
 def test_attend_large_scores(dtype):
     """Scores that differ by hundreds: the running maximum moves from block to block."""
     P, D = 32, 64
