@@ -546,6 +546,7 @@ struct Cursor {
       return b < n ? b : -1;
     }
     const int32_t* list = a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks;
+    if (a.splits == 1) return j < n ? list[j++] : -1;
     int32_t b = -1;
     while (j < n && (b = list[j++]) >= 0 && (b & (a.splits - 1)) != share) b = -1;
     return b;
