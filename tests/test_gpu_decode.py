@@ -559,6 +559,34 @@ def test_attend_far_pages():
     assert (out[0].double().cpu() - want).abs().max() <= 2.0 ** -8 * want.abs().max() + 1e-4
 
 
+def test_far_pages_give_the_same():
+    """Summaries, choices and prompts' attention on pages past 2^31 elements, and on the first ones."""
+    P, D, Hk, T, blocks = 128, 128, 8, 384 + 70, 3
+    pages = 2 ** 31 // (P * D * Hk) + 5
+    far = sd.BlockCache(torch.empty((pages, Hk, P, D), dtype=torch.float16, device=DEV),
+                        torch.empty((pages, Hk, D, P), dtype=torch.float16, device=DEV),
+                        torch.zeros((pages, Hk, D), dtype=torch.int8, device=DEV), torch.zeros((pages, Hk), device=DEV))
+    near = make_cache(0, 4, Hk, P, D, torch.float16)
+    near.means.zero_(), near.mean_scales.zero_()
+    order = [2, 0, 3, 1]
+    k, v, q = (randn(i, (T, Hk, D), torch.float16) for i in (1, 2, 3))
+    got = []
+    for cache, table in ((near, i32([order])), (far, i32([[pages - 4 + i for i in order]]))):
+        cache.append(k, v, i32(range(T)), i32([0] * T), table, rope=sd.Rope(D))
+        tokens = 70
+        pos, seq = i32(range(T - tokens, T)), i32([0] * tokens)
+        chosen = torch.empty((tokens, Hk, blocks), dtype=torch.int32, device=DEV)
+        cache.select(q[:tokens], pos, seq, table, chosen)
+        out, all_blocks = torch.empty_like(q[:tokens]), torch.empty_like(q[:tokens])
+        cache.attend(q[:tokens], out, pos, seq, table, chosen)
+        cache.attend(q[:tokens], all_blocks, pos, seq, table)
+        rows = table[0].long()
+        got.append([cache.means[rows], cache.mean_scales[rows], chosen, out, all_blocks])
+    assert (got[0][1][:3] > 0).all() and (got[0][2] >= 0).any()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 def test_attend_another_stream_and_own_workspace():
     cache, table = filled(7, 1, [3000], 2, 64, 128, torch.bfloat16)
     q = randn(5, (1, 8, 128), torch.bfloat16)
