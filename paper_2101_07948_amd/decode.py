@@ -19,7 +19,7 @@ import struct
 
 import numpy as np
 
-from . import EPI, SdnnError, _stream_handle, _torch_mod, lib
+from . import EPI, SdnnError, _torch_mod, lib
 
 LAYOUTS = {"half": 0, "interleaved": 1}
 
@@ -29,14 +29,21 @@ _TOKENS = struct.Struct("@PPPiiii")
 _HEADS = struct.Struct("@Pqqii")
 _ROTATION = struct.Struct("@Piid")
 
-_bound = None
+# Set with the library, at the first call: its handle, the types' codes, torch's types and accessors (each call of
+# these operators is a few microseconds: looked up by name they would be a good part of it).
+_bound = _codes = _INT32 = _FLOAT32 = _raw_stream = _device = None
 
 
 def _lib():
     """libsdnn.so with the argument types of these entry points set."""
-    global _bound
+    global _bound, _codes, _INT32, _FLOAT32, _raw_stream, _device
     if _bound is None:
-        L = lib()
+        L, torch = lib(), _torch_mod()
+        _codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        _INT32, _FLOAT32 = torch.int32, torch.float32
+        _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+        if hasattr(torch._C, "_cuda_getDevice"):  # what current_device calls once the GPU is in use
+            _device = torch._C._cuda_getDevice
         p, s, i32, i64 = ctypes.c_void_p, ctypes.c_char_p, ctypes.c_int32, ctypes.c_int64
         L.sdnn_rope.argtypes = [s, s, i32, i32, i32, p, s, i32, p]
         L.sdnn_cache_append.argtypes = [s, s, s, s, s, s, s, p]
@@ -55,15 +62,13 @@ def _lib():
     return _bound
 
 
-_codes = None
+def _stream_handle(stream) -> int:
+    """The raw hipStream_t of `stream` (default: the current stream)."""
+    return _raw_stream(_device()) if stream is None else stream.cuda_stream
 
 
 def _dtype_code(dtype, name: str) -> int:
     """sdnn_dtype of a torch dtype."""
-    global _codes
-    if _codes is None:
-        torch = _torch_mod()
-        _codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
     code = _codes.get(dtype)
     if code is None:
         raise TypeError(f"{name} must be float32, float16 or bfloat16, not {dtype}")
@@ -169,14 +174,15 @@ class Rope:
     def apply(self, x, y, pos, inverse: bool = False, stream=None):
         """y = x (tokens, heads, head_dim) rotated to the positions pos (tokens, int32); by the
         negative angles with inverse (which is also the gradient).  y may be x."""
-        torch = _torch_mod()
-        if x.dim() != 3:
+        L, d, shape = _lib(), x.dtype, x.shape
+        if len(shape) != 3:
             raise ValueError("x must be 3-d (tokens, heads, head_dim)")
-        T, H, D = x.shape
-        px, py = _rows(x, "x", x.dtype, T, H, D), _rows(y, "y", x.dtype, T, H, D)
-        ppos = _dense(pos, "pos", torch.int32, (T,))
-        _check(_lib().sdnn_rope(px, py, _dtype_code(x.dtype, "x"), T, D, ppos, self._packed,
-                                1 if inverse else 0, _stream_handle(stream)), "sdnn_rope")
+        T, H, D = shape
+        code = L.sdnn_rope(_rows(x, "x", d, T, H, D), _rows(y, "y", d, T, H, D), _dtype_code(d, "x"), T, D,
+                           _dense(pos, "pos", _INT32, (T,)), self._packed, 1 if inverse else 0,
+                           _stream_handle(stream))
+        if code:
+            raise SdnnError(code, "sdnn_rope")
         return y
 
 
@@ -232,11 +238,10 @@ class BlockCache:
         return s
 
     def _tokens(self, pos, seq, table) -> bytes:
-        torch = _torch_mod()
         T = pos.shape[0]
         S, blocks = table.shape
-        return _TOKENS.pack(_dense(pos, "pos", torch.int32, (T,)), _dense(seq, "seq", torch.int32, (T,)),
-                            _dense(table, "table", torch.int32, (S, blocks)), T, S, blocks, 0)
+        return _TOKENS.pack(_dense(pos, "pos", _INT32, (T,)), _dense(seq, "seq", _INT32, (T,)),
+                            _dense(table, "table", _INT32, (S, blocks)), T, S, blocks, 0)
 
     def _need(self, what: str):
         if getattr(self, what) is None:
@@ -247,30 +252,28 @@ class BlockCache:
         the mean of every block that a token fills; with q, rotates the queries into q_out (which
         may be q).  The tokens of one sequence are consecutive and ascend."""
         self._need("k_pages")
-        T, d = pos.shape[0], self.dtype
+        L, T, d = _lib(), pos.shape[0], self.dtype
         pk = _rows(k, "k", d, T, self.kv_heads, self.head_dim)
         pv = _rows(v, "v", d, T, self.kv_heads, self.head_dim)
         pq = po = None
         if q is not None:
             pq = _rows(q, "q", d, T, None, self.head_dim)
             po = _rows(q_out, "q_out", d, T, q.shape[1], self.head_dim)
-        _check(_lib().sdnn_cache_append(self._struct(d), self._tokens(pos, seq, table), pk, pv,
-                                        None if rope is None else rope._packed, pq, po,
-                                        _stream_handle(stream)), "sdnn_cache_append")
+        _check(L.sdnn_cache_append(self._struct(d), self._tokens(pos, seq, table), pk, pv,
+                                   None if rope is None else rope._packed, pq, po,
+                                   _stream_handle(stream)), "sdnn_cache_append")
 
     def select(self, q, pos, seq, table, chosen, sink: int = 1, local: int = 1, stream=None):
         """Writes to chosen (tokens, kv_heads, blocks; int32) the blocks that each token's queries
         (tokens, heads, head_dim) attend to: the first `sink`, the last `local` and those with the
         largest scores, ascending, then -1."""
         self._need("means")
-        torch = _torch_mod()
-        d = q.dtype if self.dtype is None else self.dtype
+        L, d = _lib(), q.dtype if self.dtype is None else self.dtype
         T, blocks = pos.shape[0], chosen.shape[-1]
         pq = _rows(q, "q", d, T, None, self.head_dim)
-        pc = _dense(chosen, "chosen", torch.int32, (T, self.kv_heads, blocks))
-        _check(_lib().sdnn_block_select(self._struct(d), self._tokens(pos, seq, table), pq, blocks,
-                                        int(sink), int(local), pc, _stream_handle(stream)),
-               "sdnn_block_select")
+        pc = _dense(chosen, "chosen", _INT32, (T, self.kv_heads, blocks))
+        _check(L.sdnn_block_select(self._struct(d), self._tokens(pos, seq, table), pq, blocks,
+                                   int(sink), int(local), pc, _stream_handle(stream)), "sdnn_block_select")
         return chosen
 
     def workspace_floats(self, tokens: int, heads: int, blocks: int) -> int:
@@ -285,8 +288,7 @@ class BlockCache:
         default; lse: float32 (tokens, heads), receives the logarithm of the sums of exponentials;
         workspace: a float32 tensor of workspace_floats(...) (allocated here when None)."""
         self._need("k_pages")
-        torch = _torch_mod()
-        T, d = pos.shape[0], self.dtype
+        L, T, d = _lib(), pos.shape[0], self.dtype
         pq = _rows(q, "q", d, T, None, self.head_dim)
         H = q.shape[1]
         po = _rows(out, "out", d, T, H, self.head_dim)
@@ -294,22 +296,23 @@ class BlockCache:
         pc = None
         if chosen is not None:
             blocks = chosen.shape[-1]
-            pc = _dense(chosen, "chosen", torch.int32, (T, self.kv_heads, blocks))
-        pl = None if lse is None else _dense(lse, "lse", torch.float32, (T, H))
+            pc = _dense(chosen, "chosen", _INT32, (T, self.kv_heads, blocks))
+        pl = None if lse is None else _dense(lse, "lse", _FLOAT32, (T, H))
         cache = self._struct(d)
         if workspace is None:
-            need = _lib().sdnn_block_attend_floats(cache, T, H, blocks)
+            need = L.sdnn_block_attend_floats(cache, T, H, blocks)
             if need:
+                torch = _torch_mod()
                 workspace = torch.empty(need, dtype=torch.float32, device=q.device)
                 if stream is not None:
                     workspace.record_stream(stream)
         pw, nw = None, 0
         if workspace is not None:
             nw = workspace.numel()
-            pw = _dense(workspace, "workspace", torch.float32, (nw,))
-        _check(_lib().sdnn_block_attend(cache, self._tokens(pos, seq, table), pq, po, pc, blocks,
-                                        1.0 / math.sqrt(self.head_dim) if scale is None else scale, pl,
-                                        pw, nw, _stream_handle(stream)), "sdnn_block_attend")
+            pw = _dense(workspace, "workspace", _FLOAT32, (nw,))
+        _check(L.sdnn_block_attend(cache, self._tokens(pos, seq, table), pq, po, pc, blocks,
+                                   1.0 / math.sqrt(self.head_dim) if scale is None else scale, pl,
+                                   pw, nw, _stream_handle(stream)), "sdnn_block_attend")
         return out
 
 
@@ -347,21 +350,22 @@ class Q4Plan:
     def matvec(self, x, y, bias=None, epi: str = "none", stream=None):
         """y (M, N) = epi(W @ x + bias) for x (K, N) of the same type, N few; any strides (rows of
         tokens are x.t(), y.t()).  bias: float32 (M,)."""
-        torch = _torch_mod()
-        K, N = x.shape if x.dim() == 2 else (None, None)
+        d, shape = x.dtype, x.shape
+        K, N = shape if len(shape) == 2 else (None, None)
         if K != self.K:
             raise ValueError(f"x has shape {tuple(x.shape)}, expected ({self.K}, N)")
         if y.shape != (self.M, N):
             raise ValueError(f"y has shape {tuple(y.shape)}, expected {(self.M, N)}")
-        if y.dtype is not x.dtype:
-            raise TypeError(f"y must be {x.dtype}, not {y.dtype}")
+        if y.dtype is not d:
+            raise TypeError(f"y must be {d}, not {y.dtype}")
         if not (x.is_cuda and y.is_cuda):
             raise TypeError("x and y must be CUDA/HIP torch tensors")
-        pb = None if bias is None else _dense(bias, "bias", torch.float32, (self.M,))
+        pb = None if bias is None else _dense(bias, "bias", _FLOAT32, (self.M,))
         (xf, xc), (yf, yc) = x.stride(), y.stride()
-        _check(self._lib.sdnn_qmat_apply(self.handle, x.data_ptr(), xf, xc, y.data_ptr(), yf, yc, N,
-                                         _dtype_code(x.dtype, "x"), pb, EPI[epi], _stream_handle(stream)),
-               "sdnn_qmat_apply")
+        code = self._lib.sdnn_qmat_apply(self.handle, x.data_ptr(), xf, xc, y.data_ptr(), yf, yc, N,
+                                         _dtype_code(d, "x"), pb, EPI[epi], _stream_handle(stream))
+        if code:
+            raise SdnnError(code, "sdnn_qmat_apply")
         return y
 
     def close(self):
