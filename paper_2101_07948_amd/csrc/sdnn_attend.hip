@@ -839,12 +839,15 @@ Tiles tiles_of(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int
 // once, since another round of workgroups costs more than it shares out (732 tokens of a head of 192 over 4 blocks of
 // 128: 2 shares 53 us and the join, 1 share 31; 22 tokens of 2 heads over lists of 64 blocks that are nearly empty: 24
 // shares 24 us, 11 shares 8).  A wave has a step of its own at least, and there are at most 64 shares (the lanes of
-// attend_join).
+// attend_join).  Where all blocks are 192 KiB or less, 48 to a wave, they are not shared out: the join, a launch of its
+// own, would take longer (4 tokens of 8 heads of 128 in 16 bits, a call: 4 blocks of 32 KiB 12.5 us with and 9.3
+// without, 8 11 to 12.5 and 11.1 to 12.3, 16 12.3 and 20).
 int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
   const int64_t units = (int64_t)tokens * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
   if (units == 0) return 1;
   const int step = c.dtype == SDNN_F32 ? 16 : 32;
   const int64_t steps = (int64_t)blocks * (c.block / step), most = (steps + kWaves - 1) / kWaves;
+  if (blocks * 2ll * c.block * c.head_dim * dtype_bytes(c.dtype) <= 192 * 1024) return 1;
   int64_t wanted = (1024 + units - 1) / units;
   if (steps < 4 * kWaves * wanted) wanted = 256 * attend_waves((c.head_dim + 15) / 16) / units;
   const int64_t s = wanted < most ? wanted : most;
