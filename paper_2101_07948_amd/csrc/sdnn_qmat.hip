@@ -184,9 +184,9 @@ struct Columns {
 template <typename T, int TOKENS>
 constexpr int kRowsOf = sizeof(T) == 2 ? TOKENS : TOKENS <= 4 ? 4 * TOKENS : 3 * TOKENS;
 
-// The most waves of a workgroup: 16, where their rows take 64 KiB of LDS at most.
-template <typename T, int TOKENS>
-constexpr int kWavesOf = kRowsOf<T, TOKENS> * kRowBytes * kMaxWaves <= 65536 ? kMaxWaves : kMaxWaves / 2;
+// The most waves of a workgroup; half where the registers of 16 waves do not hold the columns on their way.
+template <int TOKENS, bool FEATURES>
+constexpr int kWavesOf = TOKENS == 16 && FEATURES ? kMaxWaves / 2 : kMaxWaves;
 
 // N scales from scale i on (N bytes or more apart: one access), and zero points.
 template <int N>
@@ -243,7 +243,7 @@ struct Chunk {
 // brings all of x through LDS.  Small ones are a launch: 768 x 3072 3.8 us.
 //   STEPS: matrix instructions (of 32 columns of W) of a group within a chunk.
 template <typename T, int STEPS, int TOKENS, bool FEATURES>
-__global__ __launch_bounds__((kWavesOf<T, TOKENS> * 64)) void qmat_kernel(QmatArgs a) {
+__global__ __launch_bounds__((kWavesOf<TOKENS, FEATURES> * 64)) void qmat_kernel(QmatArgs a) {
   constexpr bool PARTS = sizeof(T) == 4, PACKED = PARTS && TOKENS <= 4;
   constexpr int REGS = TOKENS < 4 ? 1 : TOKENS / 4, SETS = PARTS && !PACKED ? 3 : 1, ROWS = kRowsOf<T, TOKENS>;
   extern __shared__ __align__(16) unsigned char lds[];  // a wave's rows, then its sums
@@ -329,10 +329,11 @@ __global__ __launch_bounds__((kWavesOf<T, TOKENS> * 64)) void qmat_kernel(QmatAr
 template <typename T, int STEPS, int TOKENS>
 hipError_t start_tokens(const QmatArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.M + kQTileRows - 1) / kQTileRows), (unsigned)((a.N + TOKENS - 1) / TOKENS));
-  // 8 waves to a tile of rows, 16 where there are fewer tiles than compute units (and LDS holds their columns), with
-  // as many chunks each as the one with most of them; 4 at least, which write the results
+  // 8 waves to a tile of rows, 16 where there are fewer tiles than compute units (1000 x 12000, 4 columns in 32 bits:
+  // 13.0 and 10.3 us; 227 x 11127, 16 contiguous columns in 16 bits: 11.8 and 11.1), with as many chunks each as the one with most
+  // of them; 4 at least, which write the results
   constexpr size_t per_wave = (size_t)kRowsOf<T, TOKENS> * kRowBytes;
-  const int most = grid.x * grid.y < 256 ? kWavesOf<T, TOKENS> : 8;
+  const int most = grid.x * grid.y >= 256 ? 8 : a.x_feature == 1 ? kWavesOf<TOKENS, false> : kWavesOf<TOKENS, true>;
   const int each = (a.chunks + most - 1) / most, needed = (a.chunks + each - 1) / each;
   const int waves = needed < 4 ? 4 : needed;
   constexpr size_t sums = (TOKENS < 4 ? 4 : TOKENS) * 64;  // of a wave
