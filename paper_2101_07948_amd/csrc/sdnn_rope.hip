@@ -2,6 +2,7 @@
 #include <type_traits>
 
 #include "sdnn_decode_device.h"
+#include "sdnn_decode_shape.h"
 
 namespace sdnn {
 namespace {
@@ -185,11 +186,6 @@ struct AppendArgs {
   int32_t passes;   // of a mean, each with a part of those rows
 };
 
-constexpr int kWindow = 64;       // the most
-constexpr int kTileBytes = 32768; // the most of a window's keys
-constexpr int kCus = 256;
-constexpr int kSumRows = 8;       // keys of a block that a thread adds
-
 // The window's rotated keys [token][head_dim], its values with rows a piece longer (so that the rows of one
 // column lie in different banks), whose place the sums of a mean take afterwards.
 struct AppendLds {
@@ -199,10 +195,6 @@ struct AppendLds {
   float sum[kMaxHeadDim];
   float top;
 };
-__host__ __device__ constexpr int key_bytes(int window, int head_dim, int size) { return (window * head_dim * size + 15) & ~15; }
-__host__ __device__ constexpr int value_bytes(int window, int head_dim, int size) {
-  return window * (head_dim * size + 16);
-}
 
 // Sum of get(0) ... get(N - 1), halves added pairwise (i with i + N / 2 first).
 template <int N, int STRIDE = 1, typename GET>
@@ -472,17 +464,9 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.freq = r ? r->freq : nullptr, a.amplitude = r ? r->amplitude : 1.0, a.pairs = r ? r->pairs : 0;
   a.tokens = t.tokens, a.sequences = t.sequences, a.max_blocks = t.max_blocks;
   a.kv_heads = c.kv_heads, a.head_dim = c.head_dim, a.block = c.block;
-  // one token to a workgroup; in prompts, and where single tokens fill the device several times, windows
-  // whose values are written in runs
   const int size = dtype_bytes(c.dtype), layout = r ? r->layout : SDNN_ROPE_HALF;
-  a.window = 1;
-  if ((int64_t)t.tokens * c.kv_heads > 4096 || t.tokens >= (int64_t)16 * t.sequences)
-    a.window = kWindow * c.head_dim * size <= kTileBytes ? kWindow : kWindow / 2;
-  // Prompts that leave compute units without one take shorter windows: a window's steps follow one another, and so do
-  // its means, while what a shorter one rotates again of a block it shares is little.  (Kernel, us: windows of 64, 32
-  // and 16: 941 tokens of 3 heads of 128, blocks of 32: 26, 15, 15; 714 of 1 head, blocks of 64: 22, 20, 17; 186 of
-  // 12 heads of 192, blocks of 128: 18, 12, 9; 1000 of 8 heads of 128 in 32 bits, blocks of 128: 29, 31, 31.)
-  while (a.window > kWindow / 4 && (int64_t)t.tokens * c.kv_heads < (int64_t)kCus * a.window) a.window /= 2;
+  const AppendShape shape = append_shape(c, t);
+  a.window = shape.window, a.before = shape.before, a.passes = shape.passes;
   // The keys' units are 16-byte ones where windows have many and the head divides by them.
   const int wide = 16 / size / (layout == SDNN_ROPE_INTERLEAVED ? 2 : 1);
   const bool whole = rope_vec(c.dtype, layout, a.pairs, c.head_dim) == wide, vec = a.window > 1 && whole;
@@ -490,22 +474,9 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.k_pairs = layout == SDNN_ROPE_HALF || rows_aligned(k.data, k.token_stride, k.head_stride, 2, c.dtype);
   a.k_aligned = vec ? a.k_whole : a.k_pairs;
   a.v_aligned = rows_aligned(v.data, v.token_stride, v.head_stride, 16 / size, c.dtype);
-  // LDS: the keys, then the values or the sums of a mean, then a block's keys from before the window; the queries'
-  // cosines and sines
-  size_t lds = value_bytes(a.window, c.head_dim, size), sums = (size_t)c.block / kSumRows * c.head_dim * sizeof(float);
-  lds = key_bytes(a.window, c.head_dim, size) + (lds > sums ? lds : sums);
-  a.before = (int32_t)((lds + 15) & ~(size_t)15);
-  a.passes = 1;
-  if (c.means && t.tokens > a.window) {
-    // (the rows may take the place that the values had, past the sums)
-    a.before = (int32_t)(key_bytes(a.window, c.head_dim, size) + ((sums + 15) & ~(size_t)15));
-    while (a.before + key_bytes(c.block / a.passes, c.head_dim, size) > 128 * 1024) a.passes *= 2;
-    const size_t with = a.before + key_bytes(c.block / a.passes, c.head_dim, size);
-    if (with > lds) lds = with;
-  }
+  size_t lds = shape.lds;  // or the queries' cosines and sines
   if (lds < (size_t)a.q.tile * a.q.pairs * sizeof(float2)) lds = (size_t)a.q.tile * a.q.pairs * sizeof(float2);
-  const int64_t windows = (t.tokens + a.window - 1) / a.window + (a.window > 1);  // one more where they are shifted
-  a.kv_blocks = (int32_t)(windows * c.kv_heads);
+  a.kv_blocks = (int32_t)(shape.windows * c.kv_heads);
   const int64_t blocks = a.kv_blocks + q_blocks;
   return by_type(c.dtype, layout, [&](auto ty, auto il) {
     typedef decltype(ty) T;

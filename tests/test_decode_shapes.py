@@ -1,0 +1,65 @@
+"""Launch shapes of the operators of sdnn_decode.h (csrc/sdnn_decode_shape.h, host arithmetic), compiled
+for the CPU and held to what the kernels index."""
+import ctypes
+import itertools
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from conftest import ROOT
+
+SOURCE = r'''
+#include "sdnn_decode_shape.h"
+using namespace sdnn;
+
+extern "C" void append(int tokens, int sequences, int kv_heads, int head_dim, int block, int dtype, int64_t* out) {
+  sdnn_block_cache c = {};
+  static int8_t means;
+  c.means = &means, c.kv_heads = kv_heads, c.head_dim = head_dim, c.block = block, c.dtype = dtype;
+  sdnn_tokens t = {};
+  t.tokens = tokens, t.sequences = sequences;
+  const AppendShape s = append_shape(c, t);
+  out[0] = s.window, out[1] = s.before, out[2] = s.passes, out[3] = (int64_t)s.lds, out[4] = s.windows;
+}
+'''
+
+
+@pytest.fixture(scope="module")
+def shapes(tmp_path_factory):
+    if not shutil.which("g++"):
+        pytest.skip("g++ not installed")
+    at = tmp_path_factory.mktemp("shapes")
+    src, lib = at / "shapes.cpp", at / "shapes.so"
+    src.write_text(SOURCE)
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-w",
+                    "-I" + os.path.join(rocm, "include"), "-I" + os.path.join(ROOT, "paper_2101_07948_amd", "csrc"),
+                    str(src), "-o", str(lib)], check=True)
+    return ctypes.CDLL(str(lib))
+
+
+def append_shape(shapes, *sizes):
+    out = (ctypes.c_int64 * 5)()
+    shapes.append(*sizes, out)
+    return list(out)
+
+
+def test_append_has_room_for_the_keys_before_every_window(shapes):
+    """A workgroup whose window does not begin with the call may rotate any of a block's earlier keys into
+    the rows at `before`: all of them have to lie within its LDS, whatever the first token's position is."""
+    later = 0
+    for (block, dim, dtype, heads), sequences, tokens in itertools.product(
+            [(32, 64, 1, 1), (32, 64, 1, 2), (64, 128, 2, 8), (128, 256, 0, 2), (128, 8, 1, 300), (64, 256, 0, 64)],
+            [0, 1, 2, 40], [1, 2, 3, 5, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 300, 5000]):
+        window, before, passes, lds, windows = append_shape(shapes, tokens, sequences, heads, dim, block, dtype)
+        size = 4 if dtype == 0 else 2
+        assert window in (1, 16, 32, 64) and block // 8 % passes == 0 and lds <= 150 * 1024
+        assert before >= window * dim * size + block // 8 * dim * 4  # the window's keys, the sums of a mean
+        assert windows * window >= tokens + window - 1               # whatever the shift
+        firsts = [max(w * window - shift, 0) for shift in range(window) for w in range(windows)]
+        if any(0 < t0 < tokens for t0 in firsts):
+            later += 1
+            assert lds >= before + block // passes * dim * size, (block, dim, dtype, heads, sequences, tokens)
+    assert later > 200

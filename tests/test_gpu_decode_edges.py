@@ -1,0 +1,43 @@
+"""GPU tests of the operators of sdnn_decode.h at edges of what their header allows, against their
+definitions in 64 bits."""
+import numpy as np
+import pytest
+
+import _decode_oracle as od
+import paper_2101_07948_amd as sd
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_gpu_decode import (DEV, check_attend, check_means, check_pages, close, filled, gen, i32, make_cache,  # noqa: E402
+                             randn, random_choice, random_q4)
+
+
+# ---------------------------------------------------------------- append
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("Hk,D,P,first,call", [
+    # (sequence, position) of the call's tokens; `first`: stored by an earlier call
+    (1, 64, 32, range(20), [(99, 5)] + [(0, p) for p in range(20, 35)]),
+    (1, 64, 32, range(17), [(-1, 8)] + [(0, p) for p in range(17, 32)]),
+    (2, 128, 64, range(50), [(7, 3)] + [(0, p) for p in range(50, 65)]),
+    (2, 256, 128, range(122), [(-1, 12)] + [(0, p) for p in range(122, 137)]),
+    (512, 16, 32, range(25), [(0, p) for p in range(25, 35)]),  # more heads than compute units
+])
+def test_append_of_no_more_tokens_than_a_window(dtype, Hk, D, P, first, call):
+    """Windows are shifted by the first token's place, that of a filler too: the block is filled in the
+    second window, with keys from the first, and from the page."""
+    table = np.array([[2, 0]], np.int32)
+    cache = make_cache(0, 3, Hk, P, D, dtype)
+    rope, freq = sd.Rope(D), sd.rope_frequencies(D)
+    calls = [[(0, p) for p in first], call]
+    keys, values = [], []
+    for i, c in enumerate(calls):
+        k, v = randn(20 + i, (len(c), Hk, D), dtype), randn(30 + i, (len(c), Hk, D), dtype)
+        keys.append(k), values.append(v)
+        seq, pos = zip(*c)
+        cache.append(k, v, i32(pos), i32(seq), i32(table), rope=rope)
+    seq, pos = zip(*(calls[0] + calls[1]))
+    written = check_pages(cache, table, list(seq), list(pos), torch.cat(keys), torch.cat(values), freq, "half", dtype)
+    assert written[2].all()
+    check_means(cache, written)
