@@ -143,8 +143,9 @@ sdnn_status sdnn_block_select(const sdnn_block_cache* cache, const sdnn_tokens* 
  * chosen for it (chosen as sdnn_block_select leaves it; NULL: in every block it sees):
  *     s_j = scale * q . k_j,  m = max s_j,  l = sum exp(s_j - m),
  *     o = (1 / l) sum exp(s_j - m) v_j,  lse = m + log l.
- * A token that sees nothing gets o = 0, lse = -infinity.  Entries of chosen that are out of
- * range or past the token's own block count for nothing; entries ascend and none repeats.
+ * A token that sees nothing gets o = 0, lse = -infinity.  Negative entries of chosen count for
+ * nothing wherever they stand; the others ascend, none repeats, and those past the token's own
+ * block or the table count for nothing.
  *   o: like q.  lse: device, [tokens][heads] float, or NULL.
  *   blocks: row length of chosen (ignored when it is NULL).
  *   workspace: device, 16-byte aligned, at least sdnn_block_attend_floats floats, scratch of

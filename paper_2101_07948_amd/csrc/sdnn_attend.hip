@@ -536,26 +536,28 @@ __device__ __forceinline__ typename Step<T>::Piece value_piece(const unsigned ch
 // Where a query is in the list of its blocks: the one it attends to next with its page, and what follows
 // it, loaded ahead so that no step waits for a list.
 struct Cursor {
-  int32_t t, seq, n, j, own;
+  int32_t t, seq, n, j;
+  int32_t last;   // block that the token may see
   int32_t share;  // blocks share, share + splits, ... are this workgroup's (splits: a power of two)
   int32_t id, page, next_id, next_page, after;
-  // The next entry of the list that is this share's; -1 past its end.
+  // The next entry of the list that is this share's; -1 past its end.  Negative entries count for nothing, the
+  // others ascend: nothing follows the last block or one past it (what -1 fill the end of a list is not read).
   __device__ __forceinline__ int32_t following(const AttendArgs& a, int h) {
     if (!a.chosen) {
       const int32_t b = j++ * a.splits + share;
       return b < n ? b : -1;
     }
     const int32_t* list = a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks;
-    if (a.splits == 1) return j < n ? list[j++] : -1;
-    int32_t b = -1;
-    while (j < n && (b = list[j++]) >= 0 && (b & (a.splits - 1)) != share) b = -1;
-    return b;
+    while (j < n) {
+      const int32_t b = list[j++];
+      if (b >= last) j = n;
+      if (b >= 0 && (b & (a.splits - 1)) == share) return b;
+    }
+    return -1;
   }
-  __device__ __forceinline__ bool valid(const AttendArgs& a, int32_t b) const {
-    return b >= 0 && b <= own && b < a.max_blocks;
-  }
+  __device__ __forceinline__ bool valid(int32_t b) const { return b >= 0 && b <= last; }
   __device__ __forceinline__ int32_t page_of(const AttendArgs& a, int32_t b) const {
-    return valid(a, b) ? a.table[(int64_t)seq * a.max_blocks + b] : -1;
+    return valid(b) ? a.table[(int64_t)seq * a.max_blocks + b] : -1;
   }
   __device__ __forceinline__ void start(const AttendArgs& a, int h) {
     j = 0;
@@ -635,10 +637,10 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
                       (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
   const bool filler = p < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
   Cursor at;
-  at.t = t, at.seq = seq, at.own = p / a.block, at.share = split;
-  at.n = filler ? 0 : a.chosen ? a.blocks : min(at.own + 1, a.max_blocks);
+  at.t = t, at.seq = seq, at.last = min(p / a.block, a.max_blocks - 1), at.share = split;
+  at.n = filler ? 0 : a.chosen ? a.blocks : at.last + 1;
   at.start(a, h);
-  const auto key = [&] { return at.valid(a, at.id) ? run << 20 | at.id : END; };
+  const auto key = [&] { return at.valid(at.id) ? run << 20 | at.id : END; };
   // One row of each token offers its next block.
   const auto offer = [&](int turn) {
     if (g == 0 && qr == 0)

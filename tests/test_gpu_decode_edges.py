@@ -41,3 +41,34 @@ def test_append_of_no_more_tokens_than_a_window(dtype, Hk, D, P, first, call):
     written = check_pages(cache, table, list(seq), list(pos), torch.cat(keys), torch.cat(values), freq, "half", dtype)
     assert written[2].all()
     check_means(cache, written)
+
+
+# ---------------------------------------------------------------- attend
+
+def with_negatives(chosen, where, seed):
+    """The same lists with their entries moved to the end of the row, or among negative ones."""
+    rng = np.random.default_rng(seed)
+    out = np.full_like(chosen, -1)
+    for row, old in zip(out.reshape(-1, chosen.shape[-1]), chosen.reshape(-1, chosen.shape[-1])):
+        ids = old[old >= 0]
+        at = np.arange(len(row) - len(ids), len(row)) if where == "front" else \
+            np.sort(rng.permutation(len(row))[:len(ids)])
+        row[:] = rng.integers(-2 ** 31, 0, len(row))
+        row[at] = ids
+    return out
+
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("where", ["front", "between"])
+@pytest.mark.parametrize("Hq,Hk,D,P,lens,new,blocks", [
+    (8, 2, 64, 32, [400], 3, 6),              # token by token
+    (32, 8, 128, 64, [700], 517, 9),          # through tiles
+    (8, 2, 64, 64, [3000], 90, 12),           # whose blocks are shared out
+    (16, 16, 64, 32, [300, 200], 200, 40),    # lists longer than what there is to choose
+])
+def test_attend_passes_over_negative_entries(dtype, where, Hq, Hk, D, P, lens, new, blocks):
+    cache, table = filled(13, len(lens), lens, Hk, P, D, dtype)
+    seq = [s for s in range(len(lens)) for _ in range(new)]
+    pos = [p for n in lens for p in range(n - new, n)]
+    chosen = with_negatives(random_choice(6, pos, Hk, blocks, P), where, 7)
+    check_attend(cache, table, randn(14, (len(pos), Hq, D), dtype), pos, seq, chosen, oracle=od.attend_many)
