@@ -63,7 +63,8 @@ def with_negatives(chosen, where, seed):
 @pytest.mark.parametrize("Hq,Hk,D,P,lens,new,blocks", [
     (8, 2, 64, 32, [400], 3, 6),              # token by token
     (32, 8, 128, 64, [700], 517, 9),          # through tiles
-    (8, 2, 64, 64, [3000], 90, 12),           # whose blocks are shared out
+    (8, 8, 64, 64, [3800], 400, 60),          # whose blocks are shared out
+    (8, 2, 64, 64, [3000], 90, 12),           # token by token, of a longer list
     (16, 16, 64, 32, [300, 200], 200, 40),    # lists longer than what there is to choose
 ])
 def test_attend_passes_over_negative_entries(dtype, where, Hq, Hk, D, P, lens, new, blocks):
