@@ -82,8 +82,9 @@ struct Step16 {
     }
   }
 
-  // o += p v.  p is split into two 16-bit parts, so that it counts with all the bits that the sum
-  // of probabilities counts it with (one part would add an error as large as the rounding of o).
+  // o += p v.  p is split into two 16-bit parts: with one its rounding would add an error as large as that of o, with two
+  // what is lost is 2^-17 of p in bf16 (a 256th of the rounding of o) and 2^-22 in f16, there at least 2^-25, which
+  // attend_step keeps apart from what counts.  The sum of probabilities takes all 24 bits.
   // PART: tokens from `stored` on may hold anything (their p is 0).
   template <bool PART, int CHUNKS, typename V>
   static __device__ __forceinline__ void accumulate(const V& vv, const float (&p)[8], int g, int stored,
@@ -204,15 +205,22 @@ __device__ __forceinline__ void store_part(const AttendArgs& a, int split, int t
 
 // One step, its scores s given: tokens [0, seen) of its are within the sight of this lane's query, tokens from `stored` on may
 // hold anything.  EMPTY: queries may see nothing here (seen <= 0), or have seen nothing yet (m = -infinity).
-//   m is a reference near the running maximum rather than the maximum: it moves only where a score is over
-// 2^8 times above it, so that most steps neither reduce over lanes nor rescale the sums (p <= 2^8 costs no bits:
-// p is a float, and its 16-bit parts are floating too).  Scores are masked one by one only where a query's
-// sight ends within the step; a query that sees nothing of it gets m = infinity for the step, p = 0.
+//   m is a reference near the running maximum rather than the maximum: it rises only where a score is over 2^HIGH times
+// above it, so that most steps neither reduce over lanes nor rescale the sums.  Scores are masked one by one only where
+// a query's sight ends within the step; a query that sees nothing of it gets m = infinity for the step, p = 0.
+//   p is a float, and its parts in bf16 have its exponents.  Parts in f16 end at 2^-24, while what an output is made of may
+// be far below the query's largest p, where that meets a value near 0.  So in f16 m is 2^HEAD below a new maximum (p up
+// to 2^15): a p of 2^-21 of the largest keeps its 16 bits, and none above 2^-37 is dropped.  And where all scores of a
+// step are below m, m comes down to them, as far as sums in 32 bits allow.  (2048 tokens over 16 of 128 blocks: 148 us
+// and 147 without; with scores that spread five times as wide, where m falls in some step of most tiles, 173 and 148.)
 template <bool EMPTY, typename T, int CHUNKS, int TILES, typename V>
 __device__ __forceinline__ void attend_step(float scale2, float (&s)[Step<T>::kTokens / 4], const V& vv, int seen,
                                             int stored, int g, State<TILES>& st) {
   constexpr int N = Step<T>::kTokens, E = N / 4;
-  constexpr float SLACK = 8.0f;
+  constexpr bool HALF = __is_same(T, _Float16);
+  constexpr float HEAD = HALF ? 12.0f : 0.0f, HIGH = HALF ? 15.0f : 8.0f, LOW = HALF ? 0.0f : -INFINITY;
+  // What m may fall by in a step, and up to which sum: none gets past 2^94 times the largest value.
+  constexpr float FALL = 30.0f, LONGEST = 0x1p64f;
   if (!EMPTY || __any(seen > 0 && seen < N)) {
 #pragma unroll
     for (int j = 0; j < E; ++j) s[j] = E * g + j < seen ? s[j] : -INFINITY;
@@ -220,8 +228,18 @@ __device__ __forceinline__ void attend_step(float scale2, float (&s)[Step<T>::kT
   float top = s[0];
 #pragma unroll
   for (int j = 1; j < E; ++j) top = fmaxf(top, s[j]);
-  if (__any((!EMPTY || seen > 0) && top * scale2 > st.m + SLACK)) {
-    const float m = fmaxf(st.m, over_groups_max(!EMPTY || seen > 0 ? top * scale2 : -INFINITY));
+  const bool sees = !EMPTY || seen > 0;
+  const float above = fmaf(top, scale2, -st.m);  // of this lane's scores
+  bool moves = __any(sees && above != __builtin_amdgcn_fmed3f(above, LOW, HIGH));
+  if (HALF && moves) {  // (below m have to be all four lanes of a query)
+    uint64_t low = __ballot(sees && above < LOW);
+    low &= low >> 32;
+    moves = (low & low >> 16 & 0xffff) || __any(sees && above > HIGH);
+  }
+  if (moves) {
+    const float row = over_groups_max(sees ? top * scale2 : -INFINITY), sum = over_groups_max(st.l);  // of the query
+    float m = fmaxf(row - HEAD, st.m);
+    if (HALF && sees && row < st.m && sum < LONGEST) m = fmaxf(row - 0.5f * HEAD, st.m - FALL);
     // 0 where this is the first step that the query sees
     const float f = EMPTY && m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st.m - m);
     st.l *= f;
@@ -229,7 +247,7 @@ __device__ __forceinline__ void attend_step(float scale2, float (&s)[Step<T>::kT
 #pragma unroll
     for (int c = 0; c < TILES; ++c) st.o[c] *= f;
   }
-  const float m = !EMPTY || seen > 0 ? st.m : INFINITY;
+  const float m = sees ? st.m : INFINITY;
 #pragma unroll
   for (int j = 0; j < E; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], scale2, -m));
   float sum = s[0];

@@ -73,3 +73,27 @@ def test_attend_passes_over_negative_entries(dtype, where, Hq, Hk, D, P, lens, n
     pos = [p for n in lens for p in range(n - new, n)]
     chosen = with_negatives(random_choice(6, pos, Hk, blocks, P), where, 7)
     check_attend(cache, table, randn(14, (len(pos), Hq, D), dtype), pos, seq, chosen, oracle=od.attend_many)
+
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("sink", [0, 1500, 2047])
+@pytest.mark.parametrize("low,high,size", [(17.4, 17.4, 1), (14, 14, 1), (12, 18, 1), (20, 20, 16), (3, 20, 1)])
+@pytest.mark.parametrize("Hq,Hk,D,tokens", [(4, 2, 64, 1), (8, 8, 8, 1), (8, 8, 64, 300)])
+def test_attend_beside_a_dominant_key_without_value(dtype, sink, low, high, size, Hq, Hk, D, tokens):
+    """A key that takes nearly all of the probability and whose value is zero: what the output is made of are
+    thousands of probabilities of e^-low ... e^-high.  The bound is the one of all attention tests (the two parts
+    of a probability: 2^-16; f16 parts end at 2^-37 of the largest, which 32 tokens beside it feel: 2^-32 of a value)."""
+    P, n = 64, 4096
+    cache, table = filled(15, 1, [n], Hk, P, D, dtype)
+    at = int(table[0, sink // P])
+    gaps = low + (high - low) * torch.rand((cache.pages, Hk, P), generator=gen(16), device=DEV)
+    cache.k_pages.mul_(0.1)
+    cache.k_pages[..., 0] = (-gaps).to(dtype)
+    cache.k_pages[at, :, sink % P] = 0
+    cache.v_pages.mul_(size)
+    cache.v_pages[at, :, :, sink % P] = 0
+    q = torch.zeros((tokens, Hq, D), dtype=dtype, device=DEV)
+    q[..., 0] = torch.linspace(1, 0.25, Hq, device=DEV)   # other heads: smaller gaps
+    q[:, Hq - 1] *= -1                                    # and one that the key is nothing to
+    pos = list(range(n - tokens, n))
+    check_attend(cache, table, q, pos, [0] * tokens, scale=1.0, oracle=od.attend_many)
