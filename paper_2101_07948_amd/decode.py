@@ -302,10 +302,10 @@ class BlockCache:
         if workspace is None:
             need = L.sdnn_block_attend_floats(cache, T, H, blocks)
             if need:
+                # of the memory of the stream that uses it: that of the current stream may still be in use there
                 torch = _torch_mod()
-                workspace = torch.empty(need, dtype=torch.float32, device=q.device)
-                if stream is not None:
-                    workspace.record_stream(stream)
+                with torch.cuda.stream(stream):  # (None: the current stream)
+                    workspace = torch.empty(need, dtype=torch.float32, device=q.device)
         pw, nw = None, 0
         if workspace is not None:
             nw = workspace.numel()

@@ -97,3 +97,34 @@ def test_attend_beside_a_dominant_key_without_value(dtype, sink, low, high, size
     q[:, Hq - 1] *= -1                                    # and one that the key is nothing to
     pos = list(range(n - tokens, n))
     check_attend(cache, table, q, pos, [0] * tokens, scale=1.0, oracle=od.attend_many)
+
+
+class Allocations:
+    """The streams whose memory torch.empty gives while this is in place."""
+
+    def __init__(self, monkeypatch):
+        self.streams, empty = [], torch.empty
+
+        def spy(*args, **kw):
+            self.streams.append(torch.cuda.current_stream())
+            return empty(*args, **kw)
+
+        monkeypatch.setattr(torch, "empty", spy)
+
+
+def test_attend_takes_its_workspace_from_the_calls_stream(monkeypatch):
+    """Memory of the current stream may still be in use there when the call's stream begins."""
+    cache, table = filled(7, 1, [3000], 2, 64, 128, torch.bfloat16)
+    q = randn(5, (1, 8, 128), torch.bfloat16)
+    out, here = [torch.empty_like(q) for _ in range(3)], torch.cuda.current_stream()
+    pos, seq, tab = i32([2999]), i32([0]), i32(table)
+    side = torch.cuda.Stream()
+    side.wait_stream(here)
+    seen = Allocations(monkeypatch)
+    cache.attend(q, out[0], pos, seq, tab, stream=side)
+    cache.attend(q, out[1], pos, seq, tab)
+    with torch.cuda.stream(side):
+        cache.attend(q, out[2], pos, seq, tab)
+    assert seen.streams == [side, here, side] and torch.cuda.current_stream() == here
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
