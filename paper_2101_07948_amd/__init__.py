@@ -349,14 +349,13 @@ class Plan:
 
     def _workspace(self, ws, N: int, stream):
         """(pointer, floats) of the caller's workspace, or of one allocated here from torch's
-        caching allocator; such a block is tied to `stream` so that it is not handed out
-        again before the call's kernels on that stream have run."""
+        caching allocator, of the memory of the stream that uses it: that of another stream
+        may still be in use there, and is handed out again before this one's kernels have run."""
         import torch
         if ws is None:
             need = self.workspace_floats(N) if int(self.info["splits"]) > 1 else 0
-            ws = torch.empty(max(need, 1), device="cuda")
-            if stream is not None:
-                ws.record_stream(stream)
+            with torch.cuda.stream(stream):  # (None: the current stream)
+                ws = torch.empty(max(need, 1), device="cuda")
         if not isinstance(ws, torch.Tensor) or ws.device.type != "cuda" or \
                 ws.dtype != torch.float32 or not ws.is_contiguous():
             raise TypeError("workspace must be a contiguous float32 CUDA/HIP tensor")

@@ -331,3 +331,28 @@ def test_split_row_permutation_equivariance_bitexact(splits):
         C1 = split_spmm(p1, B, bias, "gelu", splits=splits)
         C2 = split_spmm(p2, B, bias[pi], "gelu", splits=splits)
     assert np.array_equal(C2, C1[pi])
+
+
+def test_workspace_is_of_the_calls_stream(monkeypatch):
+    """Memory of the current stream may still be in use there when the call's stream begins."""
+    w = inputs.workload("c2", N=512)
+    L = w.layers[0]
+    Bt = torch.from_numpy(w.B).to(DEV)
+    want, got = torch.empty(768, 512, device=DEV), torch.empty(768, 512, device=DEV)
+    here, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    with sd.Plan.from_csr(L.W, split_chunks=6) as plan:
+        ws = torch.empty(plan.workspace_floats(512), device=DEV)
+        plan.spmm_split(Bt, want, workspace=ws)
+        side.wait_stream(here)
+        streams, empty = [], torch.empty
+
+        def spy(*args, **kw):
+            streams.append(torch.cuda.current_stream())
+            return empty(*args, **kw)
+
+        monkeypatch.setattr(torch, "empty", spy)
+        plan.spmm_split(Bt, got, stream=side)
+        plan.spmm_split(Bt, want)
+        assert streams == [side, here] and torch.cuda.current_stream() == here
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
