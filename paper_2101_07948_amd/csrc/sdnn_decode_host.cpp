@@ -5,6 +5,7 @@
 #include <new>
 
 #include "sdnn_decode_internal.h"
+#include "sdnn_decode_shape.h"
 
 using namespace sdnn;
 

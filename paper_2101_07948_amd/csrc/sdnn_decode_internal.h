@@ -43,9 +43,6 @@ int64_t attend_floats(const sdnn_block_cache& c, int32_t tokens, int32_t heads, 
 hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const sdnn_heads& q,
                          const sdnn_heads& o, const int32_t* chosen, int32_t blocks, float scale,
                          float* lse, float* workspace, hipStream_t stream);
-// Bytes of the laid-out weights and of their scales.
-int64_t qmat_weight_bytes(const sdnn_qmat_s& w);
-int64_t qmat_meta_bytes(const sdnn_qmat_s& w);
 hipError_t launch_qmat_pack(const sdnn_qmat_s& w, const uint8_t* packed, const void* scales,
                             const uint8_t* zeros, hipStream_t stream);
 hipError_t launch_qmat(const sdnn_qmat_s& w, const void* x, int64_t x_feature, int64_t x_column, void* y,

@@ -60,6 +60,19 @@ inline AppendShape append_shape(const sdnn_block_cache& c, const sdnn_tokens& t)
   return s;
 }
 
+// ---------------------------------------------------------------- 4-bit weights
+
+inline int32_t groups_of(const sdnn_qmat_s& w) { return (int32_t)(((int64_t)w.K + w.group - 1) / w.group); }
+// Of a tile's scales: entries along K, and scales of each entry and row.
+inline int32_t metas_of(const sdnn_qmat_s& w) { return w.group >= kQChunk ? groups_of(w) : w.chunks; }
+inline int32_t inner_of(const sdnn_qmat_s& w) { return w.group >= kQChunk ? 1 : kQChunk / w.group; }
+inline int64_t scales_of(const sdnn_qmat_s& w) { return (int64_t)w.tiles * metas_of(w) * inner_of(w) * kQTileRows; }
+// Bytes of the laid-out weights and of their scales and zero points.
+inline int64_t qmat_weight_bytes(const sdnn_qmat_s& w) { return (int64_t)w.tiles * w.chunks * 1024; }
+inline int64_t qmat_meta_bytes(const sdnn_qmat_s& w) {
+  return scales_of(w) * (dtype_bytes(w.scale_dtype) + (w.zeros ? 1 : 0));
+}
+
 }  // namespace sdnn
 
 #endif  // SDNN_DECODE_SHAPE_H_

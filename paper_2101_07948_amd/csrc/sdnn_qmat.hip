@@ -2,6 +2,7 @@
 #include <type_traits>
 
 #include "sdnn_decode_device.h"
+#include "sdnn_decode_shape.h"
 #include "sdnn_device.h"
 
 namespace sdnn {
@@ -13,7 +14,7 @@ namespace {
 // their 4 bits at bit 3 + 4 p of the dword's lower and upper half (turned by 12 for p = 3, where the upper ones
 // wrap around): after a shift and one mask they are the upper mantissa bits of two bf16 numbers 16 + n.  A wave reads
 // 1 KiB in one access.  The scales and zero points follow: [tile][group][16 rows] where groups are whole chunks,
-// else [tile][chunk][16 rows][group of the chunk], so that a lane has those of a chunk in one access.
+// else [tile][chunk][16 rows][group of the chunk], so that a lane has those of a chunk in one access (see metas_of).
 __host__ __device__ constexpr int bit_of(int i) { return (3 + 4 * (i / 2) + 16 * (i % 2)) % 32; }
 constexpr int kMaxWaves = 16;
 
@@ -364,18 +365,7 @@ hipError_t start(const QmatArgs& a, int group, hipStream_t stream) {
   return start_steps<T, 4>(a, stream);
 }
 
-int32_t groups_of(const sdnn_qmat_s& w) { return (w.K + w.group - 1) / w.group; }
-// Of a tile's scales: entries along K, and scales of each entry and row.
-int32_t metas_of(const sdnn_qmat_s& w) { return w.group >= kQChunk ? groups_of(w) : w.chunks; }
-int32_t inner_of(const sdnn_qmat_s& w) { return w.group >= kQChunk ? 1 : kQChunk / w.group; }
-int64_t scales_of(const sdnn_qmat_s& w) { return (int64_t)w.tiles * metas_of(w) * inner_of(w) * kQTileRows; }
-
 }  // namespace
-
-int64_t qmat_weight_bytes(const sdnn_qmat_s& w) { return (int64_t)w.tiles * w.chunks * 1024; }
-int64_t qmat_meta_bytes(const sdnn_qmat_s& w) {
-  return scales_of(w) * (dtype_bytes(w.scale_dtype) + (w.zeros ? 1 : 0));
-}
 
 hipError_t launch_qmat_pack(const sdnn_qmat_s& w, const uint8_t* packed, const void* scales,
                             const uint8_t* zeros, hipStream_t stream) {
@@ -402,7 +392,7 @@ hipError_t launch_qmat(const sdnn_qmat_s& w, const void* x, int64_t x_feature, i
   a.y = y, a.y_feature = y_feature, a.y_column = y_column;
   if (w.K == 1) a.x_feature = 1;  // one value is contiguous
   a.bias = bias, a.M = w.M, a.K = w.K, a.N = N, a.chunks = w.chunks;
-  const uint32_t group_chunks = w.group / kQChunk;  // (c * group_chunks < 2^32: the quotients are exact)
+  const uint32_t group_chunks = w.group / kQChunk;  // (c < 2^13, group_chunks < 2^24: the quotients are exact)
   a.group_of = group_chunks > 1 ? (uint32_t)(((1ull << 32) + group_chunks - 1) / group_chunks) : 0;
   a.scale_dtype = w.scale_dtype, a.epi = epi;
   if (dtype == SDNN_F32) return start<float>(a, w.group, stream);

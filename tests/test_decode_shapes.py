@@ -23,6 +23,13 @@ extern "C" void append(int tokens, int sequences, int kv_heads, int head_dim, in
   const AppendShape s = append_shape(c, t);
   out[0] = s.window, out[1] = s.before, out[2] = s.passes, out[3] = (int64_t)s.lds, out[4] = s.windows;
 }
+
+extern "C" void qmat(int M, int K, int group, int scale_dtype, int zeros, int64_t* out) {
+  sdnn_qmat_s w = {};
+  w.M = M, w.K = K, w.group = group, w.scale_dtype = scale_dtype, w.zeros = zeros;
+  w.chunks = (K + kQChunk - 1) / kQChunk, w.tiles = (M + kQTileRows - 1) / kQTileRows;
+  out[0] = groups_of(w), out[1] = metas_of(w), out[2] = scales_of(w), out[3] = qmat_weight_bytes(w), out[4] = qmat_meta_bytes(w);
+}
 '''
 
 
@@ -63,3 +70,14 @@ def test_append_has_room_for_the_keys_before_every_window(shapes):
             later += 1
             assert lds >= before + block // passes * dim * size, (block, dim, dtype, heads, sequences, tokens)
     assert later > 200
+
+
+@pytest.mark.parametrize("K,group,groups", [(1, 32, 1), (200, 2 ** 31 - 128, 1), (2 ** 20, 2 ** 31 - 128, 1),
+                                            (2 ** 20, 128, 8192), (129, 128, 2), (2 ** 20, 2 ** 20 - 128, 2)])
+def test_4_bit_scales_of_groups_of_any_length(shapes, K, group, groups):
+    """A group may be longer than K, up to what its 32 bits hold."""
+    out = (ctypes.c_int64 * 5)()
+    shapes.qmat(33, K, group, 0, 1, out)
+    tiles, chunks = 3, -(-K // 128)
+    entries = tiles * 16 * (groups if group >= 128 else chunks * (128 // group))
+    assert out[0] == groups and out[2] == entries and out[3] == tiles * chunks * 1024 and out[4] == entries * 5

@@ -128,3 +128,22 @@ def test_attend_takes_its_workspace_from_the_calls_stream(monkeypatch):
     assert seen.streams == [side, here, side] and torch.cuda.current_stream() == here
     torch.cuda.synchronize()
     assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+
+
+# ---------------------------------------------------------------- 4-bit products
+
+def check_q4(M, K, N, group, dtype, scale_dtype=torch.float32, zeros=True, seed=21):
+    packed, scales, z = random_q4(seed, M, K, group, scale_dtype, zeros)
+    x = randn(22, (K, N), dtype)
+    out = torch.full((M, N), float("nan"), dtype=dtype, device=DEV)
+    with sd.Q4Plan(packed, scales, z, K=K, group=group) as plan:
+        plan.matvec(x, out)
+        torch.cuda.synchronize()
+    y, tol = od.q4(packed.cpu().numpy(), od.f64(scales), None if z is None else z.cpu().numpy(), K, group, od.f64(x))
+    close(out, y, tol + od.U[dtype] * np.abs(y) * 1.01 + od.TINY[dtype], "4-bit product")
+
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("K,group", [(200, 2 ** 31 - 128), (70, 2 ** 31 - 128), (1000, 1 << 30)])
+def test_q4_of_one_long_group(dtype, K, group):
+    check_q4(40, K, 3, group, dtype)
