@@ -20,6 +20,10 @@
  *     past max_blocks hold nothing: nothing is stored there and attention passes over them.
  *   - Values must be finite, but memory of a page that no token was stored to may hold
  *     anything: it is never read into a result.
+ *   - A call whose launch would have 2^32 threads or more gets SDNN_ERR_DIM: split its tokens over
+ *     several.  None is refused for it up to these products: sdnn_rope: tokens 2^25;
+ *     sdnn_cache_append: tokens * (kv_heads + 1) 2^23; sdnn_block_select: tokens * kv_heads 2^21;
+ *     sdnn_block_attend: tokens * kv_heads * ceil(heads / kv_heads / 16) 2^23.
  */
 #ifndef SDNN_DECODE_H_
 #define SDNN_DECODE_H_

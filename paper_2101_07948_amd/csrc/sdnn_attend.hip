@@ -1,15 +1,9 @@
 // Attention over the chosen blocks of the cache.
-#include <algorithm>
-#include <cmath>
-
 #include "sdnn_decode_device.h"
+#include "sdnn_decode_shape.h"
 
 namespace sdnn {
 namespace {
-
-constexpr int kWaves = 4;
-constexpr int kTileWaves = 8;
-constexpr int kRows = 16;  // queries of a tile: the columns of one matrix instruction
 
 struct AttendArgs {
   const void* q;
@@ -260,12 +254,6 @@ __device__ __forceinline__ void attend_step(float scale2, float (&s)[Step<T>::kT
     Step<T>::template accumulate<false, CHUNKS>(vv, s, g, stored, st.o);
 }
 
-// Waves of a SIMD that the registers of attend_kernel leave room for, and so its workgroups at work at once on a compute
-// unit, for heads of up to 16 * tiles values.  (For the compiler a bound: without one it takes registers of both kinds
-// and leaves room for one wave less.  3 waves fit for heads of 128 in 16 bits too, but read worse: 64 tokens of 8 heads
-// over 32 blocks of 64 tokens, 537 MB, 107 us with 3 and 95 with 2.)
-constexpr int attend_waves(int tiles) { return tiles <= 4 ? 4 : tiles <= 6 ? 3 : tiles <= 12 ? 2 : 1; }
-
 // A workgroup handles one token, cached head, tile of up to 16 of its queries and share of its
 // blocks; its waves take blocks in turn and join their states through LDS.  Reading keys and values
 // bounds it: each page is read once for the tile of queries that shares it.  32 tokens of 12 heads of 64 in 32 bits
@@ -447,7 +435,6 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
 }
 
 // The same for at most kFewParts parts: a thread has four values of a row and loads all that they are made of at once.
-constexpr int kFewParts = 8;
 template <typename T>
 __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
   const int D = a.head_dim, units = D / 4;
@@ -757,127 +744,39 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
 }
 
 template <typename T>
-hipError_t join(const AttendArgs& a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.tokens * a.heads;
+hipError_t join(const AttendArgs& a, const AttendShape& shape, hipStream_t stream) {
   if (a.splits > 1 && a.splits <= kFewParts)
-    attend_join_few<T><<<(unsigned)((rows * (a.head_dim / 4) + 255) / 256), 256, 0, stream>>>(a);
+    attend_join_few<T><<<(unsigned)shape.join_groups, 256, 0, stream>>>(a);
   else if (a.splits > 1)
-    attend_join<T><<<(unsigned)rows, 256, 0, stream>>>(a);
+    attend_join<T><<<(unsigned)shape.join_groups, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, int CHUNKS>
-hipError_t start(const AttendArgs& a, hipStream_t stream) {
+hipError_t start(const AttendArgs& a, const AttendShape& shape, hipStream_t stream) {
   if (a.tile_tokens > 0) {
     constexpr int LONG = power_of_two(CHUNKS) * 64;  // bytes of a head's row in LDS; 16 KiB of keys to a stage at most
     constexpr int STAGE = LONG <= 256 ? 64 : 16384 / LONG;
-    const int64_t groups = (a.tokens + a.tile_tokens * kTileWaves - 1) / (a.tile_tokens * kTileWaves);
-    attend_tiles<T, CHUNKS, STAGE, kTileWaves>
-        <<<(unsigned)(groups * a.head_tiles * a.splits * a.kv_heads), kTileWaves * 64, 0, stream>>>(a);
+    attend_tiles<T, CHUNKS, STAGE, kTileWaves><<<(unsigned)shape.groups, shape.threads, 0, stream>>>(a);
   } else {
-    const unsigned grid = (unsigned)((int64_t)a.tokens * a.head_tiles * a.splits * a.kv_heads);
-    attend_kernel<T, CHUNKS><<<grid, kWaves * 64, 0, stream>>>(a);
+    attend_kernel<T, CHUNKS><<<(unsigned)shape.groups, shape.threads, 0, stream>>>(a);
   }
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : join<T>(a, stream);
+  return e != hipSuccess ? e : join<T>(a, shape, stream);
 }
 
 // Pieces of a lane: a head of up to 64, 96, 128, 192 or 256 values.
 template <typename T>
-hipError_t start_dim(const AttendArgs& a, hipStream_t stream) {
+hipError_t start_dim(const AttendArgs& a, const AttendShape& shape, hipStream_t stream) {
   constexpr int U = 8 / Step<T>::kPiece;  // pieces of 32 values
-  if (a.head_dim <= 64) return start<T, 2 * U>(a, stream);
-  if (a.head_dim <= 96) return start<T, 3 * U>(a, stream);
-  if (a.head_dim <= 128) return start<T, 4 * U>(a, stream);
-  if (a.head_dim <= 192) return start<T, 6 * U>(a, stream);
-  return start<T, 8 * U>(a, stream);
+  if (a.head_dim <= 64) return start<T, 2 * U>(a, shape, stream);
+  if (a.head_dim <= 96) return start<T, 3 * U>(a, shape, stream);
+  if (a.head_dim <= 128) return start<T, 4 * U>(a, shape, stream);
+  if (a.head_dim <= 192) return start<T, 6 * U>(a, shape, stream);
+  return start<T, 8 * U>(a, shape, stream);
 }
 
 }  // namespace
-
-namespace {
-// How attend_tiles takes a call: tokens of a wave's tile (a token's queries take a power of two of its 16 rows), and
-// shares of the blocks; tokens 0: attend_kernel does.
-struct Tiles {
-  int tokens, splits;
-};
-int tile_of(const sdnn_block_cache& c, int32_t heads) {
-  int rows = 1;
-  while (rows < heads / c.kv_heads && rows < kRows) rows *= 2;
-  return kRows / rows;
-}
-int64_t tile_groups(const sdnn_block_cache& c, int32_t tokens, int32_t heads) {
-  const int each = tile_of(c, heads) * kTileWaves;
-  return (int64_t)((tokens + each - 1) / each) * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
-}
-constexpr int64_t kTileRoom = 512;  // workgroups at work at once
-// The most shares that a call of so many tokens is split into.
-int tile_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads) {
-  const int64_t groups = tile_groups(c, tokens, heads);
-  int s = 1;
-  while (s < kFewParts && tokens >= 16 && groups * 2 * s <= kTileRoom) s *= 2;
-  return s;
-}
-
-// attend_tiles serves a call where many tokens of a sequence are neighbours and it is estimated to be faster.
-// attend_kernel reads every token's blocks from L2, at about 8 TB/s (16384 heads of 16 blocks of 32 KiB:
-// 994 us; 8760 of 3 of 128 KiB: 683).  attend_tiles takes its workgroups' unions of blocks, 512 workgroups at a
-// time, two to a compute unit, at about 3.7 us for 32 KiB, or 2.2 where they have a unit each (38 and 133 of them: 142 and
-// 288 us; the matrix instructions of 32 bits take four times as long).  How large a union is depends on the lists:
-// between three of them, where neighbours choose alike, and what lists that have nothing in common cover (107 tokens of
-// 4 of 468 blocks of 4 KiB, 12 heads: 280 blocks, 74 us; one by one 20), whose geometric mean is taken.  Where few
-// workgroups leave compute units idle the blocks are shared out, and the parts joined at the rate of a copy (512 tokens
-// at the end of 8512, 8 heads of 128: 1 share 288 us, 4 shares 123 and 8 to join; 900 tokens of a sequence's first 900,
-// whose longest lists have 15 blocks: 41, and 2 shares 33 and 11 to join).
-Tiles tiles_of(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads,
-               int32_t chosen) {
-  if (max_blocks > 1 << 20 || tokens < (int64_t)16 * sequences) return {0, 1};
-  const int tile = tile_of(c, heads), head_tiles = (heads / c.kv_heads + kRows - 1) / kRows;
-  const double page = 2.0 * c.block * c.head_dim * dtype_bytes(c.dtype);
-  const int each = chosen > 0 && chosen < max_blocks ? chosen : max_blocks;
-  const double few = chosen > 0 && chosen < max_blocks / 3 ? 3.0 * chosen : max_blocks;
-  const double many = max_blocks * (1.0 - std::pow(1.0 - (double)each / max_blocks, std::min(tokens, tile * kTileWaves)));
-  const double all = few < many ? std::sqrt(few * many) : few;
-  const double groups = (double)tile_groups(c, tokens, heads);
-  const double one_by_one = (double)tokens * c.kv_heads * head_tiles * each * page / 8e6;
-  const double parts = 8.0 * tokens * heads * (c.head_dim + 2) / 4e6;
-  const auto tiled_in = [&](int shares) {
-    const double at_once = std::min(std::max(groups * shares / 256, 1.0), 2.0), rounds = std::max(groups * shares / kTileRoom, 1.0);
-    const double block = page / 32768 * (0.7 + 1.5 * at_once * (c.dtype == SDNN_F32 ? 4 : 1));
-    return rounds * all / shares * block + (shares > 1 ? shares * parts + 5 : 0.0);
-  };
-  int best = 1;
-  for (int s = 2; s <= tile_splits(c, tokens, heads); s *= 2)
-    if (tiled_in(s) < tiled_in(best)) best = s;
-  const double tiled = tiled_in(best);
-  return tiled < one_by_one ? Tiles{tile, best} : Tiles{0, 1};
-}
-}  // namespace
-
-// Shares of a token's blocks: so many that about 1024 workgroups (4 for each compute unit) are at work, so that those of
-// long sequences have company to the end; but where a wave would have fewer than 4 steps, no more than are at work at
-// once, since another round of workgroups costs more than it shares out (732 tokens of a head of 192 over 4 blocks of
-// 128: 2 shares 53 us and the join, 1 share 31; 22 tokens of 2 heads over lists of 64 blocks that are nearly empty: 24
-// shares 24 us, 11 shares 8).  A wave has a step of its own at least, and there are at most 64 shares (the lanes of
-// attend_join).  Where all blocks are 192 KiB or less, 48 to a wave, they are not shared out: the join, a launch of its
-// own, would take longer (4 tokens of 8 heads of 128 in 16 bits, a call: 4 blocks of 32 KiB 12.5 us with and 9.3
-// without, 8 11 to 12.5 and 11.1 to 12.3, 16 12.3 and 20).
-int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
-  const int64_t units = (int64_t)tokens * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
-  if (units == 0) return 1;
-  const int step = c.dtype == SDNN_F32 ? 16 : 32;
-  const int64_t steps = (int64_t)blocks * (c.block / step), most = (steps + kWaves - 1) / kWaves;
-  if (blocks * 2ll * c.block * c.head_dim * dtype_bytes(c.dtype) <= 192 * 1024) return 1;
-  int64_t wanted = (1024 + units - 1) / units;
-  if (steps < 4 * kWaves * wanted) wanted = 256 * attend_waves((c.head_dim + 15) / 16) / units;
-  const int64_t s = wanted < most ? wanted : most;
-  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
-}
-
-int64_t attend_floats(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
-  const int s = std::max(attend_splits(c, tokens, heads, blocks), tile_splits(c, tokens, heads));
-  return s > 1 ? (int64_t)s * tokens * heads * (c.head_dim + 2) : 0;
-}
 
 hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const sdnn_heads& q,
                          const sdnn_heads& o, const int32_t* chosen, int32_t blocks, float scale,
@@ -892,18 +791,19 @@ hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.heads = q.heads, a.kv_heads = c.kv_heads, a.group = q.heads / c.kv_heads;
   a.head_tiles = (a.group + kRows - 1) / kRows;
   a.head_dim = c.head_dim, a.block = c.block;
-  const Tiles tiles = tiles_of(c, t.tokens, t.sequences, t.max_blocks, q.heads, chosen ? blocks : 0);
-  a.tile_tokens = tiles.tokens;
-  a.blocks = blocks, a.splits = a.tile_tokens ? tiles.splits : attend_splits(c, t.tokens, q.heads, blocks);
+  const AttendShape shape = attend_shape(c, t, q.heads, chosen ? blocks : 0);
+  if (!launchable(shape.groups, shape.threads) || !launchable(shape.join_groups, 256)) return hipErrorInvalidConfiguration;
+  a.tile_tokens = shape.tile_tokens;
+  a.blocks = blocks, a.splits = shape.splits;
   // (a scale of 0 makes all scores equal: so does one that is too small to part them)
   a.scale2 = fmaxf(fabsf(scale), 1e-30f) * 1.44269504f;
   a.negate = scale < 0.0f;
   const int e = dtype_bytes(c.dtype), piece = 16 / e;
   a.q_aligned = (uintptr_t)q.data % 16 == 0 && q.token_stride % piece == 0 && q.head_stride % piece == 0;
   a.o_aligned = (uintptr_t)o.data % (4 * e) == 0 && o.token_stride % 4 == 0 && o.head_stride % 4 == 0;
-  if (c.dtype == SDNN_F32) return start_dim<float>(a, stream);
-  if (c.dtype == SDNN_F16) return start_dim<_Float16>(a, stream);
-  return start_dim<__bf16>(a, stream);
+  if (c.dtype == SDNN_F32) return start_dim<float>(a, shape, stream);
+  if (c.dtype == SDNN_F16) return start_dim<_Float16>(a, shape, stream);
+  return start_dim<__bf16>(a, shape, stream);
 }
 
 }  // namespace sdnn

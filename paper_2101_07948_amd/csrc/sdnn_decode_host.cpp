@@ -16,9 +16,6 @@ bool bad_align(const void* p) { return (uintptr_t)p % 16 != 0; }
 // Strides in elements: not negative, and small enough that a row number times one fits 64 bits.
 bool bad_stride(int64_t s) { return s < 0 || s >= (int64_t)1 << 36; }
 
-// A launch's workgroups have to be countable in 32 bits (a margin below 2^31).
-constexpr int64_t kMaxGrid = (int64_t)1 << 30;
-
 sdnn_status check_cache(const sdnn_block_cache* c) {
   if (!c) return SDNN_ERR_NULL;
   if (bad_dtype(c->dtype) || c->pages < 0 || c->pages > INT32_MAX) return SDNN_ERR_DIM;
@@ -67,7 +64,10 @@ bool distinct_rows(const sdnn_heads& a, int32_t tokens, int32_t head_dim) {
   return (tokens < 2 || a.token_stride != 0) && (a.heads < 2 || a.head_stride >= head_dim);
 }
 
-sdnn_status result(hipError_t e) { return e == hipSuccess ? SDNN_OK : SDNN_ERR_HIP; }
+// (A call of more threads than a launch has is refused before it.)
+sdnn_status result(hipError_t e) {
+  return e == hipSuccess ? SDNN_OK : e == hipErrorInvalidConfiguration ? SDNN_ERR_DIM : SDNN_ERR_HIP;
+}
 
 #define SDNN_CHECK(call)                  \
   do {                                    \
@@ -114,7 +114,6 @@ sdnn_status sdnn_cache_append(const sdnn_block_cache* cache, const sdnn_tokens* 
   if (!cache->means != !cache->mean_scales) return SDNN_ERR_NULL;
   if (tokens->tokens == 0) return SDNN_OK;
   if (cache->pages > 0 && (!cache->k_pages || !cache->v_pages)) return SDNN_ERR_NULL;
-  if (tokens->tokens * ((int64_t)cache->kv_heads + 1) > kMaxGrid) return SDNN_ERR_DIM;
   return result(launch_append(*cache, *tokens, *k, *v, rotation, q, q_out, (hipStream_t)stream));
 }
 
@@ -132,7 +131,6 @@ sdnn_status sdnn_block_select(const sdnn_block_cache* cache, const sdnn_tokens* 
   if (!chosen) return SDNN_ERR_NULL;
   if (cache->pages > 0 && (!cache->means || !cache->mean_scales)) return SDNN_ERR_NULL;
   if (cache->pages == 0) return SDNN_ERR_DIM;  // the kernel reads the summary of page 0 in a missing page's place
-  if (tokens->tokens * (int64_t)cache->kv_heads > kMaxGrid) return SDNN_ERR_DIM;
   return result(launch_select(*cache, *tokens, *q, blocks, sink, local, chosen, (hipStream_t)stream));
 }
 
@@ -164,7 +162,6 @@ sdnn_status sdnn_block_attend(const sdnn_block_cache* cache, const sdnn_tokens* 
   if (need > 0 && (overlap(workspace, need * 4, lse, (int64_t)tokens->tokens * q->heads * 4) ||
                    workspace == q->data || workspace == o->data))
     return SDNN_ERR_DIM;
-  if (tokens->tokens * (int64_t)q->heads > kMaxGrid) return SDNN_ERR_DIM;
   return result(launch_attend(*cache, *tokens, *q, *o, chosen, blocks, scale, lse, workspace,
                               (hipStream_t)stream));
 }

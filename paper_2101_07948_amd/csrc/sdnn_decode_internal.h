@@ -37,9 +37,6 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
                          const sdnn_heads* q_out, hipStream_t stream);
 hipError_t launch_select(const sdnn_block_cache& c, const sdnn_tokens& t, const sdnn_heads& q,
                          int32_t blocks, int32_t sink, int32_t local, int32_t* chosen, hipStream_t stream);
-// Workgroups that share a token's blocks (1: no workspace is used).
-int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks);
-int64_t attend_floats(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks);
 hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const sdnn_heads& q,
                          const sdnn_heads& o, const int32_t* chosen, int32_t blocks, float scale,
                          float* lse, float* workspace, hipStream_t stream);

@@ -5,9 +5,23 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <cmath>
+
 #include "sdnn_decode_internal.h"
 
 namespace sdnn {
+
+// A launch has fewer than 2^32 threads.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups <= 0xffffffffll / threads; }
+
+// ---------------------------------------------------------------- rotation, append
+
+constexpr int kRopeThreads = 256;  // of both kernels
+// Tokens of a workgroup (8192 tokens of 32 heads of 128: 1, 2, 4 and 8 tokens to a workgroup 29.3, 29.1, 28.9 and 39.1 us;
+// few tokens fill the device only one by one).
+inline int rope_tile(int32_t tokens) { return tokens >= 2048 ? 4 : 1; }
+inline int64_t rope_groups(int32_t tokens) { return ((int64_t)tokens + rope_tile(tokens) - 1) / rope_tile(tokens); }
 
 constexpr int kWindow = 64;       // tokens of an append workgroup, the most
 constexpr int kTileBytes = 32768; // the most of a window's keys
@@ -57,6 +71,161 @@ inline AppendShape append_shape(const sdnn_block_cache& c, const sdnn_tokens& t)
     if (with > s.lds) s.lds = with;
   }
   s.windows = ((int64_t)t.tokens + s.window - 1) / s.window + (s.window > 1);  // one more where they are shifted
+  return s;
+}
+
+// ---------------------------------------------------------------- choice of blocks
+
+constexpr int kWaveKeys = 16;  // keys of a lane where a wave chooses alone: up to 1024 blocks
+
+struct SelectShape {
+  int32_t tile;       // tokens of a workgroup
+  int32_t per_token;  // rows of a token
+  int32_t threads;
+  int64_t groups;
+};
+
+inline SelectShape select_shape(const sdnn_block_cache& c, const sdnn_tokens& t, int32_t heads) {
+  SelectShape s = {};
+  const int group = heads / c.kv_heads;
+  // A workgroup has several tokens where most of them are of one sequence and a wave can select alone: so
+  // many that their rows fill two matrix operands (2048 tokens of 4 queries to a head over 512 blocks: one operand
+  // 44 us, two 38, four 51, whose LDS leaves fewer workgroups to a compute unit), their keys at most 64 KiB of
+  // LDS, and that the device is full.
+  // Otherwise it has one token, and so many waves that each has some blocks.
+  int rows = 1;
+  while (rows < group && rows < 16) rows *= 2;
+  const bool tiles = t.tokens >= (int64_t)16 * t.sequences && t.max_blocks <= 64 * kWaveKeys &&
+                     (int64_t)(t.tokens / (16 / rows)) * c.kv_heads >= 512 && group <= 16;
+  s.tile = 1;
+  if (tiles) {
+    s.tile = 16 / rows;
+    while (s.tile * rows < 32 && s.tile * 2 * t.max_blocks <= 16384 &&
+           (int64_t)(t.tokens / (s.tile * 2)) * c.kv_heads >= 1024)
+      s.tile *= 2;
+  }
+  s.per_token = tiles ? rows : (group + 15) & ~15;
+  s.threads = 64;
+  while (s.threads < 1024 && s.threads < t.max_blocks) s.threads *= 2;
+  if (tiles) s.threads = 256;
+  s.groups = ((int64_t)t.tokens + s.tile - 1) / s.tile * c.kv_heads;
+  return s;
+}
+
+// ---------------------------------------------------------------- attention
+
+constexpr int kWaves = 4;      // of a workgroup of attend_kernel
+constexpr int kTileWaves = 8;  // and of attend_tiles
+constexpr int kRows = 16;      // queries of a tile: the columns of one matrix instruction
+constexpr int kFewParts = 8;   // that attend_join_few joins
+
+// Waves of a SIMD that the registers of attend_kernel leave room for, and so its workgroups at work at once on a compute
+// unit, for heads of up to 16 * tiles values.  (For the compiler a bound: without one it takes registers of both kinds
+// and leaves room for one wave less.  3 waves fit for heads of 128 in 16 bits too, but read worse: 64 tokens of 8 heads
+// over 32 blocks of 64 tokens, 537 MB, 107 us with 3 and 95 with 2.)
+constexpr int attend_waves(int tiles) { return tiles <= 4 ? 4 : tiles <= 6 ? 3 : tiles <= 12 ? 2 : 1; }
+
+// How attend_tiles takes a call: tokens of a wave's tile (a token's queries take a power of two of its 16 rows), and
+// shares of the blocks; tokens 0: attend_kernel does.
+struct Tiles {
+  int tokens, splits;
+};
+inline int tile_of(const sdnn_block_cache& c, int32_t heads) {
+  int rows = 1;
+  while (rows < heads / c.kv_heads && rows < kRows) rows *= 2;
+  return kRows / rows;
+}
+inline int64_t tile_groups(const sdnn_block_cache& c, int32_t tokens, int32_t heads) {
+  const int each = tile_of(c, heads) * kTileWaves;
+  return ((int64_t)tokens + each - 1) / each * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
+}
+constexpr int64_t kTileRoom = 512;  // workgroups at work at once
+// The most shares that a call of so many tokens is split into.
+inline int tile_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads) {
+  const int64_t groups = tile_groups(c, tokens, heads);
+  int s = 1;
+  while (s < kFewParts && tokens >= 16 && groups * 2 * s <= kTileRoom) s *= 2;
+  return s;
+}
+
+// attend_tiles serves a call where many tokens of a sequence are neighbours and it is estimated to be faster.
+// attend_kernel reads every token's blocks from L2, at about 8 TB/s (16384 heads of 16 blocks of 32 KiB:
+// 994 us; 8760 of 3 of 128 KiB: 683).  attend_tiles takes its workgroups' unions of blocks, 512 workgroups at a
+// time, two to a compute unit, at about 3.7 us for 32 KiB, or 2.2 where they have a unit each (38 and 133 of them: 142 and
+// 288 us; the matrix instructions of 32 bits take four times as long).  How large a union is depends on the lists:
+// between three of them, where neighbours choose alike, and what lists that have nothing in common cover (107 tokens of
+// 4 of 468 blocks of 4 KiB, 12 heads: 280 blocks, 74 us; one by one 20), whose geometric mean is taken.  Where few
+// workgroups leave compute units idle the blocks are shared out, and the parts joined at the rate of a copy (512 tokens
+// at the end of 8512, 8 heads of 128: 1 share 288 us, 4 shares 123 and 8 to join; 900 tokens of a sequence's first 900,
+// whose longest lists have 15 blocks: 41, and 2 shares 33 and 11 to join).
+inline Tiles tiles_of(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads,
+                      int32_t chosen) {
+  if (max_blocks > 1 << 20 || tokens < (int64_t)16 * sequences) return {0, 1};
+  const int tile = tile_of(c, heads), head_tiles = (heads / c.kv_heads + kRows - 1) / kRows;
+  const double page = 2.0 * c.block * c.head_dim * dtype_bytes(c.dtype);
+  const int each = chosen > 0 && chosen < max_blocks ? chosen : max_blocks;
+  const double few = chosen > 0 && chosen < max_blocks / 3 ? 3.0 * chosen : max_blocks;
+  const double many = max_blocks * (1.0 - std::pow(1.0 - (double)each / max_blocks, std::min(tokens, tile * kTileWaves)));
+  const double all = few < many ? std::sqrt(few * many) : few;
+  const double groups = (double)tile_groups(c, tokens, heads);
+  const double one_by_one = (double)tokens * c.kv_heads * head_tiles * each * page / 8e6;
+  const double parts = 8.0 * tokens * heads * (c.head_dim + 2) / 4e6;
+  const auto tiled_in = [&](int shares) {
+    const double at_once = std::min(std::max(groups * shares / 256, 1.0), 2.0), rounds = std::max(groups * shares / kTileRoom, 1.0);
+    const double block = page / 32768 * (0.7 + 1.5 * at_once * (c.dtype == SDNN_F32 ? 4 : 1));
+    return rounds * all / shares * block + (shares > 1 ? shares * parts + 5 : 0.0);
+  };
+  int best = 1;
+  for (int s = 2; s <= tile_splits(c, tokens, heads); s *= 2)
+    if (tiled_in(s) < tiled_in(best)) best = s;
+  const double tiled = tiled_in(best);
+  return tiled < one_by_one ? Tiles{tile, best} : Tiles{0, 1};
+}
+
+// Shares of a token's blocks: so many that about 1024 workgroups (4 for each compute unit) are at work, so that those of
+// long sequences have company to the end; but where a wave would have fewer than 4 steps, no more than are at work at
+// once, since another round of workgroups costs more than it shares out (732 tokens of a head of 192 over 4 blocks of
+// 128: 2 shares 53 us and the join, 1 share 31; 22 tokens of 2 heads over lists of 64 blocks that are nearly empty: 24
+// shares 24 us, 11 shares 8).  A wave has a step of its own at least, and there are at most 64 shares (the lanes of
+// attend_join).  Where all blocks are 192 KiB or less, 48 to a wave, they are not shared out: the join, a launch of its
+// own, would take longer (4 tokens of 8 heads of 128 in 16 bits, a call: 4 blocks of 32 KiB 12.5 us with and 9.3
+// without, 8 11 to 12.5 and 11.1 to 12.3, 16 12.3 and 20).
+inline int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
+  const int64_t units = (int64_t)tokens * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
+  if (units == 0) return 1;
+  const int step = c.dtype == SDNN_F32 ? 16 : 32;
+  const int64_t steps = (int64_t)blocks * (c.block / step), most = (steps + kWaves - 1) / kWaves;
+  if (blocks * 2ll * c.block * c.head_dim * dtype_bytes(c.dtype) <= 192 * 1024) return 1;
+  int64_t wanted = (1024 + units - 1) / units;
+  if (steps < 4 * kWaves * wanted) wanted = 256 * attend_waves((c.head_dim + 15) / 16) / units;
+  const int64_t s = wanted < most ? wanted : most;
+  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+}
+
+inline int64_t attend_floats(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
+  const int s = std::max(attend_splits(c, tokens, heads, blocks), tile_splits(c, tokens, heads));
+  return s > 1 ? (int64_t)s * tokens * heads * (c.head_dim + 2) : 0;
+}
+
+struct AttendShape {
+  int32_t tile_tokens;  // 0: attend_kernel; else attend_tiles, tokens of a wave's tile
+  int32_t splits;
+  int64_t groups;
+  int32_t threads;
+  int64_t join_groups;  // of 256 threads; 0: no parts
+};
+
+// (chosen: blocks of a token's list; 0: all of them)
+inline AttendShape attend_shape(const sdnn_block_cache& c, const sdnn_tokens& t, int32_t heads, int32_t chosen) {
+  AttendShape s = {};
+  const Tiles tiles = tiles_of(c, t.tokens, t.sequences, t.max_blocks, heads, chosen);
+  s.tile_tokens = tiles.tokens;
+  s.splits = tiles.tokens ? tiles.splits : attend_splits(c, t.tokens, heads, chosen > 0 ? chosen : t.max_blocks);
+  s.threads = 64 * (tiles.tokens ? kTileWaves : kWaves);
+  const int head_tiles = (heads / c.kv_heads + kRows - 1) / kRows;
+  s.groups = s.splits * (tiles.tokens ? tile_groups(c, t.tokens, heads) : (int64_t)t.tokens * head_tiles * c.kv_heads);
+  const int64_t rows = (int64_t)t.tokens * heads;
+  s.join_groups = s.splits == 1 ? 0 : s.splits <= kFewParts ? (rows * (c.head_dim / 4) + 255) / 256 : rows;
   return s;
 }
 

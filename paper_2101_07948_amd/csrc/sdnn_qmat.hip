@@ -19,8 +19,8 @@ __host__ __device__ constexpr int bit_of(int i) { return (3 + 4 * (i / 2) + 16 *
 constexpr int kMaxWaves = 16;
 
 __global__ __launch_bounds__(256) void qmat_pack(const uint8_t* packed, int32_t M, int32_t K, int32_t chunks,
-                                                 int64_t dwords, uint32_t* out) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;  // [tile][chunk][lane][j]
+                                                 int64_t first, int64_t dwords, uint32_t* out) {
+  const int64_t at = first + (int64_t)blockIdx.x * 256 + threadIdx.x;  // [tile][chunk][lane][j]
   if (at >= dwords) return;
   const int j = at & 3, lane = (at >> 2) & 63;
   const int64_t tc = at >> 8;
@@ -48,8 +48,8 @@ __global__ __launch_bounds__(256) void qmat_pack(const uint8_t* packed, int32_t 
 // whole chunks, or chunks; `inner`: groups of a chunk, or 1.
 __global__ __launch_bounds__(256) void qmat_pack_meta(const uint8_t* scales, int32_t bytes, const uint8_t* zeros,
                                                       int32_t M, int32_t groups, int32_t outer, int32_t inner,
-                                                      int64_t count, uint8_t* out) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+                                                      int64_t first, int64_t count, uint8_t* out) {
+  const int64_t at = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= count) return;
   const int64_t to = at / (kQTileRows * inner);
   const int64_t row = to / outer * kQTileRows + at / inner % kQTileRows;
@@ -370,13 +370,16 @@ hipError_t start(const QmatArgs& a, int group, hipStream_t stream) {
 hipError_t launch_qmat_pack(const sdnn_qmat_s& w, const uint8_t* packed, const void* scales,
                             const uint8_t* zeros, hipStream_t stream) {
   const int64_t dwords = qmat_weight_bytes(w) / 4, entries = scales_of(w);
-  qmat_pack<<<(unsigned)((dwords + 255) / 256), 256, 0, stream>>>(
-      packed, w.M, w.K, w.chunks, dwords, reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(w.weights)));
+  constexpr int64_t most = (int64_t)1 << 31;  // threads of a launch
+  for (int64_t first = 0; first < dwords; first += most)
+    qmat_pack<<<(unsigned)((std::min(dwords - first, most) + 255) / 256), 256, 0, stream>>>(
+        packed, w.M, w.K, w.chunks, first, dwords, reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(w.weights)));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  qmat_pack_meta<<<(unsigned)((entries + 255) / 256), 256, 0, stream>>>(
-      static_cast<const uint8_t*>(scales), dtype_bytes(w.scale_dtype), zeros, w.M, groups_of(w), metas_of(w), inner_of(w), entries,
-      const_cast<uint8_t*>(w.meta));
+  for (int64_t first = 0; first < entries; first += most)
+    qmat_pack_meta<<<(unsigned)((std::min(entries - first, most) + 255) / 256), 256, 0, stream>>>(
+        static_cast<const uint8_t*>(scales), dtype_bytes(w.scale_dtype), zeros, w.M, groups_of(w), metas_of(w), inner_of(w),
+        first, entries, const_cast<uint8_t*>(w.meta));
   return hipGetLastError();
 }
 

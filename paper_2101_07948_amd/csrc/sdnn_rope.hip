@@ -7,7 +7,7 @@
 namespace sdnn {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kRopeThreads;
 
 struct RopeRows {
   const void* x;
@@ -152,9 +152,7 @@ RopeRows rope_args(const sdnn_heads& x, const sdnn_heads& y, int dtype, int32_t 
   const int values = a.vec * (layout == SDNN_ROPE_INTERLEAVED ? 2 : 1);
   a.x_aligned = rows_aligned(x.data, x.token_stride, x.head_stride, values, dtype);
   a.y_aligned = rows_aligned(y.data, y.token_stride, y.head_stride, values, dtype);
-  // (8192 tokens of 32 heads of 128: 1, 2, 4 and 8 tokens to a workgroup 29.3, 29.1, 28.9 and 39.1 us; few tokens
-  // fill the device only one by one)
-  a.tile = tokens >= 2048 ? 4 : 1;
+  a.tile = rope_tile(tokens);
   return a;
 }
 
@@ -436,12 +434,12 @@ hipError_t by_type(int dtype, int layout, const F& f) {
 
 hipError_t launch_rope(const sdnn_heads& x, const sdnn_heads& y, int dtype, int32_t tokens, int32_t head_dim,
                        const int32_t* pos, const sdnn_rotation& r, bool inverse, hipStream_t stream) {
+  if (!launchable(rope_groups(tokens), kThreads)) return hipErrorInvalidConfiguration;
   RopeRows a = rope_args(x, y, dtype, tokens, head_dim, pos, &r);
   if (inverse) a.inverse = 1;
-  const int blocks = (tokens + a.tile - 1) / a.tile;
   const size_t lds = (size_t)a.tile * a.pairs * sizeof(float2);
   return by_type(dtype, r.layout, [&](auto t, auto il) {
-    rope_kernel<decltype(t), decltype(il)::value><<<blocks, kThreads, lds, stream>>>(a);
+    rope_kernel<decltype(t), decltype(il)::value><<<(unsigned)rope_groups(tokens), kThreads, lds, stream>>>(a);
     return hipGetLastError();
   });
 }
@@ -454,7 +452,7 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   if (q && q->heads > 0) {
     a.q = rope_args(*q, *q_out, c.dtype, t.tokens, c.head_dim, t.pos, r);
     a.q.seq = t.seq, a.q.sequences = t.sequences;
-    q_blocks = (t.tokens + a.q.tile - 1) / a.q.tile;
+    q_blocks = rope_groups(t.tokens);
   }
   a.k = k.data, a.k_token = k.token_stride, a.k_head = k.head_stride;
   a.v = v.data, a.v_token = v.token_stride, a.v_head = v.head_stride;
@@ -466,6 +464,8 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.kv_heads = c.kv_heads, a.head_dim = c.head_dim, a.block = c.block;
   const int size = dtype_bytes(c.dtype), layout = r ? r->layout : SDNN_ROPE_HALF;
   const AppendShape shape = append_shape(c, t);
+  const int64_t blocks = shape.windows * c.kv_heads + q_blocks;
+  if (!launchable(blocks, kThreads)) return hipErrorInvalidConfiguration;
   a.window = shape.window, a.before = shape.before, a.passes = shape.passes;
   // The keys' units are 16-byte ones where windows have many and the head divides by them.
   const int wide = 16 / size / (layout == SDNN_ROPE_INTERLEAVED ? 2 : 1);
@@ -477,7 +477,6 @@ hipError_t launch_append(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   size_t lds = shape.lds;  // or the queries' cosines and sines
   if (lds < (size_t)a.q.tile * a.q.pairs * sizeof(float2)) lds = (size_t)a.q.tile * a.q.pairs * sizeof(float2);
   a.kv_blocks = (int32_t)(shape.windows * c.kv_heads);
-  const int64_t blocks = a.kv_blocks + q_blocks;
   return by_type(c.dtype, layout, [&](auto ty, auto il) {
     typedef decltype(ty) T;
     constexpr bool IL = decltype(il)::value;

@@ -1,5 +1,6 @@
 // The choice of blocks by the score of their summaries.
 #include "sdnn_decode_device.h"
+#include "sdnn_decode_shape.h"
 
 namespace sdnn {
 namespace {
@@ -166,7 +167,6 @@ __device__ __forceinline__ void wave_choose(const uint32_t* keys, int count, uin
 constexpr int kMaxWaves = 16;
 constexpr int kUnit = 32;
 constexpr int kMaxTile = 32;
-constexpr int kWaveKeys = 16;  // keys of a lane where a wave chooses alone: up to 1024 blocks
 
 struct GroupLds {
   uint32_t top[64];       // of the keys whose number is l modulo 64
@@ -529,32 +529,15 @@ hipError_t launch_select(const sdnn_block_cache& c, const sdnn_tokens& t, const 
   a.kv_heads = c.kv_heads, a.group = q.heads / c.kv_heads, a.head_dim = c.head_dim;
   a.block_shift = __builtin_ctz(c.block);
   a.blocks = blocks, a.sink = sink, a.local = local;
-  // A workgroup has several tokens where most of them are of one sequence and a wave can select alone: so
-  // many that their rows fill two matrix operands (2048 tokens of 4 queries to a head over 512 blocks: one operand
-  // 44 us, two 38, four 51, whose LDS leaves fewer workgroups to a compute unit), their keys at most 64 KiB of
-  // LDS, and that the device is full.
-  // Otherwise it has one token, and so many waves that each has some blocks.
-  int rows = 1;
-  while (rows < a.group && rows < 16) rows *= 2;
-  const bool tiles = t.tokens >= (int64_t)16 * t.sequences && t.max_blocks <= 64 * kWaveKeys &&
-                     (int64_t)(t.tokens / (16 / rows)) * c.kv_heads >= 512 && a.group <= 16;
-  a.tile = 1;
-  if (tiles) {
-    a.tile = 16 / rows;
-    while (a.tile * rows < 32 && a.tile * 2 * t.max_blocks <= 16384 &&
-           (int64_t)(t.tokens / (a.tile * 2)) * c.kv_heads >= 1024)
-      a.tile *= 2;
-  }
-  a.per_token = tiles ? rows : (a.group + 15) & ~15;
+  const SelectShape shape = select_shape(c, t, q.heads);
+  if (!launchable(shape.groups, shape.threads)) return hipErrorInvalidConfiguration;
+  a.tile = shape.tile, a.per_token = shape.per_token;
   a.q_aligned = (uintptr_t)q.data % (4 * dtype_bytes(c.dtype)) == 0 && q.token_stride % 4 == 0 && q.head_stride % 4 == 0;
-  int threads = 64;
-  while (threads < 1024 && threads < t.max_blocks) threads *= 2;
-  if (tiles) threads = 256;
   a.stride = (t.max_blocks + 63) & ~63;
   a.dtype = c.dtype;
-  if (a.head_dim <= 64) return start_rows<1>(a, threads, stream);
-  if (a.head_dim <= 128) return start_rows<2>(a, threads, stream);
-  return start_rows<4>(a, threads, stream);
+  if (a.head_dim <= 64) return start_rows<1>(a, shape.threads, stream);
+  if (a.head_dim <= 128) return start_rows<2>(a, shape.threads, stream);
+  return start_rows<4>(a, shape.threads, stream);
 }
 
 }  // namespace sdnn

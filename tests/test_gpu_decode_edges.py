@@ -147,3 +147,24 @@ def check_q4(M, K, N, group, dtype, scale_dtype=torch.float32, zeros=True, seed=
 @pytest.mark.parametrize("K,group", [(200, 2 ** 31 - 128), (70, 2 ** 31 - 128), (1000, 1 << 30)])
 def test_q4_of_one_long_group(dtype, K, group):
     check_q4(40, K, 3, group, dtype)
+
+
+def test_q4_of_more_weights_than_a_launch_has_threads():
+    """2^32 and more words of weights, 16 GiB: the first and the last rows, and some between."""
+    M, K, group = 2 ** 18 + 1, 2 ** 17, 2 ** 17
+    packed = torch.zeros((M, K // 2), dtype=torch.uint8, device=DEV)
+    rows = [0, 1, 2 ** 17 - 1, 2 ** 17, 2 ** 18 - 1, 2 ** 18]
+    packed[rows] = torch.randint(0, 256, (len(rows), K // 2), generator=gen(23), device=DEV, dtype=torch.uint8)
+    scales = torch.rand((M, 1), generator=gen(24), device=DEV) + 0.5
+    x, out = randn(25, (K, 1), torch.float16), torch.empty((M, 1), dtype=torch.float16, device=DEV)
+    with sd.Q4Plan(packed, scales, K=K, group=group) as plan:
+        plan.matvec(x, out)
+        torch.cuda.synchronize()
+    y, tol = od.q4(packed[rows].cpu().numpy(), od.f64(scales[rows]), None, K, group, od.f64(x))
+    close(out[rows], y, tol + od.U[torch.float16] * np.abs(y) * 1.01 + od.TINY[torch.float16], "4-bit product")
+    zero, _ = od.q4(np.zeros((1, K // 2), np.uint8), np.ones((1, 1)), None, K, group, od.f64(x))
+    other = torch.ones(M, dtype=torch.bool, device=DEV)
+    other[rows] = False
+    want = scales[other].double() * float(zero[0, 0])
+    bound = (K + 16) * 2.0 ** -24 * 16 * float(x.double().abs().sum()) * scales[other].double()
+    assert ((out[other].double() - want).abs() <= bound + 2.0 ** -10 * want.abs()).all()
