@@ -53,14 +53,16 @@ def build(verbose: bool = False) -> str:
 
 HOST_SANITIZED_SOURCES = [os.path.join(HERE, "csrc", "sdnn_host.cpp"),
                           os.path.join(HERE, "csrc", "sdnn_quad_pack.cpp"),
-                          os.path.join(HERE, "csrc", "sdnn_launch_stubs.cpp")]
+                          os.path.join(HERE, "csrc", "sdnn_launch_stubs.cpp"),
+                          os.path.join(HERE, "csrc", "sdnn_decode_host.cpp"),
+                          os.path.join(HERE, "csrc", "sdnn_decode_launch_stubs.cpp")]
 
 
 def build_host_sanitized(out: str) -> str:
     """The host code alone (CSR validation, row orders, packing and its self-check, the
     C ABI's argument checks) built for the CPU under AddressSanitizer and
     UndefinedBehaviorSanitizer, with the kernel launchers replaced by stubs that fail
-    (sdnn_launch_stubs.cpp).  It serves the host-only entry points; load it in a process
+    (sdnn_launch_stubs.cpp, sdnn_decode_launch_stubs.cpp).  It serves the host-only entry points; load it in a process
     started with the sanitizer runtime preloaded (tests/test_host_sanitized.py)."""
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
     cmd = ["g++", "-std=c++17", "-O1", "-g", "-fPIC", "-shared", "-fno-omit-frame-pointer",

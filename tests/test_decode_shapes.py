@@ -59,6 +59,7 @@ def shapes(tmp_path_factory):
     src.write_text(SOURCE)
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
     subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-w",
+                    *os.environ.get("CXXFLAGS", "").split(),
                     "-I" + os.path.join(rocm, "include"), "-I" + os.path.join(ROOT, "paper_2101_07948_amd", "csrc"),
                     str(src), "-o", str(lib)], check=True)
     return ctypes.CDLL(str(lib))
