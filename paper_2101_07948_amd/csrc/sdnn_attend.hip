@@ -305,7 +305,7 @@ __global__ __launch_bounds__(kWaves * 64, attend_waves(CHUNKS * Step<T>::kPiece 
     const int mine = first_step + lane * deal;
     int id = -1, page_mine = -1;
     if (lane < (last - first_step + deal - 1) / deal) id = chosen ? chosen[mine >> shift] : mine >> shift;
-    const auto seen_of = [&](int id, int t0) { return p - id * a.block + 1 - t0; };
+    const auto seen_of = [&](int id, int t0) { return min(p - id * a.block - t0, a.block) + 1; };  // (p up to 2^31 - 1)
     const auto token_of = [&](int u) { return (u & ((1 << shift) - 1)) * N; };
     if (id >= 0 && id <= own && id < a.max_blocks && seen_of(id, token_of(mine)) > 0) page_mine = table[id];
     uint64_t todo = __ballot(page_mine >= 0 && page_mine < a.pages);
@@ -662,7 +662,7 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
     block_page = __builtin_amdgcn_readfirstlane((int32_t)low);
     if (block_page >= a.pages) block_page = -1;
     const bool mine = block_key != END && key() == block_key;
-    seen = mine && block_page >= 0 ? min(a.block, p - at.id * a.block + 1) : 0;
+    seen = mine && block_page >= 0 ? min(a.block - 1, p - at.id * a.block) + 1 : 0;
     if (mine) at.advance(a, h);
   };
   const int stage = min(STAGE, a.block), stages = a.block / stage;

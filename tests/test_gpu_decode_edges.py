@@ -130,6 +130,19 @@ def test_attend_takes_its_workspace_from_the_calls_stream(monkeypatch):
     assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
 
 
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("tokens", [2, 200])  # token by token, through tiles
+def test_attend_at_the_last_position(dtype, tokens):
+    """Positions up to 2^31 - 1: a token past its table's end sees all of its blocks."""
+    P, D, Hk, last = 64, 64, 4, 2 ** 31 - 1
+    cache, table = filled(17, 1, [5 * P], Hk, P, D, dtype)
+    pos = [last - i for i in range(tokens)]
+    q = randn(18, (tokens, Hk, D), dtype)
+    check_attend(cache, table, q, pos, [0] * tokens, oracle=od.attend)
+    chosen = np.tile(np.array([0, 1, 3, 4, -1, -1], np.int64), (tokens, Hk, 1))  # (the oracle's sums past 2^31)
+    check_attend(cache, table, q, pos, [0] * tokens, chosen, oracle=od.attend)
+
+
 # ---------------------------------------------------------------- 4-bit products
 
 def check_q4(M, K, N, group, dtype, scale_dtype=torch.float32, zeros=True, seed=21):
