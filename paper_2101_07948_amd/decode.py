@@ -164,12 +164,15 @@ class Rope:
             if rotated is None:
                 raise ValueError("rotated or frequencies is required")
             frequencies = rope_frequencies(rotated, base, scaling, factor, length, turns)
-        self.freq = torch.as_tensor(frequencies, dtype=torch.float64, device=device).contiguous()
-        if self.freq.dim() != 1 or (rotated is not None and self.freq.numel() * 2 != rotated):
+        freq = torch.as_tensor(frequencies, dtype=torch.float64, device=device).contiguous()
+        if freq.dim() != 1 or (rotated is not None and freq.numel() * 2 != rotated):
             raise ValueError("frequencies must hold one value for each rotated pair")
-        self.layout = layout
-        self._packed = _ROTATION.pack(self.freq.data_ptr(), self.freq.numel(), LAYOUTS[layout],
-                                      float(amplitude))
+        self._freq, self._layout = freq, layout
+        self._packed = _ROTATION.pack(freq.data_ptr(), freq.numel(), LAYOUTS[layout], float(amplitude))
+
+    # What the calls use is fixed with the object (another rotation is another Rope).
+    freq = property(lambda self: self._freq, doc="The frequencies (float64, on the device).")
+    layout = property(lambda self: self._layout)
 
     def apply(self, x, y, pos, inverse: bool = False, stream=None):
         """y = x (tokens, heads, head_dim) rotated to the positions pos (tokens, int32); by the
@@ -191,7 +194,8 @@ class BlockCache:
     keys of every full block.  The tensors are the caller's:
         k_pages (pages, kv_heads, block, head_dim), v_pages (pages, kv_heads, head_dim, block),
         means (pages, kv_heads, head_dim) int8, mean_scales (pages, kv_heads) float32;
-    those a program's calls do not use may be None.  Every call takes the tokens' positions
+    those a program's calls do not use may be None; a cache on other tensors is another
+    BlockCache.  Every call takes the tokens' positions
     pos and sequences seq (tokens, int32) and the block table (sequences, blocks, int32): the
     page of each sequence's blocks.  A token with pos < 0 is a filler: nothing is stored for it
     and its outputs are zero."""
@@ -217,8 +221,14 @@ class BlockCache:
         if means is not None:
             at[2] = _dense(means, "means", torch.int8, (pages, heads, dim))
             at[3] = _dense(mean_scales, "mean_scales", torch.float32, (pages, heads))
-        self.k_pages, self.v_pages, self.means, self.mean_scales = k_pages, v_pages, means, mean_scales
+        self._tensors = k_pages, v_pages, means, mean_scales
         self._at, self._packed = at, {}
+
+    # The calls use the tensors' addresses, which are taken once: the tensors cannot be replaced.
+    k_pages = property(lambda self: self._tensors[0])
+    v_pages = property(lambda self: self._tensors[1])
+    means = property(lambda self: self._tensors[2])
+    mean_scales = property(lambda self: self._tensors[3])
 
     @classmethod
     def empty(cls, pages: int, kv_heads: int, head_dim: int, block: int = 64, dtype=None, device="cuda"):

@@ -143,6 +143,20 @@ def test_attend_at_the_last_position(dtype, tokens):
     check_attend(cache, table, q, pos, [0] * tokens, chosen, oracle=od.attend)
 
 
+def test_tensors_whose_addresses_are_kept_cannot_be_replaced():
+    """A call would go on using the memory of the old one, which is freed."""
+    cache, rope = make_cache(0, 2, 1, 32, 16, torch.float32), sd.Rope(16)
+    for name in ("k_pages", "v_pages", "means", "mean_scales"):
+        kept = getattr(cache, name)
+        with pytest.raises(AttributeError):
+            setattr(cache, name, kept.clone())
+        assert getattr(cache, name) is kept
+    with pytest.raises(AttributeError):
+        rope.freq = rope.freq.clone()
+    with pytest.raises(AttributeError):
+        rope.layout = "interleaved"
+
+
 # ---------------------------------------------------------------- 4-bit products
 
 def check_q4(M, K, N, group, dtype, scale_dtype=torch.float32, zeros=True, seed=21):
