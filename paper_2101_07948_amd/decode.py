@@ -167,6 +167,7 @@ class Rope:
         freq = torch.as_tensor(frequencies, dtype=torch.float64, device=device).contiguous()
         if freq.dim() != 1 or (rotated is not None and freq.numel() * 2 != rotated):
             raise ValueError("frequencies must hold one value for each rotated pair")
+        _on_gpu(freq, "frequencies")  # (the kernels read them)
         self._freq, self._layout = freq, layout
         self._packed = _ROTATION.pack(freq.data_ptr(), freq.numel(), LAYOUTS[layout], float(amplitude))
 
