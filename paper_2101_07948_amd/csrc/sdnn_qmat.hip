@@ -10,12 +10,12 @@ namespace {
 
 // Layout of the weights: tiles of 16 rows, of these chunks of 128 columns, of these 16 bytes for
 // each of 64 lanes.  Lane l has row l & 15; its dword j holds columns 32 j + 8 (l / 16) + i of the
-// chunk, i = 0 ... 7: what the lane gives to matrix instruction j as its operand.  Columns 2 p and 2 p + 1 have
-// their 4 bits at bit 3 + 4 p of the dword's lower and upper half (turned by 12 for p = 3, where the upper ones
-// wrap around): after a shift and one mask they are the upper mantissa bits of two bf16 numbers 16 + n.  A wave reads
-// 1 KiB in one access.  The scales and zero points follow: [tile][group][16 rows] where groups are whole chunks,
-// else [tile][chunk][16 rows][group of the chunk], so that a lane has those of a chunk in one access (see metas_of).
-__host__ __device__ constexpr int bit_of(int i) { return (3 + 4 * (i / 2) + 16 * (i % 2)) % 32; }
+// chunk, i = 0 ... 7: what the lane gives to matrix instruction j as its operand.  Column i < 4 is in the lower half of
+// byte i, column 4 + i in the upper half: after a mask a byte n is the 8-bit float n 2^-9 (4 bits of exponent, 3 of
+// mantissa: 0 ... 7 are its subnormals, 8 ... 15 have the least exponent).  A wave reads 1 KiB in one access.  The scales
+// and zero points follow: [tile][group][16 rows] where groups are whole chunks, else [tile][chunk][16 rows][group of
+// the chunk], so that a lane has those of a chunk in one access (see metas_of).
+__host__ __device__ constexpr int bit_of(int i) { return i < 4 ? 8 * i : 8 * (i - 4) + 4; }
 constexpr int kMaxWaves = 16;
 
 __global__ __launch_bounds__(256) void qmat_pack(const uint8_t* packed, int32_t M, int32_t K, int32_t chunks,
@@ -36,9 +36,7 @@ __global__ __launch_bounds__(256) void qmat_pack(const uint8_t* packed, int32_t 
       for (int i = 0; 2 * i < K - k0; ++i) eight |= (uint32_t)from[i] << (8 * i);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t n = k0 + i < K ? eight >> (4 * i) & 15u : 0;
-      const int to = bit_of(i);
-      w |= n << to | (to > 28 ? n >> (32 - to) : 0);
+      w |= (k0 + i < K ? eight >> (4 * i) & 15u : 0) << bit_of(i);
     }
   }
   out[at] = w;
@@ -74,26 +72,20 @@ struct QmatArgs {
   int32_t scale_dtype, epi;
 };
 
-// Pair p of a dword's numbers, at bits AT and 16 + AT.
-template <int AT>
-__device__ __forceinline__ uint32_t pair_at(uint32_t w, int p) {
-  const int right = (3 + 4 * p - AT) & 31;
-  return right == 0 ? w : __builtin_amdgcn_alignbit(w, w, right);
-}
-
-// The matrix instruction of a type.  `weights`: the 8 numbers of a dword as 16 + n, two a mask: with 16 the 4 bits
-// are the upper ones of the mantissa.
+// The matrix instruction of a type.  `weights`: the 8 numbers of a dword, from the 8-bit floats that they are.
 template <typename T, typename V8>
 struct Op16 {
   typedef V8 type;
+  template <bool UPPER>
+  static __device__ __forceinline__ int32_t pair(uint32_t four) {
+    if constexpr (__is_same(T, _Float16))
+      return __builtin_bit_cast(int32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(four, 512.0f, UPPER));
+    else
+      return __builtin_bit_cast(int32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, 512.0f, UPPER));
+  }
   static __device__ __forceinline__ V8 weights(uint32_t w) {
-    constexpr bool HALF = __is_same(T, _Float16);
-    constexpr int AT = HALF ? 6 : 3;
-    constexpr uint32_t SIXTEEN = HALF ? 0x4c004c00u : 0x41804180u, MASK = 0x000f000fu << AT;
-    i32x4 v;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) v[p] = (int32_t)((pair_at<AT>(w, p) & MASK) | SIXTEEN);
-    return __builtin_bit_cast(V8, v);
+    const uint32_t lower = w & 0x0f0f0f0fu, upper = w >> 4 & 0x0f0f0f0fu;
+    return __builtin_bit_cast(V8, i32x4{pair<false>(lower), pair<true>(lower), pair<false>(upper), pair<true>(upper)});
   }
 };
 template <typename T>
@@ -234,9 +226,8 @@ struct Chunk {
 // A workgroup has 16 rows of W and up to TOKENS columns of x; its waves share the chunks, each with the next one
 // under way while it multiplies.  The columns go through LDS (a wave's own part), where they are turned into
 // operands: rows of the first operand are columns of x, columns of the second rows of W.  With n the 4-bit numbers,
-// a group adds s (sum (16 + n) x - (16 + z) sum x): both sums come from the matrix unit, the second with ones for
-// the numbers, and are scaled once a group.  The 16 costs a bit of the 32-bit sums, and saves half of the
-// instructions that make numbers of the bits.
+// a group adds s (sum n x - z sum x): both sums come from the matrix unit, the second with ones for the numbers, and are
+// scaled once a group (and chunk).  (With 16 + n and 16 + z in their place the sums were 2.5 times as inexact.)
 //   Row p of the operand is column p / 4 + 4 (p % 4) of x, so that up to four columns are in the first of a lane's
 // four results, up to eight in two; of four columns in 32 bits rows 4 t + part, and a lane adds its results.
 //   Reading the weights bounds it: 16384 x 8192 with one column in 16 bits 14.2 us, 69 MB at 4.9 TB/s, the rate of a
@@ -283,7 +274,7 @@ __global__ __launch_bounds__((kWavesOf<TOKENS, FEATURES> * 64)) void qmat_kernel
           sx = Op<T>::mfma(xv, ones, sx);
         }
       }
-      const float s = b.scale[i], z = b.zero[i] + 16.0f;
+      const float s = b.scale[i], z = b.zero[i];
       if (PACKED) {
         acc[0] = fmaf(s, fmaf(-z, (sx[0] + sx[1]) + sx[2], (d[0] + d[1]) + d[2]), acc[0]);
       } else {

@@ -195,3 +195,51 @@ def test_q4_of_more_weights_than_a_launch_has_threads():
     want = scales[other].double() * float(zero[0, 0])
     bound = (K + 16) * 2.0 ** -24 * 16 * float(x.double().abs().sum()) * scales[other].double()
     assert ((out[other].double() - want).abs() <= bound + 2.0 ** -10 * want.abs()).all()
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("M,K,N,group", [(512, 4096, 1, 4096), (300, 4096, 4, 1024), (300, 8192, 8, 8192), (256, 4096, 2, 128),
+                                         (256, 3072, 1, 64), (256, 2000, 3, 32)])
+def test_q4_is_as_exact_as_a_plain_sum_in_32_bits(M, K, N, group, zeros):
+    """The error against 64 bits, in the mean over the outputs, is at most that of adding the products
+    (n - z) s x one after the other, each sum rounded to 32 bits."""
+    packed, scales, z = random_q4(31, M, K, group, torch.float32, zeros)
+    if zeros:
+        z = torch.randint(6, 11, z.shape, generator=gen(32), device=DEV, dtype=torch.uint8)
+    x = randn(33, (K, N), torch.float32)
+    out = torch.empty((M, N), device=DEV)
+    with sd.Q4Plan(packed, scales, z, K=K, group=group) as plan:
+        plan.matvec(x, out)
+        torch.cuda.synchronize()
+    y, _ = od.q4(packed.cpu().numpy(), od.f64(scales), None if z is None else z.cpu().numpy(), K, group, od.f64(x))
+    col = np.arange(K) // group
+    n = od.unpack4(packed.cpu().numpy(), K) - (8.0 if z is None else z.cpu().numpy()[:, col])
+    w, xs = (n * od.f64(scales)[:, col]).astype(np.float32), x.cpu().numpy()
+    plain = np.zeros((M, N), np.float32)
+    for k in range(K):
+        plain += w[:, k, None] * xs[k]
+    ours, bound = np.sqrt(np.mean((od.f64(out) - y) ** 2)), np.sqrt(np.mean((plain - y) ** 2))
+    assert ours <= bound, (ours, bound)
+
+
+@pytest.mark.parametrize("M,K,N,group", [(512, 4096, 1, 128), (512, 3072, 4, 64)])
+def test_q4_sums_numbers_without_an_offset(M, K, N, group):
+    """The error against 64 bits, in the mean, is at most that of the formula's own sums, sum n x and z sum x of
+    128 columns or a shorter group, rounded to 32 bits every 16 columns, and added up in 32 bits."""
+    packed, scales, z = random_q4(34, M, K, group, torch.float32, True)
+    x = randn(35, (K, N), torch.float32)
+    out = torch.empty((M, N), device=DEV)
+    with sd.Q4Plan(packed, scales, z, K=K, group=group) as plan:
+        plan.matvec(x, out)
+        torch.cuda.synchronize()
+    y, _ = od.q4(packed.cpu().numpy(), od.f64(scales), z.cpu().numpy(), K, group, od.f64(x))
+    n, xs, sc, zs = od.unpack4(packed.cpu().numpy(), K), od.f64(x), od.f64(scales), z.cpu().numpy().astype(np.float64)
+    model, step, f32 = np.zeros((M, N), np.float32), min(group, 128), lambda v: v.astype(np.float32).astype(np.float64)
+    for k0 in range(0, K, step):
+        d, sx = np.zeros((M, N)), np.zeros(N)
+        for k in range(k0, k0 + step, 16):
+            d, sx = f32(d + n[:, k:k + 16] @ xs[k:k + 16]), f32(sx + xs[k:k + 16].sum(0))
+        g = k0 // group
+        model += (sc[:, g, None] * f32(d - zs[:, g, None] * sx)).astype(np.float32)
+    ours, bound = (np.sqrt(np.mean((v.astype(np.float64) - y) ** 2)) for v in (out.cpu().numpy(), model))
+    assert ours <= bound, (ours, bound)
