@@ -222,7 +222,7 @@ def test_q4_is_as_exact_as_a_plain_sum_in_32_bits(M, K, N, group, zeros):
     assert ours <= bound, (ours, bound)
 
 
-@pytest.mark.parametrize("M,K,N,group", [(512, 4096, 1, 128), (512, 3072, 4, 64)])
+@pytest.mark.parametrize("M,K,N,group", [(512, 4096, 1, 128), (400, 8192, 8, 1024), (512, 3072, 4, 64)])
 def test_q4_sums_numbers_without_an_offset(M, K, N, group):
     """The error against 64 bits, in the mean, is at most that of the formula's own sums, sum n x and z sum x of
     128 columns or a shorter group, rounded to 32 bits every 16 columns, and added up in 32 bits."""
