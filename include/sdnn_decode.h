@@ -185,6 +185,8 @@ sdnn_status sdnn_qmat_create(const uint8_t* packed, const void* scales, sdnn_dty
 /* y = epi(W x + bias) for the N <= 2^18 columns of x.  Value k of column n is
  * x[k * x_feature + n * x_column] and value m of column n y[m * y_feature + n * y_column]:
  * a K x N matrix as sdnn_spmm takes it has strides (N, 1), rows of tokens (1, K).
+ *   y's memory, from its first value to its last, holds none of x or bias; of tokens' rows that lie as
+ *   far apart (x_feature = y_feature = 1, x_column = y_column) the rows themselves do not meet.
  *   bias: device, M floats, or NULL.  The products are exact and are summed in 32 bits; x
  *   must be finite.  Made for few columns: the weights are read once for every 16 of them (8 in
  *   32 bits).

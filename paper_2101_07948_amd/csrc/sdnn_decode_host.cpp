@@ -56,6 +56,15 @@ bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
   return a0 < b0 + (uintptr_t)bbytes && b0 < a0 + (uintptr_t)abytes;
 }
 
+// The same of two sets of rows of a_row and b_row bytes, `rows` of each, stride bytes apart: columns of one buffer may lie
+// side by side.
+bool overlap_rows(const void* a, int64_t a_row, const void* b, int64_t b_row, int64_t rows, int64_t stride) {
+  if (!overlap(a, (rows - 1) * stride + a_row, b, (rows - 1) * stride + b_row)) return false;
+  if (rows < 2 || stride == 0) return true;
+  const int64_t between = (int64_t)((uintptr_t)b - (uintptr_t)a) % stride, off = between < 0 ? between + stride : between;
+  return off < a_row || off + b_row > stride;
+}
+
 bool same_rows(const sdnn_heads& a, const sdnn_heads& b) {
   return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
 }
@@ -217,7 +226,10 @@ sdnn_status sdnn_qmat_apply(sdnn_qmat w, const void* x, int64_t x_feature, int64
   if ((uintptr_t)x % e || (uintptr_t)y % e) return SDNN_ERR_DIM;
   const int64_t xbytes = ((w->K - 1) * x_feature + (N - 1) * x_column + 1) * e;
   const int64_t ybytes = ((w->M - 1) * y_feature + (N - 1) * y_column + 1) * e;
-  if (overlap(x, xbytes, y, ybytes) || overlap(bias, (int64_t)w->M * 4, y, ybytes)) return SDNN_ERR_DIM;
+  const bool meet = x_feature == 1 && y_feature == 1 && x_column == y_column
+                        ? overlap_rows(x, (int64_t)w->K * e, y, (int64_t)w->M * e, N, x_column * e)
+                        : overlap(x, xbytes, y, ybytes);
+  if (meet || overlap(bias, (int64_t)w->M * 4, y, ybytes)) return SDNN_ERR_DIM;
   int device = -1;
   if (hipGetDevice(&device) != hipSuccess) return SDNN_ERR_HIP;
   if (device != w->device) return SDNN_ERR_DEVICE;

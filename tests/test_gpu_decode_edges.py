@@ -243,3 +243,28 @@ def test_q4_sums_numbers_without_an_offset(M, K, N, group):
         model += (sc[:, g, None] * f32(d - zs[:, g, None] * sx)).astype(np.float32)
     ours, bound = (np.sqrt(np.mean((v.astype(np.float64) - y) ** 2)) for v in (out.cpu().numpy(), model))
     assert ours <= bound, (ours, bound)
+
+
+def test_q4_between_columns_of_one_buffer():
+    """Tokens' rows side by side in one buffer, as a fused layer keeps them; rows that do meet are refused."""
+    M, K, N, group = 40, 70, 5, 32
+    packed, scales, z = random_q4(36, M, K, group, torch.float32, True)
+    with sd.Q4Plan(packed, scales, z, K=K, group=group) as plan:
+        x = randn(37, (N, K), torch.float32)
+        want = torch.empty((N, M), device=DEV)
+        plan.matvec(x.t(), want.t())
+        for at, to in ((0, K), (M, 0), (M + 3, 1), (0, K + 11)):  # columns of x and of y
+            rows = torch.full((N, K + M + 11), 7.0, device=DEV)
+            rows[:, at:at + K] = x
+            before = rows.clone()
+            plan.matvec(rows[:, at:at + K].t(), rows[:, to:to + M].t())
+            before[:, to:to + M] = want
+            assert torch.equal(rows, before)
+        rows = torch.full((N, K + M), 7.0, device=DEV)
+        for at, to in ((0, K - 1), (M - 1, 0), (0, 0), (10, 20), (M, 1)):
+            with pytest.raises(sd.SdnnError):
+                plan.matvec(rows[:, at:at + K].t(), rows[:, to:to + M].t())
+        one = torch.full((K + M,), 7.0, device=DEV)
+        with pytest.raises(sd.SdnnError):
+            plan.matvec(one[:K, None], one[K - 1:K - 1 + M, None])
+        assert (rows == 7.0).all() and (one == 7.0).all()
