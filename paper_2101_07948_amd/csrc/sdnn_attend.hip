@@ -258,7 +258,7 @@ __device__ __forceinline__ void attend_step(float scale2, float (&s)[Step<T>::kT
 // blocks; its waves take blocks in turn and join their states through LDS.  Reading keys and values
 // bounds it: each page is read once for the tile of queries that shares it.  32 tokens of 12 heads of 64 in 32 bits
 // over up to 2048 tokens each: 55 us, 244 MB at 4.4 TB/s.  One token of 8 cached heads over 64 blocks of 64 tokens:
-// 8.3 us for 17 MB, latency: list, page, keys and values, then two joins.
+// 8 to 9 us for 17 MB, latency: list, page, keys and values, then two joins.
 template <typename T, int CHUNKS>
 __global__ __launch_bounds__(kWaves * 64, attend_waves(CHUNKS * Step<T>::kPiece / 4)) void attend_kernel(AttendArgs a) {
   constexpr int PIECE = Step<T>::kPiece;
@@ -581,7 +581,7 @@ struct Cursor {
 // by block in ascending order, through LDS: a block is read from L2 once for all of them, the next one while
 // they compute.  Waves whose tokens did not choose a block skip it; rows of a tile that did not are masked.
 // The union is found on the way, a block ahead: each token offers its lowest block not yet passed.
-//   2048 tokens of 32 queries on 8 cached heads of 128 in 16 bits, 16 blocks of 64 each: 142 us, 34 GFLOP at 242 TFLOP/s
+//   2048 tokens of 32 queries on 8 cached heads of 128 in 16 bits, 16 blocks of 64 each: 145 us, 34 GFLOP at 232 TFLOP/s
 // (the matrix unit does 2.6 times that: rows of tokens that did not choose a block, and probabilities in two
 // parts).  Vector instructions (masks, exponentials, the parts) take 40 % of the time, matrix ones 25 %, and waves
 // wait for a stage or the matrix unit in 58 % of theirs.  Half as many waves to a SIMD, for more registers: 212 us;

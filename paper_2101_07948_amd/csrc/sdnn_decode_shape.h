@@ -148,7 +148,10 @@ inline int tile_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads)
   return s;
 }
 
-// attend_tiles serves a call where many tokens of a sequence are neighbours and it is estimated to be faster.
+// attend_tiles serves a call where many tokens of a sequence are neighbours, as far as the sizes tell, and it is estimated
+// to be faster.  (Sequences are counted by the table's rows.  What that costs where it is wrong, 2048 tokens of a sequence over
+// 16 of 128 blocks: 0.2 ms; with a table of 256 rows, token by token, 0.9; with single tokens of 64 other sequences,
+// whose lists a workgroup walks one after the other, 1.4, and over all blocks 9.4 where two calls take 0.8.)
 // attend_kernel reads every token's blocks from L2, at about 8 TB/s (16384 heads of 16 blocks of 32 KiB:
 // 994 us; 8760 of 3 of 128 KiB: 683).  attend_tiles takes its workgroups' unions of blocks, 512 workgroups at a
 // time, two to a compute unit, at about 3.7 us for 32 KiB, or 2.2 where they have a unit each (38 and 133 of them: 142 and
@@ -188,8 +191,9 @@ inline Tiles tiles_of(const sdnn_block_cache& c, int32_t tokens, int32_t sequenc
 // 128: 2 shares 53 us and the join, 1 share 31; 22 tokens of 2 heads over lists of 64 blocks that are nearly empty: 24
 // shares 24 us, 11 shares 8).  A wave has a step of its own at least, and there are at most 64 shares (the lanes of
 // attend_join).  Where all blocks are 192 KiB or less, 48 to a wave, they are not shared out: the join, a launch of its
-// own, would take longer (4 tokens of 8 heads of 128 in 16 bits, a call: 4 blocks of 32 KiB 12.5 us with and 9.3
-// without, 8 11 to 12.5 and 11.1 to 12.3, 16 12.3 and 20).
+// own, would take longer (1 to 16 tokens of 1 to 32 heads of 128 in 16 bits over blocks of 32 KiB, a call, not shared out
+// and shared out: 4 blocks 8.0 to 8.6 us and 10.3 to 10.8, 6 blocks 9.7 to 10.1 and 10.4 to 11.8; 8, shared out, 10.3 to
+// 12.3).
 inline int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
   const int64_t units = (int64_t)tokens * c.kv_heads * ((heads / c.kv_heads + kRows - 1) / kRows);
   if (units == 0) return 1;

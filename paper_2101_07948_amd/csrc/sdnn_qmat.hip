@@ -230,8 +230,8 @@ struct Chunk {
 // scaled once a group (and chunk).  (With 16 + n and 16 + z in their place the sums were 2.5 times as inexact.)
 //   Row p of the operand is column p / 4 + 4 (p % 4) of x, so that up to four columns are in the first of a lane's
 // four results, up to eight in two; of four columns in 32 bits rows 4 t + part, and a lane adds its results.
-//   Reading the weights bounds it: 16384 x 8192 with one column in 16 bits 14.2 us, 69 MB at 4.9 TB/s, the rate of a
-// large copy.  5003 x 4099 with 13 columns: 11.4 us for 12.5 MB: each of 313 workgroups, one or two to a compute unit,
+//   Reading the weights bounds it: 16384 x 8192 with one column in 16 bits 14.1 us, 69 MB at 4.9 TB/s, the rate of a
+// large copy.  5003 x 4099 with 13 columns: 11.5 us for 12.5 MB: each of 313 workgroups, one or two to a compute unit,
 // brings all of x through LDS.  Small ones are a launch: 768 x 3072 3.8 us.
 //   STEPS: matrix instructions (of 32 columns of W) of a group within a chunk.
 template <typename T, int STEPS, int TOKENS, bool FEATURES>
@@ -328,7 +328,7 @@ template <typename T, int STEPS, int TOKENS>
 hipError_t start_tokens(const QmatArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.M + kQTileRows - 1) / kQTileRows), (unsigned)((a.N + TOKENS - 1) / TOKENS));
   // 8 waves to a tile of rows, 16 where there are fewer tiles than compute units (1000 x 12000, 4 columns in 32 bits:
-  // 13.0 and 10.3 us; 227 x 11127, 16 contiguous columns in 16 bits: 11.8 and 11.1), with as many chunks each as the one with most
+  // 12.0 and 9.7 us; 227 x 11127, 16 contiguous columns in 16 bits: 11.3 and 10.5), with as many chunks each as the one with most
   // of them; 4 at least, which write the results
   constexpr size_t per_wave = (size_t)kRowsOf<T, TOKENS> * kRowBytes;
   const int most = grid.x * grid.y >= 256 ? 8 : a.x_feature == 1 ? kWavesOf<TOKENS, false> : kWavesOf<TOKENS, true>;

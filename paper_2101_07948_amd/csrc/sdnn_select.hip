@@ -306,7 +306,7 @@ __device__ __forceinline__ void load_values(const void* q, int64_t at, int dtype
 // UNIT blocks under way at a time, the first of them before the queries are there.  The scores go to LDS as
 // ordered integers.  Then, of one token, all waves search the threshold together; of several, each wave takes
 // whole tokens, whose keys stay in its registers.
-//   4 tokens of 8 cached heads over 2048 blocks of 128 values: 11 us (queries 4, scores 4, choice 3): the 256 KiB of a
+//   4 tokens of 8 cached heads over 2048 blocks of 128 values: 11 to 12 us (queries 4, scores 4, choice 3): the 256 KiB of a
 // workgroup's summaries go through one compute unit.  2048 tokens of 8 heads over 512 blocks: 38 us (queries 11,
 // scores 17, choice 10), instructions, half of them of the vector unit, and the waits between them.
 template <int STEPS, int SHIFT, int UNIT>

@@ -199,7 +199,8 @@ class BlockCache:
     BlockCache.  Every call takes the tokens' positions
     pos and sequences seq (tokens, int32) and the block table (sequences, blocks, int32): the
     page of each sequence's blocks.  A token with pos < 0 is a filler: nothing is stored for it
-    and its outputs are zero."""
+    and its outputs are zero.  Kernels are chosen by a call's sizes: prompts and single tokens
+    belong in calls of their own, a prompt's with its own sequences' rows of the table alone."""
 
     def __init__(self, k_pages=None, v_pages=None, means=None, mean_scales=None, block: int | None = None):
         torch = _torch_mod()
