@@ -183,6 +183,13 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return u + v;
 }
 
+// The logarithm of a query's sum l of exponentials taken from m (in units of log 2).  l's exponent joins m first: where m
+// is far from the maximum (see attend_step) both are large and cancel.
+__device__ __forceinline__ float log_of_sum(float m, float l) {
+  if (!(l > 0.0f)) return -INFINITY;
+  return ((m + (float)__builtin_amdgcn_frexp_expf(l)) + __log2f(__builtin_amdgcn_frexp_mantf(l))) * 0.693147181f;
+}
+
 // A share's part of a query: the sums, then for all parts their reference and total.
 template <int TILES>
 __device__ __forceinline__ void store_part(const AttendArgs& a, int split, int t, int64_t head, int g, const State<TILES>& st,
@@ -377,7 +384,7 @@ __global__ __launch_bounds__(kWaves * 64, attend_waves(CHUNKS * Step<T>::kPiece 
     store_n<4>(o + d, a.o_aligned, x);
   }
   if (g == 0 && a.lse)
-    a.lse[(int64_t)t * a.heads + head] = l > 0.0f ? (m + __log2f(l)) * 0.693147181f : -INFINITY;
+    a.lse[(int64_t)t * a.heads + head] = log_of_sum(m, l);
 }
 
 // Joins the parts of a token's head: a workgroup for each, a quarter of the parts to a wave.  Lane s has
@@ -431,7 +438,7 @@ __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
     const int d = i * 64 + lane;
     if (d < D) y[d] = (T)((((o[i] + sums[0][d]) + sums[1][d]) + sums[2][d]) * inv);
   }
-  if (lane == 0 && a.lse) a.lse[row] = l > 0.0f ? (top + __log2f(l)) * 0.693147181f : -INFINITY;
+  if (lane == 0 && a.lse) a.lse[row] = log_of_sum(top, l);
 }
 
 // The same for at most kFewParts parts: a thread has four values of a row and loads all that they are made of at once.
@@ -468,7 +475,7 @@ __global__ __launch_bounds__(256) void attend_join_few(AttendArgs a) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[i] = (T)(o[i] * inv);
   store_n<4>(static_cast<T*>(a.o) + row / a.heads * a.o_token + row % a.heads * a.o_head + d, a.o_aligned, y);
-  if (d == 0 && a.lse) a.lse[row] = sum > 0.0f ? (top + __log2f(sum)) * 0.693147181f : -INFINITY;
+  if (d == 0 && a.lse) a.lse[row] = log_of_sum(top, sum);
 }
 
 // ---------------------------------------------------------------- many tokens of a sequence
@@ -740,7 +747,7 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
     store_n<4>(o + d, a.o_aligned, x);
   }
   if (g == 0 && a.lse)
-    a.lse[(int64_t)t * a.heads + head] = l > 0.0f ? (st.m + __log2f(l)) * 0.693147181f : -INFINITY;
+    a.lse[(int64_t)t * a.heads + head] = log_of_sum(st.m, l);
 }
 
 template <typename T>

@@ -143,6 +143,23 @@ def test_attend_at_the_last_position(dtype, tokens):
     check_attend(cache, table, q, pos, [0] * tokens, chosen, oracle=od.attend)
 
 
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("tokens", [8, 300])  # token by token, through tiles
+def test_attend_logarithms_keep_their_bits(dtype, tokens):
+    """With lse between 8 and 16 three roundings at the end (of the reference with the exponent, of the logarithm,
+    of the result) are 0.29 of 2^-20 each in the mean, 4.8e-7 together; those of scores and sums are shared by thousands
+    of terms: 6e-7 in all."""
+    P, D, Hq, n = 64, 64, 8, 4000
+    cache, table = filled(41, 1, [n], Hq, P, D, dtype)
+    q = randn(42, (tokens, Hq, D), dtype)
+    pos = list(range(n - tokens, n))
+    _, lse = check_attend(cache, table, q, pos, [0] * tokens, oracle=od.attend_many)
+    _, want, _, _ = od.attend_many(od.f64(q), pos, [0] * tokens, table, np.nan_to_num(od.f64(cache.k_pages)),
+                                   np.nan_to_num(od.f64(cache.v_pages)))
+    assert (want > 8).all() and (want < 16).all()
+    assert np.sqrt(np.mean((od.f64(lse) - want) ** 2)) <= 6e-7
+
+
 def test_tensors_whose_addresses_are_kept_cannot_be_replaced():
     """A call would go on using the memory of the old one, which is freed."""
     cache, rope = make_cache(0, 2, 1, 32, 16, torch.float32), sd.Rope(16)
