@@ -453,3 +453,4 @@ def status_str(code: int) -> str:
 
 
 from .decode import BlockCache, Q4Plan, Rope, rope_frequencies  # noqa: E402  (uses the names above)
+from .serve import HeadNorm, Q8Cache, sample, sample_workspace_floats  # noqa: E402

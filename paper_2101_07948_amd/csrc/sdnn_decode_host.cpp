@@ -4,87 +4,10 @@
 
 #include <new>
 
-#include "sdnn_decode_internal.h"
+#include "sdnn_decode_check.h"
 #include "sdnn_decode_shape.h"
 
 using namespace sdnn;
-
-namespace {
-
-bool bad_dtype(int dtype) { return dtype != SDNN_F32 && dtype != SDNN_F16 && dtype != SDNN_BF16; }
-bool bad_align(const void* p) { return (uintptr_t)p % 16 != 0; }
-// Strides in elements: not negative, and small enough that a row number times one fits 64 bits.
-bool bad_stride(int64_t s) { return s < 0 || s >= (int64_t)1 << 36; }
-
-sdnn_status check_cache(const sdnn_block_cache* c) {
-  if (!c) return SDNN_ERR_NULL;
-  if (bad_dtype(c->dtype) || c->pages < 0 || c->pages > INT32_MAX) return SDNN_ERR_DIM;
-  if (c->kv_heads < 1 || c->kv_heads > 65536) return SDNN_ERR_DIM;
-  if (c->head_dim < 8 || c->head_dim > kMaxHeadDim || c->head_dim % 8) return SDNN_ERR_DIM;
-  if (c->block != 32 && c->block != 64 && c->block != 128) return SDNN_ERR_DIM;
-  if (bad_align(c->k_pages) || bad_align(c->v_pages) || bad_align(c->means) || bad_align(c->mean_scales))
-    return SDNN_ERR_DIM;
-  return SDNN_OK;
-}
-
-sdnn_status check_tokens(const sdnn_tokens* t) {
-  if (!t) return SDNN_ERR_NULL;
-  if (t->tokens < 0 || t->sequences < 0 || t->max_blocks < 0) return SDNN_ERR_DIM;
-  if (t->tokens > 0 && (!t->pos || !t->seq)) return SDNN_ERR_NULL;
-  if (t->tokens > 0 && t->sequences > 0 && t->max_blocks > 0 && !t->table) return SDNN_ERR_NULL;
-  return SDNN_OK;
-}
-
-// Rows of `heads` heads (0: any positive number) of head_dim values for `tokens` tokens.
-sdnn_status check_rows(const sdnn_heads* r, int32_t heads, int32_t tokens, int dtype) {
-  if (!r) return SDNN_ERR_NULL;
-  if (r->heads < 1 || r->heads > 65536 || (heads && r->heads != heads)) return SDNN_ERR_DIM;
-  if (bad_stride(r->token_stride) || bad_stride(r->head_stride)) return SDNN_ERR_DIM;
-  if (tokens > 0 && !r->data) return SDNN_ERR_NULL;
-  return (uintptr_t)r->data % dtype_bytes(dtype) ? SDNN_ERR_DIM : SDNN_OK;
-}
-
-sdnn_status check_rotation(const sdnn_rotation* r, int32_t head_dim) {
-  if (r->pairs < 0 || 2 * (int64_t)r->pairs > head_dim) return SDNN_ERR_DIM;
-  if (r->layout != SDNN_ROPE_HALF && r->layout != SDNN_ROPE_INTERLEAVED) return SDNN_ERR_DIM;
-  return r->pairs > 0 && !r->freq ? SDNN_ERR_NULL : SDNN_OK;
-}
-
-bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
-  if (!a || !b || abytes <= 0 || bbytes <= 0) return false;
-  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-  return a0 < b0 + (uintptr_t)bbytes && b0 < a0 + (uintptr_t)abytes;
-}
-
-// The same of two sets of rows of a_row and b_row bytes, `rows` of each, stride bytes apart: columns of one buffer may lie
-// side by side.
-bool overlap_rows(const void* a, int64_t a_row, const void* b, int64_t b_row, int64_t rows, int64_t stride) {
-  if (!overlap(a, (rows - 1) * stride + a_row, b, (rows - 1) * stride + b_row)) return false;
-  if (rows < 2 || stride == 0) return true;
-  const int64_t between = (int64_t)((uintptr_t)b - (uintptr_t)a) % stride, off = between < 0 ? between + stride : between;
-  return off < a_row || off + b_row > stride;
-}
-
-bool same_rows(const sdnn_heads& a, const sdnn_heads& b) {
-  return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
-}
-// Outputs have to lie apart from each other: a stride of zero would write one row for several.
-bool distinct_rows(const sdnn_heads& a, int32_t tokens, int32_t head_dim) {
-  return (tokens < 2 || a.token_stride != 0) && (a.heads < 2 || a.head_stride >= head_dim);
-}
-
-// (A call of more threads than a launch has is refused before it.)
-sdnn_status result(hipError_t e) {
-  return e == hipSuccess ? SDNN_OK : e == hipErrorInvalidConfiguration ? SDNN_ERR_DIM : SDNN_ERR_HIP;
-}
-
-#define SDNN_CHECK(call)                  \
-  do {                                    \
-    const sdnn_status st_ = (call);       \
-    if (st_ != SDNN_OK) return st_;       \
-  } while (0)
-
-}  // namespace
 
 extern "C" {
 
@@ -166,11 +89,7 @@ sdnn_status sdnn_block_attend(const sdnn_block_cache* cache, const sdnn_tokens* 
   if (tokens->tokens == 0) return SDNN_OK;
   if (cache->pages > 0 && (!cache->k_pages || !cache->v_pages)) return SDNN_ERR_NULL;
   const int64_t need = sdnn_block_attend_floats(cache, tokens->tokens, q->heads, blocks);
-  if (need > 0 && !workspace) return SDNN_ERR_NULL;
-  if (need > 0 && (workspace_floats < need || bad_align(workspace))) return SDNN_ERR_DIM;
-  if (need > 0 && (overlap(workspace, need * 4, lse, (int64_t)tokens->tokens * q->heads * 4) ||
-                   workspace == q->data || workspace == o->data))
-    return SDNN_ERR_DIM;
+  SDNN_CHECK(check_workspace(workspace, workspace_floats, need, *tokens, *q, *o, lse));
   return result(launch_attend(*cache, *tokens, *q, *o, chosen, blocks, scale, lse, workspace,
                               (hipStream_t)stream));
 }

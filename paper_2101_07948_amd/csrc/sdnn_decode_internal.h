@@ -40,6 +40,9 @@ hipError_t launch_select(const sdnn_block_cache& c, const sdnn_tokens& t, const 
 hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const sdnn_heads& q,
                          const sdnn_heads& o, const int32_t* chosen, int32_t blocks, float scale,
                          float* lse, float* workspace, hipStream_t stream);
+hipError_t launch_attend_shared(const sdnn_block_cache& c, const sdnn_tokens& t, const sdnn_heads& q,
+                                const sdnn_heads& o, int32_t shared, float scale, float* lse, float* workspace,
+                                hipStream_t stream);
 hipError_t launch_qmat_pack(const sdnn_qmat_s& w, const uint8_t* packed, const void* scales,
                             const uint8_t* zeros, hipStream_t stream);
 hipError_t launch_qmat(const sdnn_qmat_s& w, const void* x, int64_t x_feature, int64_t x_column, void* y,

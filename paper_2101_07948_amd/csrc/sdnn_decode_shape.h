@@ -118,6 +118,7 @@ constexpr int kWaves = 4;      // of a workgroup of attend_kernel
 constexpr int kTileWaves = 8;  // and of attend_tiles
 constexpr int kRows = 16;      // queries of a tile: the columns of one matrix instruction
 constexpr int kFewParts = 8;   // that attend_join_few joins
+constexpr int kMostParts = 64; // of a query (the lanes of attend_join)
 
 // Waves of a SIMD that the registers of attend_kernel leave room for, and so its workgroups at work at once on a compute
 // unit, for heads of up to 16 * tiles values.  (For the compiler a bound: without one it takes registers of both kinds
@@ -203,7 +204,7 @@ inline int attend_splits(const sdnn_block_cache& c, int32_t tokens, int32_t head
   int64_t wanted = (1024 + units - 1) / units;
   if (steps < 4 * kWaves * wanted) wanted = 256 * attend_waves((c.head_dim + 15) / 16) / units;
   const int64_t s = wanted < most ? wanted : most;
-  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  return (int)(s < 1 ? 1 : s > kMostParts ? kMostParts : s);
 }
 
 inline int64_t attend_floats(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks) {
@@ -219,18 +220,67 @@ struct AttendShape {
   int64_t join_groups;  // of 256 threads; 0: no parts
 };
 
+// Workgroups of the join of `parts` parts of `rows` queries (0: no parts).
+inline int64_t join_groups(int32_t parts, int64_t rows, int32_t head_dim) {
+  return parts <= 1 ? 0 : parts <= kFewParts ? (rows * (head_dim / 4) + 255) / 256 : rows;
+}
+
 // (chosen: blocks of a token's list; 0: all of them)
-inline AttendShape attend_shape(const sdnn_block_cache& c, const sdnn_tokens& t, int32_t heads, int32_t chosen) {
+inline AttendShape attend_shape(const sdnn_block_cache& c, const sdnn_tokens& t, int32_t heads, int32_t chosen,
+                                int32_t most_splits = kMostParts) {
   AttendShape s = {};
   const Tiles tiles = tiles_of(c, t.tokens, t.sequences, t.max_blocks, heads, chosen);
   s.tile_tokens = tiles.tokens;
   s.splits = tiles.tokens ? tiles.splits : attend_splits(c, t.tokens, heads, chosen > 0 ? chosen : t.max_blocks);
+  s.splits = std::min(s.splits, most_splits);
   s.threads = 64 * (tiles.tokens ? kTileWaves : kWaves);
   const int head_tiles = (heads / c.kv_heads + kRows - 1) / kRows;
   s.groups = s.splits * (tiles.tokens ? tile_groups(c, t.tokens, heads) : (int64_t)t.tokens * head_tiles * c.kv_heads);
-  const int64_t rows = (int64_t)t.tokens * heads;
-  s.join_groups = s.splits == 1 ? 0 : s.splits <= kFewParts ? (rows * (c.head_dim / 4) + 255) / 256 : rows;
+  s.join_groups = join_groups(s.splits, (int64_t)t.tokens * heads, c.head_dim);
   return s;
+}
+
+// Attention with a shared prefix (sdnn_block_attend_shared): `prefix` is a launch of attend_tiles whose rows are all tokens'
+// queries, in shares of its blocks; `own` the launch over the blocks after it (splits 0: there are none).
+struct SharedShape {
+  AttendShape prefix, own;
+  int32_t parts;
+  int64_t join_groups;
+  bool fits;
+};
+
+// Shares of the prefix: so many that two workgroups are at work on each compute unit, of two blocks at least.
+inline int prefix_splits(int64_t groups, int32_t shared) {
+  int s = 1;
+  while (s < 32 && groups * 2 * s <= kTileRoom && s * 4 <= shared) s *= 2;
+  return s;
+}
+
+inline SharedShape shared_shape(const sdnn_block_cache& c, int32_t tokens, int32_t sequences, int32_t max_blocks, int32_t heads,
+                                int32_t shared) {
+  SharedShape s = {};
+  const int64_t groups = tile_groups(c, tokens, heads);
+  s.prefix.tile_tokens = tile_of(c, heads);
+  s.prefix.splits = prefix_splits(groups, shared);
+  s.prefix.groups = s.prefix.splits * groups;
+  s.prefix.threads = 64 * kTileWaves;
+  if (max_blocks > shared) {
+    sdnn_tokens t = {};
+    t.tokens = tokens, t.sequences = sequences, t.max_blocks = max_blocks - shared;
+    s.own = attend_shape(c, t, heads, 0, kMostParts - s.prefix.splits);
+  }
+  s.parts = s.prefix.splits + s.own.splits;
+  s.join_groups = join_groups(s.parts, (int64_t)tokens * heads, c.head_dim);
+  s.fits = launchable(s.prefix.groups, s.prefix.threads) && launchable(s.own.groups, 64 * kTileWaves) &&
+           launchable(s.join_groups, 256);
+  return s;
+}
+
+// (The table's rows are not known here: the most that any number of them needs.)
+inline int64_t shared_floats(const sdnn_block_cache& c, int32_t tokens, int32_t heads, int32_t blocks, int32_t shared) {
+  const int own = std::max(attend_splits(c, tokens, heads, blocks - shared), tile_splits(c, tokens, heads));
+  const int64_t parts = prefix_splits(tile_groups(c, tokens, heads), shared) + (blocks > shared ? own : 0);
+  return std::max(parts > 1 ? parts * tokens * heads * (c.head_dim + 2) : 0, attend_floats(c, tokens, heads, blocks));
 }
 
 // ---------------------------------------------------------------- 4-bit weights

@@ -51,6 +51,10 @@ def _lib():
         L.sdnn_block_attend.argtypes = [s, s, s, s, p, i32, ctypes.c_float, p, p, i64, p]
         L.sdnn_block_attend_floats.argtypes = [s, i32, i32, i32]
         L.sdnn_block_attend_floats.restype = i64
+        L.sdnn_block_attend_shared.argtypes = [s, s, s, s, i32, ctypes.c_float, p, p, i64, p]
+        L.sdnn_block_attend_shared.restype = ctypes.c_int
+        L.sdnn_block_attend_shared_floats.argtypes = [s, i32, i32, i32, i32]
+        L.sdnn_block_attend_shared_floats.restype = i64
         L.sdnn_qmat_create.argtypes = [p, p, i32, p, i32, i32, i32, p, ctypes.POINTER(p)]
         L.sdnn_qmat_apply.argtypes = [p, p, i64, i64, p, i64, i64, i32, i32, p, i32, p]
         L.sdnn_qmat_destroy.argtypes = [p]
@@ -118,6 +122,21 @@ def _rows(t, name: str, dtype, tokens: int, heads, head_dim: int) -> bytes:
 def _check(code: int, where: str):
     if code:
         raise SdnnError(code, where)
+
+
+def _workspace(workspace, need, like, stream):
+    """(tensor, address, floats) of a call's workspace, a contiguous float32 tensor; with None need() floats are
+    allocated.  The caller keeps the tensor until its kernels are launched."""
+    if workspace is None:
+        n = need()
+        if not n:
+            return None, None, 0
+        # of the memory of the stream that uses it: that of the current stream may still be in use there
+        torch = _torch_mod()
+        with torch.cuda.stream(stream):  # (None: the current stream)
+            workspace = torch.empty(n, dtype=torch.float32, device=like.device)
+    n = workspace.numel()
+    return workspace, _dense(workspace, "workspace", _FLOAT32, (n,)), n
 
 
 def rope_frequencies(rotated: int, base: float = 10000.0, scaling: str | None = None,
@@ -288,17 +307,22 @@ class BlockCache:
                                    int(sink), int(local), pc, _stream_handle(stream)), "sdnn_block_select")
         return chosen
 
-    def workspace_floats(self, tokens: int, heads: int, blocks: int) -> int:
+    def workspace_floats(self, tokens: int, heads: int, blocks: int, shared: int = 0) -> int:
         """Floats of workspace that attend needs (blocks: of a token, chosen.shape[2], or
         table.shape[1] without chosen)."""
+        if shared:
+            return _lib().sdnn_block_attend_shared_floats(self._struct(self.dtype), int(tokens), int(heads), int(blocks),
+                                                          int(shared))
         return _lib().sdnn_block_attend_floats(self._struct(self.dtype), int(tokens), int(heads), int(blocks))
 
     def attend(self, q, out, pos, seq, table, chosen=None, scale: float | None = None, lse=None,
-               workspace=None, stream=None):
+               workspace=None, stream=None, shared: int = 0):
         """out = attention of q (tokens, heads, head_dim) over the cached positions up to each
         token's own, in its chosen blocks (None: all it sees).  scale: 1 / sqrt(head_dim) by
         default; lse: float32 (tokens, heads), receives the logarithm of the sums of exponentials;
-        workspace: a float32 tensor of workspace_floats(...) (allocated here when None)."""
+        workspace: a float32 tensor of workspace_floats(...) (allocated here when None); shared: the
+        first blocks of every sequence that are the same pages, which are read once for all (looked up
+        in the table's first row; not with chosen)."""
         self._need("k_pages")
         L, T, d = _lib(), pos.shape[0], self.dtype
         pq = _rows(q, "q", d, T, None, self.head_dim)
@@ -307,24 +331,27 @@ class BlockCache:
         blocks = table.shape[1]
         pc = None
         if chosen is not None:
+            if shared:
+                raise ValueError("a shared prefix is attended to whole: chosen must be None")
             blocks = chosen.shape[-1]
             pc = _dense(chosen, "chosen", _INT32, (T, self.kv_heads, blocks))
         pl = None if lse is None else _dense(lse, "lse", _FLOAT32, (T, H))
         cache = self._struct(d)
-        if workspace is None:
-            need = L.sdnn_block_attend_floats(cache, T, H, blocks)
-            if need:
-                # of the memory of the stream that uses it: that of the current stream may still be in use there
-                torch = _torch_mod()
-                with torch.cuda.stream(stream):  # (None: the current stream)
-                    workspace = torch.empty(need, dtype=torch.float32, device=q.device)
-        pw, nw = None, 0
-        if workspace is not None:
-            nw = workspace.numel()
-            pw = _dense(workspace, "workspace", _FLOAT32, (nw,))
+        if shared:
+            return self._attend_shared(cache, pq, po, q, out, pos, seq, table, int(shared), scale, pl, workspace, stream)
+        workspace, pw, nw = _workspace(workspace, lambda: L.sdnn_block_attend_floats(cache, T, H, blocks), q, stream)
         _check(L.sdnn_block_attend(cache, self._tokens(pos, seq, table), pq, po, pc, blocks,
                                    1.0 / math.sqrt(self.head_dim) if scale is None else scale, pl,
                                    pw, nw, _stream_handle(stream)), "sdnn_block_attend")
+        return out
+
+    def _attend_shared(self, cache, pq, po, q, out, pos, seq, table, shared, scale, pl, workspace, stream):
+        L = _bound
+        T, H, blocks = pos.shape[0], q.shape[1], table.shape[1]
+        workspace, pw, nw = _workspace(workspace, lambda: L.sdnn_block_attend_shared_floats(cache, T, H, blocks, shared), q, stream)
+        _check(L.sdnn_block_attend_shared(cache, self._tokens(pos, seq, table), pq, po, shared,
+                                          1.0 / math.sqrt(self.head_dim) if scale is None else scale, pl, pw, nw,
+                                          _stream_handle(stream)), "sdnn_block_attend_shared")
         return out
 
 
