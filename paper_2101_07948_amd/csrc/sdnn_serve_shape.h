@@ -67,10 +67,78 @@ inline sdnn_block_cache as_blocks(const sdnn_q8_cache& c) {
 
 // ---------------------------------------------------------------- sampling
 
-constexpr int kSampleThreads = 1024;
-constexpr int kSampleBins = 8192;
+constexpr int kSampleThreads = 1024;  // of a workgroup that has a row
+constexpr int kSamplePass = 256;      // of one that passes over a part of one
+constexpr int kSampleBins = 2048;
+constexpr int kSampleList = 2048;    // tokens that are put in order in LDS
+constexpr int kMostSampleParts = 64;
 
-inline int64_t sample_floats(int32_t, int32_t) { return 0; }
+// What a row asks for; limits that leave everything are 0 (top_k, min_p) or 1 (top_p).
+struct Limits {
+  float temperature, top_p, min_p, u;
+  int32_t top_k;
+  int32_t first;  // only the first token is left
+};
+
+// What a row's weights are made by.
+struct Weights {
+  float top;     // the largest logit; 0 where that is infinite
+  double scale;  // log2 e / temperature
+};
+
+// What the bins of a row's weights tell of its limits:
+//   kWhole: they leave every token that has a weight;
+//   kShort: what they leave is among the `tokens` tokens up to and with bin `edge`, which a list holds;
+//   kEdges: the last token that top_k leaves is among the `tokens` of bin `edge` (-1: no top_k, or it leaves all), after `rank`
+//           others of it; the last one that top_p leaves is among the `tokens_p` of bins `edge_p` to `end_p` (-1: no top_p);
+//   kOther: none of these.
+// mass, mass_p: before bins edge and edge_p; total: of all bins.
+enum CutKind : int32_t { kWhole, kShort, kEdges, kOther };
+struct Cut {
+  CutKind kind;
+  int32_t edge, edge_p, end_p;
+  uint32_t tokens, tokens_p, rank;
+  uint64_t mass, mass_p, total;
+};
+
+// The logits of tokens that go to lists: from at[0] on and below at[1], from at[2] on and below at[3].
+struct Ranges {
+  float at[4];
+};
+
+// The tokens that are left: those with a logit above `logit`, and of those that have it the ones up to `index`.
+struct Kept {
+  float logit;
+  int32_t index;
+};
+
+// Of a row that several workgroups share.
+struct alignas(16) SampleSpace {
+  Limits limits;
+  Weights weights;
+  Cut cut;
+  Ranges ranges;
+  Kept kept;
+  uint64_t first;                     // token, of the row
+  uint64_t firsts[kMostSampleParts];  // and of each part
+  uint64_t masses[kMostSampleParts];
+  uint64_t mass[kSampleBins];
+  uint64_t list[kSampleList], list_p[kSampleList];
+  uint32_t count[kSampleBins];
+  int32_t listed, listed_p;
+};
+
+// Workgroups that share a row, each with 8192 tokens at least; 0: a row to a workgroup, in one launch.  Seven launches take 25 us
+// before their first pass counts, and then share a row's passes out, which one workgroup makes at about 4 tokens a
+// nanosecond: rows of 50021 in 32 bits top_k and top_p 31 us and 25 (shared out, not), of 131001 in 16 bits 32 and 48, 128 of
+// these with all kinds of limits 90 and 117, 256 of them 126 and 123, of 80000 110 and 91.
+inline int sample_parts(int32_t rows, int32_t vocab) {
+  if (vocab <= 65536 || rows > vocab / 900) return 0;
+  return std::min((vocab + 8191) / 8192, std::min(kMostSampleParts, 4096 / rows));
+}
+inline int64_t sample_floats(int32_t rows, int32_t vocab) {
+  return sample_parts(rows, vocab) ? (int64_t)rows * (int64_t)(sizeof(SampleSpace) / 4) : 0;
+}
 
 }  // namespace sdnn
 

@@ -534,13 +534,14 @@ def check_sample(x, u, t=None, k=None, p=None, least=None):
 
 SETTINGS = [(1.0, 0, 1.0, 0.0), (0.7, 50, 0.9, 0.0), (0.0, 0, 1.0, 0.0), (1.0, 0, 0.95, 0.0), (1.3, 0, 1.0, 0.1),
             (0.6, 200, 0.97, 0.02), (1.0, 1, 1.0, 0.0), (2.0, 5000, 0.999, 0.0), (5.0, 3, 0.5, 0.5), (0.05, 0, 0.3, 0.0),
-            (1.0, 0, 0.0, 0.0), (1.0, -3, 2.0, -1.0), (1.0, 2, 1.0, 1.0), (100.0, 0, 0.7, 0.0)]
+            (1.0, 0, 0.0, 0.0), (1.0, -3, 2.0, -1.0), (1.0, 2, 1.0, 1.0), (100.0, 0, 0.7, 0.0), (0.2, 60_000, 0.9, 0.0),
+            (1.0, 1500, 0.98, 0.001), (1.0, 0, 0.6, 0.0), (0.5, 900, 1.0, 0.0), (4.0, 30_000, 0.9, 0.0)]
 
 
 @pytest.mark.parametrize("dtype", od.DTYPES)
 @pytest.mark.parametrize("vocab,pad", [(1, 0), (2, 3), (7, 0), (63, 1), (300, 5), (5003, 0), (50_021, 2), (131_072, 0)])
 def test_sample(dtype, vocab, pad):
-    rows = 2 * len(SETTINGS)
+    rows = 2 * len(SETTINGS)  # (a few rows at a time too: large vocabularies are shared out over workgroups then)
     x = randn(vocab, (rows, vocab + pad), dtype, 2.5)
     x[3] *= 4
     x[5, ::3] = -math.inf
