@@ -10,54 +10,72 @@ struct Q8AttendArgs : AttendArgs {
   const float* v_scales;
 };
 
-// The numbers of keys and values are whole and below 2^8: exact in bf16, which the matrix unit takes.  Queries and
-// probabilities, which have more bits than bf16, are sums of bf16 parts, each a product of its own: 3 parts hold the 24 bits
-// of a float, 2 the 11 of f16 (whose exponents bf16 has all of).  Probabilities keep 16 bits where the output has 8 or 11, and
-// 24 where it has 24.  The scale of a key multiplies its score, that of a value its probability, both in 32 bits.
+// The numbers of keys and values are whole and below 2^8: exact in 16-bit floats, which the matrix unit takes.  Queries and
+// probabilities are sums of such parts, each a product of its own.  Queries: 3 parts in bf16 hold the 24 bits of a float; those of
+// 16 bits are taken as they are, keys in their type.  Probabilities, whose exponents f16 has not: bf16, 2 parts (16 bits) where the
+// output has 8 or 11, 3 where it has 24.  The scale of a key multiplies its score, that of a value its probability, both in 32
+// bits.
 template <typename T>
-struct Parts;
+struct Parts {
+  typedef __bf16 Key;
+  typedef bf16x8 Key8;
+  static constexpr int kQ = 1, kP = 2;
+};
 template <>
 struct Parts<float> {
+  typedef __bf16 Key;
+  typedef bf16x8 Key8;
   static constexpr int kQ = 3, kP = 3;
 };
 template <>
 struct Parts<_Float16> {
-  static constexpr int kQ = 2, kP = 2;
-};
-template <>
-struct Parts<__bf16> {
+  typedef _Float16 Key;
+  typedef f16x8 Key8;
   static constexpr int kQ = 1, kP = 2;
 };
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
+__device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
 
-// Eight numbers as bf16: those of a 32-bit float that has no bits below bf16's, so that its upper half is taken.
+// Eight numbers as 16-bit floats.  bf16: the upper halves of 32-bit floats, which have no bits below.  f16: with 128 added (a
+// bit turned) a number is the lower byte of 1024 + it; 1152 is subtracted.
 __device__ __forceinline__ uint32_t widen2(int32_t w, int at) {
   const float a = (float)(int8_t)(w >> at), b = (float)(int8_t)(w >> (at + 8));
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
-__device__ __forceinline__ bf16x8 widen(int32_t lo, int32_t hi) {
+__device__ __forceinline__ void widen(int32_t lo, int32_t hi, bf16x8* y) {
   const uint32_t x[4] = {widen2(lo, 0), widen2(lo, 16), widen2(hi, 0), widen2(hi, 16)};
-  bf16x8 y;
-  __builtin_memcpy(&y, x, sizeof(y));
-  return y;
+  __builtin_memcpy(y, x, sizeof(x));
+}
+__device__ __forceinline__ void widen(int32_t lo, int32_t hi, f16x8* y) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t a = (uint32_t)lo ^ 0x80808080u, b = (uint32_t)hi ^ 0x80808080u;
+  const uint32_t x[4] = {__builtin_amdgcn_perm(0x64646464u, a, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u),
+                         __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)};
+  f16x2 z[4];
+  __builtin_memcpy(z, x, sizeof(x));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = z[i] - f16x2{(_Float16)1152.0f, (_Float16)1152.0f};
+  __builtin_memcpy(y, z, sizeof(z));
 }
 
-template <int N>
-__device__ __forceinline__ void split(float x, __bf16 (&out)[N]) {
+template <int N, typename H>
+__device__ __forceinline__ void split(float x, H (&out)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    out[i] = (__bf16)x;
-    x -= (float)out[i];
+    out[i] = (H)x;
+    if (i + 1 < N) x -= (float)out[i];
   }
 }
 
 // The queries' parts: piece i of a lane has values `at(i)` ... + 7 of its row.
 template <typename T, int PIECES, typename AT>
 __device__ __forceinline__ void load_queries(const AttendArgs& a, bool row, int t, int64_t head, const AT& at,
-                                             bf16x8 (&q)[Parts<T>::kQ][PIECES]) {
+                                             typename Parts<T>::Key8 (&q)[Parts<T>::kQ][PIECES]) {
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
     const int d = at(i);
@@ -74,7 +92,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, bool row, int 
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      __bf16 part[Parts<T>::kQ];
+      typename Parts<T>::Key part[Parts<T>::kQ];
       split((float)x[e], part);
 #pragma unroll
       for (int k = 0; k < Parts<T>::kQ; ++k) q[k][i][e] = a.negate ? -part[k] : part[k];
@@ -83,16 +101,16 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, bool row, int 
 }
 
 // One step of E tokens to a lane, their scores s (without the keys' scales) given: tokens E g ... E g + E - 1 of which the
-// first `seen` of the step's are within this lane's query's sight.  vs: their values' scales.  EMPTY: see attend_step.
-// value(c, e): piece e (tokens E g + 8 e ...) of values 16 c + r.
-template <bool EMPTY, typename T, int E, int TILES, typename V>
-__device__ __forceinline__ void q8_step(float scale2, float (&s)[E], const float (&ks)[E], const float (&vs)[E], const V& value,
-                                        int seen, int g, State<TILES>& st) {
+// first `seen` of the step's are within this lane's query's sight.  ks, vs: the scales of their keys and values; of tokens out of
+// sight they may be anything that is not infinite or not a number.  EMPTY: see attend_step.
+// Leaves what multiplies their values, in parts.
+template <bool EMPTY, typename T, int E, int TILES>
+__device__ __forceinline__ void q8_weights(float scale2, float (&s)[E], const float (&ks)[E], const float (&vs)[E], int seen, int g,
+                                           State<TILES>& st, bf16x8 (&p)[Parts<T>::kP][E / 8]) {
   constexpr float HIGH = 8.0f;
-  const bool part = __any(seen < 4 * E && (!EMPTY || seen > 0));
 #pragma unroll
   for (int j = 0; j < E; ++j) s[j] *= ks[j];
-  if (part) {  // (the scales of tokens out of sight may be anything)
+  if (__any(seen < 4 * E && (!EMPTY || seen > 0))) {
 #pragma unroll
     for (int j = 0; j < E; ++j) s[j] = E * g + j < seen ? s[j] : -INFINITY;
   }
@@ -118,24 +136,13 @@ __device__ __forceinline__ void q8_step(float scale2, float (&s)[E], const float
   for (int j = 1; j < E; ++j) sum += s[j];
   st.l += sum;
   constexpr int P = Parts<T>::kP;
-  bf16x8 p[P][E / 8];
 #pragma unroll
   for (int j = 0; j < E; ++j) {
     __bf16 x[P];
-    float w = s[j] * vs[j];
-    if (part || EMPTY) w = s[j] > 0.0f ? w : 0.0f;  // (nor may what they are to values)
-    split(w, x);
+    split(s[j] * vs[j], x);
 #pragma unroll
     for (int k = 0; k < P; ++k) p[k][j / 8][j % 8] = x[k];
   }
-#pragma unroll
-  for (int c = 0; c < TILES; ++c)
-#pragma unroll
-    for (int e = 0; e < E / 8; ++e) {
-      const bf16x8 v = value(c, e);
-#pragma unroll
-      for (int k = 0; k < P; ++k) st.o[c] = mfma(v, p[k][e], st.o[c]);
-    }
 }
 
 // Waves of a SIMD that the registers leave room for.
@@ -167,7 +174,8 @@ __global__ __launch_bounds__(kWaves * 64, q8_waves(2 * DIMS)) void q8_kernel(Q8A
   const int32_t* chosen = a.chosen ? a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks : nullptr;
   const int32_t* table = a.table + (int64_t)seq * a.max_blocks;
   const int shift = __builtin_ctz(P / N), deal = a.splits * kWaves, last = n << shift;
-  bf16x8 q[Parts<T>::kQ][2 * DIMS];
+  typedef typename Parts<T>::Key8 Key8;
+  Key8 q[Parts<T>::kQ][2 * DIMS];
   load_queries<T, 2 * DIMS>(a, r < rows, t, head, [&](int i) { return (i / 2 * 4 + g) * 16 + i % 2 * 8; }, q);
   State<TILES> st;
 #pragma unroll
@@ -209,6 +217,11 @@ __global__ __launch_bounds__(kWaves * 64, q8_waves(2 * DIMS)) void q8_kernel(Q8A
       for (int c = 0; c < TILES; ++c)
         vv[c] = *reinterpret_cast<const typename VecOf<W, int32_t>::type*>(v + min(c * 16 + r, D - 1) * P + E * g);
       __builtin_amdgcn_sched_barrier(0);
+      if (seen < N) {  // (memory that no token was stored to)
+#pragma unroll
+        for (int x = 0; x < E; ++x)
+          if (E * g + x >= seen) ks[x] = vs[x] = 0.0f;
+      }
       float s[E];
 #pragma unroll
       for (int x = 0; x < N / 16; ++x) {
@@ -217,15 +230,25 @@ __global__ __launch_bounds__(kWaves * 64, q8_waves(2 * DIMS)) void q8_kernel(Q8A
         for (int c = 0; c < DIMS; ++c)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const bf16x8 y = widen(kk[x][c][2 * e], kk[x][c][2 * e + 1]);
+            Key8 y;
+            widen(kk[x][c][2 * e], kk[x][c][2 * e + 1], &y);
 #pragma unroll
             for (int part = 0; part < Parts<T>::kQ; ++part) acc = mfma(y, q[part][2 * c + e], acc);
           }
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[4 * x + i] = acc[i];
       }
-      q8_step<false, T, E, TILES>(
-          a.scale2, s, ks, vs, [&](int c, int e) { return widen(vv[c][2 * e], vv[c][2 * e + 1]); }, seen, g, st);
+      bf16x8 w[Parts<T>::kP][E / 8];
+      q8_weights<false, T, E, TILES>(a.scale2, s, ks, vs, seen, g, st, w);
+#pragma unroll
+      for (int c = 0; c < TILES; ++c)
+#pragma unroll
+        for (int e = 0; e < E / 8; ++e) {
+          bf16x8 y;
+          widen(vv[c][2 * e], vv[c][2 * e + 1], &y);
+#pragma unroll
+          for (int x = 0; x < Parts<T>::kP; ++x) st.o[c] = mfma(y, w[x][e], st.o[c]);
+        }
     }
   }
   join_waves<T>(a, lds, split_at, t, head, r < rows, st);
@@ -233,52 +256,147 @@ __global__ __launch_bounds__(kWaves * 64, q8_waves(2 * DIMS)) void q8_kernel(Q8A
 
 // ---------------------------------------------------------------- many tokens of a sequence
 
-// A stage of `tokens` tokens on its way to LDS: a thread holds 16 numbers of a key's row and 16 of a value's, and some of
+// Tiles of 16 queries to a wave of q8_tiles: two where their queries and sums fit the registers, so that what the wave reads from
+// LDS serves both.  A workgroup has kTileWaves tiles.
+template <typename T>
+constexpr int q8_tiles_of(int chunks) {
+  return 2 * (4 * Parts<T>::kQ + 8) * chunks <= 144 ? 2 : 1;
+}
+
+// A stage of `tokens` tokens on its way to LDS: a thread holds pieces of 16 numbers of keys' rows and of values', and some of
 // the threads a scale.  They are asked for while the stage before is computed, and widened on their way into the tile, so that
 // its waves find matrix operands there.
-template <int CHUNKS, int STAGE>
+template <typename T, int CHUNKS, int STAGE, int WAVES>
 struct Q8Stage {
-  typedef Tile<__bf16, CHUNKS, STAGE> L;
-  i32x4 k, v;
+  static constexpr int kThreads = WAVES * 64, kPieces = (STAGE * CHUNKS * 2 + kThreads - 1) / kThreads;
+  typedef Tile<typename Parts<T>::Key, CHUNKS, STAGE> L;
+  static_assert(2 * STAGE <= kThreads, "a scale to a thread");
+  i32x4 k[kPieces], v[kPieces];
   float scale;
   __device__ __forceinline__ void load(const Q8AttendArgs& a, int page, int h, int t0, int tokens) {
-    const int D = a.head_dim, P = a.block, i = threadIdx.x;
+    const int D = a.head_dim, P = a.block, per = tokens / 16;  // (2 or 4)
     const int64_t at = ((int64_t)page * a.kv_heads + h) * P;
     const int8_t* kp = static_cast<const int8_t*>(a.k_pages) + (at + t0) * D;
     const int8_t* vp = static_cast<const int8_t*>(a.v_pages) + at * D + t0;
-    if (i * 16 < tokens * D) {
-      k = *reinterpret_cast<const i32x4*>(kp + i * 16);
-      const int per = tokens / 16, d = i / per;  // (a power of two: 2 or 4)
-      v = *reinterpret_cast<const i32x4*>(vp + d * P + (i - d * per) * 16);
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int i = threadIdx.x + j * kThreads, d = i / per;
+      if (i * 16 < tokens * D) {
+        k[j] = *reinterpret_cast<const i32x4*>(kp + i * 16);
+        v[j] = *reinterpret_cast<const i32x4*>(vp + d * P + (i - d * per) * 16);
+      }
     }
+    const int i = threadIdx.x;
     if (i < 2 * STAGE && i % STAGE < tokens) scale = (i < STAGE ? a.k_scales : a.v_scales)[at + t0 + i % STAGE];
   }
   __device__ __forceinline__ void store(const Q8AttendArgs& a, int tokens, unsigned char* lds, float (&scales)[2][STAGE]) const {
-    const int D = a.head_dim, i = threadIdx.x;
-    if (i * 16 < tokens * D) {
-      const int row = i * 16 / D, x = (i * 16 - row * D) / 8;
-      const int per = tokens / 16, d = i / per, y = (i - d * per) * 2;
+    const int D = a.head_dim, per = tokens / 16;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        *reinterpret_cast<bf16x8*>(const_cast<unsigned char*>(L::key(lds, row, x + e))) = widen(k[2 * e], k[2 * e + 1]);
-        *reinterpret_cast<bf16x8*>(const_cast<unsigned char*>(L::value(lds, d, y + e))) = widen(v[2 * e], v[2 * e + 1]);
+    for (int j = 0; j < kPieces; ++j) {
+      const int i = threadIdx.x + j * kThreads;
+      if (i * 16 < tokens * D) {
+        const int row = i * 16 / D, x = (i * 16 - row * D) / 8, d = i / per, y = (i - d * per) * 2;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          widen(k[j][2 * e], k[j][2 * e + 1],
+                reinterpret_cast<typename Parts<T>::Key8*>(const_cast<unsigned char*>(L::key(lds, row, x + e))));
+          widen(v[j][2 * e], v[j][2 * e + 1], reinterpret_cast<bf16x8*>(const_cast<unsigned char*>(L::value(lds, d, y + e))));
+        }
       }
     }
-    if (i < 2 * STAGE) scales[i / STAGE][i % STAGE] = scale;
+    // (where no token was stored memory may hold what is infinite or not a number)
+    const int i = threadIdx.x;
+    if (i < 2 * STAGE) scales[i / STAGE][i % STAGE] = fabsf(scale) < INFINITY ? scale : 0.0f;
   }
 };
 
-// As attend_tiles: a wave has a tile of 16 queries, the workgroup's waves walk the union of their lists block by block
-// through LDS.
-template <typename T, int CHUNKS, int STAGE, int WAVES, bool PREFIX>
-__global__ __launch_bounds__(WAVES * 64, CHUNKS <= 4 && sizeof(T) == 2 ? 4 : 2) void q8_tiles(Q8AttendArgs a) {
-  typedef Tile<__bf16, CHUNKS, STAGE> L;
-  constexpr int TILES = CHUNKS * 2, N = 32, E = N / 4;
-  constexpr int32_t END = 0x7fffffff;
+// Which blocks a workgroup goes through, in what order, and what each query sees of them.  A block's key is the run of tokens of
+// one sequence within the workgroup's, then the block.
+//   Lists: as in attend_tiles: each token offers its lowest block not yet passed, a block ahead.
+template <bool LISTS, int R>
+struct Walk;
+template <int R>
+struct Walk<true, R> {
+  struct Lds {
+    uint64_t lowest[3];  // key and page of the lowest block that is offered, in turn
+  };
+  static constexpr int32_t END = 0x7fffffff;
+  Cursor at[R];
+  int32_t run[R], pos[R], seen[R];
+  int32_t key = END, page = -1;
+  int turn = 0;
+  __device__ __forceinline__ int32_t key_of(int i) const { return at[i].valid(at[i].id) ? run[i] << 20 | at[i].id : END; }
+  __device__ __forceinline__ int next() const { return turn == 2 ? 0 : turn + 1; }
+  __device__ __forceinline__ void offer(Lds& l, bool first) const {  // first: of a token's rows
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (first)
+        atomicMin(reinterpret_cast<unsigned long long*>(&l.lowest[turn]),
+                  (unsigned long long)(uint32_t)key_of(i) << 32 | (uint32_t)at[i].page);
+  }
+  __device__ __forceinline__ void take(const AttendArgs& a, Lds& l, int h) {
+    const uint64_t low = l.lowest[turn];
+    if (threadIdx.x == 0) l.lowest[turn == 0 ? 2 : turn - 1] = ~0ull;
+    key = __builtin_amdgcn_readfirstlane((int32_t)(low >> 32));
+    page = __builtin_amdgcn_readfirstlane((int32_t)low);
+    if (page >= a.pages) page = -1;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const bool mine = key != END && key_of(i) == key;
+      seen[i] = mine && page >= 0 ? min(a.block - 1, pos[i] - at[i].id * a.block) + 1 : 0;
+      if (mine) at[i].advance(a, h);
+    }
+  }
+};
+//   All blocks: every run's, up to the last that one of its tokens sees: the same for all waves, without LDS's atomics.
+template <int R>
+struct Walk<false, R> {
+  struct Lds {
+    int32_t last[kTileWaves * 16], seq[kTileWaves * 16];  // of each run; -1: nothing to see
+  };
+  static constexpr int32_t END = 0x7fffffff;
+  int32_t run[R], pos[R], seen[R];
+  int32_t key = END, page = -1;  // (key: of a block that is there, anything but END)
+  int32_t now = -1, block = 0, last = -1, ahead = -1;
+  const int32_t* table;
+  __device__ __forceinline__ int32_t page_of(const AttendArgs& a, int32_t b) const { return b <= last ? table[b] : -1; }
+  // The block after this one; runs: how many there are.
+  __device__ __forceinline__ void take(const AttendArgs& a, const Lds& l, int split, int runs) {
+    block += a.splits;
+    while (block > last) {
+      if (++now >= runs) {
+        key = END, page = -1;
+#pragma unroll
+        for (int i = 0; i < R; ++i) seen[i] = 0;
+        return;
+      }
+      last = __builtin_amdgcn_readfirstlane(l.last[now]);
+      table = a.table + (int64_t)__builtin_amdgcn_readfirstlane(l.seq[now]) * a.max_blocks;
+      block = a.first + split;
+      ahead = page_of(a, block);
+    }
+    key = 0;
+    page = ahead >= 0 && ahead < a.pages ? ahead : -1;
+    ahead = page_of(a, block + a.splits);  // looked up a block ahead
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      seen[i] = run[i] == now && page >= 0 && pos[i] / a.block >= block ? min(a.block - 1, pos[i] - block * a.block) + 1 : 0;
+  }
+};
+
+// As attend_tiles: a workgroup's waves, tiles of neighbouring tokens of one cached head, walk their blocks through LDS.  A wave has
+// two tiles of 16 queries: with one, LDS would be read as long as the matrix unit computes.
+template <typename T, int CHUNKS, int STAGE, bool LISTS, bool PREFIX>
+__global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, 2) void q8_tiles(Q8AttendArgs a) {
+  typedef typename Parts<T>::Key Key;
+  typedef Tile<Key, CHUNKS, STAGE> L;
+  constexpr int TILES = CHUNKS * 2, N = 32, E = N / 4, R = q8_tiles_of<T>(CHUNKS), WAVES = kTileWaves / R;
+  constexpr int MOST = kTileWaves * 16;  // tokens
   __shared__ __align__(16) unsigned char lds[2][2 * L::kBytes];
   __shared__ __align__(16) float scales[2][2][STAGE];
   __shared__ uint64_t turns[2];
-  __shared__ uint64_t lowest[3];
+  __shared__ typename Walk<LISTS, R>::Lds walked;
+  static_assert(MOST <= 128, "two words of bits");
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int r = lane & 15, g = lane >> 4;
   int b = blockIdx.x;
@@ -287,94 +405,128 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS <= 4 && sizeof(T) == 2 ? 4 : 2) 
   const int split_at = b % a.splits;
   b /= a.splits;
   const int first = b % a.head_tiles * kRows;
-  const int t0 = b / a.head_tiles * (a.tile_tokens * WAVES);
+  const int t0 = b / a.head_tiles * (a.tile_tokens * kTileWaves);
   const int rows = min(kRows, a.group - first);
-  const int per_token = kRows / a.tile_tokens;
-  const int t = t0 + wave * a.tile_tokens + r / per_token, qr = r % per_token;
-  const bool row = t < a.tokens && qr < rows;
+  const int per_token = kRows / a.tile_tokens, qr = r % per_token;
   const int head = h * a.group + first + qr;
   const int D = a.head_dim;
-  bf16x8 q[Parts<T>::kQ][CHUNKS];
-  load_queries<T, CHUNKS>(a, row, t, head, [&](int i) { return (i * 4 + g) * 8; }, q);
-  State<TILES> st;
+  const auto token = [&](int i) { return t0 + (wave * R + i) * a.tile_tokens + r / per_token; };
+  const auto row = [&](int i) { return token(i) < a.tokens && qr < rows; };
+  typename Parts<T>::Key8 q[R][Parts<T>::kQ][CHUNKS];
+  State<TILES> st[R];
 #pragma unroll
-  for (int c = 0; c < TILES; ++c) st.o[c] = f32x4{0, 0, 0, 0};
-  st.m = -INFINITY, st.l = 0.0f;
+  for (int i = 0; i < R; ++i) {
+    load_queries<T, CHUNKS>(a, row(i), token(i), head, [&](int c) { return (c * 4 + g) * 8; }, q[i]);
+#pragma unroll
+    for (int c = 0; c < TILES; ++c) st[i].o[c] = f32x4{0, 0, 0, 0};
+    st[i].m = -INFINITY, st[i].l = 0.0f;
+  }
 
-  static_assert(16 * WAVES <= 128, "two words of bits");
+  // Bit i of `turns`: token i is of another sequence than token i - 1.
   if (wave < 2) {
     const int i = wave * 64 + lane, ti = t0 + i;
-    const bool turn = !PREFIX && i > 0 && i < a.tile_tokens * WAVES && ti < a.tokens && a.seq[ti] != a.seq[ti - 1];
+    const bool turn = !PREFIX && i > 0 && i < a.tile_tokens * kTileWaves && ti < a.tokens && a.seq[ti] != a.seq[ti - 1];
     const uint64_t bits = __ballot(turn);
     if (lane == 0) turns[wave] = bits;
   }
-  if (threadIdx.x < 3) lowest[threadIdx.x] = ~0ull;
-  int32_t p = -1, seq = -1;
-  if (t < a.tokens) p = a.pos[t], seq = a.seq[t];
+  if constexpr (LISTS) {
+    if (threadIdx.x < 3) walked.lowest[threadIdx.x] = ~0ull;
+  } else {
+    for (int i = threadIdx.x; i < MOST; i += WAVES * 64) walked.last[i] = -1;
+  }
+  int32_t p[R], seq[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    p[i] = seq[i] = -1;
+    if (token(i) < a.tokens) p[i] = a.pos[token(i)], seq[i] = a.seq[token(i)];
+  }
   __syncthreads();
-  const int place = t - t0;
-  const int32_t run = __popcll(turns[0] & (place >= 63 ? ~0ull : (2ull << place) - 1)) +
-                      (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
-  const bool filler = p < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
-  if (PREFIX) seq = 0, p = (int32_t)min((int64_t)p, (int64_t)a.prefix * a.block - 1);
-  Cursor at;
-  at.t = t, at.seq = seq, at.last = min(p / a.block, a.max_blocks - 1), at.share = split_at;
-  at.n = filler ? 0 : a.chosen ? a.blocks : at.last + 1;
-  at.start(a, h);
-  const auto key = [&] { return at.valid(at.id) ? run << 20 | at.id : END; };
-  const auto offer = [&](int turn) {
-    if (g == 0 && qr == 0)
-      atomicMin(reinterpret_cast<unsigned long long*>(&lowest[turn]),
-                (unsigned long long)(uint32_t)key() << 32 | (uint32_t)at.page);
+  Walk<LISTS, R> walk;
+  const auto run_of = [&](int place) {
+    return __popcll(turns[0] & (place >= 63 ? ~0ull : (2ull << place) - 1)) +
+           (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
   };
-  int32_t block_key = END, block_page = -1, seen = 0;
-  const auto take = [&](int turn) {
-    const uint64_t low = lowest[turn];
-    if (threadIdx.x == 0) lowest[turn == 0 ? 2 : turn - 1] = ~0ull;
-    block_key = __builtin_amdgcn_readfirstlane((int32_t)(low >> 32));
-    block_page = __builtin_amdgcn_readfirstlane((int32_t)low);
-    if (block_page >= a.pages) block_page = -1;
-    const bool mine = block_key != END && key() == block_key;
-    seen = mine && block_page >= 0 ? min(a.block - 1, p - at.id * a.block) + 1 : 0;
-    if (mine) at.advance(a, h);
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const bool filler = p[i] < 0 || (uint32_t)seq[i] >= (uint32_t)a.sequences;
+    if (PREFIX) seq[i] = 0, p[i] = (int32_t)min((int64_t)p[i], (int64_t)a.prefix * a.block - 1);
+    walk.run[i] = run_of(token(i) - t0), walk.pos[i] = p[i], walk.seen[i] = 0;
+    const int last = min(p[i] / a.block, a.max_blocks - 1);
+    if constexpr (LISTS) {
+      Cursor& at = walk.at[i];
+      at.t = token(i), at.seq = seq[i], at.last = last, at.share = split_at;
+      at.n = filler ? 0 : a.blocks;
+      at.start(a, h);
+    } else {
+      if (filler) walk.run[i] = -1;
+      if (!filler && g == 0 && qr == 0) {
+        atomicMax(&walked.last[walk.run[i]], last);
+        walked.seq[walk.run[i]] = seq[i];
+      }
+    }
+  }
+  const int runs = __builtin_amdgcn_readfirstlane(run_of(127) + 1);
+  const auto take = [&] {
+    if constexpr (LISTS)
+      walk.take(a, walked, h);
+    else
+      walk.take(a, walked, split_at, runs);
+  };
+  const auto offer = [&] {
+    if constexpr (LISTS) walk.offer(walked, g == 0 && qr == 0);
   };
   const int stage = min(STAGE, a.block), stages = a.block / stage;
-  Q8Stage<CHUNKS, STAGE> next_stage = {};
+  Q8Stage<T, CHUNKS, STAGE, WAVES> next_stage = {};
 
-  int turn = 0, buffer = 0, s = 0;
-  const auto next = [&] { return turn == 2 ? 0 : turn + 1; };
-  offer(turn);
+  int buffer = 0, s = 0;
+  offer();
   __syncthreads();
-  take(turn);
-  offer(turn = next());
-  if (block_key != END) {
-    if (block_page >= 0) next_stage.load(a, block_page, h, 0, stage);
+  take();
+  if constexpr (LISTS) walk.turn = walk.next();
+  offer();
+  if (walk.key != walk.END) {
+    if (walk.page >= 0) next_stage.load(a, walk.page, h, 0, stage);
     next_stage.store(a, stage, lds[0], scales[0]);
   }
-  while (block_key != END) {
-    const int32_t now_seen = seen - s * stage;
+  while (walk.key != walk.END) {
+    int32_t now_seen[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) now_seen[i] = walk.seen[i] - s * stage;
     __syncthreads();  // the stage is in LDS, the other buffer is free, the offers are made
     if (++s == stages) {
       s = 0;
-      take(turn);
-      if (block_key != END) offer(turn = next());
+      take();
+      if constexpr (LISTS) {
+        if (walk.key != walk.END) walk.turn = walk.next(), offer();
+      }
     }
-    const bool more = block_key != END && block_page >= 0;
-    if (more) next_stage.load(a, block_page, h, s * stage, stage);
-    for (int u = 0; u < stage && __any(now_seen > u); u += N) {
-      float x[E], ks[E], vs[E];
+    const bool more = walk.key != walk.END && walk.page >= 0;
+    if (more) next_stage.load(a, walk.page, h, s * stage, stage);
+    for (int u = 0; u < stage; u += N) {
+      bool any[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) any[i] = __any(now_seen[i] > u);
+      if (!any[0] && !any[R - 1]) break;
+      float x[R][E];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        f32x4 acc = {0, 0, 0, 0};
+        f32x4 acc[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) acc[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-          const bf16x8 y = key_piece<__bf16, CHUNKS, STAGE>(lds[buffer], half * CHUNKS + c, u, D, r, g);
+          const auto y = key_piece<Key, CHUNKS, STAGE>(lds[buffer], half * CHUNKS + c, u, D, r, g);
 #pragma unroll
-          for (int part = 0; part < Parts<T>::kQ; ++part) acc = mfma(y, q[part][c], acc);
+          for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int part = 0; part < Parts<T>::kQ; ++part) acc[i] = mfma(y, q[i][part][c], acc[i]);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * half + i] = acc[i];
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[i][4 * half + e] = acc[i][e];
       }
+      float ks[E], vs[E];
 #pragma unroll
       for (int i = 0; i < E; i += 4) {
         const f32x4 y = *reinterpret_cast<const f32x4*>(&scales[buffer][0][u + E * g + i]);
@@ -382,29 +534,41 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS <= 4 && sizeof(T) == 2 ? 4 : 2) 
 #pragma unroll
         for (int e = 0; e < 4; ++e) ks[i + e] = y[e], vs[i + e] = z[e];
       }
-      q8_step<true, T, E, TILES>(
-          a.scale2, x, ks, vs, [&](int c, int) { return value_piece<__bf16, CHUNKS, STAGE>(lds[buffer], c, u, r, g); },
-          now_seen - u, g, st);
+      bf16x8 w[R][Parts<T>::kP][1];
+#pragma unroll
+      for (int i = 0; i < R; ++i) q8_weights<true, T, E, TILES>(a.scale2, x[i], ks, vs, now_seen[i] - u, g, st[i], w[i]);
+#pragma unroll
+      for (int c = 0; c < TILES; ++c) {
+        const bf16x8 v = value_piece<__bf16, CHUNKS, STAGE>(lds[buffer], c, u, r, g);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int k = 0; k < Parts<T>::kP; ++k) st[i].o[c] = mfma(v, w[i][k][0], st[i].o[c]);
+      }
     }
     if (more) next_stage.store(a, stage, lds[buffer ^ 1], scales[buffer ^ 1]);
     buffer ^= 1;
   }
 
-  const float l = over_groups_sum(st.l);
-  if (!row) return;
-  if (a.parts > 1)
-    store_part(a, split_at, t, head, g, st, l);
-  else
-    store_row<T>(a, t, head, g, st, st.m, l);
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const float l = over_groups_sum(st[i].l);
+    if (!row(i)) continue;
+    if (a.parts > 1)
+      store_part(a, split_at, token(i), head, g, st[i], l);
+    else
+      store_row<T>(a, token(i), head, g, st[i], st[i].m, l);
+  }
 }
 
 template <typename T, int DIMS, int CHUNKS>
 hipError_t start(const Q8AttendArgs& a, const AttendShape& shape, hipStream_t stream) {
   if (a.tile_tokens > 0) {
     constexpr int LONG = power_of_two(CHUNKS) * 64, STAGE = LONG <= 256 ? 64 : 16384 / LONG;
-    static_assert(STAGE * CHUNKS * 32 <= kTileWaves * 64 * 16, "a thread has one piece of a stage's keys");
-    const auto kernel = a.prefix ? q8_tiles<T, CHUNKS, STAGE, kTileWaves, true> : q8_tiles<T, CHUNKS, STAGE, kTileWaves, false>;
-    kernel<<<(unsigned)shape.groups, shape.threads, 0, stream>>>(a);
+    const auto kernel = a.prefix   ? q8_tiles<T, CHUNKS, STAGE, false, true>
+                        : a.chosen ? q8_tiles<T, CHUNKS, STAGE, true, false>
+                                   : q8_tiles<T, CHUNKS, STAGE, false, false>;
+    kernel<<<(unsigned)shape.groups, kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, 0, stream>>>(a);
   } else {
     const auto kernel = a.block == 32 ? q8_kernel<T, DIMS, 32> : q8_kernel<T, DIMS, 64>;
     kernel<<<(unsigned)shape.groups, shape.threads, 0, stream>>>(a);
