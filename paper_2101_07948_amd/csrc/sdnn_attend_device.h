@@ -530,6 +530,172 @@ struct Cursor {
   }
 };
 
+// The tiles of a wave: R of 16 queries each, of neighbouring tokens of one cached head, 16 / group tokens to a tile (a token's
+// queries take a power of two of its rows); a workgroup has kTileWaves tiles.
+template <int R>
+struct TileRows {
+  int h, split, t0, rows, per_token, qr, head, wave, r, g;
+  int32_t tokens, tile_tokens;
+  __device__ __forceinline__ explicit TileRows(const AttendArgs& a) {
+    const int lane = threadIdx.x % 64;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, g = lane >> 4;
+    int b = blockIdx.x;
+    h = b % a.kv_heads;
+    b /= a.kv_heads;
+    split = b % a.splits;
+    b /= a.splits;
+    const int first = b % a.head_tiles * kRows;
+    t0 = b / a.head_tiles * (a.tile_tokens * kTileWaves);
+    rows = min(kRows, a.group - first);
+    per_token = kRows / a.tile_tokens, qr = r % per_token;
+    head = h * a.group + first + qr;
+    tokens = a.tokens, tile_tokens = a.tile_tokens;
+  }
+  __device__ __forceinline__ int token(int i) const { return t0 + (wave * R + i) * tile_tokens + r / per_token; }
+  __device__ __forceinline__ bool row(int i) const { return token(i) < tokens && qr < rows; }
+};
+
+// Which blocks a workgroup goes through, in what order, and what each query sees of them.  `key` is END past the last, `page` the
+// block's (-1: none), `seen` the tokens of it that this lane's queries see (0 and less: none).  A run: tokens of one sequence
+// within the workgroup's.
+template <bool LISTS, int R>
+struct Walk;
+
+struct WalkRuns {
+  uint64_t turns[2];  // bit i: token i is of another sequence than token i - 1 (a workgroup has at most 128)
+  static_assert(16 * kTileWaves <= 128, "two words of bits");
+  template <bool PREFIX>
+  __device__ __forceinline__ void find(const AttendArgs& a, int t0) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    if (wave >= 2) return;
+    const int i = wave * 64 + lane, t = t0 + i;
+    const bool turn = !PREFIX && i > 0 && i < a.tile_tokens * kTileWaves && t < a.tokens && a.seq[t] != a.seq[t - 1];
+    const uint64_t bits = __ballot(turn);
+    if (lane == 0) turns[wave] = bits;
+  }
+  __device__ __forceinline__ int32_t run_of(int place) const {
+    return __popcll(turns[0] & (place >= 63 ? ~0ull : (2ull << place) - 1)) +
+           (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
+  }
+};
+
+// Lists: as in attend_tiles: each token offers its lowest block not yet passed, a block ahead; the lowest is next.
+template <int R>
+struct Walk<true, R> {
+  struct Lds {
+    WalkRuns runs;
+    uint64_t lowest[3];  // key and page of the lowest block that is offered, in turn
+  };
+  static constexpr int32_t END = 0x7fffffff;
+  Cursor at[R];
+  int32_t run[R], pos[R], seen[R];
+  int32_t key = END, page = -1;
+  int turn = 0;
+  __device__ __forceinline__ int32_t key_of(int i) const { return at[i].valid(at[i].id) ? run[i] << 20 | at[i].id : END; }
+  __device__ __forceinline__ void offer(const TileRows<R>& t, Lds& l) const {  // one row of each token
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (t.g == 0 && t.qr == 0)
+        atomicMin(reinterpret_cast<unsigned long long*>(&l.lowest[turn]),
+                  (unsigned long long)(uint32_t)key_of(i) << 32 | (uint32_t)at[i].page);
+  }
+  template <bool PREFIX>
+  __device__ __forceinline__ void start(const AttendArgs& a, const TileRows<R>& t, Lds& l) {
+    l.runs.template find<PREFIX>(a, t.t0);
+    if (threadIdx.x < 3) l.lowest[threadIdx.x] = ~0ull;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      int32_t seq = -1;
+      pos[i] = -1;
+      if (t.token(i) < a.tokens) pos[i] = a.pos[t.token(i)], seq = a.seq[t.token(i)];
+      run[i] = l.runs.run_of(t.token(i) - t.t0), seen[i] = 0;
+      Cursor& c = at[i];
+      c.t = t.token(i), c.seq = seq, c.last = min(pos[i] / a.block, a.max_blocks - 1), c.share = t.split;
+      c.n = pos[i] < 0 || (uint32_t)seq >= (uint32_t)a.sequences ? 0 : a.blocks;
+      c.start(a, t.h);
+    }
+    offer(t, l);
+    __syncthreads();
+    advance(a, t, l, true);
+  }
+  // To the next block; after a barrier past the offers.
+  __device__ __forceinline__ void advance(const AttendArgs& a, const TileRows<R>& t, Lds& l, bool first = false) {
+    const uint64_t low = l.lowest[turn];
+    if (threadIdx.x == 0) l.lowest[turn == 0 ? 2 : turn - 1] = ~0ull;  // all waves have read it: room for the next but one
+    key = __builtin_amdgcn_readfirstlane((int32_t)(low >> 32));
+    page = __builtin_amdgcn_readfirstlane((int32_t)low);
+    if (page >= a.pages) page = -1;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const bool mine = key != END && key_of(i) == key;
+      seen[i] = mine && page >= 0 ? min(a.block - 1, pos[i] - at[i].id * a.block) + 1 : 0;
+      if (mine) at[i].advance(a, t.h);
+    }
+    if (key == END && !first) return;
+    turn = turn == 2 ? 0 : turn + 1;
+    offer(t, l);
+  }
+};
+
+// All blocks: every run's from `first` on, up to the last that one of its tokens sees: the same for all waves.  (PREFIX: those of
+// AttendArgs::prefix, one run of tokens whatever their sequences.)
+template <int R>
+struct Walk<false, R> {
+  struct Lds {
+    WalkRuns runs;
+    int32_t last[kTileWaves * 16], seq[kTileWaves * 16];  // of each run; last -1: nothing to see
+  };
+  static constexpr int32_t END = 0x7fffffff;
+  int32_t run[R], pos[R], seen[R];
+  int32_t key = END, page = -1;
+  int32_t runs, now = -1, block = 0, last = -1, ahead = -1;
+  const int32_t* table;
+  __device__ __forceinline__ int32_t page_of(int32_t b) const { return b <= last ? table[b] : -1; }
+  template <bool PREFIX>
+  __device__ __forceinline__ void start(const AttendArgs& a, const TileRows<R>& t, Lds& l) {
+    l.runs.template find<PREFIX>(a, t.t0);
+    for (int i = threadIdx.x; i < kTileWaves * 16; i += blockDim.x) l.last[i] = -1;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      int32_t seq = -1;
+      pos[i] = -1;
+      if (t.token(i) < a.tokens) pos[i] = a.pos[t.token(i)], seq = a.seq[t.token(i)];
+      const bool filler = pos[i] < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
+      if (PREFIX) seq = 0, pos[i] = (int32_t)min((int64_t)pos[i], (int64_t)a.prefix * a.block - 1);
+      run[i] = filler ? -1 : l.runs.run_of(t.token(i) - t.t0), seen[i] = 0;
+      if (!filler && t.g == 0 && t.qr == 0) {
+        atomicMax(&l.last[run[i]], min(pos[i] / a.block, a.max_blocks - 1));
+        l.seq[run[i]] = seq;
+      }
+    }
+    runs = __builtin_amdgcn_readfirstlane(l.runs.run_of(127) + 1);
+    __syncthreads();
+    advance(a, t, l);
+  }
+  __device__ __forceinline__ void advance(const AttendArgs& a, const TileRows<R>& t, const Lds& l) {
+    block += a.splits;
+    while (block > last) {
+      if (++now >= runs) {
+        key = END, page = -1;
+#pragma unroll
+        for (int i = 0; i < R; ++i) seen[i] = 0;
+        return;
+      }
+      last = __builtin_amdgcn_readfirstlane(l.last[now]);
+      table = a.table + (int64_t)__builtin_amdgcn_readfirstlane(l.seq[now]) * a.max_blocks;
+      block = a.first + t.split;
+      ahead = page_of(block);
+    }
+    key = 0;
+    page = ahead >= 0 && ahead < a.pages ? ahead : -1;
+    ahead = page_of(block + a.splits);  // looked up a block ahead
+#pragma unroll
+    for (int i = 0; i < R; ++i) seen[i] = run[i] == now && page >= 0 ? min(a.block - 1, pos[i] - block * a.block) + 1 : 0;
+  }
+};
+
 template <typename T>
 hipError_t join(const AttendArgs& a, int64_t groups, hipStream_t stream) {
   if (a.parts > 1 && a.parts <= kFewParts)

@@ -256,16 +256,18 @@ __global__ __launch_bounds__(kWaves * 64, q8_waves(2 * DIMS)) void q8_kernel(Q8A
 
 // ---------------------------------------------------------------- many tokens of a sequence
 
-// Tiles of 16 queries to a wave of q8_tiles: two where their queries and sums fit the registers, so that what the wave reads from
-// LDS serves both.  A workgroup has kTileWaves tiles.
+// Tiles of 16 queries to a wave of q8_tiles.  In 32 bits, whose parts make three products of what is read from LDS, two where
+// they fit the registers; in 16 bits one, which leaves room for four waves to a SIMD.  (One and two: 2048 tokens at the end of
+// 8192, 32 queries on 8 heads of 128, 450 us and 461; at the end of 4096, 12 heads of 64, 80 and 93; 512 tokens, 16 queries on 4
+// heads of 192, 68 and 103; 512 tokens of 12 heads of 64 in 32 bits 55 and 48.)
 template <typename T>
 constexpr int q8_tiles_of(int chunks) {
-  return 2 * (4 * Parts<T>::kQ + 8) * chunks <= 144 ? 2 : 1;
+  return sizeof(T) == 4 && chunks <= 3 ? 2 : 1;
 }
 
 // A stage of `tokens` tokens on its way to LDS: a thread holds pieces of 16 numbers of keys' rows and of values', and some of
 // the threads a scale.  They are asked for while the stage before is computed, and widened on their way into the tile, so that
-// its waves find matrix operands there.
+// its waves find matrix operands there.  Where a thread's pieces come from and go to is worked out once.
 template <typename T, int CHUNKS, int STAGE, int WAVES>
 struct Q8Stage {
   static constexpr int kThreads = WAVES * 64, kPieces = (STAGE * CHUNKS * 2 + kThreads - 1) / kThreads;
@@ -273,220 +275,92 @@ struct Q8Stage {
   static_assert(2 * STAGE <= kThreads, "a scale to a thread");
   i32x4 k[kPieces], v[kPieces];
   float scale;
-  __device__ __forceinline__ void load(const Q8AttendArgs& a, int page, int h, int t0, int tokens) {
-    const int D = a.head_dim, P = a.block, per = tokens / 16;  // (2 or 4)
+  int32_t from[kPieces], k_to[kPieces][2], v_to[kPieces][2];  // from: of values; those of keys lie one after the other
+  bool there[kPieces], scaled;
+  __device__ __forceinline__ Q8Stage(const AttendArgs& a, int tokens) {
+    const int D = a.head_dim, per = tokens / 16;  // (2 or 4)
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int i = threadIdx.x + j * kThreads, d = i / per, y = i - d * per, row = i * 16 / D, x = (i * 16 - row * D) / 8;
+      there[j] = i * 16 < tokens * D;
+      from[j] = d * a.block + y * 16;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        k_to[j][e] = (int)(L::key(nullptr, row, x + e) - static_cast<const unsigned char*>(nullptr));
+        v_to[j][e] = (int)(L::value(nullptr, d, y * 2 + e) - static_cast<const unsigned char*>(nullptr));
+      }
+      k[j] = v[j] = i32x4{0, 0, 0, 0};
+    }
+    scaled = threadIdx.x < 2 * STAGE && (int)threadIdx.x % STAGE < tokens;
+    scale = 0.0f;
+  }
+  __device__ __forceinline__ void load(const Q8AttendArgs& a, int page, int h, int t0) {
+    const int D = a.head_dim, P = a.block;
     const int64_t at = ((int64_t)page * a.kv_heads + h) * P;
     const int8_t* kp = static_cast<const int8_t*>(a.k_pages) + (at + t0) * D;
     const int8_t* vp = static_cast<const int8_t*>(a.v_pages) + at * D + t0;
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = threadIdx.x + j * kThreads, d = i / per;
-      if (i * 16 < tokens * D) {
-        k[j] = *reinterpret_cast<const i32x4*>(kp + i * 16);
-        v[j] = *reinterpret_cast<const i32x4*>(vp + d * P + (i - d * per) * 16);
+    for (int j = 0; j < kPieces; ++j)
+      if (there[j]) {
+        k[j] = *reinterpret_cast<const i32x4*>(kp + (threadIdx.x + j * kThreads) * 16);
+        v[j] = *reinterpret_cast<const i32x4*>(vp + from[j]);
       }
-    }
-    const int i = threadIdx.x;
-    if (i < 2 * STAGE && i % STAGE < tokens) scale = (i < STAGE ? a.k_scales : a.v_scales)[at + t0 + i % STAGE];
+    if (scaled) scale = (threadIdx.x < STAGE ? a.k_scales : a.v_scales)[at + t0 + threadIdx.x % STAGE];
   }
-  __device__ __forceinline__ void store(const Q8AttendArgs& a, int tokens, unsigned char* lds, float (&scales)[2][STAGE]) const {
-    const int D = a.head_dim, per = tokens / 16;
+  __device__ __forceinline__ void store(unsigned char* lds, float* scales) const {
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-      const int i = threadIdx.x + j * kThreads;
-      if (i * 16 < tokens * D) {
-        const int row = i * 16 / D, x = (i * 16 - row * D) / 8, d = i / per, y = (i - d * per) * 2;
+    for (int j = 0; j < kPieces; ++j)
+      if (there[j]) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          widen(k[j][2 * e], k[j][2 * e + 1],
-                reinterpret_cast<typename Parts<T>::Key8*>(const_cast<unsigned char*>(L::key(lds, row, x + e))));
-          widen(v[j][2 * e], v[j][2 * e + 1], reinterpret_cast<bf16x8*>(const_cast<unsigned char*>(L::value(lds, d, y + e))));
+          widen(k[j][2 * e], k[j][2 * e + 1], reinterpret_cast<typename Parts<T>::Key8*>(lds + k_to[j][e]));
+          widen(v[j][2 * e], v[j][2 * e + 1], reinterpret_cast<bf16x8*>(lds + v_to[j][e]));
         }
       }
-    }
     // (where no token was stored memory may hold what is infinite or not a number)
-    const int i = threadIdx.x;
-    if (i < 2 * STAGE) scales[i / STAGE][i % STAGE] = fabsf(scale) < INFINITY ? scale : 0.0f;
+    if (threadIdx.x < 2 * STAGE) scales[threadIdx.x] = fabsf(scale) < INFINITY ? scale : 0.0f;
   }
 };
 
-// Which blocks a workgroup goes through, in what order, and what each query sees of them.  A block's key is the run of tokens of
-// one sequence within the workgroup's, then the block.
-//   Lists: as in attend_tiles: each token offers its lowest block not yet passed, a block ahead.
-template <bool LISTS, int R>
-struct Walk;
-template <int R>
-struct Walk<true, R> {
-  struct Lds {
-    uint64_t lowest[3];  // key and page of the lowest block that is offered, in turn
-  };
-  static constexpr int32_t END = 0x7fffffff;
-  Cursor at[R];
-  int32_t run[R], pos[R], seen[R];
-  int32_t key = END, page = -1;
-  int turn = 0;
-  __device__ __forceinline__ int32_t key_of(int i) const { return at[i].valid(at[i].id) ? run[i] << 20 | at[i].id : END; }
-  __device__ __forceinline__ int next() const { return turn == 2 ? 0 : turn + 1; }
-  __device__ __forceinline__ void offer(Lds& l, bool first) const {  // first: of a token's rows
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-      if (first)
-        atomicMin(reinterpret_cast<unsigned long long*>(&l.lowest[turn]),
-                  (unsigned long long)(uint32_t)key_of(i) << 32 | (uint32_t)at[i].page);
-  }
-  __device__ __forceinline__ void take(const AttendArgs& a, Lds& l, int h) {
-    const uint64_t low = l.lowest[turn];
-    if (threadIdx.x == 0) l.lowest[turn == 0 ? 2 : turn - 1] = ~0ull;
-    key = __builtin_amdgcn_readfirstlane((int32_t)(low >> 32));
-    page = __builtin_amdgcn_readfirstlane((int32_t)low);
-    if (page >= a.pages) page = -1;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const bool mine = key != END && key_of(i) == key;
-      seen[i] = mine && page >= 0 ? min(a.block - 1, pos[i] - at[i].id * a.block) + 1 : 0;
-      if (mine) at[i].advance(a, h);
-    }
-  }
-};
-//   All blocks: every run's, up to the last that one of its tokens sees: the same for all waves, without LDS's atomics.
-template <int R>
-struct Walk<false, R> {
-  struct Lds {
-    int32_t last[kTileWaves * 16], seq[kTileWaves * 16];  // of each run; -1: nothing to see
-  };
-  static constexpr int32_t END = 0x7fffffff;
-  int32_t run[R], pos[R], seen[R];
-  int32_t key = END, page = -1;  // (key: of a block that is there, anything but END)
-  int32_t now = -1, block = 0, last = -1, ahead = -1;
-  const int32_t* table;
-  __device__ __forceinline__ int32_t page_of(const AttendArgs& a, int32_t b) const { return b <= last ? table[b] : -1; }
-  // The block after this one; runs: how many there are.
-  __device__ __forceinline__ void take(const AttendArgs& a, const Lds& l, int split, int runs) {
-    block += a.splits;
-    while (block > last) {
-      if (++now >= runs) {
-        key = END, page = -1;
-#pragma unroll
-        for (int i = 0; i < R; ++i) seen[i] = 0;
-        return;
-      }
-      last = __builtin_amdgcn_readfirstlane(l.last[now]);
-      table = a.table + (int64_t)__builtin_amdgcn_readfirstlane(l.seq[now]) * a.max_blocks;
-      block = a.first + split;
-      ahead = page_of(a, block);
-    }
-    key = 0;
-    page = ahead >= 0 && ahead < a.pages ? ahead : -1;
-    ahead = page_of(a, block + a.splits);  // looked up a block ahead
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-      seen[i] = run[i] == now && page >= 0 && pos[i] / a.block >= block ? min(a.block - 1, pos[i] - block * a.block) + 1 : 0;
-  }
-};
-
-// As attend_tiles: a workgroup's waves, tiles of neighbouring tokens of one cached head, walk their blocks through LDS.  A wave has
-// two tiles of 16 queries: with one, LDS would be read as long as the matrix unit computes.
+// As attend_tiles: a workgroup's waves, tiles of neighbouring tokens of one cached head, walk their blocks through LDS.
 template <typename T, int CHUNKS, int STAGE, bool LISTS, bool PREFIX>
-__global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, 2) void q8_tiles(Q8AttendArgs a) {
+__global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, CHUNKS <= 4 && sizeof(T) == 2 ? 4 : 2) void q8_tiles(Q8AttendArgs a) {
   typedef typename Parts<T>::Key Key;
   typedef Tile<Key, CHUNKS, STAGE> L;
   constexpr int TILES = CHUNKS * 2, N = 32, E = N / 4, R = q8_tiles_of<T>(CHUNKS), WAVES = kTileWaves / R;
-  constexpr int MOST = kTileWaves * 16;  // tokens
-  __shared__ __align__(16) unsigned char lds[2][2 * L::kBytes];
-  __shared__ __align__(16) float scales[2][2][STAGE];
-  __shared__ uint64_t turns[2];
+  __shared__ __align__(16) unsigned char lds[2 * 2 * L::kBytes];
+  __shared__ __align__(16) float scales[2 * 2 * STAGE];  // of keys, of values; twice
   __shared__ typename Walk<LISTS, R>::Lds walked;
-  static_assert(MOST <= 128, "two words of bits");
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int r = lane & 15, g = lane >> 4;
-  int b = blockIdx.x;
-  const int h = b % a.kv_heads;
-  b /= a.kv_heads;
-  const int split_at = b % a.splits;
-  b /= a.splits;
-  const int first = b % a.head_tiles * kRows;
-  const int t0 = b / a.head_tiles * (a.tile_tokens * kTileWaves);
-  const int rows = min(kRows, a.group - first);
-  const int per_token = kRows / a.tile_tokens, qr = r % per_token;
-  const int head = h * a.group + first + qr;
-  const int D = a.head_dim;
-  const auto token = [&](int i) { return t0 + (wave * R + i) * a.tile_tokens + r / per_token; };
-  const auto row = [&](int i) { return token(i) < a.tokens && qr < rows; };
+  const TileRows<R> t(a);
+  const int r = t.r, g = t.g, D = a.head_dim;
   typename Parts<T>::Key8 q[R][Parts<T>::kQ][CHUNKS];
   State<TILES> st[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    load_queries<T, CHUNKS>(a, row(i), token(i), head, [&](int c) { return (c * 4 + g) * 8; }, q[i]);
+    load_queries<T, CHUNKS>(a, t.row(i), t.token(i), t.head, [&](int c) { return (c * 4 + g) * 8; }, q[i]);
 #pragma unroll
     for (int c = 0; c < TILES; ++c) st[i].o[c] = f32x4{0, 0, 0, 0};
     st[i].m = -INFINITY, st[i].l = 0.0f;
   }
-
-  // Bit i of `turns`: token i is of another sequence than token i - 1.
-  if (wave < 2) {
-    const int i = wave * 64 + lane, ti = t0 + i;
-    const bool turn = !PREFIX && i > 0 && i < a.tile_tokens * kTileWaves && ti < a.tokens && a.seq[ti] != a.seq[ti - 1];
-    const uint64_t bits = __ballot(turn);
-    if (lane == 0) turns[wave] = bits;
-  }
-  if constexpr (LISTS) {
-    if (threadIdx.x < 3) walked.lowest[threadIdx.x] = ~0ull;
-  } else {
-    for (int i = threadIdx.x; i < MOST; i += WAVES * 64) walked.last[i] = -1;
-  }
-  int32_t p[R], seq[R];
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    p[i] = seq[i] = -1;
-    if (token(i) < a.tokens) p[i] = a.pos[token(i)], seq[i] = a.seq[token(i)];
-  }
-  __syncthreads();
   Walk<LISTS, R> walk;
-  const auto run_of = [&](int place) {
-    return __popcll(turns[0] & (place >= 63 ? ~0ull : (2ull << place) - 1)) +
-           (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
-  };
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const bool filler = p[i] < 0 || (uint32_t)seq[i] >= (uint32_t)a.sequences;
-    if (PREFIX) seq[i] = 0, p[i] = (int32_t)min((int64_t)p[i], (int64_t)a.prefix * a.block - 1);
-    walk.run[i] = run_of(token(i) - t0), walk.pos[i] = p[i], walk.seen[i] = 0;
-    const int last = min(p[i] / a.block, a.max_blocks - 1);
-    if constexpr (LISTS) {
-      Cursor& at = walk.at[i];
-      at.t = token(i), at.seq = seq[i], at.last = last, at.share = split_at;
-      at.n = filler ? 0 : a.blocks;
-      at.start(a, h);
-    } else {
-      if (filler) walk.run[i] = -1;
-      if (!filler && g == 0 && qr == 0) {
-        atomicMax(&walked.last[walk.run[i]], last);
-        walked.seq[walk.run[i]] = seq[i];
-      }
-    }
-  }
-  const int runs = __builtin_amdgcn_readfirstlane(run_of(127) + 1);
-  const auto take = [&] {
-    if constexpr (LISTS)
-      walk.take(a, walked, h);
-    else
-      walk.take(a, walked, split_at, runs);
-  };
-  const auto offer = [&] {
-    if constexpr (LISTS) walk.offer(walked, g == 0 && qr == 0);
-  };
+  walk.template start<PREFIX>(a, t, walked);
   const int stage = min(STAGE, a.block), stages = a.block / stage;
-  Q8Stage<T, CHUNKS, STAGE, WAVES> next_stage = {};
+  Q8Stage<T, CHUNKS, STAGE, WAVES> next_stage(a, stage);
+
+  // Where this lane's pieces of a step's keys and values lie: 32 tokens on, and 4, keys' rows are permuted alike, and so are
+  // values' 16 on.
+  int key_at[CHUNKS], value_at[STAGE / N];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c)
+    key_at[c] = (int)(L::key(nullptr, 8 * (r >> 2) + (r & 3), min(c * 4 + g, D / 8 - 1)) - static_cast<const unsigned char*>(nullptr));
+#pragma unroll
+  for (int u = 0; u < STAGE; u += N)
+    value_at[u / N] = (int)(L::value(nullptr, r, u / 8 + g) - static_cast<const unsigned char*>(nullptr));
 
   int buffer = 0, s = 0;
-  offer();
-  __syncthreads();
-  take();
-  if constexpr (LISTS) walk.turn = walk.next();
-  offer();
   if (walk.key != walk.END) {
-    if (walk.page >= 0) next_stage.load(a, walk.page, h, 0, stage);
-    next_stage.store(a, stage, lds[0], scales[0]);
+    if (walk.page >= 0) next_stage.load(a, walk.page, t.h, 0);
+    next_stage.store(lds, scales);
   }
   while (walk.key != walk.END) {
     int32_t now_seen[R];
@@ -495,19 +369,15 @@ __global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, 2) void q
     __syncthreads();  // the stage is in LDS, the other buffer is free, the offers are made
     if (++s == stages) {
       s = 0;
-      take();
-      if constexpr (LISTS) {
-        if (walk.key != walk.END) walk.turn = walk.next(), offer();
-      }
+      walk.advance(a, t, walked);
     }
     const bool more = walk.key != walk.END && walk.page >= 0;
-    if (more) next_stage.load(a, walk.page, h, s * stage, stage);
-    for (int u = 0; u < stage; u += N) {
-      bool any[R];
-#pragma unroll
-      for (int i = 0; i < R; ++i) any[i] = __any(now_seen[i] > u);
-      if (!any[0] && !any[R - 1]) break;
-      float x[R][E];
+    if (more) next_stage.load(a, walk.page, t.h, s * stage);
+    const unsigned char* tile = lds + buffer * 2 * L::kBytes;
+    const float* factors = scales + buffer * 2 * STAGE + E * g;
+    // a step of tokens u ...
+    const auto step = [&](int u) {
+      float x[R][E], ks[E], vs[E];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         f32x4 acc[R];
@@ -515,7 +385,7 @@ __global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, 2) void q
         for (int i = 0; i < R; ++i) acc[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-          const auto y = key_piece<Key, CHUNKS, STAGE>(lds[buffer], half * CHUNKS + c, u, D, r, g);
+          const auto y = *reinterpret_cast<const typename Parts<T>::Key8*>(tile + key_at[c] + (u + 4 * half) * L::kKeyPieces * 16);
 #pragma unroll
           for (int i = 0; i < R; ++i)
 #pragma unroll
@@ -526,11 +396,10 @@ __global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, 2) void q
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[i][4 * half + e] = acc[i][e];
       }
-      float ks[E], vs[E];
 #pragma unroll
       for (int i = 0; i < E; i += 4) {
-        const f32x4 y = *reinterpret_cast<const f32x4*>(&scales[buffer][0][u + E * g + i]);
-        const f32x4 z = *reinterpret_cast<const f32x4*>(&scales[buffer][1][u + E * g + i]);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(factors + u + i);
+        const f32x4 z = *reinterpret_cast<const f32x4*>(factors + STAGE + u + i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) ks[i + e] = y[e], vs[i + e] = z[e];
       }
@@ -539,25 +408,31 @@ __global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, 2) void q
       for (int i = 0; i < R; ++i) q8_weights<true, T, E, TILES>(a.scale2, x[i], ks, vs, now_seen[i] - u, g, st[i], w[i]);
 #pragma unroll
       for (int c = 0; c < TILES; ++c) {
-        const bf16x8 v = value_piece<__bf16, CHUNKS, STAGE>(lds[buffer], c, u, r, g);
+        const bf16x8 v = *reinterpret_cast<const bf16x8*>(tile + value_at[u / N] + c * 16 * L::kValuePieces * 16);
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
           for (int k = 0; k < Parts<T>::kP; ++k) st[i].o[c] = mfma(v, w[i][k][0], st[i].o[c]);
       }
-    }
-    if (more) next_stage.store(a, stage, lds[buffer ^ 1], scales[buffer ^ 1]);
+    };
+    int32_t most = now_seen[0];
+#pragma unroll
+    for (int i = 1; i < R; ++i) most = max(most, now_seen[i]);
+#pragma unroll
+    for (int u = 0; u < STAGE; u += N)
+      if (u < stage && __any(most > u)) step(u);
+    if (more) next_stage.store(lds + (buffer ^ 1) * 2 * L::kBytes, scales + (buffer ^ 1) * 2 * STAGE);
     buffer ^= 1;
   }
 
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const float l = over_groups_sum(st[i].l);
-    if (!row(i)) continue;
+    if (!t.row(i)) continue;
     if (a.parts > 1)
-      store_part(a, split_at, token(i), head, g, st[i], l);
+      store_part(a, t.split, t.token(i), t.head, g, st[i], l);
     else
-      store_row<T>(a, token(i), head, g, st[i], st[i].m, l);
+      store_row<T>(a, t.token(i), t.head, g, st[i], st[i].m, l);
   }
 }
 
