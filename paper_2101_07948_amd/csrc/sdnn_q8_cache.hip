@@ -26,9 +26,9 @@ struct RowArgs {
   const int32_t* seq;  // NULL: every token has rows (sdnn_norm_rope)
   const int32_t* table;
   const double* freq;
-  double amplitude, eps;
+  double amplitude, eps, inverse_dim;
   int32_t tokens, sequences, max_blocks, head_dim, pairs, norm;
-  int32_t lanes, waves;
+  int32_t lanes, waves, run, shares;  // see RowShape (waves) and RunShape (run, shares)
   // the cache
   int8_t* k_codes;
   int8_t* v_codes;
@@ -37,7 +37,7 @@ struct RowArgs {
   int64_t pages;
   int32_t kv_heads, block;
   int32_t row_groups;  // workgroups below this one do rows, the others windows of values
-  int32_t v_by_rows;   // values are written (read) with the keys, not by windows
+  int32_t v_by_rows;   // values are written with the keys, not by windows
   int32_t v_vec;       // windows: v's rows can be read 16 bytes at a time
 };
 
@@ -48,14 +48,34 @@ __device__ __forceinline__ int32_t page_of(const RowArgs& a, int32_t p, int32_t 
   return page >= 0 && page < a.pages ? page : -1;
 }
 
-template <typename X>
-__device__ __forceinline__ X over_lanes_sum(X x, int lanes) {
-  for (int s = 1; s < lanes; s *= 2) x += __shfl_xor(x, s);
+// x of another lane of its row of 16: quad_perm (0 to 0xff), mirrored (0x140), mirrored by halves (0x141).
+template <int CTRL>
+__device__ __forceinline__ float other(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double other(double x) {
+  const int64_t b = __double_as_longlong(x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xf, 0xf, true);
+  return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+// Over groups of `lanes` lanes (a power of two, uniform; every lane of the wave takes part), neighbours first.
+template <typename X, typename F>
+__device__ __forceinline__ X over_lanes(X x, int lanes, const F& f) {
+  if (lanes >= 2) x = f(x, other<0xb1>(x));
+  if (lanes >= 4) x = f(x, other<0x4e>(x));
+  if (lanes >= 8) x = f(x, other<0x141>(x));
+  if (lanes >= 16) x = f(x, other<0x140>(x));
+  if (lanes >= 32) x = f(x, __shfl_xor(x, 16));
+  if (lanes >= 64) x = f(x, __shfl_xor(x, 32));
   return x;
 }
+__device__ __forceinline__ double over_lanes_sum(double x, int lanes) {
+  return over_lanes(x, lanes, [](double a, double b) { return a + b; });
+}
 __device__ __forceinline__ float over_lanes_max(float x, int lanes) {
-  for (int s = 1; s < lanes; s *= 2) x = fmaxf(x, __shfl_xor(x, s));
-  return x;
+  return over_lanes(x, lanes, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // What a row is multiplied by to become numbers from -127 to 127, and its scale.  (Below 2^-100 the factor would leave the
@@ -69,42 +89,60 @@ __device__ __forceinline__ int8_t code_of(float x, float f) {
   return (int8_t)fminf(fmaxf(rintf(x * f), -127.0f), 127.0f);
 }
 
-// N codes in a row: one store where N bytes are a vector's.
-template <int N>
-__device__ __forceinline__ void store_codes(int8_t* p, const int8_t (&c)[N]) {
-  store_n<N>(p, true, c);
+// One kind's rows: fields of q, k or v by a uniform choice, value by value (a reference to one of them would put the kernel's
+// arguments into scratch memory).
+__device__ __forceinline__ HeadRows pick(const RowArgs& a, int kind) {
+  const bool q = kind == 0, k = kind == 1;
+  HeadRows r;
+  r.x = q ? a.q.x : k ? a.k.x : a.v.x;
+  r.y = q ? a.q.y : k ? a.k.y : a.v.y;
+  r.weight = q ? a.q.weight : k ? a.k.weight : a.v.weight;
+  r.x_token = q ? a.q.x_token : k ? a.k.x_token : a.v.x_token;
+  r.x_head = q ? a.q.x_head : k ? a.k.x_head : a.v.x_head;
+  r.y_token = q ? a.q.y_token : k ? a.k.y_token : a.v.y_token;
+  r.y_head = q ? a.q.y_head : k ? a.k.y_head : a.v.y_head;
+  r.heads = q ? a.q.heads : k ? a.k.heads : a.v.heads;
+  r.weight_head = q ? a.q.weight_head : k ? a.k.weight_head : a.v.weight_head;
+  r.x_aligned = q ? a.q.x_aligned : k ? a.k.x_aligned : a.v.x_aligned;
+  r.y_aligned = q ? a.q.y_aligned : k ? a.k.y_aligned : a.v.y_aligned;
+  return r;
 }
 
-// A wave's tasks: heads of one token, 64 / lanes of them at a time; a lane has 2 VP values of a row (ITER times: long heads
-// whose parts only divide by one), pairs in place, so that norm, rotation and the largest value need no more than a few
-// exchanges within a row's lanes.  The token's cosines and sines are computed once, by the wave together.
+// 1 / sqrt(m), rounded to 32 bits.  The instruction's estimate y has 20 bits at the least; with e = 1 - m y^2 what it lacks is
+// the factor 1 + e / 2 + 3/8 e^2 + ..., whose next term is below 2^-56.  (0 and infinity have the estimate's own answers.)
+// A root and a division of the library, one after the other, take several times the instructions.
+__device__ __forceinline__ float inverse_root(double m) {
+  const double y = __builtin_amdgcn_rsq(m), e = fma(-m * y, y, 1.0);
+  const double z = fma(y * e, fma(e, 0.375, 0.5), y);
+  return (float)(m > 0.0 && m < INFINITY ? z : y);
+}
+
+// What a workgroup of rows holds for its run of tokens.
+struct RunLds {
+  float2 cs[kRowRun * kMaxHeadDim / 2];
+  int32_t pos[kRowRun], page[kRowRun], filler[kRowRun];
+};
+
+// A workgroup has a run of tokens.  Their cosines and sines, 64-bit arithmetic, are computed once for all heads; an item of a
+// wave is 64 / lanes heads (a task) of B tokens, loaded while the item before is worked on; a wave has neighbouring
+// items, of few tasks, so that it seldom reads weights.  A lane has 2 VP values of a row (ITER
+// times: long heads whose parts only divide by one), pairs in place, so that norm, rotation and the largest value need no more
+// than a few exchanges within a row's lanes.
+//   The work is moving bytes.  Norms of 8001 tokens of 40 heads of 128 in 16 bits with weights of each head: 42.5 us, 164 MB at 3.9
+// TB/s; of 32768 tokens 137 to 140 us, 4.8 TB/s, a large copy's rate.  With a token to a wave, which read the weights of every head
+// anew: 52 us.  B = 4 where a lane has 16 values: 163 instead of 129 registers, and 169 us instead of 137.
 //   The sum of squares is one of 64-bit products, exact for 16-bit values, and its root is rounded once: a key comes out the
-// same whatever lanes its values lie in.
+// same whatever lanes its values lie in.  Where a row has lanes enough, lane b of a quad takes the root for token b of the batch.
 template <typename T, int VP, bool INTERLEAVED, bool CACHE>
-__device__ __forceinline__ void token_rows(const RowArgs& a, float2* cs) {
-  constexpr int ITER = VP == 1 ? 2 : 1;
-  const int lane = threadIdx.x % 64, D = a.head_dim;
-  const int64_t w = (int64_t)blockIdx.x * kRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int t = (int)(w / a.waves), part = (int)(w % a.waves);
-  const bool there = t < a.tokens;
-  int32_t p = 0, page = -1;
-  bool filler = false;
-  if (there) {
-    if (a.pos) p = a.pos[t];
-    if (a.seq) {
-      const int32_t s = a.seq[t];
-      filler = p < 0 || (uint32_t)s >= (uint32_t)a.sequences;
-      if (CACHE) page = page_of(a, p, s);
-    }
-    for (int i = lane; i < a.pairs; i += 64) cs[i] = rotation_of(a.freq, a.amplitude, p, i);
-  }
-  __syncthreads();
-  if (!there) return;
+__device__ __forceinline__ void token_rows(const RowArgs& a, RunLds& l) {
+  constexpr int ITER = VP == 1 ? 2 : 1, B = VP >= 8 ? 2 : 4;
+  const int lane = threadIdx.x % 64, D = a.head_dim, block = blockIdx.x;
+  const int t0 = (block / a.shares) * a.run, n = min(a.run, a.tokens - t0);
+  const int wave = block % a.shares * kRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int units = D / (2 * VP), turning = a.pairs / VP;
   const int u0 = lane & (a.lanes - 1), per = 64 / a.lanes, slot = lane / a.lanes;
   // this lane's values of a row: lo at d0, hi at d1 (neighbours: even and odd ones of 2 VP from d0)
   int d0[ITER], d1[ITER];
-  float2 f[ITER][VP];
 #pragma unroll
   for (int i = 0; i < ITER; ++i) {
     const int u = u0 + i * 64;
@@ -114,179 +152,230 @@ __device__ __forceinline__ void token_rows(const RowArgs& a, float2* cs) {
       d0[i] = u * VP, d1[i] = a.pairs + u * VP;
     else
       d0[i] = 2 * a.pairs + (u - turning) * 2 * VP, d1[i] = d0[i] + VP;
-#pragma unroll
-    for (int e = 0; e < VP; ++e)
-      if (u < turning) f[i][e] = cs[u * VP + e];
   }
   const auto has = [&](int i) { return u0 + i * 64 < units; };
-  const auto load = [&](const T* x, bool aligned, int i, bool paired, float (&lo)[VP], float (&hi)[VP]) {
-    if (INTERLEAVED && paired) {
-      T v[2 * VP];
-      load_n<2 * VP>(x + d0[i], aligned, v);
+  const int q_tasks = (a.q.heads + per - 1) / per, k_tasks = (a.k.heads + per - 1) / per;
+  const int v_tasks = CACHE && a.v_by_rows ? (a.v.heads + per - 1) / per : 0;
+  const int shift = a.run > B ? __builtin_ctz(a.run / B) : 0;  // batches of a run: a power of two
+  const int items = (q_tasks + k_tasks + v_tasks) << shift, each = (items + a.shares * kRowWaves - 1) / (a.shares * kRowWaves);
+  const int first = wave * each, end = min(first + each, items);
+  const auto kind_of = [&](int task) { return task < q_tasks ? 0 : task < q_tasks + k_tasks ? 1 : 2; };
+  const auto task_head = [&](int task, int kind) { return kind == 0 ? task : kind == 1 ? task - q_tasks : task - q_tasks - k_tasks; };
+  T next[B][ITER][2 * VP];
+  const auto load = [&](int item) {
+    const int task = item >> shift, b0 = (item - (task << shift)) * B;
+    const int kind = kind_of(task), h = task_head(task, kind) * per + slot;
+    const HeadRows r = pick(a, kind);
+    const T* x = static_cast<const T*>(r.x) + (t0 + b0) * r.x_token + (int64_t)h * r.x_head;
 #pragma unroll
-      for (int e = 0; e < VP; ++e) lo[e] = (float)v[2 * e], hi[e] = (float)v[2 * e + 1];
-    } else {
-      T l[VP], h[VP];
-      load_n<VP>(x + d0[i], aligned, l);
-      load_n<VP>(x + d1[i], aligned, h);
+    for (int b = 0; b < B; ++b)
 #pragma unroll
-      for (int e = 0; e < VP; ++e) lo[e] = (float)l[e], hi[e] = (float)h[e];
-    }
-  };
-  // Heads `h` of q or k: normed, rotated, then stored.
-  const auto rows = [&](const HeadRows& r, bool keys, int first) {
-    const int tasks = (r.heads + per - 1) / per;
-    int task = part - first % a.waves;
-    if (task < 0) task += a.waves;
-    if (task >= tasks) return;
-    float wl[ITER][VP], wh[ITER][VP];
-    const auto weights = [&](int h) {
+      for (int i = 0; i < ITER; ++i) {
 #pragma unroll
-      for (int i = 0; i < ITER; ++i)
+        for (int e = 0; e < 2 * VP; ++e) next[b][i][e] = (T)0.0f;
+        if (b0 + b >= n || h >= r.heads || !has(i)) continue;
+        const T* y = x + b * r.x_token;
+        if (INTERLEAVED) {
+          load_n<2 * VP>(y + d0[i], r.x_aligned, next[b][i]);
+        } else {
+          T lo[VP], hi[VP];
+          load_n<VP>(y + d0[i], r.x_aligned, lo);
+          load_n<VP>(y + d1[i], r.x_aligned, hi);
 #pragma unroll
-        for (int e = 0; e < VP; ++e) {
-          wl[i][e] = wh[i][e] = 1.0f;
-          if (a.norm && r.weight && has(i) && h < r.heads) {
-            const float* w = r.weight + (int64_t)h * r.weight_head;
-            wl[i][e] = w[INTERLEAVED ? d0[i] + 2 * e : d0[i] + e];
-            wh[i][e] = w[INTERLEAVED ? d0[i] + 2 * e + 1 : d1[i] + e];
-          }
+          for (int e = 0; e < VP; ++e) next[b][i][e] = lo[e], next[b][i][VP + e] = hi[e];
         }
-    };
-    if (r.weight_head == 0) weights(0);
-    for (; task < tasks; task += a.waves) {
-      const int h = task * per + slot;
-      const bool row = h < r.heads;
-      if (r.weight_head) weights(h);
-      float lo[ITER][VP] = {}, hi[ITER][VP] = {};
-      const T* x = static_cast<const T*>(r.x) + (int64_t)t * r.x_token + (int64_t)h * r.x_head;
+      }
+  };
+  if (first < end) load(first);
+  if (threadIdx.x < (unsigned)n) {
+    const int t = t0 + threadIdx.x;
+    const int32_t p = a.pos ? a.pos[t] : 0, s = a.seq ? a.seq[t] : 0;
+    l.pos[threadIdx.x] = p;
+    l.filler[threadIdx.x] = a.seq && (p < 0 || (uint32_t)s >= (uint32_t)a.sequences);
+    l.page[threadIdx.x] = CACHE ? page_of(a, p, s) : -1;
+  }
+  if (a.pairs)
+    for (int i = threadIdx.x; i < n * a.pairs; i += kRowThreads) {
+      const int t = i / a.pairs;
+      l.cs[i] = rotation_of(a.freq, a.amplitude, a.pos[t0 + t], i - t * a.pairs);
+    }
+  __syncthreads();
+  float w[ITER][2 * VP];  // the weights of `weighted`'s heads
+  int weighted = -1;
+  for (int item = first; item < end; ++item) {
+    const int task = item >> shift, b0 = (item - (task << shift)) * B;
+    const int kind = kind_of(task), h = task_head(task, kind) * per + slot;
+    const bool queries = kind == 0, values = kind == 2;
+    const HeadRows r = pick(a, kind);
+    const bool row = h < r.heads;
+    float x[B][ITER][2 * VP];  // pairs as they lie (neighbours), or firsts and then seconds
+#pragma unroll
+    for (int b = 0; b < B; ++b)
 #pragma unroll
       for (int i = 0; i < ITER; ++i)
-        if (row && has(i)) load(x, r.x_aligned, i, true, lo[i], hi[i]);
+#pragma unroll
+        for (int e = 0; e < 2 * VP; ++e) x[b][i][e] = (float)next[b][i][e];
+    if (item + 1 < end) load(item + 1);
+    if (!values) {
       if (a.norm) {
-        double s = 0.0;
+        if (task != weighted) {
+          weighted = task;
 #pragma unroll
-        for (int i = 0; i < ITER; ++i)
+          for (int i = 0; i < ITER; ++i)
 #pragma unroll
-          for (int e = 0; e < VP; ++e) {
-            s = fma((double)lo[i][e], (double)lo[i][e], s);
-            s = fma((double)hi[i][e], (double)hi[i][e], s);
-          }
-        s = over_lanes_sum(s, a.lanes);
-        const float root = (float)(1.0 / sqrt(s / D + a.eps));
+            for (int e = 0; e < 2 * VP; ++e) {
+              w[i][e] = 1.0f;
+              if (r.weight && has(i) && row)
+                w[i][e] = r.weight[(int64_t)h * r.weight_head + (INTERLEAVED || e < VP ? d0[i] + e : d1[i] + e - VP)];
+            }
+        }
+        double s[B];
 #pragma unroll
-        for (int i = 0; i < ITER; ++i)
+        for (int b = 0; b < B; ++b) {
+          s[b] = 0.0;
 #pragma unroll
-          for (int e = 0; e < VP; ++e) lo[i][e] = lo[i][e] * root * wl[i][e], hi[i][e] = hi[i][e] * root * wh[i][e];
+          for (int i = 0; i < ITER; ++i)
+#pragma unroll
+            for (int e = 0; e < 2 * VP; ++e) s[b] = fma((double)x[b][i][e], (double)x[b][i][e], s[b]);
+          s[b] = over_lanes_sum(s[b], a.lanes);
+        }
+        float root[B];
+        const auto root_of = [&](double s) { return inverse_root(fma(s, a.inverse_dim, a.eps)); };
+        if (a.lanes >= B) {
+          double mine = s[0];
+#pragma unroll
+          for (int b = 1; b < B; ++b) mine = (lane & (B - 1)) == b ? s[b] : mine;
+          const float r = root_of(mine);
+          if constexpr (B == 2)
+            root[0] = other<0xa0>(r), root[1] = other<0xf5>(r);
+          else
+            root[0] = other<0x00>(r), root[1] = other<0x55>(r), root[2] = other<0xaa>(r), root[3] = other<0xff>(r);
+        } else {
+#pragma unroll
+          for (int b = 0; b < B; ++b) root[b] = root_of(s[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+          for (int i = 0; i < ITER; ++i)
+#pragma unroll
+            for (int e = 0; e < 2 * VP; ++e) x[b][i][e] = x[b][i][e] * root[b] * w[i][e];
       }
 #pragma unroll
-      for (int i = 0; i < ITER; ++i)
-        if (u0 + i * 64 < turning) {
+      for (int i = 0; i < ITER; ++i) {
+        const int u = u0 + i * 64;
+        if (u >= turning) continue;
 #pragma unroll
-          for (int e = 0; e < VP; ++e) rotate(lo[i][e], hi[i][e], f[i][e], &lo[i][e], &hi[i][e]);
+        for (int b = 0; b < B; ++b) {
+          if (b0 + b >= n) continue;
+#pragma unroll
+          for (int e = 0; e < VP; ++e) {
+            const float2 f = l.cs[(b0 + b) * a.pairs + u * VP + e];
+            float& lo = x[b][i][INTERLEAVED ? 2 * e : e];
+            float& hi = x[b][i][INTERLEAVED ? 2 * e + 1 : VP + e];
+            rotate(lo, hi, f, &lo, &hi);
+          }
         }
-      if (CACHE && keys) {
+      }
+    }
+    if (CACHE && !queries) {
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
         float top = 0.0f, scale;
 #pragma unroll
         for (int i = 0; i < ITER; ++i)
 #pragma unroll
-          for (int e = 0; e < VP; ++e) top = fmaxf(top, fmaxf(fabsf(lo[i][e]), fabsf(hi[i][e])));
+          for (int e = 0; e < 2 * VP; ++e) top = fmaxf(top, fabsf(x[b][i][e]));
         const float c = code_factor(over_lanes_max(top, a.lanes), &scale);
-        if (!row || page < 0) continue;
-        const int64_t at = ((int64_t)page * a.kv_heads + h) * a.block + p % a.block;
-        int8_t* y = a.k_codes + at * D;
-        if (u0 == 0) a.k_scales[at] = scale;
+        if (b0 + b >= n || !row || l.page[b0 + b] < 0) continue;
+        const int place = l.pos[b0 + b] & (a.block - 1);
+        const int64_t head = (int64_t)l.page[b0 + b] * a.kv_heads + h;
+        if (u0 == 0) (values ? a.v_scales : a.k_scales)[head * a.block + place] = scale;
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
           if (!has(i)) continue;
-          int8_t n[2 * VP];
+          int8_t c8[2 * VP];
 #pragma unroll
-          for (int e = 0; e < VP; ++e) {
-            n[INTERLEAVED ? 2 * e : e] = code_of(lo[i][e], c);
-            n[INTERLEAVED ? 2 * e + 1 : VP + e] = code_of(hi[i][e], c);
+          for (int e = 0; e < 2 * VP; ++e) c8[e] = code_of(x[b][i][e], c);
+          if (values) {  // single tokens: a byte to each of the page's rows
+            int8_t* y = a.v_codes + head * D * a.block + place;
+#pragma unroll
+            for (int e = 0; e < 2 * VP; ++e) y[(INTERLEAVED || e < VP ? d0[i] + e : d1[i] + e - VP) * a.block] = c8[e];
+            continue;
           }
+          int8_t* y = a.k_codes + (head * a.block + place) * D;
           if (INTERLEAVED) {
-            store_codes<2 * VP>(y + d0[i], n);
+            store_n<2 * VP>(y + d0[i], true, c8);
           } else {
-            int8_t l[VP], g[VP];
+            int8_t lo[VP], hi[VP];
 #pragma unroll
-            for (int e = 0; e < VP; ++e) l[e] = n[e], g[e] = n[VP + e];
-            store_codes<VP>(y + d0[i], l);
-            store_codes<VP>(y + d1[i], g);
+            for (int e = 0; e < VP; ++e) lo[e] = c8[e], hi[e] = c8[VP + e];
+            store_n<VP>(y + d0[i], true, lo);
+            store_n<VP>(y + d1[i], true, hi);
           }
         }
-        continue;
       }
-      if (!row) continue;
-      T* y = static_cast<T*>(r.y) + (int64_t)t * r.y_token + (int64_t)h * r.y_head;
+      continue;
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      if (b0 + b >= n || !row) continue;
+      const bool filler = l.filler[b0 + b];
+      T* y = static_cast<T*>(r.y) + (t0 + b0 + b) * r.y_token + (int64_t)h * r.y_head;
 #pragma unroll
       for (int i = 0; i < ITER; ++i) {
         if (!has(i)) continue;
-        if (INTERLEAVED) {
-          T v[2 * VP];
+        T v[2 * VP];
 #pragma unroll
-          for (int e = 0; e < VP; ++e) v[2 * e] = (T)(filler ? 0.0f : lo[i][e]), v[2 * e + 1] = (T)(filler ? 0.0f : hi[i][e]);
+        for (int e = 0; e < 2 * VP; ++e) v[e] = (T)(filler ? 0.0f : x[b][i][e]);
+        if (INTERLEAVED) {
           store_n<2 * VP>(y + d0[i], r.y_aligned, v);
         } else {
-          T l[VP], g[VP];
+          T lo[VP], hi[VP];
 #pragma unroll
-          for (int e = 0; e < VP; ++e) l[e] = (T)(filler ? 0.0f : lo[i][e]), g[e] = (T)(filler ? 0.0f : hi[i][e]);
-          store_n<VP>(y + d0[i], r.y_aligned, l);
-          store_n<VP>(y + d1[i], r.y_aligned, g);
+          for (int e = 0; e < VP; ++e) lo[e] = v[e], hi[e] = v[VP + e];
+          store_n<VP>(y + d0[i], r.y_aligned, lo);
+          store_n<VP>(y + d1[i], r.y_aligned, hi);
         }
-      }
-    }
-  };
-  const int q_tasks = (a.q.heads + per - 1) / per, k_tasks = (a.k.heads + per - 1) / per;
-  rows(a.q, false, 0);
-  rows(a.k, CACHE, q_tasks);
-  if (!CACHE || !a.v_by_rows || page < 0) return;
-  // Values of single tokens: a byte to each of the page's rows.
-#pragma unroll
-  for (int i = 0; i < ITER; ++i) d0[i] = (u0 + i * 64) * 2 * VP, d1[i] = d0[i] + VP;
-  const int tasks = (a.v.heads + per - 1) / per;
-  int task = part - (q_tasks + k_tasks) % a.waves;
-  if (task < 0) task += a.waves;
-  for (; task < tasks; task += a.waves) {
-    const int h = task * per + slot;
-    const bool row = h < a.v.heads;
-    float lo[ITER][VP] = {}, hi[ITER][VP] = {}, top = 0.0f, scale;
-    const T* x = static_cast<const T*>(a.v.x) + (int64_t)t * a.v.x_token + (int64_t)h * a.v.x_head;
-#pragma unroll
-    for (int i = 0; i < ITER; ++i) {
-      if (row && has(i)) load(x, a.v.x_aligned, i, false, lo[i], hi[i]);
-#pragma unroll
-      for (int e = 0; e < VP; ++e) top = fmaxf(top, fmaxf(fabsf(lo[i][e]), fabsf(hi[i][e])));
-    }
-    const float c = code_factor(over_lanes_max(top, a.lanes), &scale);
-    if (!row) continue;
-    const int64_t head = (int64_t)page * a.kv_heads + h;
-    const int place = p % a.block;
-    if (u0 == 0) a.v_scales[head * a.block + place] = scale;
-    int8_t* y = a.v_codes + head * D * a.block + place;
-#pragma unroll
-    for (int i = 0; i < ITER; ++i) {
-      if (!has(i)) continue;
-#pragma unroll
-      for (int e = 0; e < VP; ++e) {
-        y[(int64_t)(d0[i] + e) * a.block] = code_of(lo[i][e], c);
-        y[(int64_t)(d1[i] + e) * a.block] = code_of(hi[i][e], c);
       }
     }
   }
 }
 
 // The turned values of a window of tokens in LDS, [token][value], rows a bank longer than the head.
+//   The tokens whose places in a page share a word of four are moved together if they are neighbours: group q has tokens
+// `lead` - 4 + 4 q ... + 3 of the window (lead: of the window's first token; in a window of several sequences the later ones' may
+// not fit).  group[q]: their page; -1: those that are in the window are taken one by one, from the list.
 struct TurnLds {
-  int32_t pos[kQ8Window], seq[kQ8Window], page[kQ8Window];
-  float scale[kQ8Window];
+  int32_t pos[kQ8Window], page[kQ8Window], loose[kQ8Window];
+  int32_t group[kQ8Window / 4 + 1], lead, singles;
+  float k_scale[kQ8Window], v_scale[kQ8Window];
   __align__(16) int8_t codes[kQ8Window * (kMaxHeadDim + 4)];
 };
 
+// PARTS: groups with fewer than four tokens in the window count as such (they can be read, but not written, by words).
+template <bool PARTS>
 __device__ __forceinline__ void load_window(const RowArgs& a, TurnLds& l, int t0, int n) {
-  for (int i = threadIdx.x; i < n; i += kRowThreads) {
-    const int32_t p = a.pos[t0 + i], s = a.seq[t0 + i];
-    l.pos[i] = p, l.seq[i] = s, l.page[i] = page_of(a, p, s);
+  const int i = threadIdx.x;
+  if (i < kQ8Window) {  // the first wave
+    static_assert(kQ8Window == 64, "a wave");
+    int32_t p = -1, s = -1, page = -1;
+    if (i < n) p = a.pos[t0 + i], s = a.seq[t0 + i], page = page_of(a, p, s);
+    l.pos[i] = p, l.page[i] = page;
+    const int32_t p0 = __builtin_amdgcn_readfirstlane(p), lead = p0 < 0 ? 0 : -p0 & 3;
+    const int q = (i - lead + 4) >> 2, begin = lead - 4 + 4 * q;  // this token's group and that one's first token
+    // Does the token lie where its group says?  Sequences' and pages' neighbours have neighbouring lanes.
+    const int from = max(begin, 0);
+    const int32_t fp = __shfl(p, from), fs = __shfl(s, from), fpage = __shfl(page, from);
+    const bool fits = page >= 0 && fpage == page && fs == s && p - fp == i - from && ((p - i + begin) & 3) == 0;
+    const uint64_t fit = __ballot(fits), there = __ballot(i < n);
+    const uint64_t mine = begin < 0 ? 15ull >> -begin : 15ull << begin;
+    const bool together = PARTS ? (there & mine) == (fit & mine) && (there & mine) : begin >= 0 && (fit & mine) == mine && begin + 4 <= kQ8Window;
+    if (i == from) l.group[q] = together ? page : -1;
+    if (i == 0 && lead == 0) l.group[0] = -1;  // no token is in it
+    const uint64_t singles = __ballot(i < n && !together);
+    if (i < n && !together) l.loose[__popcll(singles & ((1ull << i) - 1))] = i;
+    if (i == 0) l.lead = lead, l.singles = __popcll(singles);
   }
   __syncthreads();
 }
@@ -299,118 +388,109 @@ __device__ __forceinline__ void turn4(const uint32_t (&x)[4], uint32_t (&y)[4]) 
   y[2] = __builtin_amdgcn_perm(d, b, 0x05040100u), y[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
-// Groups of four tokens of a window whose places begin at a multiple of four: group q begins with token `lead` - 4 + 4 q
-// (lead: of the window's first token; in a window of several sequences groups of the later ones may not, which are taken
-// token by token).
-struct Groups {
-  int lead, count;
-  __device__ __forceinline__ Groups(const TurnLds& l, int n) {
-    lead = (4 - (l.pos[0] & 3)) & 3;
-    if (l.pos[0] < 0) lead = 0;
-    count = 1 + (max(n - lead, 0) + 3) / 4;
-  }
-  __device__ __forceinline__ int first(int q) const { return lead - 4 + 4 * q; }
-  // The four are neighbours of one page.
-  __device__ __forceinline__ bool whole(const TurnLds& l, int i, int n) const {
-    if (i < 0 || i + 4 > n || l.page[i] < 0 || (l.pos[i] & 3)) return false;
-    bool same = true;
-#pragma unroll
-    for (int j = 1; j < 4; ++j) same = same && l.seq[i + j] == l.seq[i] && l.pos[i + j] == l.pos[i] + j;
-    return same;
-  }
-};
+// What moves a window's tokens that no group has: f(token, value), the tokens dealt to the waves.
+template <typename F>
+__device__ __forceinline__ void each_loose(const TurnLds& l, int D, const F& f) {
+  for (int k = threadIdx.x / 64; k < l.singles; k += kRowWaves)
+    for (int d = threadIdx.x % 64; d < D; d += 64) f(l.loose[k], d);
+}
 
 // Values of a prompt: a window of one head's tokens is quantised, a row to a few lanes, and turned through LDS, so that four
 // tokens' numbers are one store and the window's are runs of 64 bytes of the page's rows.
 template <typename T>
 __device__ __forceinline__ void append_window(const RowArgs& a, TurnLds& l, int b) {
-  constexpr int V = 16 / sizeof(T);
+  constexpr int V = 16 / sizeof(T), B = 4;
   const int h = b % a.v.heads, t0 = b / a.v.heads * kQ8Window, n = min(kQ8Window, a.tokens - t0);
   const int D = a.head_dim, stride = D + 4;
-  load_window(a, l, t0, n);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int lanes = 1 << (32 - __builtin_clz(D / V - 1)), per = 64 / lanes;  // D / V >= 2
-  const int u = lane & (lanes - 1), d = u * V;
-  for (int i = wave * per + lane / lanes; i < n; i += kRowWaves * per) {
-    T x[V] = {};
-    if (d < D)
-      load_n<V>(static_cast<const T*>(a.v.x) + (t0 + i) * a.v.x_token + h * a.v.x_head + d, a.v_vec, x);
-    float top = 0.0f, scale;
+  const int d = (lane & (lanes - 1)) * V, step = kRowWaves * per;
+  for (int i0 = wave * per + lane / lanes, first = 1; first || i0 - lane / lanes < n; i0 += B * step, first = 0) {
+    T x[B][V] = {};
 #pragma unroll
-    for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf((float)x[e]));
-    const float c = code_factor(over_lanes_max(top, lanes), &scale);
-    if (u == 0 && l.page[i] >= 0)
-      a.v_scales[((int64_t)l.page[i] * a.kv_heads + h) * a.block + l.pos[i] % a.block] = scale;
-    if (d < D) {
+    for (int j = 0; j < B; ++j) {
+      const int i = i0 + j * step;
+      if (i < n && d < D)
+        load_n<V>(static_cast<const T*>(a.v.x) + (t0 + i) * a.v.x_token + h * a.v.x_head + d, a.v_vec, x[j]);
+    }
+    if (first) load_window<false>(a, l, t0, n);
+#pragma unroll
+    for (int j = 0; j < B; ++j) {
+      const int i = i0 + j * step;
+      float top = 0.0f, scale;
+#pragma unroll
+      for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf((float)x[j][e]));
+      const float c = code_factor(over_lanes_max(top, lanes), &scale);
+      if (i >= n || d >= D) continue;
+      if (d == 0 && l.page[i] >= 0)
+        a.v_scales[((int64_t)l.page[i] * a.kv_heads + h) * a.block + (l.pos[i] & (a.block - 1))] = scale;
 #pragma unroll
       for (int e = 0; e < V; e += 4) {
         uint32_t w = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w |= (uint32_t)(uint8_t)code_of((float)x[e + j], c) << (8 * j);
+        for (int k = 0; k < 4; ++k) w |= (uint32_t)(uint8_t)code_of((float)x[j][e + k], c) << (8 * k);
         *reinterpret_cast<uint32_t*>(l.codes + i * stride + d + e) = w;
       }
     }
   }
   __syncthreads();
-  const Groups groups(l, n);
-  // tokens first: 16 lanes write 64 bytes of a row of the page
-  for (int j = threadIdx.x; j < groups.count * (D / 4); j += kRowThreads) {
-    const int q = j % groups.count, x0 = j / groups.count * 4, i = groups.first(q);
-    if (groups.whole(l, i, n)) {
-      uint32_t x[4], y[4];
+  // tokens first: 16 lanes write 64 bytes of a row of the page (group 0 has fewer than four tokens or none)
+  constexpr int G = kQ8Window / 4;
+  for (int j = threadIdx.x; j < G * (D / 4); j += kRowThreads) {
+    const int q = 1 + j % G, x0 = j / G * 4, page = l.group[q];
+    if (page < 0) continue;
+    const int i = l.lead - 4 + 4 * q;
+    uint32_t x[4], y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const uint32_t*>(l.codes + (i + e) * stride + x0);
-      turn4(x, y);
-      int8_t* to = a.v_codes + (((int64_t)l.page[i] * a.kv_heads + h) * D + x0) * a.block + l.pos[i] % a.block;
+    for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const uint32_t*>(l.codes + (i + e) * stride + x0);
+    turn4(x, y);
+    int8_t* to = a.v_codes + (((int64_t)page * a.kv_heads + h) * D + x0) * a.block + (l.pos[i] & (a.block - 1));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(to + (int64_t)e * a.block) = y[e];
-      continue;
-    }
-    for (int k = max(i, 0); k < min(i + 4, n); ++k) {
-      if (l.page[k] < 0) continue;
-      int8_t* to = a.v_codes + (((int64_t)l.page[k] * a.kv_heads + h) * D + x0) * a.block + l.pos[k] % a.block;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) to[(int64_t)e * a.block] = l.codes[k * stride + x0 + e];
-    }
+    for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(to + e * a.block) = y[e];
   }
+  each_loose(l, D, [&](int i, int d) {
+    if (l.page[i] >= 0)
+      a.v_codes[(((int64_t)l.page[i] * a.kv_heads + h) * D + d) * a.block + (l.pos[i] & (a.block - 1))] =
+          l.codes[i * stride + d];
+  });
 }
 
 template <typename T, bool INTERLEAVED, bool CACHE>
-__device__ __forceinline__ void token_rows_vec(const RowArgs& a, int vec, float2* cs) {
+__device__ __forceinline__ void token_rows_vec(const RowArgs& a, int vec, RunLds& l) {
   constexpr int WIDE = 16 / sizeof(T) / (INTERLEAVED ? 2 : 1);
   if (vec == WIDE)
-    token_rows<T, WIDE, INTERLEAVED, CACHE>(a, cs);
+    token_rows<T, WIDE, INTERLEAVED, CACHE>(a, l);
   else if (WIDE > 4 && vec == 4)
-    token_rows<T, (WIDE > 4 ? 4 : 1), INTERLEAVED, CACHE>(a, cs);
+    token_rows<T, (WIDE > 4 ? 4 : 1), INTERLEAVED, CACHE>(a, l);
   else if (WIDE > 2 && vec == 2)
-    token_rows<T, (WIDE > 2 ? 2 : 1), INTERLEAVED, CACHE>(a, cs);
+    token_rows<T, (WIDE > 2 ? 2 : 1), INTERLEAVED, CACHE>(a, l);
   else
-    token_rows<T, 1, INTERLEAVED, CACHE>(a, cs);
+    token_rows<T, 1, INTERLEAVED, CACHE>(a, l);
 }
 
 template <typename T, bool INTERLEAVED>
 __global__ __launch_bounds__(kRowThreads) void norm_kernel(RowArgs a, int vec) {
-  __shared__ float2 cs[kRowWaves][kMaxHeadDim / 2];
-  token_rows_vec<T, INTERLEAVED, false>(a, vec, cs[threadIdx.x / 64]);
+  __shared__ RunLds l;
+  token_rows_vec<T, INTERLEAVED, false>(a, vec, l);
 }
 
 template <typename T, bool INTERLEAVED>
 __global__ __launch_bounds__(kRowThreads) void q8_append_kernel(RowArgs a, int vec) {
   __shared__ union {
-    float2 cs[kRowWaves][kMaxHeadDim / 2];
+    RunLds run;
     TurnLds turn;
   } l;
   if ((int)blockIdx.x >= a.row_groups)
     append_window<T>(a, l.turn, blockIdx.x - a.row_groups);
   else
-    token_rows_vec<T, INTERLEAVED, true>(a, vec, l.cs[threadIdx.x / 64]);
+    token_rows_vec<T, INTERLEAVED, true>(a, vec, l.run);
 }
 
 // ---------------------------------------------------------------- means
 
 // Sum of get(0) ... get(N - 1), halves added pairwise (i with i + N / 2 first).
-template <int N, int STRIDE = 1, typename GET>
-__device__ __forceinline__ float halves(const GET& get, int first = 0) {
+template <int N, int STRIDE, typename GET>
+__device__ __forceinline__ f32x4 halves(const GET& get, int first) {
   if constexpr (STRIDE == N)
     return get(first);
   else
@@ -418,11 +498,12 @@ __device__ __forceinline__ float halves(const GET& get, int first = 0) {
 }
 
 // The means of the blocks that the call's tokens fill, after all of its keys are stored.  A workgroup looks through `range`
-// tokens for one head; a thread adds one value of the block's keys.
+// tokens for one head; a lane adds four values of a quarter of the block's keys, and the quarters meet in LDS.
 __global__ __launch_bounds__(kRowThreads) void q8_means_kernel(sdnn_q8_cache c, sdnn_tokens t, int range) {
-  __shared__ float tops[kRowWaves];
+  __shared__ f32x4 part[kRowWaves][kMaxHeadDim / 4];
+  static_assert(kRowWaves == 4, "quarters");
   const int h = blockIdx.x % c.kv_heads, t0 = blockIdx.x / c.kv_heads * range;
-  const int lane = threadIdx.x % 64, P = c.block, D = c.head_dim, d = threadIdx.x;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, P = c.block, D = c.head_dim;
   int32_t page = -1;
   if (lane < range && t0 + lane < t.tokens) {
     const int32_t p = t.pos[t0 + lane], s = t.seq[t0 + lane];
@@ -432,23 +513,34 @@ __global__ __launch_bounds__(kRowThreads) void q8_means_kernel(sdnn_q8_cache c, 
   }
   for (uint64_t full = __ballot(page >= 0); full; full &= full - 1) {
     const int64_t row = (int64_t)__builtin_amdgcn_readlane(page, __builtin_ctzll(full)) * c.kv_heads + h;
-    float sum = 0.0f;
-    if (d < D) {
-      const int8_t* k = c.k_codes + row * P * D + d;
+    if (lane < D / 4) {
+      const int8_t* k = c.k_codes + row * P * D + 4 * lane;
       const float* scale = c.k_scales + row * P;
-      const auto get = [&](int i) { return scale[i] * (float)k[i * D]; };
-      sum = P == 32 ? halves<32>(get) : P == 64 ? halves<64>(get) : halves<128>(get);
+      const auto get = [&](int i) {
+        typedef int8_t i8x4 __attribute__((ext_vector_type(4)));
+        const i8x4 n = *reinterpret_cast<const i8x4*>(k + i * D);
+        return scale[i] * f32x4{(float)n[0], (float)n[1], (float)n[2], (float)n[3]};
+      };
+      part[wave][lane] = P == 32 ? halves<32, 4>(get, wave) : P == 64 ? halves<64, 4>(get, wave) : halves<128, 4>(get, wave);
     }
-    float top = fabsf(sum);
+    __syncthreads();
+    if (wave == 0) {
+      f32x4 sum = {0, 0, 0, 0};
+      if (lane < D / 4) sum = (part[0][lane] + part[2][lane]) + (part[1][lane] + part[3][lane]);
+      float top = 0.0f;
 #pragma unroll
-    for (int s = 32; s; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
-    if (lane == 0) tops[threadIdx.x / 64] = top;
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(sum[e]));
+      top = over_lanes_max(top, 64);
+      const float f = top > 0.0f ? 127.0f * (1.0f / top) : 0.0f;
+      if (lane < D / 4) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w |= (uint32_t)(uint8_t)code_of(sum[e], f) << (8 * e);
+        *reinterpret_cast<uint32_t*>(c.means + row * D + 4 * lane) = w;
+      }
+      if (lane == 0) c.mean_scales[row] = top / (127.0f * P);
+    }
     __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    __syncthreads();
-    const float f = top > 0.0f ? 127.0f * (1.0f / top) : 0.0f;
-    if (d < D) c.means[row * D + d] = (int8_t)fminf(fmaxf(rintf(sum * f), -127.0f), 127.0f);
-    if (d == 0) c.mean_scales[row] = top / (127.0f * P);
   }
 }
 
@@ -467,7 +559,7 @@ __device__ __forceinline__ void write8(const int8_t (&n)[8], float scale, T* y, 
   }
 }
 
-// A token's rows, a row to `lanes` lanes of 8 values: keys, and values where they are read one by one.
+// A token's rows, a row to `lanes` lanes of 8 values.
 template <typename T>
 __device__ __forceinline__ void read_rows(const RowArgs& a) {
   const int lane = threadIdx.x % 64, D = a.head_dim;
@@ -477,7 +569,7 @@ __device__ __forceinline__ void read_rows(const RowArgs& a) {
   const int32_t p = a.pos[t], page = page_of(a, p, a.seq[t]);
   const int d = (lane & (a.lanes - 1)) * 8, per = 64 / a.lanes, slot = lane / a.lanes;
   if (d >= D) return;
-  const int k_tasks = (a.k.heads + per - 1) / per, tasks = k_tasks + (a.v_by_rows ? (a.v.heads + per - 1) / per : 0);
+  const int k_tasks = (a.k.heads + per - 1) / per, tasks = k_tasks + (a.v.heads + per - 1) / per;
   const int place = page >= 0 ? p % a.block : 0;
   for (int task = part; task < tasks; task += a.waves) {
     const bool keys = task < k_tasks;
@@ -500,48 +592,112 @@ __device__ __forceinline__ void read_rows(const RowArgs& a) {
   }
 }
 
-// Values of neighbouring tokens: as append_window, the other way round.
+// A window of neighbouring tokens of one head: keys as they lie, values turned as in append_window.  All of a thread's loads
+// are under way before the first is used, and tokens of words that the window shares with others are read with them too: taken one by
+// one they had two more latencies and 91 us for 32 thousand tokens of 8 heads of 128 instead of 50 (221 MB at 4.4 TB/s).
 template <typename T>
 __device__ __forceinline__ void read_window(const RowArgs& a, TurnLds& l, int b) {
-  const int h = b % a.v.heads, t0 = b / a.v.heads * kQ8Window, n = min(kQ8Window, a.tokens - t0);
-  const int D = a.head_dim, stride = D + 4;
-  load_window(a, l, t0, n);
-  for (int i = threadIdx.x; i < n; i += kRowThreads)
-    l.scale[i] = l.page[i] < 0 ? 0.0f : a.v_scales[((int64_t)l.page[i] * a.kv_heads + h) * a.block + l.pos[i] % a.block];
-  const Groups groups(l, n);
-  for (int j = threadIdx.x; j < groups.count * (D / 4); j += kRowThreads) {
-    const int q = j % groups.count, x0 = j / groups.count * 4, i = groups.first(q);
-    if (groups.whole(l, i, n)) {
-      const int8_t* from = a.v_codes + (((int64_t)l.page[i] * a.kv_heads + h) * D + x0) * a.block + l.pos[i] % a.block;
-      uint32_t x[4], y[4];
+  constexpr int G = kQ8Window / 4, U = G * (kMaxHeadDim / 4) / kRowThreads + 1, W = 4;
+  const int heads = max(a.k.heads, a.v.heads);
+  const int h = b % heads, t0 = b / heads * kQ8Window, n = min(kQ8Window, a.tokens - t0);
+  const int D = a.head_dim, stride = D + 4, row8 = D / 8;
+  load_window<true>(a, l, t0, n);
+  const int tid = threadIdx.x;
+  const auto place = [&](int i) { return l.pos[i] & (a.block - 1); };
+  const auto head = [&](int page) { return (int64_t)page * a.kv_heads + h; };
+  float scale = 0.0f;
+  if (tid < 2 * kQ8Window) {
+    const int i = tid % kQ8Window;
+    const float* from = tid < kQ8Window ? a.k_scales : a.v_scales;
+    if (l.page[i] >= 0 && (tid < kQ8Window ? a.k.y : a.v.y)) scale = from[head(l.page[i]) * a.block + place(i)];
+  }
+  // groups 1 ... 16, tokens first; then group 0
+  const auto unit = [&](int u, int* q, int* x0) {
+    const int j = tid + u * kRowThreads;
+    *q = u < U - 1 ? 1 + j % G : 0, *x0 = u < U - 1 ? j / G * 4 : tid * 4;
+    return *x0 < D && l.group[*q] >= 0;
+  };
+  uint32_t x[U][4] = {};
+  if (a.v.y) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const uint32_t*>(from + (int64_t)e * a.block);
-      turn4(x, y);
+    for (int u = 0; u < U; ++u) {
+      int q, x0;
+      if (!unit(u, &q, &x0)) continue;
+      const int8_t* from = a.v_codes + (head(l.group[q]) * D + x0) * a.block + (place(max(l.lead - 4 + 4 * q, 0)) & ~3);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(l.codes + (i + e) * stride + x0) = y[e];
-      continue;
-    }
-    for (int k = max(i, 0); k < min(i + 4, n); ++k) {
-      const int8_t* from = a.v_codes + (((int64_t)max(l.page[k], 0) * a.kv_heads + h) * D + x0) * a.block + (l.pos[k] & (a.block - 1));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) l.codes[k * stride + x0 + e] = l.page[k] < 0 ? 0 : from[(int64_t)e * a.block];
+      for (int e = 0; e < 4; ++e) x[u][e] = *reinterpret_cast<const uint32_t*>(from + e * a.block);
     }
   }
+  // a thread's pieces of keys: W at a time
+  const auto piece = [&](int j, int* i, int* d) {
+    *i = j / row8, *d = (j - *i * row8) * 8;
+    return j < n * row8;
+  };
+  int8_t key[W][8] = {};
+  const auto load_keys = [&](int j0) {
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      int i, d;
+      if (!piece(j0 + w * kRowThreads, &i, &d)) continue;
+      if (l.page[i] >= 0)
+        load_n<8>(a.k_codes + (head(l.page[i]) * a.block + place(i)) * D + d, true, key[w]);
+      else
+        __builtin_memset(key[w], 0, 8);
+    }
+  };
+  if (a.k.y) load_keys(tid);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(x[u][e]));
+  if (tid < kQ8Window)
+    l.k_scale[tid] = scale;
+  else if (tid < 2 * kQ8Window)
+    l.v_scale[tid - kQ8Window] = scale;
+  if (a.v.y) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      int q, x0;
+      if (!unit(u, &q, &x0)) continue;
+      uint32_t y[4];
+      turn4(x[u], y);
+      const int i = l.lead - 4 + 4 * q;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (i + e >= 0 && i + e < n) *reinterpret_cast<uint32_t*>(l.codes + (i + e) * stride + x0) = y[e];
+    }
+    each_loose(l, D, [&](int i, int d) {
+      l.codes[i * stride + d] = l.page[i] < 0 ? 0 : a.v_codes[(head(l.page[i]) * D + d) * a.block + place(i)];
+    });
+  }
   __syncthreads();
-  for (int j = threadIdx.x; j < n * (D / 8); j += kRowThreads) {
-    const int i = j / (D / 8), d = (j - i * (D / 8)) * 8;
-    int8_t x[8];
-    __builtin_memcpy(x, l.codes + i * stride + d, 4);
-    __builtin_memcpy(x + 4, l.codes + i * stride + d + 4, 4);
-    write8<T>(x, l.scale[i], static_cast<T*>(a.v.y) + (t0 + i) * a.v.y_token + h * a.v.y_head + d, a.v.y_aligned);
+  if (a.k.y) {
+    for (int j0 = tid; j0 < n * row8; j0 += W * kRowThreads) {
+      if (j0 != tid) load_keys(j0);
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        int i, d;
+        if (!piece(j0 + w * kRowThreads, &i, &d)) continue;
+        write8<T>(key[w], l.k_scale[i], static_cast<T*>(a.k.y) + (t0 + i) * a.k.y_token + h * a.k.y_head + d, a.k.y_aligned);
+      }
+    }
+  }
+  if (!a.v.y) return;
+  for (int j = tid; j < n * row8; j += kRowThreads) {
+    int i, d;
+    piece(j, &i, &d);
+    int8_t v[8];
+    __builtin_memcpy(v, l.codes + i * stride + d, 4);
+    __builtin_memcpy(v + 4, l.codes + i * stride + d + 4, 4);
+    write8<T>(v, l.v_scale[i], static_cast<T*>(a.v.y) + (t0 + i) * a.v.y_token + h * a.v.y_head + d, a.v.y_aligned);
   }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void q8_read_kernel(RowArgs a) {
   __shared__ TurnLds l;
-  if ((int)blockIdx.x >= a.row_groups)
-    read_window<T>(a, l, blockIdx.x - a.row_groups);
+  if (a.row_groups == 0)
+    read_window<T>(a, l, blockIdx.x);
   else
     read_rows<T>(a);
 }
@@ -594,10 +750,10 @@ hipError_t launch_norm(const sdnn_heads& q, const sdnn_heads& q_out, const sdnn_
   if (k) a.k = head_rows(*k, k_out, norm.k_weight, norm.k_head_stride, values, dtype);
   a.pos = pairs ? pos : nullptr;
   set_rotation(a, rotation);
-  a.eps = norm.eps, a.norm = 1, a.tokens = tokens, a.head_dim = head_dim;
-  const RowShape s = row_shape(tokens, head_dim / (2 * vec), {a.q.heads, a.k.heads, 0});
+  a.eps = norm.eps, a.inverse_dim = 1.0 / head_dim, a.norm = 1, a.tokens = tokens, a.head_dim = head_dim;
+  const RunShape s = run_shape(tokens, head_dim / (2 * vec), {a.q.heads, a.k.heads, 0});
   if (!launchable(s.groups, kRowThreads)) return hipErrorInvalidConfiguration;
-  a.lanes = s.lanes, a.waves = s.waves;
+  a.lanes = s.lanes, a.run = s.run, a.shares = s.shares;
   return by_type(dtype, layout, [&](auto t, auto il) {
     norm_kernel<decltype(t), decltype(il)::value><<<(unsigned)s.groups, kRowThreads, 0, stream>>>(a, vec);
     return hipGetLastError();
@@ -612,17 +768,17 @@ hipError_t launch_q8_append(const sdnn_q8_cache& c, const sdnn_tokens& t, int dt
   RowArgs a = {};
   set_cache(a, c, t);
   set_rotation(a, rotation);
-  if (norm) a.norm = 1, a.eps = norm->eps;
+  if (norm) a.norm = 1, a.eps = norm->eps, a.inverse_dim = 1.0 / c.head_dim;
   if (q) a.q = head_rows(*q, q_out, norm ? norm->q_weight : nullptr, norm ? norm->q_head_stride : 0, values, dtype);
   a.k = head_rows(k, nullptr, norm ? norm->k_weight : nullptr, norm ? norm->k_head_stride : 0, values, dtype);
-  a.v = head_rows(v, nullptr, nullptr, 0, vec, dtype);
+  a.v = head_rows(v, nullptr, nullptr, 0, values, dtype);
   a.v_vec = rows_aligned(v, 16 / dtype_bytes(dtype), dtype);
   const bool windows = by_windows(t);
-  const RowShape s = row_shape(t.tokens, c.head_dim / (2 * vec), {a.q.heads, a.k.heads, windows ? 0 : a.v.heads});
+  const RunShape s = run_shape(t.tokens, c.head_dim / (2 * vec), {a.q.heads, a.k.heads, windows ? 0 : a.v.heads});
   const int64_t groups = s.groups + (windows ? window_groups(t, c.kv_heads) : 0);
   if (!launchable(groups, kRowThreads) || !launchable(mean_groups(t, c.kv_heads), kRowThreads))
     return hipErrorInvalidConfiguration;
-  a.lanes = s.lanes, a.waves = s.waves, a.row_groups = (int32_t)s.groups;
+  a.lanes = s.lanes, a.run = s.run, a.shares = s.shares, a.row_groups = (int32_t)s.groups;
   a.v_by_rows = !windows;
   const hipError_t e = by_type(dtype, layout, [&](auto ty, auto il) {
     q8_append_kernel<decltype(ty), decltype(il)::value><<<(unsigned)groups, kRowThreads, 0, stream>>>(a, vec);
@@ -641,13 +797,11 @@ hipError_t launch_q8_read(const sdnn_q8_cache& c, const sdnn_tokens& t, int dtyp
   const int values = dtype == SDNN_F32 ? 4 : 8;
   if (k) a.k = head_rows(*k, k, nullptr, 0, values, dtype);
   if (v) a.v = head_rows(*v, v, nullptr, 0, values, dtype);
-  const bool windows = v && by_windows(t);
-  const RowShape s = row_shape(t.tokens, c.head_dim / 8, {a.k.heads, windows ? 0 : a.v.heads, 0});
-  const int64_t rows = s.tasks > 0 ? s.groups : 0, groups = rows + (windows ? window_groups(t, c.kv_heads) : 0);
+  const bool windows = by_windows(t);
+  const RowShape s = row_shape(t.tokens, c.head_dim / 8, {a.k.heads, a.v.heads, 0});
+  const int64_t groups = windows ? window_groups(t, c.kv_heads) : s.groups;
   if (!launchable(groups, kRowThreads)) return hipErrorInvalidConfiguration;
-  if (groups == 0) return hipSuccess;
-  a.lanes = s.lanes, a.waves = s.waves, a.row_groups = (int32_t)rows;
-  a.v_by_rows = !windows;
+  a.lanes = s.lanes, a.waves = s.waves, a.row_groups = windows ? 0 : (int32_t)s.groups;
   return by_type(dtype, [&](auto ty) {
     q8_read_kernel<decltype(ty)><<<(unsigned)groups, kRowThreads, 0, stream>>>(a);
     return hipGetLastError();

@@ -96,7 +96,7 @@ sdnn_status sdnn_q8_read(const sdnn_q8_cache* cache, const sdnn_tokens* tokens, 
     SDNN_CHECK(check_rows(r, cache->kv_heads, tokens->tokens, dtype));
     if (!distinct_rows(*r, tokens->tokens, cache->head_dim)) return SDNN_ERR_DIM;
   }
-  if (tokens->tokens == 0) return SDNN_OK;
+  if (tokens->tokens == 0 || (!k && !v)) return SDNN_OK;
   if (k && v && k->data == v->data) return SDNN_ERR_DIM;
   if (!has_pages(*cache)) return SDNN_ERR_NULL;
   return result(launch_q8_read(*cache, *tokens, dtype, k, v, (hipStream_t)stream));

@@ -16,22 +16,21 @@ hipError_t launch_norm(const sdnn_heads& q, const sdnn_heads&, const sdnn_heads*
                        int32_t tokens, int32_t head_dim, const int32_t*, const sdnn_head_norm&, const sdnn_rotation* r,
                        hipStream_t) {
   const int vec = row_pairs(dtype, r ? r->layout : SDNN_ROPE_HALF, r ? r->pairs : 0, head_dim);
-  return launched(launchable(row_shape(tokens, head_dim / (2 * vec), {q.heads, k ? k->heads : 0, 0}).groups, kRowThreads));
+  return launched(launchable(run_shape(tokens, head_dim / (2 * vec), {q.heads, k ? k->heads : 0, 0}).groups, kRowThreads));
 }
 hipError_t launch_q8_append(const sdnn_q8_cache& c, const sdnn_tokens& t, int dtype, const sdnn_heads&, const sdnn_heads&,
                             const sdnn_head_norm*, const sdnn_rotation* r, const sdnn_heads* q, const sdnn_heads*,
                             hipStream_t) {
   const int vec = row_pairs(dtype, r ? r->layout : SDNN_ROPE_HALF, r ? r->pairs : 0, c.head_dim);
   const bool windows = by_windows(t);
-  const RowShape s = row_shape(t.tokens, c.head_dim / (2 * vec), {q ? q->heads : 0, c.kv_heads, windows ? 0 : c.kv_heads});
+  const RunShape s = run_shape(t.tokens, c.head_dim / (2 * vec), {q ? q->heads : 0, c.kv_heads, windows ? 0 : c.kv_heads});
   return launched(launchable(s.groups + (windows ? window_groups(t, c.kv_heads) : 0), kRowThreads) &&
                   launchable(mean_groups(t, c.kv_heads), kRowThreads));
 }
 hipError_t launch_q8_read(const sdnn_q8_cache& c, const sdnn_tokens& t, int, const sdnn_heads* k, const sdnn_heads* v,
                           hipStream_t) {
-  const bool windows = v && by_windows(t);
-  const RowShape s = row_shape(t.tokens, c.head_dim / 8, {k ? c.kv_heads : 0, v && !windows ? c.kv_heads : 0, 0});
-  return launched(launchable(s.groups + (windows ? window_groups(t, c.kv_heads) : 0), kRowThreads));
+  const RowShape s = row_shape(t.tokens, c.head_dim / 8, {k ? c.kv_heads : 0, v ? c.kv_heads : 0, 0});
+  return launched(launchable(by_windows(t) ? window_groups(t, c.kv_heads) : s.groups, kRowThreads));
 }
 hipError_t launch_q8_attend(const sdnn_q8_cache& c, const sdnn_tokens& t, int, const sdnn_heads& q, const sdnn_heads&,
                             const int32_t* chosen, int32_t blocks, int32_t shared, float, float*, float*, hipStream_t) {

@@ -11,6 +11,7 @@ namespace sdnn {
 
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / 64;
+constexpr int kRowRun = 8;     // most tokens of a workgroup that has rows of heads
 constexpr int kQ8Window = 64;  // tokens of a workgroup that turns values
 
 // Pairs to a unit: a lane holds 2 of these values of a row, in two accesses (pairs half a head apart) or one (neighbours), of
@@ -40,6 +41,23 @@ inline RowShape row_shape(int32_t tokens, int units, const int (&heads)[3]) {
   s.waves = 1;
   while (s.waves < s.tasks && (int64_t)tokens * s.waves < 4096) ++s.waves;
   s.groups = ((int64_t)tokens * s.waves + kRowWaves - 1) / kRowWaves;
+  return s;
+}
+
+// Rows that are normed, rotated and stored: a workgroup has a run of tokens and `shares` workgroups share a run's tasks.  Long
+// runs share cosines and sines among more heads and keep loads under way, where they leave workgroups enough for the device.
+struct RunShape {
+  int32_t lanes, tasks, run, shares;
+  int64_t groups;
+};
+inline RunShape run_shape(int32_t tokens, int units, const int (&heads)[3]) {
+  RunShape s = {};
+  s.lanes = row_lanes(units);
+  for (const int h : heads) s.tasks += row_tasks(h, s.lanes);
+  s.run = 1, s.shares = 1;
+  while (s.run < kRowRun && tokens >= 640 * s.run) s.run *= 2;
+  while (s.run == 1 && s.shares * kRowWaves < s.tasks && tokens * s.shares < 2048) ++s.shares;
+  s.groups = ((int64_t)tokens + s.run - 1) / s.run * s.shares;
   return s;
 }
 
