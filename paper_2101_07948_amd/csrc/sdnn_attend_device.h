@@ -44,6 +44,20 @@ struct AttendArgs {
 template <typename T>
 struct Step;
 
+// Two numbers rounded to T, and what they lack in x.  (In bf16 by one conversion of the pair, whose halves are floats' upper 16
+// bits: one by one, each is converted twice, for the difference and to be packed.)
+__device__ __forceinline__ void take_pair(float (&x)[2], typename VecOf<2, __bf16>::type* h) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  *h = __builtin_convertvector((f32x2{x[0], x[1]}), typename VecOf<2, __bf16>::type);
+  uint32_t bits;
+  __builtin_memcpy(&bits, h, 4);
+  x[0] -= __uint_as_float(bits << 16), x[1] -= __uint_as_float(bits & 0xffff0000u);
+}
+__device__ __forceinline__ void take_pair(float (&x)[2], typename VecOf<2, _Float16>::type* h) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) (*h)[i] = (_Float16)x[i], x[i] -= (float)(*h)[i];
+}
+
 // 16-bit values: 32 tokens, v_mfma_f32_16x16x32.  Row r of half s of the keys is token
 // 8 (r / 4) + 4 s + r % 4, so that lane group g ends up with scores of tokens 8 g ... 8 g + 7.
 template <typename T, typename V8>
@@ -94,9 +108,12 @@ struct Step16 {
                                                     f32x4 (&o)[2 * CHUNKS]) {
     V8 hi, lo;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      hi[j] = (T)p[j];
-      lo[j] = (T)(p[j] - (float)hi[j]);
+    for (int j = 0; j < 8; j += 2) {
+      typename VecOf<2, T>::type h;
+      float low[2] = {p[j], p[j + 1]};
+      take_pair(low, &h);
+      hi[j] = h[0], hi[j + 1] = h[1];
+      lo[j] = (T)low[0], lo[j + 1] = (T)low[1];
     }
 #pragma unroll
     for (int c = 0; c < 2 * CHUNKS; ++c) {

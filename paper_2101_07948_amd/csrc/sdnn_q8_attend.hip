@@ -135,13 +135,15 @@ __device__ __forceinline__ void q8_weights(float scale2, float (&s)[E], const fl
 #pragma unroll
   for (int j = 1; j < E; ++j) sum += s[j];
   st.l += sum;
-  constexpr int P = Parts<T>::kP;
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    __bf16 x[P];
-    split(s[j] * vs[j], x);
+  for (int j = 0; j < E; j += 2) {
+    float x[2] = {s[j] * vs[j], s[j + 1] * vs[j + 1]};
 #pragma unroll
-    for (int k = 0; k < P; ++k) p[k][j / 8][j % 8] = x[k];
+    for (int k = 0; k < Parts<T>::kP; ++k) {
+      typename VecOf<2, __bf16>::type h;
+      take_pair(x, &h);
+      p[k][j / 8][j % 8] = h[0], p[k][j / 8][j % 8 + 1] = h[1];
+    }
   }
 }
 
