@@ -245,6 +245,88 @@ def test_q8_fillers_and_missing_pages_and_reading_back(dtype, tokens):
         assert torch.equal(only, kr)
 
 
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("P,D,Hk,at", [
+    (64, 128, 8, [(0, 1999, 6000)]),
+    (32, 80, 3, [(0, 3, 70), (1, 17, 30), (2, 0, 1), (1, 30, 95), (0, 64, 65)]),
+    (128, 256, 1, [(2, 126, 131), (0, 5, 270), (1, 0, 64)]),
+    (32, 16, 2, [(1, 1, 3), (0, 0, 2), (2, 4, 7), (0, 2, 6), (1, 3, 90)]),
+])
+def test_q8_rows_are_their_numbers_times_their_scales(dtype, P, D, Hk, at):
+    """Each product rounded to 32 bits, then to the rows' type; runs of tokens that begin and end anywhere, in windows with
+    others, with gaps, backwards and with fillers among them."""
+    seq, pos = [s for s, a, b in at for _ in range(a, b)], [p for _, a, b in at for p in range(a, b)]
+    width = max(pos) // P + 1
+    pages = 3 * width + 1
+    table = torch.randperm(pages, generator=gen(3), device=DEV)[:3 * width].reshape(3, width).to(torch.int32)
+    cache = sd.Q8Cache.empty(pages, Hk, D, P, device=DEV)
+    for x in (cache.k_codes, cache.v_codes):
+        x.copy_(torch.randint(-127, 128, x.shape, generator=gen(x.shape[2]), device=DEV))
+    for x, s in ((cache.k_scales, 4), (cache.v_scales, 5)):
+        x.copy_(torch.rand(x.shape, generator=gen(s), device=DEV) * 0.02 + 0.01)
+    seq, pos = i32(seq), i32(pos)
+    orders = [torch.arange(len(pos), device=DEV), torch.arange(len(pos), device=DEV).flip(0),
+              torch.arange(0, len(pos), 2, device=DEV)]
+    for order in orders:
+        s, p = seq[order].contiguous(), pos[order].contiguous()
+        p[len(p) // 2] = -1
+        there = p >= 0
+        page = table[s.long(), p.clamp(min=0).long() // P].long()
+        place = p.clamp(min=0).long() % P
+        want_k = (cache.k_codes[page, :, place].float() * cache.k_scales[page, :, place][..., None]).to(dtype)
+        want_v = (cache.v_codes[page, :, :, place].float() * cache.v_scales[page, :, place][..., None]).to(dtype)
+        want_k[~there], want_v[~there] = 0, 0
+        k, v = (torch.full((len(p), Hk, D), 7.0, dtype=dtype, device=DEV) for _ in range(2))
+        cache.read(p, s, table, k=k, v=v)
+        assert torch.equal(k, want_k) and torch.equal(v, want_v)
+
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("D,rot,layout,Hq,Hk,per_head", [
+    (128, 64, "interleaved", 32, 8, True), (64, 64, "half", 5, 2, False), (16, 16, "half", 3, 1, True),
+    (2, 2, "interleaved", 4, 4, False), (256, 128, "half", 3, 1, True), (250, 122, "half", 2, 1, False),
+    (96, 0, "half", 7, 7, True)])
+def test_norms_of_prompts_are_those_of_their_tokens(dtype, D, rot, layout, Hq, Hk, per_head):
+    """Calls whose workgroups have runs of 2, 4 and 8 tokens, the last one short: bit for bit what few tokens get."""
+    n = 2569
+    q, k = randn(1, (n, Hq, D), dtype, 2.0), randn(2, (n, Hk, D), dtype, 2.0)
+    wq, wk = ((1 + 0.2 * randn(s, (h, D) if per_head else (D,), torch.float32)) for s, h in ((3, Hq), (4, Hk)))
+    norm, rope = sd.HeadNorm(wq, wk), sd.Rope(rot, layout=layout) if rot else None
+    pos = torch.arange(5, 5 + n, dtype=torch.int32, device=DEV)
+
+    def by(step, n):
+        qo, ko = torch.full_like(q[:n], float("nan")), torch.full_like(k[:n], float("nan"))
+        for a in range(0, n, step):
+            b = slice(a, min(a + step, n))
+            norm.apply(q[b], qo[b], k[b], ko[b], pos=pos[b] if rope else None, rope=rope)
+        return qo, ko
+
+    few = by(300, n)
+    for m in (641, 1283, n):
+        for x, y in zip(by(m, m), few):
+            assert torch.equal(x, y[:m])
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_q8_long_prompts_store_what_short_calls_do(layout):
+    P, D, Hk, n = 64, 128, 3, 2600
+    table = i32([list(range(n // P + 2))])
+    k, v, q = (randn(s, (n, h, D), torch.float16) for s, h in ((1, Hk), (2, Hk), (3, 6)))
+    rope, norm = sd.Rope(D, layout=layout), sd.HeadNorm(None, 1 + 0.3 * randn(4, (Hk, D), torch.float32))
+    pos, seq = torch.arange(7, 7 + n, dtype=torch.int32, device=DEV), i32([0] * n)
+    caches, outs = [], []
+    for step in (3, 1290, n):
+        cache, out = make_q8(n // P + 2, Hk, P, D), torch.empty_like(q)
+        for a in range(0, n, step):
+            b = slice(a, min(a + step, n))
+            cache.append(k[b], v[b], pos[b], seq[b], table, rope=rope, norm=norm, q=q[b], q_out=out[b])
+        caches.append(cache), outs.append(out)
+    for cache, out in zip(caches[1:], outs[1:]):
+        assert torch.equal(out, outs[0])
+        for x, y in zip(cache._tensors, caches[0]._tensors):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
 def test_q8_rows_of_zeros_of_tiny_and_of_large_values():
     P, D = 32, 32
     cache = make_q8(1, 1, P, D)
