@@ -153,6 +153,9 @@ constexpr int q8_waves(int pieces) { return pieces <= 4 ? 2 : 1; }
 // Single tokens: as attend_kernel, with steps of N tokens, 4 N / 16 to a lane.  A lane reads 16 numbers of a key at a time
 // (DIMS pieces of 64 values for the four lane groups), and of a value N / 4 tokens' numbers: each instruction takes whole runs
 // of 64 bytes and more of a page.  Everything a step needs is asked for before its first product.
+//   Reading bounds it.  A token of 32 queries on 8 heads of 128 over 131072 tokens: 54 us, 277 MB at 5.1 TB/s, and 6 to join;
+// 32 sequences of up to 4096 tokens, 12 heads of 64 in 32 bits: 36 us, 131 MB at 3.6 TB/s, and 5 to join (sequences of different
+// lengths end at different times).
 template <typename T, int DIMS, int N>
 __global__ __launch_bounds__(kWaves * 64, q8_waves(2 * DIMS)) void q8_kernel(Q8AttendArgs a) {
   constexpr int TILES = DIMS * 4, E = N / 4, W = E / 4;  // W: words of a lane's piece of a value
@@ -325,6 +328,10 @@ struct Q8Stage {
 };
 
 // As attend_tiles: a workgroup's waves, tiles of neighbouring tokens of one cached head, walk their blocks through LDS.
+//   2048 tokens at the end of 8192, 32 queries on 8 heads of 128 in 16 bits: 427 to 438 us, 241 GFLOP at 560 TFLOP/s.  A step is
+// 24 matrix instructions, 8 of them for the probabilities' second part, and 140 vector ones (scales, exponentials, sums, parts):
+// the vector unit is busy for half of the time, the matrix unit for a third, and waves wait in 46 % of theirs.  Blocks found by
+// lists as in attend_tiles: 779 us; places in LDS worked out for each stage, two tiles to a wave: 459.  Two steps of 32 tokens under way at once: 524, registers spill.
 template <typename T, int CHUNKS, int STAGE, bool LISTS, bool PREFIX>
 __global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, CHUNKS <= 4 && sizeof(T) == 2 ? 4 : 2) void q8_tiles(Q8AttendArgs a) {
   typedef typename Parts<T>::Key Key;

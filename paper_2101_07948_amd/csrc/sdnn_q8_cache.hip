@@ -506,7 +506,9 @@ __device__ __forceinline__ f32x4 halves(const GET& get, int first) {
 }
 
 // The means of the blocks that the call's tokens fill, after all of its keys are stored.  A workgroup looks through `range`
-// tokens for one head; a lane adds four values of a quarter of the block's keys, and the quarters meet in LDS.
+// tokens for one head; a lane adds four values of a quarter of the block's keys, and the quarters meet in LDS.  It is the latency
+// of a launch and of token, page and keys one after the other: with 8 heads of 128 in blocks of 64, 64 tokens 3.2 us, 4096 tokens
+// 4.7, 32768 17 (34 MB).
 __global__ __launch_bounds__(kRowThreads) void q8_means_kernel(sdnn_q8_cache c, sdnn_tokens t, int range) {
   __shared__ f32x4 part[kRowWaves][kMaxHeadDim / 4];
   static_assert(kRowWaves == 4, "quarters");
