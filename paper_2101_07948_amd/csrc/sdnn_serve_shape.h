@@ -148,12 +148,14 @@ struct alignas(16) SampleSpace {
 
 // Workgroups that share a row, each with 4096 tokens at least; 0: a row to a workgroup, in one launch.  Seven launches take 24 us
 // before their first pass counts, and then share a row's passes out, which one workgroup makes at about 4 tokens a
-// nanosecond: rows of 50021 in 32 bits top_k and top_p 31 us and 25 (shared out, not), of 131001 in 16 bits 28 and 48, 128 of
+// nanosecond.  One row in 32 bits, in one launch and shared out: of 32000 tokens top_k and top_p 20 us and 29, top_p alone 32 and
+// 37, no limit 17 and 25; of 50021 25 and 28, 41 and 35, 23 and 25; of 65000 30 and 28, 51 and 34, 26 and 26; of 131001 in 16
+// bits top_k and top_p 48 and 28.  128 of
 // these with all kinds of limits 87 and 117, 256 of them 126 and 123.  (Parts of 2048, 4096, 8192 and 16384 tokens: one row 27,
 // 28, 32 and 40 us, 32 rows 65, 59, 62 and 80.  Four launches, in which the last of a row's workgroups goes on with what all have
 // left in memory: one row 24 us, but 128 rows 145 to 173: each workgroup's release writes its XCD's L2 back.)
 inline int sample_parts(int32_t rows, int32_t vocab) {
-  if (vocab <= 65536 || rows > vocab / 900) return 0;
+  if (vocab <= 57344 || rows > vocab / 900) return 0;
   return std::min((vocab + 4095) / 4096, std::min(kMostSampleParts, 4096 / rows));
 }
 inline int64_t sample_floats(int32_t rows, int32_t vocab) {
