@@ -97,8 +97,7 @@ __global__ __launch_bounds__(kWaves * 64, attend_waves(CHUNKS * Step<T>::kPiece 
 // parts).  Vector instructions (masks, exponentials, the parts) take 40 % of the time, matrix ones 25 %, and waves
 // wait for a stage or the matrix unit in 58 % of theirs.  Half as many waves to a SIMD, for more registers: 212 us;
 // 4 waves to a workgroup: 226; stages of 32 tokens: 174.
-//   PREFIX: of all tokens' shared first blocks (AttendArgs::prefix): no list, and one run of tokens whatever their sequences.
-template <typename T, int CHUNKS, int STAGE, int WAVES, bool PREFIX>
+template <typename T, int CHUNKS, int STAGE, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void attend_tiles(AttendArgs a) {
   typedef Tile<T, CHUNKS, STAGE> L;
   constexpr int TILES = CHUNKS * L::kPiece / 4, N = Step<T>::kTokens;
@@ -141,7 +140,7 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   static_assert(16 * WAVES <= 128, "two words of bits");
   if (wave < 2) {
     const int i = wave * 64 + lane, ti = t0 + i;
-    const bool turn = !PREFIX && i > 0 && i < a.tile_tokens * WAVES && ti < a.tokens && a.seq[ti] != a.seq[ti - 1];
+    const bool turn = i > 0 && i < a.tile_tokens * WAVES && ti < a.tokens && a.seq[ti] != a.seq[ti - 1];
     const uint64_t bits = __ballot(turn);
     if (lane == 0) turns[wave] = bits;
   }
@@ -153,7 +152,6 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   const int32_t run = __popcll(turns[0] & (place >= 63 ? ~0ull : (2ull << place) - 1)) +
                       (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
   const bool filler = p < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
-  if (PREFIX) seq = 0, p = (int32_t)min((int64_t)p, (int64_t)a.prefix * a.block - 1);
   Cursor at;
   at.t = t, at.seq = seq, at.last = min(p / a.block, a.max_blocks - 1), at.share = split;
   at.n = filler ? 0 : a.chosen ? a.blocks : at.last + 1;
@@ -243,13 +241,92 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
     store_row<T>(a, t, head, g, st, st.m, l);
 }
 
+// Of all tokens' shared first blocks (AttendArgs::prefix): as attend_tiles, but all of a workgroup's waves go through the same
+// blocks, which need no offers: 64 tokens of 32 queries on 8 heads of 128 over 16384, 39.5 us, 17 GFLOP at 435 TFLOP/s, and 42.5
+// with offers; 8 tokens over 32768, a call, 48 and 52.
+template <typename T, int CHUNKS, int STAGE>
+__global__ __launch_bounds__(kTileWaves * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void prefix_tiles(AttendArgs a) {
+  typedef Tile<T, CHUNKS, STAGE> L;
+  constexpr int TILES = CHUNKS * L::kPiece / 4, N = Step<T>::kTokens;
+  __shared__ __align__(16) unsigned char lds[2][2 * L::kBytes];
+  __shared__ typename Walk<false, 1>::Lds walked;
+  const TileRows<1> t(a);
+  const int r = t.r, g = t.g, D = a.head_dim;
+  typename Step<T>::Piece q[CHUNKS];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int d = (c * 4 + g) * L::kPiece;
+    T x[L::kPiece] = {};
+    if (t.row(0) && d < D)
+      load_n<L::kPiece>(static_cast<const T*>(a.q) + t.token(0) * a.q_token + t.head * a.q_head + d, a.q_aligned, x);
+    __builtin_memcpy(&q[c], x, sizeof(x));
+    if (a.negate) q[c] = -q[c];
+  }
+  State<TILES> st;
+#pragma unroll
+  for (int c = 0; c < TILES; ++c) st.o[c] = f32x4{0, 0, 0, 0};
+  st.m = -INFINITY, st.l = 0.0f;
+  Walk<false, 1> walk;
+  walk.template start<true>(a, t, walked);
+  const int stage = min(STAGE, a.block), stages = a.block / stage;
+  const auto fetch = [&](int s, int buffer) {
+    if (walk.page < 0) return;
+    const int64_t from = ((int64_t)walk.page * a.kv_heads + t.h) * a.block * D;
+    L::template fetch<kTileWaves * 64>(static_cast<const T*>(a.k_pages) + from + (int64_t)s * stage * D,
+                                       static_cast<const T*>(a.v_pages) + from + s * stage, stage, D, a.block, lds[buffer]);
+  };
+  int buffer = 0, s = 0;
+  if (walk.key != walk.END) fetch(0, 0);
+  while (walk.key != walk.END) {
+    const int32_t now_seen = walk.seen[0] - s * stage;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // the stage is in LDS, the other buffer is free
+    if (++s == stages) s = 0, walk.advance(a, t, walked);
+    if (walk.key != walk.END) fetch(s, buffer ^ 1);
+    const auto scores = [&](int u, float (&x)[N / 4]) {
+      Step<T>::template scores<CHUNKS>([&](int i) { return key_piece<T, CHUNKS, STAGE>(lds[buffer], i, u, D, r, g); }, q, x);
+    };
+    const auto step = [&](int u, float (&x)[N / 4], int stored) {
+      attend_step<true, T, CHUNKS, TILES>(
+          a.scale2, x, [&](int i) { return value_piece<T, CHUNKS, STAGE>(lds[buffer], i, u, r, g); }, now_seen - u, stored,
+          g, st);
+    };
+    int u = 0;
+    for (; u + 2 * N <= stage && __any(now_seen >= u + 2 * N); u += 2 * N) {
+      float x[N / 4], y[N / 4];
+      scores(u, x);
+      scores(u + N, y);
+      step(u, x, N);
+      step(u + N, y, N);
+    }
+    for (; u < stage && __any(now_seen > u); u += N) {
+      int stored = N;
+      if (!__any(now_seen >= u + N)) {
+        stored = max(now_seen - u, 0);
+#pragma unroll
+        for (int x = 1; x < 16; x <<= 1) stored = max(stored, __shfl_xor(stored, x));
+      }
+      float x[N / 4];
+      scores(u, x);
+      step(u, x, stored);
+    }
+    buffer ^= 1;
+  }
+  const float l = over_groups_sum(st.l);
+  if (!t.row(0)) return;
+  if (a.parts > 1)
+    store_part(a, t.split, t.token(0), t.head, g, st, l);
+  else
+    store_row<T>(a, t.token(0), t.head, g, st, st.m, l);
+}
+
 template <typename T, int CHUNKS>
 hipError_t start(const AttendArgs& a, const AttendShape& shape, hipStream_t stream) {
   if (a.tile_tokens > 0) {
     constexpr int LONG = power_of_two(CHUNKS) * 64;  // bytes of a head's row in LDS; 16 KiB of keys to a stage at most
     constexpr int STAGE = LONG <= 256 ? 64 : 16384 / LONG;
     const auto kernel =
-        a.prefix ? attend_tiles<T, CHUNKS, STAGE, kTileWaves, true> : attend_tiles<T, CHUNKS, STAGE, kTileWaves, false>;
+        a.prefix ? prefix_tiles<T, CHUNKS, STAGE> : attend_tiles<T, CHUNKS, STAGE, kTileWaves>;
     kernel<<<(unsigned)shape.groups, shape.threads, 0, stream>>>(a);
   } else {
     attend_kernel<T, CHUNKS><<<(unsigned)shape.groups, shape.threads, 0, stream>>>(a);
@@ -303,9 +380,9 @@ hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const 
 
 // Attention with a shared prefix: the prefix's part for all tokens together, each token's part of its own blocks, then the
 // parts of both joined.
-//   64 sequences of 1 to 700 tokens behind 16384 that they share, 32 queries on 8 heads of 128 in 16 bits: 87 us.  The prefix 42
-// (17 GFLOP at 410 TFLOP/s; vector instructions beside the matrix unit, as in attend_tiles), the tokens' own blocks 33 (110 MB at
-// 3.3 TB/s), the join of 33 parts 12.  Both in one launch, a prefix's workgroup in turn with two others: 122 us; the prefix's
+//   64 sequences of 1 to 700 tokens behind 16384 that they share, 32 queries on 8 heads of 128 in 16 bits: 84 us.  The prefix 39.5
+// (17 GFLOP at 435 TFLOP/s; vector instructions beside the matrix unit, as in attend_tiles), the tokens' own blocks 33 (110 MB at
+// 3.3 TB/s), the join of 33 parts 12.  Both in one launch, a prefix's workgroup in turn with two others: 122 us (for 87); the prefix's
 // LDS leaves a compute unit two workgroups, and its registers are too few for the others.  Two tiles to a wave of the prefix: 48
 // us for 42; half and a quarter as many shares of it are slower.
 hipError_t launch_attend_shared(const sdnn_block_cache& c, const sdnn_tokens& t, const sdnn_heads& q, const sdnn_heads& o,
