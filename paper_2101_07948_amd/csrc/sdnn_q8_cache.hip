@@ -51,8 +51,9 @@ struct RowArgs {
 
 // The page of a token's block, -1: nothing is stored there.
 __device__ __forceinline__ int32_t page_of(const RowArgs& a, int32_t p, int32_t s) {
-  if (p < 0 || (uint32_t)s >= (uint32_t)a.sequences || p / a.block >= a.max_blocks) return -1;
-  const int32_t page = a.table[(int64_t)s * a.max_blocks + p / a.block];
+  const int32_t b = p >> __builtin_ctz(a.block);
+  if (p < 0 || (uint32_t)s >= (uint32_t)a.sequences || b >= a.max_blocks) return -1;
+  const int32_t page = a.table[(int64_t)s * a.max_blocks + b];
   return page >= 0 && page < a.pages ? page : -1;
 }
 
