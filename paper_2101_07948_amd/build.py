@@ -82,8 +82,9 @@ def build_host_sanitized(out: str) -> str:
     """The host code alone (CSR validation, row orders, packing and its self-check, the
     C ABI's argument checks) built for the CPU under AddressSanitizer and
     UndefinedBehaviorSanitizer, with the kernel launchers replaced by stubs that fail
-    (sdnn_launch_stubs.cpp, sdnn_decode_launch_stubs.cpp, sdnn_serve_launch_stubs.cpp).  It serves the host-only entry points; load it in a process
-    started with the sanitizer runtime preloaded (tests/test_host_sanitized.py)."""
+    (sdnn_launch_stubs.cpp, sdnn_decode_launch_stubs.cpp, sdnn_serve_launch_stubs.cpp).  It
+    serves the host-only entry points; load it in a process started with the sanitizer runtime
+    preloaded (tests/test_host_sanitized.py)."""
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
     cmd = ["g++", "-std=c++17", "-O1", "-g", "-fPIC", "-shared", "-fno-omit-frame-pointer",
            "-fsanitize=address,undefined", "-fno-sanitize-recover=all",

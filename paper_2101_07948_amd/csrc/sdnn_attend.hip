@@ -382,8 +382,8 @@ hipError_t launch_attend(const sdnn_block_cache& c, const sdnn_tokens& t, const 
 // parts of both joined.
 //   64 sequences of 1 to 700 tokens behind 16384 that they share, 32 queries on 8 heads of 128 in 16 bits: 84 us.  The prefix 39.5
 // (17 GFLOP at 435 TFLOP/s; vector instructions beside the matrix unit, as in attend_tiles), the tokens' own blocks 33 (110 MB at
-// 3.3 TB/s), the join of 33 parts 12.  Both in one launch, a prefix's workgroup in turn with two others: 122 us (for 87); the prefix's
-// LDS leaves a compute unit two workgroups, and its registers are too few for the others.  Two tiles to a wave of the prefix: 48
+// 3.3 TB/s), the join of 33 parts 12.  Both in one launch, a prefix's workgroup in turn with two others: 122 us (for 87); the
+// prefix's LDS leaves a compute unit two workgroups, and its registers are too few for the others.  Two tiles to a wave of the prefix: 48
 // us for 42; half and a quarter as many shares of it are slower.
 hipError_t launch_attend_shared(const sdnn_block_cache& c, const sdnn_tokens& t, const sdnn_heads& q, const sdnn_heads& o,
                                 int32_t shared, float scale, float* lse, float* workspace, hipStream_t stream) {

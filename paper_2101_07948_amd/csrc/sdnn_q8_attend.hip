@@ -331,9 +331,11 @@ struct Q8Stage {
 //   2048 tokens at the end of 8192, 32 queries on 8 heads of 128 in 16 bits: 427 to 438 us, 241 GFLOP at 560 TFLOP/s.  A step is
 // 24 matrix instructions, 8 of them for the probabilities' second part, and 140 vector ones (scales, exponentials, sums, parts):
 // the vector unit is busy for half of the time, the matrix unit for a third, and waves wait in 46 % of theirs.  Blocks found by
-// lists as in attend_tiles: 779 us; places in LDS worked out for each stage, two tiles to a wave: 459.  Two steps of 32 tokens under way at once: 524, registers spill.
+// lists as in attend_tiles: 779 us; places in LDS worked out for each stage, two tiles to a wave: 459.  Two steps of 32 tokens
+// under way at once: 524, registers spill.
 template <typename T, int CHUNKS, int STAGE, bool LISTS, bool PREFIX>
-__global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, CHUNKS <= 4 && sizeof(T) == 2 ? 4 : 2) void q8_tiles(Q8AttendArgs a) {
+__global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, CHUNKS <= 4 && sizeof(T) == 2 ? 4 : 2)
+void q8_tiles(Q8AttendArgs a) {
   typedef typename Parts<T>::Key Key;
   typedef Tile<Key, CHUNKS, STAGE> L;
   constexpr int TILES = CHUNKS * 2, N = 32, E = N / 4, R = q8_tiles_of<T>(CHUNKS), WAVES = kTileWaves / R;
@@ -361,7 +363,8 @@ __global__ __launch_bounds__(kTileWaves / q8_tiles_of<T>(CHUNKS) * 64, CHUNKS <=
   int key_at[CHUNKS], value_at[STAGE / N];
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c)
-    key_at[c] = (int)(L::key(nullptr, 8 * (r >> 2) + (r & 3), min(c * 4 + g, D / 8 - 1)) - static_cast<const unsigned char*>(nullptr));
+    key_at[c] = (int)(L::key(nullptr, 8 * (r >> 2) + (r & 3), min(c * 4 + g, D / 8 - 1)) -
+                      static_cast<const unsigned char*>(nullptr));
 #pragma unroll
   for (int u = 0; u < STAGE; u += N)
     value_at[u / N] = (int)(L::value(nullptr, r, u / 8 + g) - static_cast<const unsigned char*>(nullptr));

@@ -137,9 +137,9 @@ struct RunLds {
 // items, of few tasks, so that it seldom reads weights.  A lane has 2 VP values of a row (ITER
 // times: long heads whose parts only divide by one), pairs in place, so that norm, rotation and the largest value need no more
 // than a few exchanges within a row's lanes.
-//   The work is moving bytes.  Norms of 8001 tokens of 40 heads of 128 in 16 bits with weights of each head: 42.5 us, 164 MB at 3.9
-// TB/s; of 32768 tokens 137 to 140 us, 4.8 TB/s, a large copy's rate.  With a token to a wave, which read the weights of every head
-// anew: 52 us.  B = 4 where a lane has 16 values: 163 instead of 129 registers, and 169 us instead of 137.
+//   The work is moving bytes.  Norms of 8001 tokens of 40 heads of 128 in 16 bits with weights of each head: 42.5 us, 164 MB
+// at 3.9 TB/s; of 32768 tokens 137 to 140 us, 4.8 TB/s, a large copy's rate.  With a token to a wave, which read the weights of
+// every head anew: 52 us.  B = 4 where a lane has 16 values: 163 instead of 129 registers, and 169 us instead of 137.
 //   The sum of squares is one of 64-bit products, exact for 16-bit values, and its root is rounded once: a key comes out the
 // same whatever lanes its values lie in.  Where a row has lanes enough, lane b of a quad takes the root for token b of the batch.
 template <typename T, int VP, bool INTERLEAVED, bool CACHE>
@@ -169,7 +169,9 @@ __device__ __forceinline__ void token_rows(const RowArgs& a, RunLds& l) {
   const int items = (q_tasks + k_tasks + v_tasks) << shift, each = (items + a.shares * kRowWaves - 1) / (a.shares * kRowWaves);
   const int first = wave * each, end = min(first + each, items);
   const auto kind_of = [&](int task) { return task < q_tasks ? 0 : task < q_tasks + k_tasks ? 1 : 2; };
-  const auto task_head = [&](int task, int kind) { return kind == 0 ? task : kind == 1 ? task - q_tasks : task - q_tasks - k_tasks; };
+  const auto task_head = [&](int task, int kind) {
+    return kind == 0 ? task : kind == 1 ? task - q_tasks : task - q_tasks - k_tasks;
+  };
   T next[B][ITER][2 * VP];
   const auto load = [&](int item) {
     const int task = item >> shift, b0 = (item - (task << shift)) * B;
@@ -379,7 +381,8 @@ __device__ __forceinline__ void load_window(const RowArgs& a, TurnLds& l, int t0
     const bool fits = page >= 0 && fpage == page && fs == s && p - fp == i - from && ((p - i + begin) & 3) == 0;
     const uint64_t fit = __ballot(fits), there = __ballot(i < n);
     const uint64_t mine = begin < 0 ? 15ull >> -begin : 15ull << begin;
-    const bool together = PARTS ? (there & mine) == (fit & mine) && (there & mine) : begin >= 0 && (fit & mine) == mine && begin + 4 <= kQ8Window;
+    const bool all = (there & mine) == (fit & mine) && (there & mine), four = begin >= 0 && begin + 4 <= min(n, kQ8Window);
+    const bool together = all && (PARTS || four);
     if (i == from) l.group[q] = together ? page : -1;
     if (i == 0 && lead == 0) l.group[0] = -1;  // no token is in it
     const uint64_t singles = __ballot(i < n && !together);

@@ -364,7 +364,7 @@ static_assert(kOctaves <= 0.034 * kBins, "a bin's weights are within a factor of
 __device__ __forceinline__ float range_of(const Cut& c, const Weights& w, int which) {
   // the last bin of a range, or the one before its first
   const int ends[4] = {c.edge, c.edge - 1, c.end_p, c.edge_p - 1}, b = ends[which];
-  const bool asked = which < 2 ? c.edge >= 0 && !(c.kind == kShort && which == 1) : c.edge_p >= 0 && !(c.kind == kShort && which == 2);
+  const bool asked = (which < 2 ? c.edge : c.edge_p) >= 0 && !(c.kind == kShort && (which == 1 || which == 2));
   if (c.kind == kWhole || c.kind == kOther || !asked || b < 0) return INFINITY;
   return lowest_where([&](float x) { return bin_of(exponent_of(w, x)) <= b; });
 }
@@ -545,8 +545,8 @@ __device__ __forceinline__ void pick_by_bins(const SampleArgs& a, int r, SampleL
 
 // The row's token from the list of its first tokens (more than the limits leave, see kShort).  edge: what the logits of the
 // tokens of bin edge_p are below.
-__device__ __forceinline__ void pick_from_list(const SampleArgs& a, int r, SampleLds& l, const Weights& w, const Limits& limits, const Cut& cut,
-                               float edge) {
+__device__ __forceinline__ void pick_from_list(const SampleArgs& a, int r, SampleLds& l, const Weights& w, const Limits& limits,
+                                               const Cut& cut, float edge) {
   const int tid = threadIdx.x, n = (int)cut.tokens;
   const bool by_p = cut.edge_p >= 0;  // it ends with the bin in which top_p does, not top_k
   if (n > kRanked && by_p) {
@@ -626,7 +626,8 @@ __device__ __forceinline__ void pick_from_list(const SampleArgs& a, int r, Sampl
 // The last token that the limits leave where the last bins' tokens tell (see kEdges); load(which): l.list from the row's list of
 // those of bin edge, or of bins edge_p to end_p.
 template <typename F>
-__device__ __forceinline__ uint64_t last_of_edges(SampleLds& l, const Weights& w, const Limits& limits, const Cut& cut, const F& load) {
+__device__ __forceinline__ uint64_t last_of_edges(SampleLds& l, const Weights& w, const Limits& limits, const Cut& cut,
+                                                  const F& load) {
   uint64_t last = ~0ull, kept = cut.total;
   if (cut.edge >= 0) {
     load(0);
@@ -726,8 +727,9 @@ __device__ __forceinline__ uint64_t last_of(SampleLds& l, const Row<T>& row, con
 // of the one that the token lies in, until a wave has few enough to look at them one by one.  total: all masses of the row where
 // they are known (then begin ... end is the part with the token, and `before` what is before it), else 0.
 template <typename T>
-__device__ __forceinline__ void pick_by_index(const SampleArgs& a, int r, uint64_t (&lds)[kWavesOf], const Row<T>& row, const Weights& w,
-                              const Limits& limits, const Kept& kept, int begin, int end, uint64_t before, uint64_t total) {
+__device__ __forceinline__ void pick_by_index(const SampleArgs& a, int r, uint64_t (&lds)[kWavesOf], const Row<T>& row,
+                                              const Weights& w, const Limits& limits, const Kept& kept, int begin, int end,
+                                              uint64_t before, uint64_t total) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   uint64_t target = total ? target_of(limits.u, total) : 0;
   while (!total || end - begin > 64) {
@@ -824,9 +826,9 @@ struct Part {
   }
 };
 
-// 128 rows of 131001 in 16 bits that ask for all kinds of limits: 87 us in seven launches.  sample_first 9, sample_bins 23 (a
-// third of them, with four times as long parts, 20: adding the bins in memory), sample_cut 8, sample_gather 12, sample_order 18
-// (lists of up to 2048 tokens), sample_masses 11, sample_pick 7, of which about 3 are each launch's own.
+// 128 rows of 131001 in 16 bits that ask for all kinds of limits: 87 us in seven launches, sample_first 9, sample_bins 23 (21
+// with four parts to a workgroup of four times the threads, a call 85), sample_cut 8, sample_gather 12, sample_order 18 (lists of
+// up to 2048 tokens), sample_masses 11, sample_pick 7, of which about 3 are each launch's own.
 
 // The first token of each part; the row's bins and its lists are emptied.
 template <typename T>

@@ -348,7 +348,8 @@ class BlockCache:
     def _attend_shared(self, cache, pq, po, q, out, pos, seq, table, shared, scale, pl, workspace, stream):
         L = _bound
         T, H, blocks = pos.shape[0], q.shape[1], table.shape[1]
-        workspace, pw, nw = _workspace(workspace, lambda: L.sdnn_block_attend_shared_floats(cache, T, H, blocks, shared), q, stream)
+        workspace, pw, nw = _workspace(workspace, lambda: L.sdnn_block_attend_shared_floats(cache, T, H, blocks, shared),
+                                       q, stream)
         _check(L.sdnn_block_attend_shared(cache, self._tokens(pos, seq, table), pq, po, shared,
                                           1.0 / math.sqrt(self.head_dim) if scale is None else scale, pl, pw, nw,
                                           _stream_handle(stream)), "sdnn_block_attend_shared")
