@@ -687,6 +687,41 @@ def test_sample_is_fair():
     assert (np.abs(share - p) <= 5 * np.sqrt(p * (1 - p) / n) + 1.0 / n).all()
 
 
+@pytest.mark.parametrize("rows,vocab", [(3, 9001), (3, 60_001), (70, 66_000)])
+def test_sample_in_a_graph(rows, vocab):
+    """One launch or rows shared out, replayed with other logits and other limits: what an eager call draws."""
+    x, u = torch.empty((rows, vocab), device=DEV), torch.empty(rows, device=DEV)
+    t, k = torch.empty(rows, device=DEV), torch.empty(rows, dtype=torch.int32, device=DEV)
+    p, least = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    token, logprob = torch.empty(rows, dtype=torch.int32, device=DEV), torch.empty(rows, device=DEV)
+    workspace = torch.empty(max(1, sd.sample_workspace_floats(rows, vocab)), device=DEV)
+
+    def inputs(seed):
+        x.copy_(randn(seed, (rows, vocab), torch.float32, 2.5))
+        u.copy_(torch.rand(rows, generator=gen(seed), device=DEV))
+        for i in range(rows):
+            t[i], k[i], p[i], least[i] = SETTINGS[(i + seed) % len(SETTINGS)]
+
+    def call(token, logprob, workspace):
+        sd.sample(x, u, token, temperature=t, top_k=k, top_p=p, min_p=least, logprob=logprob, workspace=workspace)
+
+    inputs(0)
+    call(token, logprob, workspace)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(token, logprob, workspace)
+    for seed in range(1, 5):
+        inputs(seed)
+        workspace.fill_(float("nan"))  # nothing of an earlier call is needed
+        token.fill_(-9), logprob.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, wantp = torch.empty_like(token), torch.empty_like(logprob)
+        call(want, wantp, None)
+        assert torch.equal(token, want) and torch.equal(logprob, wantp)
+
+
 def test_sample_refusals():
     x, u = randn(1, (3, 50), torch.float32), torch.zeros(3, device=DEV)
     token = torch.zeros(3, dtype=torch.int32, device=DEV)
