@@ -102,7 +102,8 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, bool row, int 
 
 // One step of E tokens to a lane, their scores s (without the keys' scales) given: tokens E g ... E g + E - 1 of which the
 // first `seen` of the step's are within this lane's query's sight.  ks, vs: the scales of their keys and values; of tokens out of
-// sight they may be anything that is not infinite or not a number.  EMPTY: see attend_step.
+// sight they may be anything finite: their scores, which such a scale may make infinite, are masked wherever some query of the
+// tile does not see all of the step, one that sees nothing of it included.  EMPTY: see attend_step.
 // Leaves what multiplies their values, in parts.
 template <bool EMPTY, typename T, int E, int TILES>
 __device__ __forceinline__ void q8_weights(float scale2, float (&s)[E], const float (&ks)[E], const float (&vs)[E], int seen, int g,
@@ -110,7 +111,7 @@ __device__ __forceinline__ void q8_weights(float scale2, float (&s)[E], const fl
   constexpr float HIGH = 8.0f;
 #pragma unroll
   for (int j = 0; j < E; ++j) s[j] *= ks[j];
-  if (__any(seen < 4 * E && (!EMPTY || seen > 0))) {
+  if (__any(seen < 4 * E)) {
 #pragma unroll
     for (int j = 0; j < E; ++j) s[j] = E * g + j < seen ? s[j] : -INFINITY;
   }
