@@ -135,7 +135,8 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   for (int c = 0; c < TILES; ++c) st.o[c] = f32x4{0, 0, 0, 0};
   st.m = -INFINITY, st.l = 0.0f;
 
-  // A block's key: the run of tokens of one sequence within the workgroup's, then the block.
+  // A block's key: the run of tokens of one sequence within the workgroup's, then the block, counted from the launch's first
+  // (tiles_of bounds only the blocks from there on by the key's 20 bits: a prefix may have as many before them).
   // Bit i of `turns`: token i is of another sequence than token i - 1 (a workgroup has at most 16 WAVES).
   static_assert(16 * WAVES <= 128, "two words of bits");
   if (wave < 2) {
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   at.t = t, at.seq = seq, at.last = min(p / a.block, a.max_blocks - 1), at.share = split;
   at.n = filler ? 0 : a.chosen ? a.blocks : at.last + 1;
   at.start(a, h);
-  const auto key = [&] { return at.valid(at.id) ? run << 20 | at.id : END; };
+  const auto key = [&] { return at.valid(at.id) ? run << 20 | (at.id - a.first) : END; };
   // One row of each token offers its next block.
   const auto offer = [&](int turn) {
     if (g == 0 && qr == 0)

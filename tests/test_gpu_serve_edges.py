@@ -8,7 +8,7 @@ import paper_2101_07948_amd as sd
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_decode import DEV, close, i32, randn  # noqa: E402
+from test_gpu_decode import DEV, close, filled, i32, randn  # noqa: E402
 from test_gpu_serve import PARTS, Widened, filled_q8  # noqa: E402
 
 INF, NAN = float("inf"), float("nan")
@@ -62,3 +62,29 @@ def test_what_lies_in_unstored_places_is_nothing_s_concern(left, dtype, kind, Hq
     assert np.array_equal(np.isneginf(got), np.isneginf(l)), "empty rows"
     fin = np.isfinite(l)
     assert (np.abs(got[fin] - l[fin]) <= PARTS * lt[fin]).all()
+
+
+# ---------------------------------------------------------------- far blocks
+
+@pytest.mark.parametrize("kind", ["plain", "q8"])
+@pytest.mark.parametrize("new", [60, 1])
+def test_own_blocks_past_the_20_bits_of_a_key(kind, new):
+    """Sequences behind a prefix of 2^20 blocks, the most, of which three have a page: two prompts, whose tokens
+    are neighbours in a workgroup, keep to their own blocks."""
+    Hq, Hk, D, P, dtype, shared, own = 32, 8, 64, 32, torch.float16, 1 << 20, [250, 200]
+    lens = [3 * P + n for n in own]
+    cache, near = (filled_q8(4, 2, lens, Hk, P, D, 3) if kind == "q8" else filled(4, 2, lens, Hk, P, D, dtype))
+    near[:, :3] = near[0, :3]
+    far = np.full((2, shared - 3 + near.shape[1]), -1, np.int32)
+    far[:, shared:] = near[:, 3:]
+    far[0, [0, 1, shared - 1]] = near[0, :3]
+    pos, seq = [p for n in lens for p in range(n - new, n)], [s for s in range(2) for _ in range(new)]
+    q = randn(9, (len(pos), Hq, D), dtype)
+    out, lse = torch.full_like(q, 7.0), torch.full((len(pos), Hq), 7.0, device=DEV)
+    cache.attend(q, out, i32([p + (shared - 3) * P for p in pos]), i32(seq), i32(far), shared=shared, lse=lse)
+    w = Widened(cache) if kind == "q8" else None
+    k, v = (w.k, w.v) if w else (np.nan_to_num(od.f64(cache.k_pages)), np.nan_to_num(od.f64(cache.v_pages)))
+    o, l, ot, lt = od.attend_many(od.f64(q), pos, seq, near, k, v)
+    f = PARTS if w else 1.0
+    close(out, o, f * ot + od.U[dtype] * np.abs(o) * 1.01 + od.TINY[dtype], "out")
+    close(lse, l, f * lt, "lse")
