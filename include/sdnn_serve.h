@@ -56,8 +56,11 @@ sdnn_status sdnn_norm_rope(const sdnn_heads* q, const sdnn_heads* q_out, const s
  *   means, mean_scales: as in sdnn_block_cache, or both NULL.
  * A row x (32-bit values) becomes, with a = max |x_d|,
  *     f = 127 * (1 / a),  n_d = rint(x_d f),  scale = a * (1 / 127)
- * each operation rounded to 32 bits (1 / 127 too); all zeros where a < 2^-100.  The arrays are
- * 16-byte aligned. */
+ * each operation rounded to 32 bits (1 / 127 too); all zeros where a < 2^-100.  Of a row with a
+ * value that is infinite or not a number (a key also after its norm) the scale is NaN, and its
+ * numbers mean nothing: it is read back as NaN, outputs of tokens that see it are NaN, sums over
+ * such keys too, and the mean of a block with such a key counts as 0.  The arrays are 16-byte
+ * aligned. */
 typedef struct {
   int8_t* k_codes;
   int8_t* v_codes;

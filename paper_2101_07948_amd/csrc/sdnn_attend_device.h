@@ -212,7 +212,7 @@ __device__ __forceinline__ float over_groups_sum(float x) {
 // The logarithm of a query's sum l of exponentials taken from m (in units of log 2).  l's exponent joins m first: where m
 // is far from the maximum (see attend_step) both are large and cancel.
 __device__ __forceinline__ float log_of_sum(float m, float l) {
-  if (!(l > 0.0f)) return -INFINITY;
+  if (l == 0.0f) return -INFINITY;
   return ((m + (float)__builtin_amdgcn_frexp_expf(l)) + __log2f(__builtin_amdgcn_frexp_mantf(l))) * 0.693147181f;
 }
 
@@ -325,7 +325,7 @@ __device__ __forceinline__ void join_waves(const AttendArgs& a, JoinLds<TILES>& 
   for (int w = 1; w < kWaves; ++w) m = fmaxf(m, lds.tops[w][r]);
   float l = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) l += m > -INFINITY ? lds.totals[w][r] * __builtin_amdgcn_exp2f(lds.tops[w][r] - m) : 0.0f;
+  for (int w = 0; w < kWaves; ++w) l += lds.totals[w][r] * (m > -INFINITY ? __builtin_amdgcn_exp2f(lds.tops[w][r] - m) : 0.0f);
   const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(st.m - m) : 0.0f;
 #pragma unroll
   for (int c = 0; c < TILES; ++c) st.o[c] *= f;

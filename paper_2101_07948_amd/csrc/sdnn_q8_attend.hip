@@ -72,10 +72,11 @@ __device__ __forceinline__ void split(float x, H (&out)[N]) {
   }
 }
 
-// The queries' parts: piece i of a lane has values `at(i)` ... + 7 of its row.
+// The queries' parts: piece i of a lane has values `at(i)` ... + 7 of its row.  Returns the largest magnitude of them.
 template <typename T, int PIECES, typename AT>
-__device__ __forceinline__ void load_queries(const AttendArgs& a, bool row, int t, int64_t head, const AT& at,
-                                             typename Parts<T>::Key8 (&q)[Parts<T>::kQ][PIECES]) {
+__device__ __forceinline__ float load_queries(const AttendArgs& a, bool row, int t, int64_t head, const AT& at,
+                                              typename Parts<T>::Key8 (&q)[Parts<T>::kQ][PIECES]) {
+  float most = 0.0f;
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
     const int d = at(i);
@@ -94,26 +95,34 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, bool row, int 
     for (int e = 0; e < 8; ++e) {
       typename Parts<T>::Key part[Parts<T>::kQ];
       split((float)x[e], part);
+      most = fmaxf(most, fabsf((float)x[e]));
 #pragma unroll
       for (int k = 0; k < Parts<T>::kQ; ++k) q[k][i][e] = a.negate ? -part[k] : part[k];
     }
   }
+  return most;
 }
 
 // One step of E tokens to a lane, their scores s (without the keys' scales) given: tokens E g ... E g + E - 1 of which the
-// first `seen` of the step's are within this lane's query's sight.  ks, vs: the scales of their keys and values; of tokens out of
-// sight they may be anything finite: their scores, which such a scale may make infinite, are masked wherever some query of the
-// tile does not see all of the step, one that sees nothing of it included.  EMPTY: see attend_step.
-// Leaves what multiplies their values, in parts.
+// first `seen` of the step's are within this lane's query's sight.  ks, scales: those of their keys and values.  EMPTY: see
+// attend_step; a query that sees nothing of a step has m = infinity for it and so p = 0, if its scores, which are not masked
+// where no query of the tile sees a part of the step, are finite.  odd: they may not be, or a value's scale is not (of a row that is
+// not finite, or what memory held that no token was stored to): all that is out of sight is masked.  (Masks in all steps
+// that some query sees nothing of: 2048 tokens over 16 of 128 blocks each 195 us for 169.)  A scale that is NaN within sight makes
+// the query's sums NaN.  Leaves what multiplies the tokens' values, in parts.
 template <bool EMPTY, typename T, int E, int TILES>
-__device__ __forceinline__ void q8_weights(float scale2, float (&s)[E], const float (&ks)[E], const float (&vs)[E], int seen, int g,
-                                           State<TILES>& st, bf16x8 (&p)[Parts<T>::kP][E / 8]) {
+__device__ __forceinline__ void q8_weights(float scale2, float (&s)[E], const float (&ks)[E], const float (&scales)[E], bool odd,
+                                           int seen, int g, State<TILES>& st, bf16x8 (&p)[Parts<T>::kP][E / 8]) {
   constexpr float HIGH = 8.0f;
+  float vs[E];
 #pragma unroll
-  for (int j = 0; j < E; ++j) s[j] *= ks[j];
-  if (__any(seen < 4 * E)) {
+  for (int j = 0; j < E; ++j) s[j] *= ks[j], vs[j] = scales[j];
+  if (odd || __any(seen < 4 * E && (!EMPTY || seen > 0))) {
 #pragma unroll
-    for (int j = 0; j < E; ++j) s[j] = E * g + j < seen ? s[j] : -INFINITY;
+    for (int j = 0; j < E; ++j) {
+      const bool in_sight = E * g + j < seen;
+      s[j] = in_sight ? s[j] : -INFINITY, vs[j] = in_sight ? vs[j] : 0.0f;
+    }
   }
   float top = s[0];
 #pragma unroll
@@ -223,11 +232,6 @@ __global__ __launch_bounds__(kWaves * 64, q8_waves(2 * DIMS)) void q8_kernel(Q8A
       for (int c = 0; c < TILES; ++c)
         vv[c] = *reinterpret_cast<const typename VecOf<W, int32_t>::type*>(v + min(c * 16 + r, D - 1) * P + E * g);
       __builtin_amdgcn_sched_barrier(0);
-      if (seen < N) {  // (memory that no token was stored to)
-#pragma unroll
-        for (int x = 0; x < E; ++x)
-          if (E * g + x >= seen) ks[x] = vs[x] = 0.0f;
-      }
       float s[E];
 #pragma unroll
       for (int x = 0; x < N / 16; ++x) {
@@ -245,7 +249,7 @@ __global__ __launch_bounds__(kWaves * 64, q8_waves(2 * DIMS)) void q8_kernel(Q8A
         for (int i = 0; i < 4; ++i) s[4 * x + i] = acc[i];
       }
       bf16x8 w[Parts<T>::kP][E / 8];
-      q8_weights<false, T, E, TILES>(a.scale2, s, ks, vs, seen, g, st, w);
+      q8_weights<false, T, E, TILES>(a.scale2, s, ks, vs, false, seen, g, st, w);
 #pragma unroll
       for (int c = 0; c < TILES; ++c)
 #pragma unroll
@@ -270,6 +274,10 @@ template <typename T>
 constexpr int q8_tiles_of(int chunks) {
   return sizeof(T) == 4 && chunks <= 3 ? 2 : 1;
 }
+
+// With scales of keys below the first, and queries (times the scale of scores, where that is above 1) below the second, a score of
+// up to 256 numbers of up to 2^7 is below 2^127.
+constexpr float kLargeScale = 0x1p20f, kLargeQuery = 0x1p92f;
 
 // A stage of `tokens` tokens on its way to LDS: a thread holds pieces of 16 numbers of keys' rows and of values', and some of
 // the threads a scale.  They are asked for while the stage before is computed, and widened on their way into the tile, so that
@@ -313,7 +321,8 @@ struct Q8Stage {
       }
     if (scaled) scale = (threadIdx.x < STAGE ? a.k_scales : a.v_scales)[at + t0 + threadIdx.x % STAGE];
   }
-  __device__ __forceinline__ void store(unsigned char* lds, float* scales) const {
+  // (odd: of each wave that has scales, whether one of them is large, infinite or not a number.)
+  __device__ __forceinline__ void store(unsigned char* lds, float* scales, int32_t* odd) const {
 #pragma unroll
     for (int j = 0; j < kPieces; ++j)
       if (there[j]) {
@@ -323,8 +332,11 @@ struct Q8Stage {
           widen(v[j][2 * e], v[j][2 * e + 1], reinterpret_cast<bf16x8*>(lds + v_to[j][e]));
         }
       }
-    // (where no token was stored memory may hold what is infinite or not a number)
-    if (threadIdx.x < 2 * STAGE) scales[threadIdx.x] = fabsf(scale) < INFINITY ? scale : 0.0f;
+    if (threadIdx.x < 2 * STAGE) {
+      scales[threadIdx.x] = scale;
+      const bool any = __any(!(fabsf(scale) < kLargeScale));
+      if (threadIdx.x % 64 == 0) odd[threadIdx.x / 64] = any;
+    }
   }
 };
 
@@ -342,18 +354,21 @@ void q8_tiles(Q8AttendArgs a) {
   constexpr int TILES = CHUNKS * 2, N = 32, E = N / 4, R = q8_tiles_of<T>(CHUNKS), WAVES = kTileWaves / R;
   __shared__ __align__(16) unsigned char lds[2 * 2 * L::kBytes];
   __shared__ __align__(16) float scales[2 * 2 * STAGE];  // of keys, of values; twice
+  __shared__ int32_t odd[2][2 * STAGE / 64];             // see Q8Stage::store
   __shared__ typename Walk<LISTS, R>::Lds walked;
   const TileRows<R> t(a);
   const int r = t.r, g = t.g, D = a.head_dim;
   typename Parts<T>::Key8 q[R][Parts<T>::kQ][CHUNKS];
   State<TILES> st[R];
+  float most = 0.0f;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    load_queries<T, CHUNKS>(a, t.row(i), t.token(i), t.head, [&](int c) { return (c * 4 + g) * 8; }, q[i]);
+    most = fmaxf(most, load_queries<T, CHUNKS>(a, t.row(i), t.token(i), t.head, [&](int c) { return (c * 4 + g) * 8; }, q[i]));
 #pragma unroll
     for (int c = 0; c < TILES; ++c) st[i].o[c] = f32x4{0, 0, 0, 0};
     st[i].m = -INFINITY, st[i].l = 0.0f;
   }
+  const bool large = __any(!(most * fmaxf(a.scale2, 1.0f) < kLargeQuery));
   Walk<LISTS, R> walk;
   walk.template start<PREFIX>(a, t, walked);
   const int stage = min(STAGE, a.block), stages = a.block / stage;
@@ -373,7 +388,7 @@ void q8_tiles(Q8AttendArgs a) {
   int buffer = 0, s = 0;
   if (walk.key != walk.END) {
     if (walk.page >= 0) next_stage.load(a, walk.page, t.h, 0);
-    next_stage.store(lds, scales);
+    next_stage.store(lds, scales, odd[0]);
   }
   while (walk.key != walk.END) {
     int32_t now_seen[R];
@@ -388,6 +403,9 @@ void q8_tiles(Q8AttendArgs a) {
     if (more) next_stage.load(a, walk.page, t.h, s * stage);
     const unsigned char* tile = lds + buffer * 2 * L::kBytes;
     const float* factors = scales + buffer * 2 * STAGE + E * g;
+    int32_t masked = large;  // (of each lane, so that it is not waited for before a step's scores are there)
+#pragma unroll
+    for (int i = 0; i < 2 * STAGE / 64; ++i) masked |= odd[buffer][i];
     // a step of tokens u ...
     const auto step = [&](int u) {
       float x[R][E], ks[E], vs[E];
@@ -417,8 +435,9 @@ void q8_tiles(Q8AttendArgs a) {
         for (int e = 0; e < 4; ++e) ks[i + e] = y[e], vs[i + e] = z[e];
       }
       bf16x8 w[R][Parts<T>::kP][1];
+      const bool any = __builtin_amdgcn_readfirstlane(masked);
 #pragma unroll
-      for (int i = 0; i < R; ++i) q8_weights<true, T, E, TILES>(a.scale2, x[i], ks, vs, now_seen[i] - u, g, st[i], w[i]);
+      for (int i = 0; i < R; ++i) q8_weights<true, T, E, TILES>(a.scale2, x[i], ks, vs, any, now_seen[i] - u, g, st[i], w[i]);
 #pragma unroll
       for (int c = 0; c < TILES; ++c) {
         const bf16x8 v = *reinterpret_cast<const bf16x8*>(tile + value_at[u / N] + c * 16 * L::kValuePieces * 16);
@@ -434,7 +453,7 @@ void q8_tiles(Q8AttendArgs a) {
 #pragma unroll
     for (int u = 0; u < STAGE; u += N)
       if (u < stage && __any(most > u)) step(u);
-    if (more) next_stage.store(lds + (buffer ^ 1) * 2 * L::kBytes, scales + (buffer ^ 1) * 2 * STAGE);
+    if (more) next_stage.store(lds + (buffer ^ 1) * 2 * L::kBytes, scales + (buffer ^ 1) * 2 * STAGE, odd[buffer ^ 1]);
     buffer ^= 1;
   }
 

@@ -83,15 +83,17 @@ __device__ __forceinline__ X over_lanes(X x, int lanes, const F& f) {
 __device__ __forceinline__ double over_lanes_sum(double x, int lanes) {
   return over_lanes(x, lanes, [](double a, double b) { return a + b; });
 }
+// The larger of both, or NaN where one is.
+__device__ __forceinline__ float max_or_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float over_lanes_max(float x, int lanes) {
-  return over_lanes(x, lanes, [](float a, float b) { return fmaxf(a, b); });
+  return over_lanes(x, lanes, [](float a, float b) { return max_or_nan(a, b); });
 }
 
 // What a row is multiplied by to become numbers from -127 to 127, and its scale.  (Below 2^-100 the factor would leave the
-// floats: such rows are zeros.)
+// floats: such rows are zeros.  A row whose largest magnitude is infinite or not a number has no numbers: its scale says so.)
 __device__ __forceinline__ float code_factor(float top, float* scale) {
   const bool some = top >= 0x1p-100f;
-  *scale = some ? top * (1.0f / 127.0f) : 0.0f;
+  *scale = !(top < INFINITY) ? NAN : some ? top * (1.0f / 127.0f) : 0.0f;
   return some ? 127.0f * (1.0f / top) : 0.0f;
 }
 __device__ __forceinline__ int8_t code_of(float x, float f) {
@@ -296,7 +298,7 @@ __device__ __forceinline__ void token_rows(const RowArgs& a, RunLds& l) {
 #pragma unroll
         for (int i = 0; i < ITER; ++i)
 #pragma unroll
-          for (int e = 0; e < 2 * VP; ++e) top = fmaxf(top, fabsf(x[b][i][e]));
+          for (int e = 0; e < 2 * VP; ++e) top = max_or_nan(top, fabsf(x[b][i][e]));
         const float c = code_factor(over_lanes_max(top, a.lanes), &scale);
         if (b0 + b >= n || !row || l.page[b0 + b] < 0) continue;
         const int place = l.pos[b0 + b] & (a.block - 1);
@@ -431,7 +433,7 @@ __device__ __forceinline__ void append_window(const RowArgs& a, TurnLds& l, int 
       const int i = i0 + j * step;
       float top = 0.0f, scale;
 #pragma unroll
-      for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf((float)x[j][e]));
+      for (int e = 0; e < V; ++e) top = max_or_nan(top, fabsf((float)x[j][e]));
       const float c = code_factor(over_lanes_max(top, lanes), &scale);
       if (i >= n || d >= D) continue;
       if (d == 0 && l.page[i] >= 0)
@@ -486,8 +488,9 @@ __global__ __launch_bounds__(kRowThreads) void norm_kernel(RowArgs a, int vec) {
   token_rows_vec<T, INTERLEAVED, false>(a, vec, l);
 }
 
+// (Registers for three waves to a SIMD: with a few more, for two, 4093 tokens of 32 + 8 heads of 128 take 32 us for 29.)
 template <typename T, bool INTERLEAVED>
-__global__ __launch_bounds__(kRowThreads) void q8_append_kernel(RowArgs a, int vec) {
+__global__ __launch_bounds__(kRowThreads, 3) void q8_append_kernel(RowArgs a, int vec) {
   __shared__ union {
     RunLds run;
     TurnLds turn;
@@ -541,7 +544,7 @@ __global__ __launch_bounds__(kRowThreads) void q8_means_kernel(sdnn_q8_cache c, 
     if (wave == 0) {
       f32x4 sum = {0, 0, 0, 0};
       if (lane < D / 4) sum = (part[0][lane] + part[2][lane]) + (part[1][lane] + part[3][lane]);
-      float top = 0.0f;
+      float top = 0.0f;  // (0 where a key's scale is not a number, and so all sums: such a block's mean counts as 0)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(sum[e]));
       top = over_lanes_max(top, 64);

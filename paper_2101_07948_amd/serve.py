@@ -118,7 +118,8 @@ class Q8Cache:
         k_codes (pages, kv_heads, block, head_dim), v_codes (pages, kv_heads, head_dim, block) int8,
         k_scales, v_scales (pages, kv_heads, block) float32,
         means (pages, kv_heads, head_dim) int8, mean_scales (pages, kv_heads) float32, or both None
-    (as in BlockCache, for select).  Every call takes positions, sequences and the block table as
+    (as in BlockCache, for select).  A row with a value that is not finite has the scale NaN: it is read back as
+    NaN, and NaN is what tokens that see it get.  Every call takes positions, sequences and the block table as
     BlockCache's do; rows may be of any of the three types, another in each call."""
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales, means=None, mean_scales=None):

@@ -64,6 +64,26 @@ def test_what_lies_in_unstored_places_is_nothing_s_concern(left, dtype, kind, Hq
     assert (np.abs(got[fin] - l[fin]) <= PARTS * lt[fin]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("large", [1.0, 2.0 ** 100, 2.0 ** 112])
+def test_large_queries_beside_unstored_places(dtype, large):
+    """Large queries and small keys, whose scores are ordinary; with what memory held past the keys they would not be
+    finite."""
+    lens = [40, 40, 116]
+    cache, table = filled_q8(5, 3, lens, 12, 64, 64)
+    cache.k_scales.div_(large)
+    w = Widened(cache)
+    for scales in (cache.k_scales, cache.v_scales):
+        scales.nan_to_num_(nan=1e6)
+    pos, seq = [p for n in lens for p in range(n)], [s for s in range(3) for _ in range(lens[s])]
+    q = randn(9, (len(pos), 12, 64), torch.float32).mul(large).to(dtype)
+    out, lse = torch.full_like(q, NAN), torch.full((len(pos), 12), NAN, device=DEV)
+    cache.attend(q, out, i32(pos), i32(seq), i32(table), lse=lse)
+    o, l, ot, lt = od.attend_many(od.f64(q), pos, seq, table, w.k, w.v)
+    close(out, o, PARTS * ot + od.U[dtype] * np.abs(o) * 1.01 + od.TINY[dtype], "out")
+    close(lse, l, PARTS * lt, "lse")
+
+
 # ---------------------------------------------------------------- far blocks
 
 @pytest.mark.parametrize("kind", ["plain", "q8"])
@@ -88,3 +108,117 @@ def test_own_blocks_past_the_20_bits_of_a_key(kind, new):
     f = PARTS if w else 1.0
     close(out, o, f * ot + od.U[dtype] * np.abs(o) * 1.01 + od.TINY[dtype], "out")
     close(lse, l, f * lt, "lse")
+
+
+# ---------------------------------------------------------------- values that are not finite
+
+def appended(k, v, pos, seq, table, P, **kw):
+    cache = sd.Q8Cache.empty(int(table.max()) + 1, k.shape[1], k.shape[2], P, device=DEV)
+    for codes in (cache.k_codes, cache.v_codes):
+        codes.zero_()
+    for scales in (cache.k_scales, cache.v_scales):
+        scales.fill_(7.0)
+    cache.append(k, v, pos, seq, i32(table), **kw)
+    return cache
+
+
+def read(cache, pos, seq, table, dtype, rows):
+    k = torch.full((len(pos), cache.kv_heads, cache.head_dim), 5.0, dtype=dtype, device=DEV)
+    v = torch.full_like(k, 5.0)
+    t = i32(np.tile(table, (rows, 1)))  # (more rows than the call's tokens count for prompts: read one by one)
+    cache.read(pos, seq, t, k=k, v=v)
+    return k, v
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("how", ["plain", "half", "interleaved", "norm"])
+@pytest.mark.parametrize("D,P", [(64, 32), (80, 64), (256, 128)])
+@pytest.mark.parametrize("prompt", [True, False])
+def test_q8_row_with_a_value_that_is_not_finite_is_read_back_as_nan(bad, dtype, how, D, P, prompt):
+    """In keys and values, written by prompts and by single tokens, read back in both ways: the whole row is not a
+    number, and every other row as without it.  The mean of a filled block with such a key counts as 0."""
+    n, Hk = 150, 3
+    k, v = randn(1, (n, Hk, D), dtype), randn(2, (n, Hk, D), dtype)
+    kb, vb = k.clone(), v.clone()
+    for rows, x, at in ((kb, bad, [(0, 0, 0), (37, 1, D - 1), (63, 2, D // 2), (149, 0, 3)]),
+                        (vb, bad, [(0, 2, 5), (36, 0, D - 1), (39, 1, 0), (148, 1, D // 2)])):
+        for t, h, d in at:
+            rows[t, h, d] = x
+    vb[70, 0] = bad  # a row of nothing else
+    kw = {} if how == "plain" else dict(rope=sd.Rope(D, layout=how if how != "norm" else "half"))
+    if how == "norm":
+        kw["norm"] = sd.HeadNorm(None, 1 + 0.1 * randn(5, (D,), torch.float32))
+    if prompt:
+        table, seq, pos = np.arange(-(-n // P), dtype=np.int32)[None], i32([0] * n), i32(range(n))
+    else:
+        table, seq, pos = np.arange(n, dtype=np.int32)[:, None], i32(range(n)), i32([t % P for t in range(n)])
+    good, got = appended(k, v, pos, seq, table, P, **kw), appended(kb, vb, pos, seq, table, P, **kw)
+    for rows in (1, n):
+        for x, y, was in zip(read(got, pos, seq, table, dtype, rows), read(good, pos, seq, table, dtype, rows), (kb, vb)):
+            hurt = ~was.isfinite().all(-1)
+            assert bool(x[hurt].isnan().all()) and torch.equal(x[~hurt], y[~hurt]) and bool(y.isfinite().all())
+    if prompt:
+        hurt = torch.zeros((table.shape[1], Hk), dtype=torch.bool, device=DEV)
+        for t, h in (~kb.isfinite().all(-1)).nonzero().tolist():
+            hurt[t // P, h] = True
+        full = n // P
+        assert bool((got.mean_scales[:full][hurt[:full]] == 0).all())
+        for a, b in ((got.mean_scales, good.mean_scales), (got.means, good.means)):
+            assert torch.equal(a[:full][~hurt[:full]], b[:full][~hurt[:full]])
+
+
+def test_q8_key_that_its_norm_makes_infinite_is_read_back_as_nan():
+    n, D = 20, 64
+    k, v = 0.5 * torch.ones((n, 1, D), device=DEV), randn(2, (n, 1, D), torch.float32)
+    k[:, 0, 9] = 0.01
+    k[4, 0], k[4, 0, 9] = 0.0, 2.0  # one value has all of the row: 8 after the norm
+    w = torch.ones(D, device=DEV)
+    w[9] = 3e38
+    pos, seq, table = i32(range(n)), i32([0] * n), np.zeros((1, 1), np.int32)
+    cache = appended(k, v, pos, seq, table, 32, norm=sd.HeadNorm(None, w))
+    for rows in (1, n):
+        x, y = read(cache, pos, seq, table, torch.float32, rows)
+        assert bool(x[4].isnan().all()) and bool(x[:4].isfinite().all()) and bool(x[5:].isfinite().all())
+        assert bool(y.isfinite().all())
+
+
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("kind", ["all", "lists", "prefix"])
+@pytest.mark.parametrize("G,D,P", [(1, 64, 64), (4, 64, 32), (2, 128, 64), (3, 256, 32)])
+@pytest.mark.parametrize("tiles", [True, False])
+def test_q8_attention_tells_those_who_see_a_value_that_is_not_finite(bad, dtype, kind, G, D, P, tiles):
+    """Keys of head 0 and values of head 1 that are not finite: outputs of the queries that see them are not a number, nor
+    are sums over such keys; all others are as the definition has them."""
+    n, Hk, first = 70, 3, {"prefix": 2 * P}.get(kind, 0)
+    k, v = randn(1, (first + n, Hk, D), dtype), randn(2, (first + n, Hk, D), dtype)
+    k[first + 5, 0, 3], k[first + 40, 0, 0], v[first + 33, 1, D - 1] = bad, -bad, bad
+    pos, seq, blocks = list(range(first, first + n)), [0] * n, -(-(first + n) // P)
+    table = np.arange(blocks, dtype=np.int32)[None]
+    cache = appended(k, v, i32(range(first + n)), i32([0] * (first + n)), table, P)
+    w = Widened(cache)
+    chosen = lists(pos, Hk, blocks, P) if kind == "lists" else None
+    q = randn(9, (n, Hk * G, D), dtype)
+    out, lse = torch.full_like(q, 7.0), torch.full((n, Hk * G), 7.0, device=DEV)
+    asked = np.repeat(table, 2 if tiles else 40, axis=0)
+    cache.attend(q, out, i32(pos), i32(seq), i32(asked), None if chosen is None else i32(chosen), shared=first // P, lse=lse)
+    o, l, ot, lt = od.attend_many(od.f64(q), pos, seq, table, w.k, w.v, chosen)
+    p = np.array(pos)[:, None]
+
+    def sees(at):  # (tokens, heads)
+        there = p >= first + at
+        if chosen is not None:
+            there = there & (chosen == (first + at) // P).any(-1)
+        return np.broadcast_to(there, (n, Hk)).repeat(G, axis=1)
+
+    head = np.arange(Hk * G)[None] // G
+    no_sum = (head == 0) & (sees(5) | sees(40))
+    no_out = no_sum | ((head == 1) & sees(33))
+    got, sums = od.f64(out), lse.double().cpu().numpy()
+    assert np.isnan(got[no_out]).all() and np.isnan(sums[no_sum]).all()
+    tol = PARTS * ot + od.U[dtype] * np.abs(o) * 1.01 + od.TINY[dtype]
+    assert (np.abs(got - o) <= tol)[~no_out].all()
+    fin = ~no_sum & np.isfinite(l)
+    assert np.array_equal(np.isneginf(sums[~no_sum]), np.isneginf(l[~no_sum]))
+    assert (np.abs(sums[fin] - l[fin]) <= PARTS * lt[fin]).all()
