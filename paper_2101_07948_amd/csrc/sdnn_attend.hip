@@ -156,6 +156,8 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   Cursor at;
   at.t = t, at.seq = seq, at.last = min(p / a.block, a.max_blocks - 1), at.share = split;
   at.n = filler ? 0 : a.chosen ? a.blocks : at.last + 1;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) q[c] = filler ? typename Step<T>::Piece{} : q[c];  // (they may hold anything)
   at.start(a, h);
   const auto key = [&] { return at.valid(at.id) ? run << 20 | (at.id - a.first) : END; };
   // One row of each token offers its next block.
@@ -269,6 +271,8 @@ __global__ __launch_bounds__(kTileWaves * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) v
   st.m = -INFINITY, st.l = 0.0f;
   Walk<false, 1> walk;
   walk.template start<true>(a, t, walked);
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) q[c] = walk.filler(0) ? typename Step<T>::Piece{} : q[c];  // (they may hold anything)
   const int stage = min(STAGE, a.block), stages = a.block / stage;
   const auto fetch = [&](int s, int buffer) {
     if (walk.page < 0) return;

@@ -608,6 +608,7 @@ struct Walk<true, R> {
   int32_t run[R], pos[R], seen[R];
   int32_t key = END, page = -1;
   int turn = 0;
+  __device__ __forceinline__ bool filler(int i) const { return at[i].n == 0; }
   __device__ __forceinline__ int32_t key_of(int i) const { return at[i].valid(at[i].id) ? run[i] << 20 | at[i].id : END; }
   __device__ __forceinline__ void offer(const TileRows<R>& t, Lds& l) const {  // one row of each token
 #pragma unroll
@@ -668,6 +669,7 @@ struct Walk<false, R> {
   int32_t key = END, page = -1;
   int32_t runs, now = -1, block = 0, last = -1, ahead = -1;
   const int32_t* table;
+  __device__ __forceinline__ bool filler(int i) const { return run[i] < 0; }
   // The entry of block b of this run, of its last one past it.  (By the vector unit: a scalar load would be waited for by the
   // next read of LDS; without a condition, behind which the compiler waits; and a run's first is waited for by itself, or its
   // register would be waited for in every block.  8 sequences behind 32768 tokens in common, 32 queries on 8 heads of 128: 61 us

@@ -360,17 +360,27 @@ void q8_tiles(Q8AttendArgs a) {
   const int r = t.r, g = t.g, D = a.head_dim;
   typename Parts<T>::Key8 q[R][Parts<T>::kQ][CHUNKS];
   State<TILES> st[R];
-  float most = 0.0f;
+  float most[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    most = fmaxf(most, load_queries<T, CHUNKS>(a, t.row(i), t.token(i), t.head, [&](int c) { return (c * 4 + g) * 8; }, q[i]));
+    most[i] = load_queries<T, CHUNKS>(a, t.row(i), t.token(i), t.head, [&](int c) { return (c * 4 + g) * 8; }, q[i]);
 #pragma unroll
     for (int c = 0; c < TILES; ++c) st[i].o[c] = f32x4{0, 0, 0, 0};
     st[i].m = -INFINITY, st[i].l = 0.0f;
   }
-  const bool large = __any(!(most * fmaxf(a.scale2, 1.0f) < kLargeQuery));
   Walk<LISTS, R> walk;
   walk.template start<PREFIX>(a, t, walked);
+  bool large = false;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const bool filler = walk.filler(i);  // (whose queries may hold anything)
+    large = large || (!filler && !(most[i] * fmaxf(a.scale2, 1.0f) < kLargeQuery));
+#pragma unroll
+    for (int part = 0; part < Parts<T>::kQ; ++part)
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) q[i][part][c] = filler ? typename Parts<T>::Key8{} : q[i][part][c];
+  }
+  large = __any(large);
   const int stage = min(STAGE, a.block), stages = a.block / stage;
   Q8Stage<T, CHUNKS, STAGE, WAVES> next_stage(a, stage);
 

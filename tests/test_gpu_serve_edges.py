@@ -222,3 +222,39 @@ def test_q8_attention_tells_those_who_see_a_value_that_is_not_finite(bad, dtype,
     fin = ~no_sum & np.isfinite(l)
     assert np.array_equal(np.isneginf(sums[~no_sum]), np.isneginf(l[~no_sum]))
     assert (np.abs(sums[fin] - l[fin]) <= PARTS * lt[fin]).all()
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, 3e38])
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("cached", ["plain", "q8"])
+@pytest.mark.parametrize("kind", ["all", "lists", "prefix"])
+@pytest.mark.parametrize("Hq,Hk,D,P,new", [(12, 12, 64, 32, 37), (8, 2, 128, 64, 40), (32, 8, 64, 32, 1)])
+def test_fillers_rows_are_zero_whatever_their_queries_are(bad, dtype, cached, kind, Hq, Hk, D, P, new):
+    """A padded batch, whose fillers' queries are what memory held: their outputs are zero and their sums empty, and all
+    others are as without them."""
+    shared = 3 if kind == "prefix" else 0
+    lens = [shared * P + max(n, new) for n in (70, 45, 90)]
+    if cached == "q8":
+        cache, table = filled_q8(4, 3, lens, Hk, P, D, shared)
+        w = Widened(cache)
+        k, v, f = w.k, w.v, PARTS
+    else:
+        cache, table = filled(4, 3, lens, Hk, P, D, dtype)
+        table[:, :shared] = table[0, :shared]
+        k, v, f = np.nan_to_num(od.f64(cache.k_pages)), np.nan_to_num(od.f64(cache.v_pages)), 1.0
+    pos, seq = [], []
+    for s, n in enumerate(lens):
+        pos += list(range(n - new, n)) + [-1, 7]
+        seq += [s] * new + [s, 3 + s]  # a position below 0, a sequence that the table does not have
+    filler = np.array([p < 0 or s > 2 for p, s in zip(pos, seq)])
+    chosen = lists(pos, Hk, table.shape[1], P) if kind == "lists" else None
+    q = randn(9, (len(pos), Hq, D), dtype)
+    q[torch.from_numpy(filler).to(DEV)] = min(bad, torch.finfo(dtype).max) if bad == bad else bad
+    out, lse = torch.full_like(q, 7.0), torch.full((len(pos), Hq), 7.0, device=DEV)
+    cache.attend(q, out, i32(pos), i32(seq), i32(table), None if chosen is None else i32(chosen), shared=shared, lse=lse)
+    assert bool((out[torch.from_numpy(filler).to(DEV)] == 0).all())
+    o, l, ot, lt = od.attend_many(np.where(filler[:, None, None], 0.0, od.f64(q)), pos, seq, table, k, v, chosen)
+    close(out, o, f * ot + od.U[dtype] * np.abs(o) * 1.01 + od.TINY[dtype], "out")
+    got, fin = lse.cpu().numpy().astype(np.float64), np.isfinite(l)
+    assert not fin[filler].any() and np.array_equal(np.isneginf(got), ~fin)
+    assert (np.abs(got[fin] - l[fin]) <= f * lt[fin]).all()
