@@ -56,7 +56,8 @@ sdnn_status sdnn_norm_rope(const sdnn_heads* q, const sdnn_heads* q_out, const s
   if (k) {
     SDNN_CHECK(check_rows(k, 0, tokens, dtype));
     SDNN_CHECK(check_out(k, k_out, tokens, head_dim, dtype));
-    if (tokens > 0 && k_out->data == q_out->data) return SDNN_ERR_DIM;
+    // (rows of one that workgroups write while others read those of the other)
+    if (tokens > 0 && (k_out->data == q_out->data || q_out->data == k->data || k_out->data == q->data)) return SDNN_ERR_DIM;
   }
   if (rotation) SDNN_CHECK(check_rotation(rotation, head_dim));
   if (tokens == 0) return SDNN_OK;
