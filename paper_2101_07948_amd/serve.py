@@ -205,12 +205,11 @@ class Q8Cache:
         table.shape[1] without chosen)."""
         return _lib().sdnn_q8_attend_floats(self._packed, int(tokens), int(heads), int(blocks), int(shared))
 
-    def attend(self, q, out, pos, seq, table, chosen=None, shared: int = 0, scale: float | None = None, lse=None,
-               workspace=None, stream=None):
+    def attend(self, q, out, pos, seq, table, chosen=None, scale: float | None = None, lse=None, workspace=None,
+               stream=None, shared: int = 0):
         """out = attention of q (tokens, heads, head_dim) over the cached positions up to each
-        token's own, in its chosen blocks (None: all it sees).  shared: the first blocks of every
-        sequence that are the same pages, which are read once for all (looked up in the table's first
-        row).  scale, lse, workspace: as BlockCache.attend."""
+        token's own, in its chosen blocks (None: all it sees).  scale, lse, workspace, shared: as
+        BlockCache.attend, whose order they are in."""
         L, T, d = _lib(), pos.shape[0], q.dtype
         pq = _rows(q, "q", d, T, None, self.head_dim)
         H = q.shape[1]
