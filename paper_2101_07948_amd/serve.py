@@ -54,7 +54,7 @@ def _weight(w, name: str):
         return 0, 0, None
     torch = _torch_mod()
     _on_gpu(w, name)
-    if w.dim() not in (1, 2):
+    if w.dim() not in (1, 2) or 0 in w.shape:
         raise ValueError(f"{name} has shape {tuple(w.shape)}, expected (head_dim,) or (heads, head_dim)")
     return _dense(w, name, torch.float32, tuple(w.shape)), w.shape[0] if w.dim() == 2 else 0, w.shape[-1]
 

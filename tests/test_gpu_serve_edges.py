@@ -258,3 +258,11 @@ def test_fillers_rows_are_zero_whatever_their_queries_are(bad, dtype, cached, ki
     got, fin = lse.cpu().numpy().astype(np.float64), np.isfinite(l)
     assert not fin[filler].any() and np.array_equal(np.isneginf(got), ~fin)
     assert (np.abs(got[fin] - l[fin]) <= f * lt[fin]).all()
+
+
+def test_head_norm_refuses_weights_of_no_heads():
+    """They are not the same as none, which count as 1."""
+    for shape in ((0, 64), (0,), (3, 0)):
+        for name in ("q_weight", "k_weight"):
+            with pytest.raises(ValueError):
+                sd.HeadNorm(**{name: torch.ones(shape, device=DEV)})
