@@ -135,8 +135,8 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
   for (int c = 0; c < TILES; ++c) st.o[c] = f32x4{0, 0, 0, 0};
   st.m = -INFINITY, st.l = 0.0f;
 
-  // A block's key: the run of tokens of one sequence within the workgroup's, then the block, counted from the launch's first
-  // (tiles_of bounds only the blocks from there on by the key's 20 bits: a prefix may have as many before them).
+  // A block's key: the run of tokens of one sequence within the workgroup's, then the block, counted from the launch's first, as
+  // positions are from here on (tiles_of bounds the blocks from there on by the key's 20 bits: a prefix may have as many before).
   // Bit i of `turns`: token i is of another sequence than token i - 1 (a workgroup has at most 16 WAVES).
   static_assert(16 * WAVES <= 128, "two words of bits");
   if (wave < 2) {
@@ -154,12 +154,11 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
                       (place < 64 ? 0 : __popcll(turns[1] & (place == 127 ? ~0ull : (2ull << (place - 64)) - 1)));
   const bool filler = p < 0 || (uint32_t)seq >= (uint32_t)a.sequences;
   Cursor at;
-  at.t = t, at.seq = seq, at.last = min(p / a.block, a.max_blocks - 1), at.share = split;
+  at.t = t, at.seq = seq, at.last = min(p / a.block, a.max_blocks - 1) - a.first, at.share = split;
   at.n = filler ? 0 : a.chosen ? a.blocks : at.last + 1;
-#pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) q[c] = filler ? typename Step<T>::Piece{} : q[c];  // (they may hold anything)
+  p -= filler ? 0 : a.first * a.block;
   at.start(a, h);
-  const auto key = [&] { return at.valid(at.id) ? run << 20 | (at.id - a.first) : END; };
+  const auto key = [&] { return at.valid(at.id) ? run << 20 | at.id : END; };
   // One row of each token offers its next block.
   const auto offer = [&](int turn) {
     if (g == 0 && qr == 0)
@@ -236,8 +235,9 @@ __global__ __launch_bounds__(WAVES * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) void a
     buffer ^= 1;
   }
 
-  const float l = over_groups_sum(st.l);
+  float l = over_groups_sum(st.l);
   if (!row) return;
+  if (at.n <= 0) l = no_sums(st);
   if (a.parts > 1)
     store_part(a, split, t, head, g, st, l);
   else
@@ -271,8 +271,6 @@ __global__ __launch_bounds__(kTileWaves * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) v
   st.m = -INFINITY, st.l = 0.0f;
   Walk<false, 1> walk;
   walk.template start<true>(a, t, walked);
-#pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) q[c] = walk.filler(0) ? typename Step<T>::Piece{} : q[c];  // (they may hold anything)
   const int stage = min(STAGE, a.block), stages = a.block / stage;
   const auto fetch = [&](int s, int buffer) {
     if (walk.page < 0) return;
@@ -317,8 +315,9 @@ __global__ __launch_bounds__(kTileWaves * 64, CHUNKS * sizeof(T) <= 8 ? 4 : 2) v
     }
     buffer ^= 1;
   }
-  const float l = over_groups_sum(st.l);
+  float l = over_groups_sum(st.l);
   if (!t.row(0)) return;
+  if (walk.filler(0)) l = no_sums(st);
   if (a.parts > 1)
     store_part(a, t.split, t.token(0), t.head, g, st, l);
   else

@@ -209,6 +209,14 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return u + v;
 }
 
+// The sums of a filler, whose query may have been anything; returns their total.
+template <int TILES>
+__device__ __forceinline__ float no_sums(State<TILES>& st) {
+#pragma unroll
+  for (int c = 0; c < TILES; ++c) st.o[c] = f32x4{0, 0, 0, 0};
+  return 0.0f;
+}
+
 // The logarithm of a query's sum l of exponentials taken from m (in units of log 2).  l's exponent joins m first: where m
 // is far from the maximum (see attend_step) both are large and cancel.
 __device__ __forceinline__ float log_of_sum(float m, float l) {
@@ -510,7 +518,7 @@ __device__ __forceinline__ typename Step<T>::Piece value_piece(const unsigned ch
 }
 
 // Where a query is in the list of its blocks: the one it attends to next with its page, and what follows
-// it, loaded ahead so that no step waits for a list.
+// it, loaded ahead so that no step waits for a list.  Blocks count from AttendArgs::first (0 where there are lists).
 struct Cursor {
   int32_t t, seq, n, j;
   int32_t last;   // block that the token may see
@@ -520,7 +528,7 @@ struct Cursor {
   // others ascend: nothing follows the last block or one past it (what -1 fill the end of a list is not read).
   __device__ __forceinline__ int32_t following(const AttendArgs& a, int h) {
     if (!a.chosen) {
-      const int32_t b = a.first + j++ * a.splits + share;
+      const int32_t b = j++ * a.splits + share;
       return b < n ? b : -1;
     }
     const int32_t* list = a.chosen + ((int64_t)t * a.kv_heads + h) * a.blocks;
@@ -533,7 +541,7 @@ struct Cursor {
   }
   __device__ __forceinline__ bool valid(int32_t b) const { return b >= 0 && b <= last; }
   __device__ __forceinline__ int32_t page_of(const AttendArgs& a, int32_t b) const {
-    return valid(b) ? a.table[(int64_t)seq * a.max_blocks + b] : -1;
+    return valid(b) ? a.table[(int64_t)seq * a.max_blocks + a.first + b] : -1;
   }
   __device__ __forceinline__ void start(const AttendArgs& a, int h) {
     j = 0;

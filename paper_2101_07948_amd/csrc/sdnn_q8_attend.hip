@@ -341,9 +341,10 @@ struct Q8Stage {
 };
 
 // As attend_tiles: a workgroup's waves, tiles of neighbouring tokens of one cached head, walk their blocks through LDS.
-//   2048 tokens at the end of 8192, 32 queries on 8 heads of 128 in 16 bits: 427 to 438 us, 241 GFLOP at 560 TFLOP/s.  A step is
-// 24 matrix instructions, 8 of them for the probabilities' second part, and 140 vector ones (scales, exponentials, sums, parts):
-// the vector unit is busy for half of the time, the matrix unit for a third, and waves wait in 46 % of theirs.  Blocks found by
+//   2048 tokens at the end of 8192, 32 queries on 8 heads of 128 in 16 bits: 415 to 431 us, 241 GFLOP at 570 TFLOP/s; over 16 of
+// 128 blocks each 170 us.  A step is 24 matrix instructions, 8 of them for the probabilities' second part, and 140 vector ones
+// (scales, exponentials, sums, parts).  Waiting bounds it: the vector unit is busy for half of the time, the matrix unit for a
+// third, and waves wait in 44 % of theirs, those of a workgroup being in the same part of a step between the same barriers.  Blocks found by
 // lists as in attend_tiles: 779 us; places in LDS worked out for each stage, two tiles to a wave: 459.  Two steps of 32 tokens
 // under way at once: 524, registers spill.
 template <typename T, int CHUNKS, int STAGE, bool LISTS, bool PREFIX>
@@ -372,14 +373,7 @@ void q8_tiles(Q8AttendArgs a) {
   walk.template start<PREFIX>(a, t, walked);
   bool large = false;
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const bool filler = walk.filler(i);  // (whose queries may hold anything)
-    large = large || (!filler && !(most[i] * fmaxf(a.scale2, 1.0f) < kLargeQuery));
-#pragma unroll
-    for (int part = 0; part < Parts<T>::kQ; ++part)
-#pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) q[i][part][c] = filler ? typename Parts<T>::Key8{} : q[i][part][c];
-  }
+  for (int i = 0; i < R; ++i) large = large || (!walk.filler(i) && !(most[i] * fmaxf(a.scale2, 1.0f) < kLargeQuery));
   large = __any(large);
   const int stage = min(STAGE, a.block), stages = a.block / stage;
   Q8Stage<T, CHUNKS, STAGE, WAVES> next_stage(a, stage);
@@ -469,8 +463,9 @@ void q8_tiles(Q8AttendArgs a) {
 
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const float l = over_groups_sum(st[i].l);
+    float l = over_groups_sum(st[i].l);
     if (!t.row(i)) continue;
+    if (walk.filler(i)) l = no_sums(st[i]);
     if (a.parts > 1)
       store_part(a, t.split, t.token(i), t.head, g, st[i], l);
     else
