@@ -266,3 +266,67 @@ def test_head_norm_refuses_weights_of_no_heads():
         for name in ("q_weight", "k_weight"):
             with pytest.raises(ValueError):
                 sd.HeadNorm(**{name: torch.ones(shape, device=DEV)})
+
+
+# ---------------------------------------------------------------- the same every time
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("cached", ["plain", "q8"])
+@pytest.mark.parametrize("shared,new,ctx", [(0, 1, 30_000), (0, 90, 900), (40, 1, 500), (40, 50, 300)])
+def test_attention_gives_the_same_bits_every_time(dtype, cached, shared, new, ctx):
+    """Also where blocks are shared out over workgroups, whose parts are joined."""
+    Hq, Hk, D, P = 16, 4, 128, 64
+    lens = [shared * P + ctx, shared * P + ctx // 2]
+    if cached == "q8":
+        cache, table = filled_q8(4, 2, lens, Hk, P, D, shared)
+    else:
+        cache, table = filled(4, 2, lens, Hk, P, D, dtype)
+        table[:, :shared] = table[0, :shared]
+    pos, seq = [p for n in lens for p in range(n - new, n)], [s for s in range(2) for _ in range(new)]
+    q, at = randn(9, (len(pos), Hq, D), dtype), (i32(pos), i32(seq), i32(table))
+    first = None
+    for _ in range(10):
+        out, lse = torch.full_like(q, 7.0), torch.full((len(pos), Hq), 7.0, device=DEV)
+        cache.attend(q, out, *at, shared=shared, lse=lse)
+        first = first or (out, lse)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
+# ---------------------------------------------------------------- fillers in the other calls
+
+@pytest.mark.parametrize("dtype", od.DTYPES)
+@pytest.mark.parametrize("cached", ["plain", "q8"])
+@pytest.mark.parametrize("rows", [3, 90])  # of the table: tokens are handled as prompts, or one by one
+def test_fillers_rows_may_hold_anything(dtype, cached, rows):
+    """append and select of a padded batch: the same with fillers of NaN and infinities as with zeros."""
+    P, D, Hk, Hq, width = 32, 64, 2, 8, 4
+    pos = [-1, *range(30, 70), -1, -5, *range(0, 33), -1, *range(64, 96), -1, -1]  # (a sequence's tokens are neighbours)
+    seq = [0] + [0] * 40 + [0, 1] + [1] * 33 + [-1] + [2] * 32 + [2, 0]
+    T = len(pos)
+    filler = torch.tensor([p < 0 for p in pos], device=DEV)
+    table = i32(np.concatenate([np.arange(3 * width).reshape(3, width)] * (rows // 3)))
+    got = []
+    for bad in (0.0, NAN, INF):
+        k, v, q = randn(1, (T, Hk, D), dtype), randn(2, (T, Hk, D), dtype), randn(3, (T, Hq, D), dtype)
+        for x in (k, v, q):
+            x[filler] = bad
+        at = i32(pos), i32(seq), table
+        q_out = torch.full_like(q, 7.0)
+        if cached == "q8":
+            cache = sd.Q8Cache.empty(3 * width, Hk, D, P, device=DEV)
+            stored = cache.k_codes, cache.v_codes, cache.k_scales, cache.v_scales, cache.means, cache.mean_scales
+            norm = dict(norm=sd.HeadNorm())
+        else:
+            cache = sd.BlockCache.empty(3 * width, Hk, D, P, dtype, device=DEV)
+            stored = cache.k_pages, cache.v_pages, cache.means, cache.mean_scales
+            norm = {}
+        for x in stored:
+            x.zero_()
+        cache.append(k, v, *at, rope=sd.Rope(D), q=q, q_out=q_out, **norm)
+        chosen = torch.full((T, Hk, 3), 9, dtype=torch.int32, device=DEV)
+        cache.select(q, *at, chosen, sink=1, local=1)
+        got.append((*stored, q_out, chosen))
+    assert bool((got[0][-2][filler] == 0).all()) and bool((got[0][-1][filler] == -1).all())
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.equal(a, b)
