@@ -18,8 +18,9 @@
  *   - table[s * max_blocks + b] is the page that holds block b (positions b * block ...
  *     b * block + block - 1) of sequence s.  A page outside [0, pages) and a block at or
  *     past max_blocks hold nothing: nothing is stored there and attention passes over them.
- *   - Values must be finite, but memory of a page that no token was stored to may hold
- *     anything: it is never read into a result.
+ *   - Values must be finite, and scores of attention below 2^24 in magnitude.  But memory of a page
+ *     that no token was stored to may hold anything, and so may fillers' rows: they are never
+ *     read into a result.
  *   - Kernels are chosen by a call's sizes, the rows of its table among them; seq is not looked at.  A call
  *     of 16 tokens and more for each row of the table is taken for prompts, whose neighbouring tokens
  *     share what they read; else each token is handled for itself.  So prompts and single tokens

@@ -147,8 +147,10 @@ typedef struct {
  * token = the lowest index i at which the weights kept, summed up to and with i in the order of
  * indexes, exceed u times their sum M; logprob = log(w_token / M).  A row without a logit above
  * -infinity gets token -1 and logprob -infinity.
- *   Weights are held as whole numbers of 2^-44, so that sums are the same in any order and a
- *   token of weight below 2^-44 is never drawn; the exponents are computed in 64 bits.
+ *   A weight's exponent is computed in 64 bits, its power of two in 32, to 2^-22 of itself, and
+ *   held as a whole number of 2^-44, cut off: so sums are the same in any order, a token of weight
+ *   below 2^-44 is never drawn, and a border of the weights within 2^-21 M of u M (or that near to
+ *   top_p's limit) may count as on either side of it.
  *   logits: device, row r at logits + r * row_stride (elements, at least vocab), of dtype.
  *   u: device, rows floats in [0, 1) (others count as the nearest of these).
  *   token: device, rows int32.  logprob: device, rows floats, or NULL.

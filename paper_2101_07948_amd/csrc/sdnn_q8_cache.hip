@@ -611,7 +611,7 @@ __device__ __forceinline__ void read_rows(const RowArgs& a) {
 
 // A window of neighbouring tokens of one head: keys as they lie, values turned as in append_window.  All of a thread's loads
 // are under way before the first is used, and tokens of words that the window shares with others are read with them too: taken one by
-// one they had two more latencies and 91 us for 32 thousand tokens of 8 heads of 128 instead of 50 (221 MB at 4.4 TB/s).
+// one they had two more latencies and 91 us for 32 thousand tokens of 8 heads of 128 instead of 50 (199 MB at 4.0 TB/s).
 template <typename T>
 __device__ __forceinline__ void read_window(const RowArgs& a, TurnLds& l, int b) {
   constexpr int G = kQ8Window / 4, U = G * (kMaxHeadDim / 4) / kRowThreads + 1, W = 4;

@@ -34,7 +34,8 @@ struct SampleArgs {
 // The exponent of a token's weight, not above 0; -infinity (or not a number, which has no weight either) where the logit is.
 // (Where the largest logit is infinite it counts as 0 and all others as -infinity: see Row.)
 __device__ __forceinline__ double exponent_of(const Weights& w, float l) { return ((double)l - (double)w.top) * w.scale; }
-// 2^z as a whole number of 2^-kUnit: the fraction's power is a float of 24 bits, shifted by the whole part.
+// 2^z as a whole number of 2^-kUnit: the fraction's power is a float of 24 bits, shifted by the whole part.  It is off by 2^-22 of
+// itself at the most: the fraction's rounding 2^-26, the instruction's last place 2^-23, the cut to a whole number 2^-23.5.
 __device__ __forceinline__ uint64_t weight_of(double z) {
   if (!(z > -(double)kOctaves)) return 0;
   const double n = rint(z);

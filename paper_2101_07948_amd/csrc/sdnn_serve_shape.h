@@ -146,7 +146,8 @@ struct alignas(16) SampleSpace {
   int32_t listed, listed_p;
 };
 
-// Workgroups that share a row, each with 4096 tokens at least; 0: a row to a workgroup, in one launch.  Seven launches take 24 us
+// Workgroups that share a row, each with about 4096 tokens (more where a row has kMostSampleParts of them or all rows 4096);
+// 0: a row to a workgroup, in one launch.  Seven launches take 24 us
 // before their first pass counts, and then share a row's passes out, which one workgroup makes at about 4 tokens a
 // nanosecond.  One row in 32 bits, in one launch and shared out: of 32000 tokens top_k and top_p 20 us and 29, top_p alone 32 and
 // 37, no limit 17 and 25; of 50021 25 and 28, 41 and 35, 23 and 25; of 65000 30 and 28, 51 and 34, 26 and 26; of 131001 in 16
