@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kWaves * 64, attend_waves(CHUNKS * Step<T>::kPiece 
 // by block in ascending order, through LDS: a block is read from L2 once for all of them, the next one while
 // they compute.  Waves whose tokens did not choose a block skip it; rows of a tile that did not are masked.
 // The union is found on the way, a block ahead: each token offers its lowest block not yet passed.
-//   2048 tokens of 32 queries on 8 cached heads of 128 in 16 bits, 16 blocks of 64 each: 145 us, 34 GFLOP at 232 TFLOP/s
+//   2048 tokens of 32 queries on 8 cached heads of 128 in 16 bits, 16 blocks of 64 each: 148 us, 34 GFLOP at 232 TFLOP/s
 // (the matrix unit does 2.6 times that: rows of tokens that did not choose a block, and probabilities in two
 // parts).  Vector instructions (masks, exponentials, the parts) take 40 % of the time, matrix ones 25 %, and waves
 // wait for a stage or the matrix unit in 58 % of theirs.  Half as many waves to a SIMD, for more registers: 212 us;
